@@ -244,6 +244,77 @@ int spkv_set_tau(spkv_cache_t *cache, float tau);
 int spkv_set_head_tau(spkv_cache_t *cache, int32_t layer, int32_t kv_head, float tau,
                       spkv_stream_t stream);
 
+/* ---- rows before the cache: per-head norm and position rotation -------------------------------- */
+
+/* (No counterpart in the paper: what an attention layer does to its projected rows before the calls
+ * below see them, and the backward pass of it for training.)  For every token and every query / key
+ * head, a row x of head_dim elements becomes
+ *     u = x / sqrt(mean(x^2) + eps),  y = w * u                  (a side with its SPKV_NORM_* bit set)
+ *     (y_lo, y_hi) -> scale * (y_lo cos t - y_hi sin t,  y_hi cos t + y_lo sin t)
+ * for each rotated pair, t = position[axis of the pair][token] * inv_freq[pair]; dims from rot_dim on
+ * are not rotated, value rows are handed on unchanged.  Sums and products are float32, each result is
+ * rounded once.  Angles are exact for every int32 position (negative ones too): a frequency is held
+ * as a 64-bit fraction of a turn and the product is taken modulo one turn. */
+enum { SPKV_BF16 = 0, SPKV_F16 = 1, SPKV_F32 = 2 };
+enum { SPKV_NORM_Q = 1, SPKV_NORM_K = 2 };
+#define SPKV_MAX_ROW_DIM 256
+#define SPKV_MAX_AXES 4
+
+/* A tensor of rows: row (token, head) starts at ptr + token * token_stride + head * head_stride
+ * elements and is head_dim contiguous elements.  Device pointer, 16-byte aligned, strides multiples of
+ * 16 bytes: heads of a fused projection, head-major tensors and padded rows are all read in place. */
+typedef struct {
+  void *ptr;
+  int64_t token_stride, head_stride;
+} spkv_rows_t;
+
+/* Filled by spkv_rope_init, then read-only. */
+typedef struct {
+  int32_t rot_dim, interleaved, n_axes;
+  float scale;
+  uint64_t turn[SPKV_MAX_ROW_DIM / 2];   /* inv_freq / 2 pi modulo one, in units of 2^-64 */
+  uint8_t axis[SPKV_MAX_ROW_DIM / 2];
+} spkv_rope_t;
+
+/* rot_dim: rotated dims, a multiple of 16 up to SPKV_MAX_ROW_DIM (0: no rotation); interleaved = 0: pair p is
+ * dims (p, p + rot_dim / 2), otherwise (2p, 2p + 1); n_axes 1 .. SPKV_MAX_AXES position axes; scale: factor
+ * on every rotated dim (context-length scalings that change the attention temperature; 1 otherwise);
+ * h_inv_freq HOST [rot_dim / 2], radians per position, finite; h_axis HOST [rot_dim / 2], the axis of
+ * each pair, or NULL for axis 0 throughout.  Host only. */
+int spkv_rope_init(spkv_rope_t *rope, int32_t rot_dim, int32_t interleaved, int32_t n_axes, float scale,
+                   const double *h_inv_freq, const uint8_t *h_axis);
+
+typedef struct {
+  int32_t dtype;              /* SPKV_BF16 / SPKV_F16 / SPKV_F32, of every row tensor of the call        */
+  int32_t weight_dtype;       /* of d_wq, d_wk                                                           */
+  int32_t head_dim;           /* a multiple of 16 up to SPKV_MAX_ROW_DIM (the cache itself takes 128)    */
+  int32_t n_q_heads, n_kv_heads;   /* either may be 0: that side's tensors are then ignored              */
+  int32_t norm;               /* OR of SPKV_NORM_Q, SPKV_NORM_K; 0 = rotation only                       */
+  float eps;
+  const void *d_wq, *d_wk;    /* [head_dim] device, NULL = ones                                          */
+} spkv_qk_norm_t;
+
+/* d_pos [n_axes, n_tok] int32 device (may be NULL when rot_dim is 0).  v and v_out both NULL or both given.
+ * An output may be its own input (same pointer and strides); any other overlap is not allowed.
+ * Asynchronous on `stream`; n_tok = 0 does nothing. */
+int spkv_norm_rope(const spkv_qk_norm_t *norm, const spkv_rope_t *rope, int32_t n_tok, const int32_t *d_pos,
+                   const spkv_rows_t *q, const spkv_rows_t *k, const spkv_rows_t *v, const spkv_rows_t *q_out,
+                   const spkv_rows_t *k_out, const spkv_rows_t *v_out, spkv_stream_t stream);
+
+/* Gradients.  q, k: the forward call's INPUT rows (read only for a normed side; may be NULL otherwise);
+ * q_grad, k_grad, v_grad: gradients of its outputs; dq, dk, dv: gradients of its inputs (each may be its
+ * own upstream gradient or input row tensor, same pointer and strides); d_dwq, d_dwk [head_dim] float32:
+ * gradients of the norm weights, overwritten (NULL = not wanted; of a normed side only).  The sums
+ * over the rows have a fixed order: the same inputs give the same bits.
+ * d_workspace: >= spkv_norm_rope_workspace_bytes(norm) bytes, 16-byte aligned, needed for weight
+ * gradients only; calls that share it must not overlap on the GPU.  n_tok = 0 zeroes d_dwq, d_dwk. */
+size_t spkv_norm_rope_workspace_bytes(const spkv_qk_norm_t *norm);
+int spkv_norm_rope_backward(const spkv_qk_norm_t *norm, const spkv_rope_t *rope, int32_t n_tok, const int32_t *d_pos,
+                            const spkv_rows_t *q, const spkv_rows_t *k, const spkv_rows_t *q_grad,
+                            const spkv_rows_t *k_grad, const spkv_rows_t *v_grad, const spkv_rows_t *dq,
+                            const spkv_rows_t *dk, const spkv_rows_t *dv, float *d_dwq, float *d_dwk, void *d_workspace,
+                            size_t workspace_bytes, spkv_stream_t stream);
+
 /* ---- the hot path ------------------------------------------------------------------ */
 
 /* Step 1, score + threshold (Eq. 1-2).  d_x [n_tok, d_in] bf16 -> d_logits_out

@@ -55,6 +55,27 @@ class Stats(C.Structure):
                 ("density_cache", C.c_double)]
 
 
+BF16, F16, F32 = 0, 1, 2          # SPKV_BF16 / SPKV_F16 / SPKV_F32
+_DTYPE = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+NORM_Q, NORM_K = 1, 2             # SPKV_NORM_Q / SPKV_NORM_K
+MAX_ROW_DIM, MAX_AXES = 256, 4    # SPKV_MAX_ROW_DIM / SPKV_MAX_AXES
+
+
+class Rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("scale", C.c_float),
+                ("turn", C.c_uint64 * (MAX_ROW_DIM // 2)), ("axis", C.c_uint8 * (MAX_ROW_DIM // 2))]
+
+
+class QkNorm(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("weight_dtype", C.c_int32), ("head_dim", C.c_int32), ("n_q_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float), ("d_wq", C.c_void_p),
+                ("d_wk", C.c_void_p)]
+
+
 class SpkvError(RuntimeError):
     def __init__(self, code, where):
         self.code = code
@@ -101,6 +122,10 @@ def lib():
         "spkv_decode_attention_static": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, f32, vp]),
         "spkv_prefill_workspace_bytes": (sz, [cfgp, i32]),
         "spkv_prefill": (C.c_int, [vp, i32, i32, i32, vp, vp, vp, vp, vp, f32, vp, sz, vp]),
+        "spkv_rope_init": (C.c_int, [vp, i32, i32, i32, f32, vp, vp]),
+        "spkv_norm_rope": (C.c_int, [vp, vp, i32] + [vp] * 8),
+        "spkv_norm_rope_workspace_bytes": (sz, [vp]),
+        "spkv_norm_rope_backward": (C.c_int, [vp, vp, i32] + [vp] * 12 + [sz, vp]),
         "spkv_softgate_workspace_bytes": (sz, [i32, i32, i32]),
         "spkv_softgate_forward": (C.c_int, [i32, i32, i32, i32, vp, vp, vp, vp, f32, f32, f32, i32, vp, vp, vp, sz,
                                             vp, vp]),
@@ -488,6 +513,128 @@ def spkv_stream_read(buf, passes=5, stream=None):
     if int(status.item()) != 0:
         raise SpkvError(int(status.item()), "spkv_stream_read")
     return nbytes * passes / (e0.elapsed_time(e1) * 1e-3) / 1e9
+
+
+class NormRope:
+    """Descriptor of an attention layer's per-head norm and position rotation (make_norm_rope)."""
+
+    def __init__(self, norm, rope, dtype, keep):
+        self.norm, self.rope, self.dtype, self._keep = norm, rope, dtype, keep
+        self._n, self._r = C.addressof(norm), C.addressof(rope)
+        self.heads, self.head_dim = (norm.n_q_heads, norm.n_kv_heads), norm.head_dim
+        self.workspace_bytes = lib().spkv_norm_rope_workspace_bytes(self._n)
+        self._ws = {}
+
+    def workspace(self, device, stream):
+        """Scratch of the weight gradients: one per stream, so that calls on two streams do not share it."""
+        ws = self._ws.get((device, stream))
+        if ws is None:
+            ws = self._ws[device, stream] = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
+        return ws
+
+
+def make_norm_rope(n_q_heads, n_kv_heads, head_dim=128, dtype=torch.bfloat16, wq=None, wk=None, norm=True, eps=1e-6,
+                   rot_dim=None, theta=10000.0, inv_freq=None, axis=None, n_axes=1, interleaved=False, scale=1.0):
+    """norm: True (queries and keys), False, "q" or "k"; wq, wk [head_dim] device tensors of one type or None
+    (ones), read at every call.  inv_freq [rot_dim / 2] (default theta^(-2 i / rot_dim)) and axis
+    [rot_dim / 2] (the position axis of each pair) are host sequences."""
+    import numpy as np
+    rot_dim = head_dim if rot_dim is None else rot_dim
+    inv = np.ascontiguousarray(theta ** (-np.arange(rot_dim // 2) * 2.0 / max(rot_dim, 1)) if inv_freq is None
+                               else inv_freq, dtype=np.float64)
+    ax = None if axis is None else np.ascontiguousarray(axis, dtype=np.uint8)
+    if inv.shape != (rot_dim // 2,) or (ax is not None and ax.shape != inv.shape):
+        raise ValueError("inv_freq and axis take one entry per rotated pair")
+    rope = Rope()
+    _check(lib().spkv_rope_init(C.addressof(rope), rot_dim, int(bool(interleaved)), n_axes, scale, inv.ctypes.data,
+                                None if ax is None else ax.ctypes.data), "spkv_rope_init")
+    for w in (wq, wk):
+        if w is not None and (w.shape != (head_dim,) or (wq is not None and w.dtype != wq.dtype)):
+            raise ValueError("norm weights are [head_dim] tensors of one type")
+    wd = next((w.dtype for w in (wq, wk) if w is not None), torch.float32)
+    which = {True: NORM_Q | NORM_K, False: 0, "q": NORM_Q, "k": NORM_K}[norm]
+    d = QkNorm(_DTYPE[dtype], _DTYPE[wd], head_dim, n_q_heads, n_kv_heads, which, eps, _ptr(wq), _ptr(wk))
+    return NormRope(d, rope, dtype, (wq, wk))
+
+
+def _rows(nr, t, heads, n, what):
+    """spkv_rows_t of a [n, heads, head_dim] tensor of any token and head stride."""
+    if t.dtype != nr.dtype or t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or t.shape[2] != nr.head_dim:
+        raise ValueError(f"{what}: expected {nr.dtype} [{n}, {heads}, {nr.head_dim}], got {t.dtype} {tuple(t.shape)}")
+    st = t.stride()
+    if (st[2] != 1 and nr.head_dim > 1) or not t.is_cuda:
+        raise ValueError(f"{what}: a device tensor whose rows are contiguous")
+    return Rows(t.data_ptr(), st[0] if n > 1 else 0, st[1] if heads > 1 else 0)   # (the stride of a single entry says nothing)
+
+
+def _positions(nr, pos):
+    """n_tok of an int32 [n_tok] or [n_axes, n_tok] device tensor"""
+    n = pos.shape[-1]
+    if pos.dtype != torch.int32 or not pos.is_cuda or not pos.is_contiguous() or pos.numel() != nr.rope.n_axes * n:
+        raise ValueError(f"positions: contiguous int32 [{nr.rope.n_axes}, n_tok] on the device")
+    return n
+
+
+def _same_device(first, *others):
+    if any(t is not None and t.device != first.device for t in others):
+        raise ValueError("all tensors of a call live on one device")
+
+
+def spkv_norm_rope(nr, positions, q, k, v=None, q_out=None, k_out=None, v_out=None, stream=None):
+    """Norm + rotation of q [n_tok, n_q_heads, head_dim] and k [n_tok, n_kv_heads, head_dim] (any strides;
+    e.g. views of one fused projection), v handed on.  Returns (q_out, k_out, v_out), contiguous
+    tensors unless given; v_out is None without v."""
+    n = _positions(nr, positions)
+    hq, hkv = nr.heads
+    shape_k = (n, hkv, nr.head_dim)
+    if q_out is None:
+        q_out = torch.empty((n, hq, nr.head_dim), dtype=nr.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty(shape_k, dtype=nr.dtype, device=q.device)
+    if v is not None and v_out is None:
+        v_out = torch.empty(shape_k, dtype=nr.dtype, device=q.device)
+    _same_device(q, k, v, q_out, k_out, v_out, positions, *nr._keep)
+    a = [C.byref(_rows(nr, t, h, n, w)) for t, h, w in ((q, hq, "q"), (k, hkv, "k"))]
+    a.append(None if v is None else C.byref(_rows(nr, v, hkv, n, "v")))
+    a += [C.byref(_rows(nr, t, h, n, w)) for t, h, w in ((q_out, hq, "q_out"), (k_out, hkv, "k_out"))]
+    a.append(None if v is None else C.byref(_rows(nr, v_out, hkv, n, "v_out")))
+    with torch.cuda.device(q.device):
+        _check(lib().spkv_norm_rope(nr._n, nr._r, n, positions.data_ptr(), *a, _stream(stream)), "spkv_norm_rope")
+    return q_out, k_out, v_out
+
+
+def spkv_norm_rope_backward(nr, positions, q, k, q_grad, k_grad, v_grad=None, dq=None, dk=None, dv=None,
+                            weight_grads=True, stream=None):
+    """Gradients of spkv_norm_rope: q, k its input rows (None for a side without norm), q_grad, k_grad,
+    v_grad those of its outputs.  Returns (dq, dk, dv, dwq, dwk); dwq, dwk float32, None for a
+    side without norm or weight_grads=False; dv None without v_grad."""
+    n = _positions(nr, positions)
+    hq, hkv = nr.heads
+    dev, D = q_grad.device, nr.head_dim
+    if dq is None:
+        dq = torch.empty((n, hq, D), dtype=nr.dtype, device=dev)
+    if dk is None:
+        dk = torch.empty((n, hkv, D), dtype=nr.dtype, device=dev)
+    if v_grad is not None and dv is None:
+        dv = torch.empty((n, hkv, D), dtype=nr.dtype, device=dev)
+    normed = nr.norm.norm
+    dwq = torch.empty(D, dtype=torch.float32, device=dev) if weight_grads and normed & NORM_Q else None
+    dwk = torch.empty(D, dtype=torch.float32, device=dev) if weight_grads and normed & NORM_K else None
+    _same_device(q_grad, q, k, k_grad, v_grad, dq, dk, dv, positions, *nr._keep)
+
+    def rows(t, h, what):
+        return None if t is None else C.byref(_rows(nr, t, h, n, what))
+
+    with torch.cuda.device(dev):
+        st = _stream(stream)
+        ws = nr.workspace(dev, st.value) if dwq is not None or dwk is not None else None
+        _check(lib().spkv_norm_rope_backward(
+            nr._n, nr._r, n, positions.data_ptr(), rows(q, hq, "q"), rows(k, hkv, "k"), rows(q_grad, hq, "q_grad"),
+            rows(k_grad, hkv, "k_grad"), rows(v_grad, hkv, "v_grad"), rows(dq, hq, "dq"), rows(dk, hkv, "dk"),
+            rows(dv if v_grad is not None else None, hkv, "dv"), None if dwq is None else dwq.data_ptr(),
+            None if dwk is None else dwk.data_ptr(), None if ws is None else ws.data_ptr(),
+            0 if ws is None else ws.numel(), st), "spkv_norm_rope_backward")
+    return dq, dk, dv if v_grad is not None else None, dwq, dwk
 
 
 _softgate_ws = {}
