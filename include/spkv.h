@@ -64,7 +64,9 @@ enum {
                                    skipped or redirected to a page of the unit's own          */
   SPKV_E_CANARY = -14,          /* SPKV_FLAG_DEBUG_BOUNDS: a canary block between two regions of
                                    the arena no longer holds its pattern                      */
-  SPKV_E_ATTACH = -15           /* spkv_cache_attach: no cache of this configuration in the arena */
+  SPKV_E_ATTACH = -15,          /* spkv_cache_attach: no cache of this configuration in the arena */
+  SPKV_E_FORK = -16             /* device: spkv_seq_fork onto a sequence that is not empty; it was left
+                                   as it is                                                */
 };
 
 typedef struct {
@@ -130,6 +132,11 @@ typedef struct {
  * 256-byte canary blocks that separate the metadata regions of the arena (SPKV_E_CANARY). */
 #define SPKV_FLAG_DEBUG_BOUNDS 4
 
+/* SPKV_FLAG_FORK (off by default): sequences of this cache may share pages (spkv_seq_fork).  Adds 4
+ * bytes per pool page to the arena (an owner count), so it is part of the layout: the flag has
+ * to be given at spkv_cache_attach as it was at creation.  Without it arenas are laid out as ever. */
+#define SPKV_FLAG_FORK 8
+
 /* Utility predictor f of Eq. 1 (the sigmoid is never evaluated: the decision is taken
  * in logit space, u >= tau  <=>  logit >= log(tau/(1-tau))).
  *   kind 0, linear:  logit[h] = <W1[h,:], x> + b1[h]            W1 [n_kv_heads, d_in]
@@ -182,7 +189,7 @@ int spkv_cache_create(const spkv_config_t *cfg, void *d_arena, size_t arena_byte
  * device, to the host, to a file), and a copy placed in device memory again -- at any 256-byte
  * aligned address, in this or a later process -- becomes a cache by attaching to it.
  * spkv_cache_attach checks the header cache_create wrote (magic, layout version, a hash of every
- * configuration field that fixes the layout; tau and flags may differ and take effect as given)
+ * configuration field that fixes the layout; tau and flags other than SPKV_FLAG_FORK may differ and take effect as given)
  * and returns a handle without initialising anything; SPKV_E_ATTACH if the header does not
  * match.  Synchronises `stream`.  Two handles on one arena must not be used at the same time. */
 int spkv_cache_attach(const spkv_config_t *cfg, void *d_arena, size_t arena_bytes,
@@ -228,6 +235,18 @@ int spkv_cache_destroy(spkv_cache_t *cache);
 
 /* Empties every unit of sequence `seq` (all layers) and returns its pages to the pool. */
 int spkv_cache_reset_seq(spkv_cache_t *cache, int32_t seq, spkv_stream_t stream);
+
+/* (No counterpart in the paper.)  Makes the n empty sequences h_dst (HOST array of distinct ids, none of
+ * them src) continuations of sequence src, in every layer: the same positions received, the same
+ * window and the same compact cache.  Full pages of the compact cache are shared, not copied -- they are
+ * never written again; the partly filled last page and the ring are copied -- so each destination
+ * takes one page per unit whose last page is partly filled, and from here on the sequences go their own
+ * ways: any call of this interface works on any of them.  A page returns to the pool when the last
+ * sequence that holds it is reset, in whatever order.  Needs SPKV_FLAG_FORK (SPKV_E_UNSUPPORTED
+ * otherwise).  On the device: a unit of a destination that has received pairs is left as it is
+ * (SPKV_E_FORK), one for which no page is free stays empty (SPKV_E_POOL_EXHAUSTED); after either,
+ * reset the destinations.  Asynchronous on `stream`. */
+int spkv_seq_fork(spkv_cache_t *cache, int32_t src, const int32_t *h_dst, int32_t n, spkv_stream_t stream);
 
 /* Changes tau for all FUTURE evictions (the paper adjusts sparsity a posteriori by
  * changing the threshold; pairs already dropped stay dropped). */
@@ -405,6 +424,35 @@ int spkv_decode_attention_f32(spkv_cache_t *cache, int32_t layer, const int32_t 
 int spkv_decode_attention_static(spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids,
                                  int32_t B, const void *d_q, void *d_out, float *d_lse_opt,
                                  float sm_scale, spkv_stream_t stream);
+
+/* (No counterpart in the paper.)  Decode attention of a batch whose sequences share a prefix: what
+ * spkv_decode_attention computes, but the compact-cache pages that ALL B sequences have in common (they
+ * were forked from one sequence, or from each other) are read once for the whole batch.  The
+ * queries of all sequences and of a KV head's group, B * G rows, attend to those pages on the tensor
+ * cores; each sequence's own pages and ring go through the decode kernel; the parts are joined by
+ * their log-sum-exp weights.  Three launches.
+ *
+ * spkv_share_plan finds the common pages of every (layer, KV head) from the page tables and cuts them into
+ * blocks' shares.  One plan serves every layer and every later step of the same list of sequences.
+ * The attention call checks each unit against the page tables as they are: where a unit no longer
+ * starts with the plan's pages (a sequence was reset, rolled back or replaced) that unit is read in
+ * full, as is everything when the plan was made for another B -- a stale plan costs time, never the
+ * result.  After sequences changed, make a new one.
+ *   d_plan: spkv_share_plan_bytes(cfg) bytes of device memory, 16-byte aligned, filled by spkv_share_plan
+ *   and otherwise left alone (the attention call only reads it: several calls and graphs may share it). */
+size_t spkv_share_plan_bytes(const spkv_config_t *cfg);
+int spkv_share_plan(spkv_cache_t *cache, const int32_t *d_seq_ids, int32_t B, void *d_plan, size_t plan_bytes,
+                    spkv_stream_t stream);
+
+/* Arguments as spkv_decode_attention.  d_workspace: >= spkv_decode_shared_workspace_bytes(cfg, B) bytes, 256-byte
+ * aligned, used by this entry point of this cache only, zero-filled once before its first use; calls
+ * that share it must not overlap on the GPU.  Always ordered after everything earlier on `stream`, also under
+ * SPKV_FLAG_OVERLAP.  Weights times values as in spkv_prefill for the shared pages (SPKV_FLAG_PREFILL_PV_BF16
+ * included), sm_scale positive and finite. */
+size_t spkv_decode_shared_workspace_bytes(const spkv_config_t *cfg, int32_t B);
+int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B,
+                                 const void *d_q, void *d_out, float *d_lse_opt, float sm_scale, const void *d_plan,
+                                 size_t plan_bytes, void *d_workspace, size_t workspace_bytes, spkv_stream_t stream);
 
 /* Workspace bytes spkv_prefill needs for a chunk of C pairs. */
 size_t spkv_prefill_workspace_bytes(const spkv_config_t *cfg, int32_t C);

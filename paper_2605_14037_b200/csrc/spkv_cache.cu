@@ -68,13 +68,15 @@ static void make_layout(const spkv_config_t *c, Layout *l) {
   l->off_sync = region((size_t)c->n_layers * 4 * 8);
   l->off_vmax = region(units * 4);
   l->off_trow = region(units * 4);
+  l->off_extra = (c->flags & SPKV_FLAG_FORK) ? region((size_t)c->pool_pages * 4) : 0;
+  l->n_canaries = n_can;
   o = align_up(o, 1024);
   l->off_pages = o;  o += (units * ring_pages + (size_t)c->pool_pages) * kPageBytes;
   l->total = o;
 }
 
 // What an arena must agree on with a configuration to be attached to: everything that fixes the
-// layout (FNV-1a over the fields; tau and flags are run-time settings and may differ).
+// layout (FNV-1a over the fields; tau and the flags but SPKV_FLAG_FORK are run-time settings and may differ).
 static uint64_t layout_hash(const spkv_config_t *c) {
   const int64_t f[] = {c->n_layers, c->max_seqs, c->n_q_heads, c->n_kv_heads, c->head_dim, c->window,
                        c->page_tokens, c->max_context, c->pool_pages, c->sink_tokens};
@@ -83,6 +85,7 @@ static uint64_t layout_hash(const spkv_config_t *c) {
     for (int b = 0; b < 8; ++b) { h ^= (uint64_t)(v >> (8 * b)) & 0xff; h *= 1099511628211ULL; }
   if (c->h_local_only)   // which heads have no page table is part of the layout
     for (int i = 0; i < c->n_layers * c->n_kv_heads; ++i) { h ^= c->h_local_only[i] ? 1 : 0; h *= 1099511628211ULL; }
+  if (c->flags & SPKV_FLAG_FORK) { h ^= SPKV_FLAG_FORK; h *= 1099511628211ULL; }   // one region more
   return h;
 }
 constexpr uint32_t kMagic = 0x564B5053u;   // "SPKV"
@@ -124,10 +127,31 @@ __global__ void reset_seq_kernel(CacheView c, int seq) {
   const int u = unit_index(c, layer, seq, kvh);
   const int n_pages = (c.len[u] + kP - 1) / kP;
   __shared__ int base;
-  if (threadIdx.x == 0) base = n_pages ? atomicAdd(&c.status[1], n_pages) : 0;
-  __syncthreads();
-  for (int j = threadIdx.x; j < n_pages; j += blockDim.x)   // (n_pages > 0: the unit has a page table)
-    c.free_stack[base + j] = unit_table(c, c.table_row[u])[j];
+  if (c.extra_owners) {
+    // pages that another unit still holds lose an owner, the others go back to the pool
+    const int lane = threadIdx.x & 31;
+    for (int j0 = threadIdx.x - lane; j0 < n_pages; j0 += blockDim.x) {
+      const int j = j0 + lane;
+      int page = -1;
+      if (j < n_pages) page = checked_page(c, unit_table(c, c.table_row[u])[j], -1);
+      bool last = false;
+      if (page >= 0) {
+        int32_t *extra = &c.extra_owners[page - c.n_ring_pages_total];
+        last = atomicSub(extra, 1) == 0;
+        if (last) *extra = 0;
+      }
+      const unsigned mask = __ballot_sync(0xffffffffu, last);
+      int top = 0;
+      if (lane == 0 && mask) top = atomicAdd(&c.status[1], __popc(mask));
+      top = __shfl_sync(0xffffffffu, top, 0);
+      if (last) c.free_stack[top + __popc(mask & ((1u << lane) - 1u))] = page;
+    }
+  } else {
+    if (threadIdx.x == 0) base = n_pages ? atomicAdd(&c.status[1], n_pages) : 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < n_pages; j += blockDim.x)   // (n_pages > 0: the unit has a page table)
+      c.free_stack[base + j] = unit_table(c, c.table_row[u])[j];
+  }
   uint4 *ring = reinterpret_cast<uint4 *>(c.pages + ring_page(c, u, 0) * kPageElems);
   const int n16 = c.ring_pages * (kPageBytes / 16);
   for (int i = threadIdx.x; i < n16; i += blockDim.x) ring[i] = make_uint4(0, 0, 0, 0);
@@ -202,6 +226,7 @@ static int make_handle(const spkv_config_t *cfg, void *d_arena, const Layout &l,
   v.sync_ctr = reinterpret_cast<unsigned long long *>(base + l.off_sync);
   v.vmax = reinterpret_cast<uint32_t *>(base + l.off_vmax);
   v.table_row = reinterpret_cast<int32_t *>(base + l.off_trow);
+  v.extra_owners = (cfg->flags & SPKV_FLAG_FORK) ? reinterpret_cast<int32_t *>(base + l.off_extra) : nullptr;
   v.pages = reinterpret_cast<__nv_bfloat16 *>(base + l.off_pages);
   int dev = 0;
   cudaDeviceProp prop;
@@ -238,7 +263,7 @@ extern "C" int spkv_cache_create(const spkv_config_t *cfg, void *d_arena, size_t
   cudaStream_t s = as_stream(stream);
   // metadata and ring pages start at zero; pool pages are zeroed when first allocated
   cudaError_t e = cudaMemsetAsync(base, 0, l.off_pages + (size_t)v.n_ring_pages_total * kPageBytes, s);
-  for (int i = 0; i < kCanaries && e == cudaSuccess; ++i)
+  for (int i = 0; i < l.n_canaries && e == cudaSuccess; ++i)
     e = cudaMemsetAsync(base + l.canary[i], kCanaryByte, kCanaryBytes, s);
   if (e == cudaSuccess) {
     // what spkv_cache_attach recognises the arena by (pageable host source: copied before the call returns)
@@ -331,8 +356,8 @@ extern "C" int spkv_arena_canaries(const spkv_config_t *cfg, size_t *h_offsets, 
   if (rc) return rc;
   Layout l;
   make_layout(cfg, &l);
-  if (n_out) *n_out = kCanaries;
-  for (int i = 0; h_offsets && i < kCanaries && i < cap; ++i) h_offsets[i] = l.canary[i];
+  if (n_out) *n_out = l.n_canaries;
+  for (int i = 0; h_offsets && i < l.n_canaries && i < cap; ++i) h_offsets[i] = l.canary[i];
   return SPKV_OK;
 }
 
@@ -458,7 +483,7 @@ extern "C" int spkv_status(spkv_cache_t *cache, spkv_stream_t stream) {
   if (st == SPKV_OK && (cache->cfg.flags & SPKV_FLAG_DEBUG_BOUNDS)) {
     // the canary blocks between the metadata regions must still hold their pattern
     unsigned char blk[kCanaryBytes];
-    for (int i = 0; i < kCanaries; ++i) {
+    for (int i = 0; i < cache->layout.n_canaries; ++i) {
       if (cudaMemcpy(blk, static_cast<char *>(cache->arena) + cache->layout.canary[i], kCanaryBytes,
                      cudaMemcpyDeviceToHost) != cudaSuccess)
         return SPKV_E_CUDA;
@@ -599,6 +624,7 @@ extern "C" int spkv_cache_stats(spkv_cache_t *cache, spkv_stream_t stream, spkv_
       if (lg[(size_t)u * v.w + s] >= thr) out->gates_open++;
   }
   out->pages_free = hdr[1];
+  if (v.extra_owners) out->pages_in_use = v.pool_pages - hdr[1];   // (a page that several units hold counts once)
   out->bytes_resident = (out->pairs_kept + out->pairs_in_window) * 2 * kRowBytes;
   out->density_all = out->pairs_seen ? (double)out->gates_open / (double)out->pairs_seen : 0.0;
   out->density_cache = out->pairs_evicted ? (double)out->pairs_kept / (double)out->pairs_evicted : 0.0;
@@ -622,6 +648,7 @@ extern "C" const char *spkv_error_string(int code) {
     case SPKV_E_ORDER_APPEND: return "overlap mode: append gave up waiting for its layer's decode launches";
     case SPKV_E_BOUNDS_PAGE: return "debug bounds: page index outside the pool";
     case SPKV_E_CANARY: return "debug bounds: a canary block between arena regions was overwritten";
+    case SPKV_E_FORK: return "fork destination is not empty";
     case SPKV_E_ATTACH: return "arena does not hold a cache of this configuration";
     default: return "unknown error";
   }

@@ -14,6 +14,7 @@
 //   vmax[]      : largest finite |value| in a unit's compact cache u32 [n_units] (fp32 bit pattern)
 //   sync_ctr[]  : blocks started / finished per layer and kernel u64   [L][4]    (launch overlap)
 //   table_row[] : row of a unit in table[], -1 = none            int32 [n_units]
+//   extra_owners[]: units beyond the first that hold a pool page  int32 [pool_pages]   (SPKV_FLAG_FORK only)
 //   pages       : ring pages of every unit ([n_units][ring_pages]) followed by the pool
 //
 // A page holds P = 64 pairs: a 16 KB key block followed by a 16 KB value block.  Each
@@ -61,17 +62,19 @@ struct CacheView {
   // multiplies P.V in fp16 after scaling the values by a power of two; it takes that factor from
   // the largest |v| its queries can see: this word, the ring and the chunk.
   uint32_t *vmax;
+  int32_t *extra_owners;  // [pool_pages] units beyond the first whose page table holds the page; null without SPKV_FLAG_FORK
   __nv_bfloat16 *pages;
 };
 
-constexpr int kCanaries = 11;          // one 256-byte block after each metadata region
+constexpr int kMaxCanaries = 12;       // one 256-byte block after each metadata region (the last one with SPKV_FLAG_FORK only)
 constexpr int kCanaryBytes = 256;
 constexpr unsigned char kCanaryByte = 0xC5;
 struct Layout {
   size_t off_header, off_t, off_len, off_table, off_free, off_pos, off_rlogit, off_htau, off_sync, off_vmax, off_trow,
-      off_pages, total;
+      off_extra, off_pages, total;
   size_t n_table_rows;
-  size_t canary[kCanaries];
+  int n_canaries;
+  size_t canary[kMaxCanaries];
 };
 
 // largest finite |x| among the eight bf16 of a 16-byte chunk, as the upper half of an fp32 bit

@@ -138,20 +138,6 @@ __device__ inline WalkSlots walk_slots(const PrefillArgs &a, int walk) {
   }
   return w;
 }
-// Is the unit "wide" (two-term bf16 P.V), and otherwise the power of two that brings the largest
-// visible |v| into [2^14, 2^15), with its inverse.  vm: fp32 bit pattern of that largest |v|.
-constexpr uint32_t kWideFrom = 0x49800000u;   // 2^20
-__device__ inline bool value_scale(uint32_t vm, int force_wide, float &v_scale, float &v_unscale) {
-  v_scale = v_unscale = 1.f;
-  if (force_wide || vm >= kWideFrom) return true;
-  if (vm) {
-    const int k = min(14 - ((int)(vm >> 23) - 127), 126);
-    v_scale = __int_as_float((127 + k) << 23);
-    v_unscale = __int_as_float((127 - k) << 23);
-  }
-  return false;
-}
-
 // Pages of a walk: the compact-cache pages its last query sees (*n_ptiles), then the band pages
 // sp_lo ... of the staging area; the soft-gated forward walks every page from the start.
 template <bool kSoft>

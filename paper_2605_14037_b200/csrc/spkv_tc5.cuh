@@ -172,4 +172,19 @@ __device__ inline void tmem_st16u(uint32_t taddr, const uint32_t (&r)[16]) {
 }
 
 }  // namespace tc5
+
+// Is the unit "wide" (two-term bf16 P.V), and otherwise the power of two that brings the largest
+// visible |v| into [2^14, 2^15), with its inverse.  vm: fp32 bit pattern of that largest |v|.
+constexpr uint32_t kWideFrom = 0x49800000u;   // 2^20
+__device__ inline bool value_scale(uint32_t vm, int force_wide, float &v_scale, float &v_unscale) {
+  v_scale = v_unscale = 1.f;
+  if (force_wide || vm >= kWideFrom) return true;
+  if (vm) {
+    const int k = min(14 - ((int)(vm >> 23) - 127), 126);
+    v_scale = __int_as_float((127 + k) << 23);
+    v_unscale = __int_as_float((127 - k) << 23);
+  }
+  return false;
+}
+
 }  // namespace spkv

@@ -24,13 +24,14 @@ ERRORS = {
     -1: "SPKV_E_INVALID", -2: "SPKV_E_ARENA_TOO_SMALL", -3: "SPKV_E_UNSUPPORTED", -4: "SPKV_E_CUDA",
     -5: "SPKV_E_POOL_EXHAUSTED", -6: "SPKV_E_CONTEXT_OVERFLOW", -7: "SPKV_E_WORKSPACE",
     -8: "SPKV_E_TIMEOUT", -9: "SPKV_E_BOUNDS", -10: "SPKV_E_SCRATCH_LIMIT", -11: "SPKV_E_ORDER_DECODE",
-    -12: "SPKV_E_ORDER_APPEND", -13: "SPKV_E_BOUNDS_PAGE", -14: "SPKV_E_CANARY", -15: "SPKV_E_ATTACH",
+    -12: "SPKV_E_ORDER_APPEND", -13: "SPKV_E_BOUNDS_PAGE", -14: "SPKV_E_CANARY", -15: "SPKV_E_ATTACH", -16: "SPKV_E_FORK",
 }
 
 
 FLAG_OVERLAP = 1          # SPKV_FLAG_OVERLAP
 FLAG_PREFILL_PV_BF16 = 2  # SPKV_FLAG_PREFILL_PV_BF16
 FLAG_DEBUG_BOUNDS = 4      # SPKV_FLAG_DEBUG_BOUNDS
+FLAG_FORK = 8              # SPKV_FLAG_FORK
 
 
 class Config(C.Structure):
@@ -120,6 +121,11 @@ def lib():
         "spkv_wait_selftest": (C.c_int, [vp, C.c_longlong, vp, vp]),
         "spkv_decode_attention_f32": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, vp, f32, vp, sz, vp]),
         "spkv_decode_attention_static": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, f32, vp]),
+        "spkv_seq_fork": (C.c_int, [vp, i32, vp, i32, vp]),
+        "spkv_share_plan_bytes": (sz, [cfgp]),
+        "spkv_share_plan": (C.c_int, [vp, vp, i32, vp, sz, vp]),
+        "spkv_decode_shared_workspace_bytes": (sz, [cfgp, i32]),
+        "spkv_decode_attention_shared": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, f32, vp, sz, vp, sz, vp]),
         "spkv_prefill_workspace_bytes": (sz, [cfgp, i32]),
         "spkv_prefill": (C.c_int, [vp, i32, i32, i32, vp, vp, vp, vp, vp, f32, vp, sz, vp]),
         "spkv_rope_init": (C.c_int, [vp, i32, i32, i32, f32, vp, vp]),
@@ -356,6 +362,31 @@ class Cache:
             "spkv_decode_attention_static")
         return out
 
+    def spkv_share_plan(self, seq_ids, plan=None, stream=None):
+        """The plan a batch with a common prefix decodes by (a device tensor; one for all layers and steps of
+        the same sequences)."""
+        if plan is None:
+            plan = torch.zeros(lib().spkv_share_plan_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=self.device)
+        _check(lib().spkv_share_plan(self._h, _ptr(seq_ids, torch.int32), seq_ids.numel(), _ptr(plan, torch.uint8),
+                                     plan.numel(), _stream(stream)), "spkv_share_plan")
+        return plan
+
+    def spkv_decode_attention_shared(self, layer, seq_ids, q, plan, out=None, lse=None, sm_scale=None, want_lse=False,
+                                     stream=None):
+        """spkv_decode_attention with the pages that all sequences have in common read once for the batch.
+        Returns out, or (out, lse) with want_lse."""
+        B = seq_ids.numel()
+        if out is None:
+            out = torch.empty_like(q)
+        if want_lse and lse is None:
+            lse = torch.empty((B, self.cfg.n_q_heads), dtype=torch.float32, device=q.device)
+        ws = self._workspace("decode_shared", lib().spkv_decode_shared_workspace_bytes(C.byref(self.cfg), B))
+        _check(lib().spkv_decode_attention_shared(
+            self._h, layer, _ptr(seq_ids, torch.int32), B, _ptr(q, torch.bfloat16), _ptr(out, torch.bfloat16),
+            _ptr(lse, torch.float32), self.default_scale if sm_scale is None else sm_scale, _ptr(plan, torch.uint8),
+            plan.numel(), _ptr(ws), ws.numel(), _stream(stream)), "spkv_decode_attention_shared")
+        return (out, lse) if want_lse else out
+
     def spkv_prefill(self, layer, seq, k, v, logits, q=None, out=None, sm_scale=None, stream=None):
         Cn = k.shape[0]
         if q is not None and out is None:
@@ -431,6 +462,13 @@ class Cache:
     # -- maintenance / introspection ---------------------------------------------------
     def spkv_cache_reset_seq(self, seq, stream=None):
         _check(lib().spkv_cache_reset_seq(self._h, seq, _stream(stream)), "spkv_cache_reset_seq")
+
+    def spkv_seq_fork(self, src, dst, stream=None):
+        """Makes the empty sequences `dst` (host ints) continuations of sequence src (FLAG_FORK caches)."""
+        import numpy as np
+        ids = np.ascontiguousarray(np.asarray(list(dst), dtype=np.int32))
+        _check(lib().spkv_seq_fork(self._h, int(src), ids.ctypes.data if ids.size else None, int(ids.size),
+                                   _stream(stream)), "spkv_seq_fork")
 
     def spkv_set_tau(self, tau):
         _check(lib().spkv_set_tau(self._h, tau), "spkv_set_tau")
