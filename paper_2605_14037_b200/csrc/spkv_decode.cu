@@ -55,7 +55,6 @@
 
 #include "spkv_decode_common.cuh"
 #include "spkv_mma.cuh"
-#include "spkv_share.cuh"
 
 namespace spkv {
 
@@ -99,25 +98,9 @@ __device__ inline unsigned long long gtimer() {
 #define SPKV_STAMP_T(i, cond)
 #endif
 
-// Common pages of a batch with a shared prefix that this unit (page-table row trow, length len) leaves to
-// the prefix kernel: the plan's count for its KV head, if the unit's table and that of the batch's first
-// sequence still name the same page there (then all pages before it agree too); 0 otherwise.
-__device__ inline int shared_pages_of(const CacheView &c, const SharedDecode &sd, int layer, int B, int seq0, int kvh,
-                                      int trow, int len) {
-  if (__ldcg(sd.plan) != B || __ldcg(sd.plan + 1) != c.L || __ldcg(sd.plan + 2) != c.Hkv) return 0;
-  const int n = min(__ldcg(share_record(sd.plan, c.Hkv, layer) + kShareHdr + kvh), c.max_pages);
-  if (n <= 0 || trow < 0 || len / kP < n || seq0 < 0 || seq0 >= c.S) return 0;
-  const int u0 = unit_index(c, layer, seq0, kvh), row0 = unit_table_row(c, u0);
-  if (row0 < 0 || ldcg_keep(&c.len[u0]) / kP < n) return 0;
-  return ldcg_keep(&unit_table(c, trow)[n - 1]) == ldcg_keep(&unit_table(c, row0)[n - 1]) ? n : 0;
-}
-
-// kShared: the launch behind a prefix kernel (spkv_decode_shared.cu).  A unit starts behind the pages it
-// leaves to that kernel.  Everything before the prefix launch is complete when this one starts; the prefix
-// launch itself, which this one does not read, is waited for at the end.
-template <int NH, bool kShared = false>  // NH: 8-head tiles on the N side: 1 for G <= 8, 2 for G <= 16
+template <int NH>  // 8-head tiles on the N side: 1 for G <= 8, 2 for G <= 16
 __global__ void __launch_bounds__(kTcThreads, 1)
-decode_tc_kernel(DecodeArgs a, int GP, int n_stages, int red_bufs, SharedDecode sd) {
+decode_tc_kernel(DecodeArgs a, int GP, int n_stages, int red_bufs) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
   const int n = a.n_items;
@@ -174,16 +157,15 @@ decode_tc_kernel(DecodeArgs a, int GP, int n_stages, int red_bufs, SharedDecode 
   // beside the counter reads below.
   int seq_first = -1;
   if (a.wait_mode == 1 && tid < n) seq_first = a.seq_ids[tid / c.Hkv];
-  if (!kShared && a.wait_mode == 0) pdl_wait();
+  if (a.wait_mode == 0) pdl_wait();
   // (the counter reads run beside thread 32's count-in: one trip to L2 for both)
   if (a.wait_mode == 1 && tid == 0 &&
       !sync_wait_finished(c, a.layer, kSyncAppStart, a.prev_half_layer, kSyncDecStart))
     set_status(c, SPKV_E_ORDER_DECODE);
   __syncthreads();  // the block is counted in before any of its threads lets dependents launch
   pdl_trigger();
-  if (kShared || a.wait_mode == 1)
+  if (a.wait_mode == 1)
     asm volatile("fence.proxy.async;" ::: "memory");  // the appends wrote the pages the bulk copies read
-  unsigned left_out = 0;   // kShared: which of this thread's units (n <= 1024: at most 4) leave their first pages out
   for (int i = tid; i < n; i += kTcThreads) {
     const int b = i / c.Hkv, kvh = i % c.Hkv;
     const int seq = (a.wait_mode == 1 && i == tid) ? seq_first : a.seq_ids[b];
@@ -195,16 +177,9 @@ decode_tc_kernel(DecodeArgs a, int GP, int n_stages, int red_bufs, SharedDecode 
       // and an SM's L1 is not coherent with other SMs' stores)
       len = ldcg_keep(&c.len[u]);
       n_ring = min(ldcg_keep(&c.t[u]), c.w);
-      if (kShared) {
-        const int skip = shared_pages_of(c, sd, a.layer, a.B, a.seq_ids[0], kvh, trow, len);
-        if (skip) left_out |= 1u << (i / kTcThreads);
-        len -= skip * kP;
-        if (blockIdx.x == 0) sd.item_skip[i] = skip;
-      }
       np = (len + kP - 1) / kP + (n_ring + kP - 1) / kP;
     } else if (blockIdx.x == 0) {
       set_status(c, SPKV_E_BOUNDS);
-      if (kShared) sd.item_skip[i] = 0;
     }
     s_np[i] = np > 0 ? np + 1 : 0;  // + the marker position
     s_unit[i] = u; s_len[i] = len; s_ring[i] = n_ring; s_row[i] = trow;
@@ -220,10 +195,6 @@ decode_tc_kernel(DecodeArgs a, int GP, int n_stages, int red_bufs, SharedDecode 
   }
   __syncthreads();
   block_exclusive_scan(s_np, s_pre, n, s_tmp);
-  if (kShared)   // s_np has done its duty: from here on it holds the pages a unit leaves out
-    for (int i = tid; i < n; i += kTcThreads)
-      s_np[i] = (left_out >> (i / kTcThreads)) & 1
-                    ? min(__ldcg(share_record(sd.plan, c.Hkv, a.layer) + kShareHdr + i % c.Hkv), c.max_pages) : 0;
   const int VP = s_pre[n];
   // Blocks per launch.  A small launch is latency-bound: as many blocks as have four positions
   // each (tiny calls would otherwise be cut into single pages and spend their time merging).
@@ -266,7 +237,7 @@ decode_tc_kernel(DecodeArgs a, int GP, int n_stages, int red_bufs, SharedDecode 
           const int u = s_unit[item], len = s_len[item], nk = (len + kP - 1) / kP;
           if (j < nk) {
             // (debug bounds: a table entry that names no pool page is read from the unit's ring instead)
-            gq.gpage = checked_page(c, ldcg_keep(&unit_table(c, s_row[item])[kShared ? s_np[item] + j : j]), (int)ring_page(c, u, 0));
+            gq.gpage = checked_page(c, ldcg_keep(&unit_table(c, s_row[item])[j]), (int)ring_page(c, u, 0));
             gq.valid = min(kP, len - j * kP);
           } else {
             gq.gpage = (int)ring_page(c, u, j - nk);
@@ -423,7 +394,6 @@ decode_tc_kernel(DecodeArgs a, int GP, int n_stages, int red_bufs, SharedDecode 
     { unsigned smid; asm volatile("mov.u32 %0, %%smid;" : "=r"(smid)); dbg[blockIdx.x * 16 + 15] = smid; }
   }
 #endif
-  if (kShared) pdl_wait();   // the merge behind this launch reads the prefix launch's parts too
   __syncthreads();
   if (tid == 0) sync_count_finish(c, a.layer, kSyncDecFin);
   SPKV_STAMP_T(5, tid == 0);
@@ -439,8 +409,7 @@ extern "C" size_t spkv_decode_workspace_bytes(const spkv_config_t *cfg, int32_t 
 }
 
 // Argument checks of a decode call that need no workspace (B > 0 on SPKV_OK with *empty = false).
-namespace spkv {
-int decode_check_args(const spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B,
+int spkv::decode_check_args(const spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B,
                              const void *d_q, const void *d_out, const float *d_out_f32, bool *empty) {
   *empty = false;
   if (!cache || layer < 0 || layer >= cache->cfg.n_layers || B < 0 || B > cache->cfg.max_seqs)
@@ -451,12 +420,10 @@ int decode_check_args(const spkv_cache_t *cache, int32_t layer, const int32_t *d
   if (B * cache->view.Hkv > 1024) return SPKV_E_UNSUPPORTED;
   return SPKV_OK;
 }
-}  // namespace spkv
 
 static int decode_attention_impl(spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B,
                                  const void *d_q, void *d_out, float *d_out_f32, float *d_lse_opt, float sm_scale,
-                                 void *d_workspace, size_t workspace_bytes, spkv_stream_t stream,
-                                 const SharedDecode *sd = nullptr) {
+                                 void *d_workspace, size_t workspace_bytes, spkv_stream_t stream) {
   bool empty;
   const int rc_args = decode_check_args(cache, layer, d_seq_ids, B, d_q, d_out, d_out_f32, &empty);
   if (rc_args || empty) return rc_args;
@@ -517,24 +484,14 @@ static int decode_attention_impl(spkv_cache_t *cache, int32_t layer, const int32
   TcSmem L = tc_smem_layout(n_items, GP, n_stages, red_bufs);
   while (L.total > limit && n_stages > 2) L = tc_smem_layout(n_items, GP, --n_stages, red_bufs);
   if (L.total > limit) return SPKV_E_UNSUPPORTED;
-  void (*kernel)(DecodeArgs, int, int, int, SharedDecode) =
-      sd ? (GP > 8 ? decode_tc_kernel<2, true> : decode_tc_kernel<1, true>)
-         : (GP > 8 ? decode_tc_kernel<2> : decode_tc_kernel<1>);
+  void (*kernel)(DecodeArgs, int, int, int) = GP > 8 ? decode_tc_kernel<2> : decode_tc_kernel<1>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L.total) != cudaSuccess)
     return SPKV_E_CUDA;
   const int grid = min(kMaxGrid, cache->sm_count);
   // (a programmatic dependent launch in every mode: with wait_mode 0 the kernel runs only its
   // block-local prologue before griddepcontrol.wait orders it after everything earlier on the stream)
   return check_stream_error(
-      launch_overlapped(kernel, dim3(grid), dim3(kTcThreads), (size_t)L.total, s, a, GP, n_stages, red_bufs,
-                        sd ? *sd : SharedDecode{}));
-}
-
-int spkv::decode_suffix(spkv_cache *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B, const void *d_q, void *d_out,
-                        float *d_out_f32, float *d_lse, float sm_scale, void *d_workspace, size_t workspace_bytes,
-                        const SharedDecode &sd, spkv_stream_t stream) {
-  return decode_attention_impl(cache, layer, d_seq_ids, B, d_q, d_out, d_out_f32, d_lse, sm_scale, d_workspace,
-                               workspace_bytes, stream, &sd);
+      launch_overlapped(kernel, dim3(grid), dim3(kTcThreads), (size_t)L.total, s, a, GP, n_stages, red_bufs));
 }
 
 extern "C" int spkv_decode_attention(spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids,

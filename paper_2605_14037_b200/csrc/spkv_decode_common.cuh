@@ -455,6 +455,9 @@ __device__ inline void finish_segment(const CacheView &c, int G, int GP, const S
   }
 }
 
+int decode_check_args(const spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B, const void *d_q,
+                      const void *d_out, const float *d_out_f32, bool *empty);
+
 struct DecodeWs {
   size_t off_gcnt, off_ml, off_acc, total;
 };

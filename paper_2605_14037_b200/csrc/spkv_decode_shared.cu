@@ -1,15 +1,17 @@
 // Decode attention of a batch whose sequences share a prefix (spkv_decode_attention_shared).
 //
 // Three launches:
-//   prefix  (here)  the compact-cache pages that all sequences have in common, once for the batch: the
-//           B * G query rows of a KV head are the M side of tcgen05 tiles, a block takes 128 or 256 of
-//           them over one share of the head's common pages and leaves (m, l, O) per row;
-//   suffix  (spkv_decode.cu)  the decode kernel over what is left of every unit: its own pages and ring;
-//   merge   (here)  joins a row's parts by their log-sum-exp weights.
-// The suffix launch does not depend on the prefix launch and starts on every SM as the prefix block there
-// leaves (programmatic dependent launch; the prefix kernel has waited for everything earlier on the
-// stream before it lets dependents start); it waits for the prefix launch at its own end, so that
-// the merge, which waits for the suffix, may read both.
+//   prefix  the compact-cache pages that all sequences have in common, once for the batch: the B * G query
+//           rows of a KV head are the M side of tcgen05 tiles, a block takes 128 or 256 of them over one
+//           share of the head's common pages and leaves (m, l, O) per row;
+//   tail    what is left of every unit, its own pages and its ring: one small block per unit (several for a long
+//           one), mma.sync tiles of the unit's G query heads as in the decode kernel; leaves (m, l, O) too;
+//   merge   joins a row's parts by their log-sum-exp weights.
+// The tail does not depend on the prefix launch.  Its blocks are small (4 warps, two page stages), so that
+// one fits on an SM beside a prefix block of up to 128 rows, and are launched as programmatic
+// dependents: the prefix kernel has waited for everything earlier on the stream before it lets them start.
+// The tail waits for the prefix launch at its own end, so that the merge, which waits for the tail,
+// may read both.
 //
 // Prefix kernel.  Per page and 128-row slot: S = Q K^T (8 MMAs M128 N64 K16 into tensor memory), softmax
 // in registers (thread = row = TMEM lane), P in fp16 back over the scores, O += P V with the page's values
@@ -20,14 +22,13 @@
 //   * At most 128 rows (kAlt): both slots hold the same rows and take alternate pages, which halves the
 //     softmax time per page; scores of a slot's next page are issued behind P.V of its last one.  One of the two
 //     is joined into the other through shared memory at the end.
-// Shared memory: Q (64 KB; kAlt 32 KB) + 5 (6) page stages.  Tensor memory: score buffer b of slot h at
+// Shared memory: Q (64 KB; kAlt 32 KB) + 5 (4, which leaves room for a tail block) page stages.  Tensor memory: score buffer b of slot h at
 // [64 (2h + b), +64), O of slot h at [256 + 128 h, +128).
-// Warps: 0 MMA issue slot 0, 1 page loader + TMEM, 2-3 value conversion, 4-7 / 8-11 softmax of slot 0 / 1,
+// Warps: 0 MMA issue slot 0, 1 page loader, 2-3 value conversion (2: tensor memory), 4-7 / 8-11 softmax of slot 0 / 1,
 // 12 MMA issue slot 1.  All waits are bounded.
 #include <algorithm>
 #include <math.h>
 
-#include "spkv_decode_common.cuh"
 #include "spkv_share.cuh"
 #include "spkv_tc5.cuh"
 
@@ -35,11 +36,11 @@ namespace spkv {
 
 namespace shp {
 constexpr int kThreads = 416;
-constexpr int kMmaWarp0 = 0, kMmaWarp1 = 12, kLoaderWarp = 1;
+constexpr int kMmaWarp0 = 0, kMmaWarp1 = 12, kLoaderWarp = 1, kTmemWarp = 2;
 constexpr int kTmemCols = 512, kConvThreads = 64;
 constexpr float kPBias = 7.f;   // P is stored as 2^7 p
 enum { B_KV_FULL = 0, B_KV_EMPTY = 8, B_V_READY = 16, B_S_FULL = 24 /* [2h+b] */, B_P_FULL = 28, B_O_DONE = 32, B_COUNT = 36 };
-__host__ __device__ constexpr int stages(bool alt) { return alt ? 6 : 5; }
+__host__ __device__ constexpr int stages(bool alt) { return alt ? 4 : 5; }
 __host__ __device__ constexpr int off_kv(bool alt) { return alt ? 32768 : 65536; }
 __host__ __device__ constexpr int off_bar(bool alt) { return off_kv(alt) + stages(alt) * kPageBytes; }
 __host__ __device__ constexpr int smem_bytes(bool alt) { return off_bar(alt) + 512; }
@@ -48,24 +49,35 @@ constexpr int kJoinStride = 132;   // floats per row of the hand-over between th
 
 struct SharedArgs {
   CacheView c;
-  int layer, B, n_tiles, rows_per_block;
+  int layer, B, n_items, n_tiles, rows_per_block, sig;
   const int32_t *seq_ids;
   const __nv_bfloat16 *q;       // [B][Hq][128]
+  const int32_t *rec;           // the layer's record of the plan
   const int32_t *plan;
   float scale_log2;
   int force_wide;
-  float *part_o, *part_ml;      // [block][rows_per_block][128], [block][rows_per_block][2]: m (log2 domain), l
+  float *part_o, *part_ml;      // prefix: [block][rows_per_block][128], [block][rows_per_block][2]: m (log2 domain), l
   int max_blocks;
-  // merge
-  const float *suf_o, *suf_lse;       // [B * Hq][128], [B * Hq]
-  const int32_t *item_skip;           // [B * Hkv] common pages the suffix left out (0: it read the unit in full)
+  float *tail_o, *tail_ml;      // tail: [share][item][G][128], [share][item][G][2]
+  int max_tail;                 // shares the workspace holds
+  int32_t *item_skip;           // [n_items] common pages the tail left out (0: it read the unit in full)
   __nv_bfloat16 *out;
   float *lse;
 };
 
-// A plan that was made for this batch size and configuration
-__device__ inline bool plan_fits(const CacheView &c, const int32_t *plan, int B) {
-  return __ldcg(plan) == B && __ldcg(plan + 1) == c.L && __ldcg(plan + 2) == c.Hkv;
+__device__ inline int4 ldcg4(const int32_t *p) { return __ldcg(reinterpret_cast<const int4 *>(p)); }
+
+// page j of a share into its stage (one thread)
+template <bool kAlt>
+__device__ inline void load_page(const SharedArgs &a, unsigned char *smem, uint64_t *bar, int j, int gp, uint64_t pol) {
+  using namespace shp;
+  const int s = j % stages(kAlt);
+  unsigned char *dst = smem + off_kv(kAlt) + s * kPageBytes;
+  const __nv_bfloat16 *src = a.c.pages + (int64_t)gp * kPageElems;
+  mbar_arrive_expect_tx(&bar[B_KV_FULL + s], kPageBytes);
+  // a page that several row tiles read stays in L2 for the others
+  if (a.n_tiles == 1) bulk_load_hint(dst, src, kPageBytes, &bar[B_KV_FULL + s], pol);
+  else bulk_load(dst, src, kPageBytes, &bar[B_KV_FULL + s]);
 }
 
 template <bool kAlt>
@@ -79,43 +91,12 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
   uint64_t *bar = reinterpret_cast<uint64_t *>(smem + off_bar(kAlt));
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bar + B_COUNT);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  pdl_wait();
-  pdl_trigger();   // (only now: what follows may then rely on everything before this launch)
-  // ---- this block's share
-  const int32_t *rec = share_record(a.plan, c.Hkv, a.layer);
-  if (!plan_fits(c, a.plan, a.B)) return;
-  const int per_share = max(1, __ldcg(rec)), n_blocks = min(__ldcg(rec + 1), a.max_blocks);
-  if ((int)blockIdx.x >= n_blocks) return;
-  int kvh = 0;
-  {
-    int lo = 0, hi = c.Hkv;   // last head whose first block is <= this one
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (__ldcg(rec + kShareHdr + c.Hkv + mid) <= (int)blockIdx.x) lo = mid; else hi = mid;
-    }
-    kvh = lo;
-    while (kvh > 0 && __ldcg(rec + kShareHdr + kvh) == 0) --kvh;   // (heads without common pages start where the next one does)
-  }
-  const int common = min(__ldcg(rec + kShareHdr + kvh), c.max_pages);
-  const int rem = (int)blockIdx.x - __ldcg(rec + kShareHdr + c.Hkv + kvh);
-  const int tile = rem % a.n_tiles, share = rem / a.n_tiles;
-  const int seq0 = a.seq_ids[0];
-  if (common <= 0 || rem < 0 || seq0 < 0 || seq0 >= c.S) return;
-  const int u = unit_index(c, a.layer, seq0, kvh), trow = unit_table_row(c, u);
-  // (stale plan: the unit is shorter by now; nobody reads this share's result)
-  if (trow < 0 || ldcg_keep(&c.len[u]) / kP < common) return;
-  const int j_begin = share * per_share, n_pages = min(per_share, common - j_begin);
-  if (n_pages <= 0) return;
-  const int rows_all = a.B * c.G, row_base = tile * kShareRows;
-  const int n_rows = min(kShareRows, rows_all - row_base);
-  const bool two = kAlt ? n_pages > 1 : n_rows > 128;     // is slot 1 in use
-  float v_scale, v_unscale;
-  const bool wide = value_scale(__ldcg(&c.vmax[u]), a.force_wide, v_scale, v_unscale);
-
-  if (tid == 0) {
+  volatile int *s_desc = reinterpret_cast<volatile int *>(tmem_slot + 1);   // [8] descriptor, [8] share is valid, [9] vmax
+  // ---- block-local set-up, then this block's share.  The loader warp goes ahead: descriptor (one trip to
+  // memory), page-table entries (the second), first pages; the others load Q meanwhile.
+  if (warp == kLoaderWarp && lane == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&bar[B_KV_FULL + i], 1);
-      mbar_init(&bar[B_KV_EMPTY + i], (!kAlt && two) ? 2 : 1);   // one commit per MMA warp that uses the page
       mbar_init(&bar[B_V_READY + i], kConvThreads);
     }
     // per slot and parity of the slot's page count: one phase per two of its pages
@@ -124,55 +105,91 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
       mbar_init(&bar[B_P_FULL + i], 128);
       mbar_init(&bar[B_O_DONE + i], 1);
     }
-    mbar_fence_init();
   }
-  // Q rows -> two slabs of 128 rows x 128 B per slot, 128-byte swizzle; rows past the last are zero
-  for (int x = tid; x < (kAlt ? 1 : 2) * 128 * 16; x += kThreads) {
-    const int h = x >> 11, r = (x >> 4) & 127, ch = x & 15;
-    const int R = row_base + h * 128 + r;
-    uint4 val = make_uint4(0, 0, 0, 0);
-    if (h * 128 + r < n_rows) {
-      const int b = R / c.G, g = R - b * c.G;
-      val = *reinterpret_cast<const uint4 *>(a.q + ((size_t)b * c.Hq + kvh * c.G + g) * kD + ch * 8);
-    }
-    *reinterpret_cast<uint4 *>(smem + h * 32768 + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val;
-  }
-  fence_async_smem();
+  pdl_wait();
+  pdl_trigger();   // (only now: what follows may then rely on everything before this launch)
   if (warp == kLoaderWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
-                 "n"(kTmemCols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    const int32_t *dp = share_desc(c, a.rec, blockIdx.x);
+    if (lane < 8) s_desc[lane] = __ldcg(dp + lane);
+    __syncwarp();
+    // one commit per MMA warp that uses a page
+    if (lane == 0) {
+      const int left = a.B * c.G - s_desc[1] * kShareRows;
+      for (int i = 0; i < kStages; ++i) mbar_init(&bar[B_KV_EMPTY + i], (!kAlt && left > 128) ? 2 : 1);
+      mbar_fence_init();
+    }
+  }
+  __syncthreads();
+  const int kvh = s_desc[0], tile = s_desc[1], j_begin = s_desc[2], n_pages = s_desc[3];
+  const int common = s_desc[4], trow = s_desc[5], u = s_desc[6];
+  const int row_base = tile * kShareRows, n_rows = min(kShareRows, a.B * c.G - row_base);
+  // (no work, another batch's plan, or not a plan at all)
+  if (n_pages <= 0 || s_desc[7] != a.sig || kvh < 0 || kvh >= c.Hkv || n_rows <= 0 || j_begin < 0 ||
+      j_begin + n_pages > min(common, c.max_pages) || u < 0 || u >= c.n_units || trow < 0 || trow >= c.n_units)
+    return;
+  const bool two = kAlt ? n_pages > 1 : n_rows > 128;     // is slot 1 in use
+  uint64_t pol = 0;
+  int first_entry = 0;
+  if (warp == kLoaderWarp) {
+    pol = l2_evict_first_policy();
+    const int len = ldcg_keep(&c.len[u]);
+    const uint32_t vm = __ldcg(&c.vmax[u]);
+    if (lane < n_pages) first_entry = ldcg_keep(&unit_table(c, trow)[j_begin + lane]);
+    // (stale plan: the unit is shorter by now; the tail sees the same and nobody reads this share's result)
+    const bool valid = len / kP >= common;
+    if (valid) first_entry = checked_page(c, first_entry, (int)ring_page(c, u, 0));
+    for (int j = 0; j < min(n_pages, kStages) && valid; ++j) {
+      const int gp = __shfl_sync(0xffffffffu, first_entry, j);
+      if (lane == 0) load_page<kAlt>(a, smem, bar, j, gp, pol);
+    }
+    if (lane == 0) { s_desc[8] = valid; s_desc[9] = (int)vm; }
+  } else {
+    // Q rows -> two slabs of 128 rows x 128 B per slot, 128-byte swizzle; rows past the last are zero
+    const int qt = warp == 0 ? lane : tid - 32;   // the threads but for the loader warp
+    for (int x = qt; x < (kAlt ? 1 : 2) * 128 * 16; x += kThreads - 32) {
+      const int h = x >> 11, r = (x >> 4) & 127, ch = x & 15;
+      const int R = row_base + h * 128 + r;
+      uint4 val = make_uint4(0, 0, 0, 0);
+      if (h * 128 + r < n_rows) {
+        const int b = R / c.G, g = R - b * c.G;
+        val = *reinterpret_cast<const uint4 *>(a.q + ((size_t)b * c.Hq + kvh * c.G + g) * kD + ch * 8);
+      }
+      *reinterpret_cast<uint4 *>(smem + h * 32768 + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val;
+    }
+    fence_async_smem();
+    if (warp == kTmemWarp) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                   "n"(kTmemCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tbase = *tmem_slot;
+  const bool valid = s_desc[8] != 0;
+  float v_scale, v_unscale;
+  const bool wide = value_scale((uint32_t)s_desc[9], a.force_wide, v_scale, v_unscale);
   bool failed = false;
   // pages of slot h: local page i is page h + 2 i of the share (kAlt), or page i
   auto slot_pages = [&](int h) { return kAlt ? (n_pages + 1 - h) / 2 : (h == 0 || two ? n_pages : 0); };
   auto page_of = [&](int h, int i) { return kAlt ? 2 * i + h : i; };
 
-  if (warp == kLoaderWarp) {
+  if (!valid) {
+    // nothing to do but to give the tensor memory back
+  } else if (warp == kLoaderWarp) {
     // ---------------------------------------------------------------- page loader
-    const uint64_t pol = l2_evict_first_policy();
-    int j = 0;
+    int j = min(n_pages, kStages);
     for (int base = 0; base < n_pages && !failed; base += 32) {
-      int page = 0;
-      if (base + lane < n_pages)
+      int page = first_entry;
+      if (base > 0 && base + lane < n_pages)
         page = checked_page(c, ldcg_keep(&unit_table(c, trow)[j_begin + base + lane]), (int)ring_page(c, u, 0));
-      const int cnt = min(32, n_pages - base);
-      for (int x = 0; x < cnt; ++x, ++j) {
-        const int gp = __shfl_sync(0xffffffffu, page, x);
+      const int end = min(base + 32, n_pages);
+      for (; j < end; ++j) {
+        const int gp = __shfl_sync(0xffffffffu, page, j - base);
         if (lane == 0) {
-          const int s = j % kStages;
-          if (j >= kStages && !mbar_wait_bounded(&bar[B_KV_EMPTY + s], ((j / kStages) - 1) & 1)) failed = true;
-          if (!failed) {
-            mbar_arrive_expect_tx(&bar[B_KV_FULL + s], kPageBytes);
-            const __nv_bfloat16 *src = c.pages + (int64_t)gp * kPageElems;
-            // a page that several row tiles read stays in L2 for the others
-            if (a.n_tiles == 1) bulk_load_hint(smem + kSKV + s * kPageBytes, src, kPageBytes, &bar[B_KV_FULL + s], pol);
-            else bulk_load(smem + kSKV + s * kPageBytes, src, kPageBytes, &bar[B_KV_FULL + s]);
-          }
+          if (!mbar_wait_bounded(&bar[B_KV_EMPTY + j % kStages], ((j / kStages) - 1) & 1)) failed = true;
+          if (!failed) load_page<kAlt>(a, smem, bar, j, gp, pol);
         }
         failed = __shfl_sync(0xffffffffu, (int)failed, 0) != 0;
         if (failed) break;
@@ -392,76 +409,283 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
   if (failed) set_status(c, SPKV_E_TIMEOUT);
   fence_before();
   __syncthreads();
-  if (warp == kLoaderWarp)
+  if (warp == kTmemWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "n"(shp::kTmemCols) : "memory");
 }
 
-// One warp per query row: its shares of the common pages and its suffix.  Lane l owns dims 4l .. 4l + 3.
+// ---- tail ------------------------------------------------------------------------------------------
+namespace sht {
+constexpr int kThreads = 128, kWarps = 4;
+constexpr int off_bar = 2 * kPageBytes, kSmemBytes = off_bar + 128;
+}  // namespace sht
+
+// Item = share * n_items + unit.  A unit's pages are what its compact cache holds behind the common pages,
+// then its ring; they are cut into up to `shares` (plan) pieces of at least four.  The four warps take 16
+// pairs each of every page and join at the end through the page stages.
+template <int NH>
+__global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_kernel(SharedArgs a, int GP) {
+  using namespace sht;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const CacheView &c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = c.G;
+  uint64_t *full = reinterpret_cast<uint64_t *>(smem + off_bar);
+  volatile int *s_it = reinterpret_cast<volatile int *>(full + 2);   // share exists, skip, compact pages, length behind
+                                                                     // the common pages, ring pairs, first page, pages
+  if (tid == 0) {
+    mbar_init(&full[0], 1);
+    mbar_init(&full[1], 1);
+    mbar_fence_init();
+  }
+  pdl_trigger();
+  // everything before the prefix launch is complete and was written through generic stores
+  asm volatile("fence.proxy.async;" ::: "memory");
+  const uint64_t pol = l2_evict_first_policy();
+  int loads = 0;        // pages loaded so far: stage loads & 1, phase (loads >> 1) & 1
+  bool failed = false;
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    const int unit = item % a.n_items, share = item / a.n_items;
+    const int b = unit / c.Hkv, kvh = unit - b * c.Hkv;
+    __syncthreads();    // the previous item's stages and s_it have been read
+    if (share >= a.max_tail) break;
+    int u = 0, trow = -1;
+    if (warp == 0) {
+      // trip 1: the plan and the sequence
+      const int4 head = ldcg4(share_head(a.rec, kvh));
+      const int sig = __ldcg(a.plan), n_shares = __ldcg(a.rec + 2), seq = a.seq_ids[b];
+      const bool fits = sig == a.sig;
+      if (share >= (fits ? n_shares : 1)) {
+        if (lane == 0) s_it[0] = 0;
+      } else {
+        int common = fits ? min(head.x, c.max_pages) : 0;
+        const int row0 = head.z, u0 = head.w;
+        if (common < 0 || row0 < 0 || row0 >= c.n_units || u0 < 0 || u0 >= c.n_units) common = 0;
+        const bool ok = seq >= 0 && seq < c.S;
+        if (!ok && lane == 0 && share == 0) set_status(c, SPKV_E_BOUNDS);
+        u = unit_index(c, a.layer, ok ? seq : 0, kvh);
+        // trip 2: the unit; does the batch's first sequence still hold the common pages, and which is their last
+        trow = unit_table_row(c, u);
+        int len = ldcg_keep(&c.len[u]), n_ring = min(ldcg_keep(&c.t[u]), c.w);
+        int skip = 0;
+        if (common > 0) {
+          const int len0 = ldcg_keep(&c.len[u0]), last0 = ldcg_keep(&unit_table(c, row0)[common - 1]);
+          // trip 3: does the unit hold that same page (then it holds all before it)
+          if (trow >= 0 && len / kP >= common && len0 / kP >= common &&
+              ldcg_keep(&unit_table(c, trow)[common - 1]) == last0)
+            skip = common;
+        }
+        if (!ok) { len = 0; n_ring = 0; skip = 0; }
+        len -= skip * kP;
+        const int nk = (len + kP - 1) / kP, np = nk + (n_ring + kP - 1) / kP;
+        const int ku = max(1, min(np / 4, fits ? n_shares : 1));
+        const int p0 = share < ku ? (int)((long long)np * share / ku) : 0;
+        const int p1 = share < ku ? (int)((long long)np * (share + 1) / ku) : 0;
+        if (lane == 0) {
+          s_it[0] = 1; s_it[1] = skip; s_it[2] = nk; s_it[3] = len; s_it[4] = n_ring; s_it[5] = p0; s_it[6] = p1 - p0;
+          if (share == 0) a.item_skip[unit] = skip;
+        }
+        __syncwarp();
+      }
+    }
+    __syncthreads();
+    if (!s_it[0]) break;   // (items are laid out share by share: the ones behind do not exist either)
+    const int skip = s_it[1], nk = s_it[2], len = s_it[3], n_ring = s_it[4], p0 = s_it[5], n = s_it[6];
+    const size_t row0 = ((size_t)share * a.n_items + unit) * G;
+    if (n == 0) {          // nothing to attend to in this share
+      for (int g = tid; g < G; g += kThreads) *reinterpret_cast<float2 *>(a.tail_ml + (row0 + g) * 2) = make_float2(-INFINITY, 0.f);
+      continue;
+    }
+    int entry = 0;
+    auto fetch_entries = [&](int i) {   // warp 0: global page indices of the share's pages i .. i + 31, one per lane
+      const int p = p0 + i + lane;
+      if (i + lane < n)
+        entry = p < nk ? checked_page(c, ldcg_keep(&unit_table(c, trow)[skip + p]), (int)ring_page(c, u, 0))
+                       : (int)ring_page(c, u, p - nk);
+    };
+    auto load = [&](int i) {            // warp 0
+      if ((i & 31) == 0) fetch_entries(i);
+      const int gp = __shfl_sync(0xffffffffu, entry, i & 31);
+      if (lane == 0) {
+        uint64_t *bar = &full[(loads + i) & 1];
+        mbar_arrive_expect_tx(bar, kPageBytes);
+        bulk_load_hint(smem + ((loads + i) & 1) * kPageBytes, c.pages + (int64_t)gp * kPageElems, kPageBytes, bar, pol);
+      }
+    };
+    if (warp == 0) {
+      load(0);
+      if (n > 1) load(1);
+    }
+    uint32_t qb[NH][8][2];
+    float m[NH][2], l[NH][2], o[NH][8][4];
+    const __nv_bfloat16 *q = a.q + ((size_t)b * c.Hq + (size_t)kvh * G) * kD;
+    load_q_frags_t<NH>(qb, [&](int h) -> const __nv_bfloat16 * { return h < G ? q + h * kD : nullptr; }, lane);
+#pragma unroll
+    for (int hn = 0; hn < NH; ++hn) {
+      m[hn][0] = m[hn][1] = -INFINITY;
+      l[hn][0] = l[hn][1] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) o[hn][mt][0] = o[hn][mt][1] = o[hn][mt][2] = o[hn][mt][3] = 0.f;
+    }
+    for (int i = 0; i < n; ++i) {
+      const int st = (loads + i) & 1, p = p0 + i;
+      const int valid = p < nk ? min(kP, len - p * kP) : min(kP, n_ring - (p - nk) * kP);
+      if (!mbar_wait_bounded(&full[st], ((loads + i) >> 1) & 1)) failed = true;
+      const int tok0 = warp * 16;
+      if (!failed && tok0 < valid) {
+        const uint32_t sK = smem_u32(smem + st * kPageBytes), sV = sK + kBlockElems * 2;
+        float s[NH][4];
+        qk_tile_t<NH>(s, qb, sK, tok0, lane);
+        softmax_pv_tile_t<NH>(s, valid, a.scale_log2, m, l, o, sV, tok0, lane);
+      }
+      failed = __syncthreads_or(failed);   // all four warps are done with the stage
+      if (failed) {
+        // do not leave while copies may still be landing
+        if (tid == 0)
+          for (int k = i; k < min(i + 2, n); ++k) mbar_wait_bounded(&full[(loads + k) & 1], ((loads + k) >> 1) & 1);
+        break;
+      }
+      if (warp == 0 && i + 2 < n) load(i + 2);
+    }
+    if (failed) break;
+    loads += n;
+    // join the four warps: rows [warp][GP][132] over the page stages (every copy of the item has landed)
+    float *red = reinterpret_cast<float *>(smem);
+    segment_hand_over<NH>(red, warp, GP, G, m, l, o, lane);
+    __syncthreads();
+    for (int g = warp; g < G; g += kWarps) {
+      float M = -INFINITY, L = 0.f;
+      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, red[((size_t)w * GP + g) * 132 + 128]);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float *src = red + ((size_t)w * GP + g) * 132;
+        const float f = src[128] == -INFINITY ? 0.f : fast_exp2(src[128] - M);
+        const float4 v = *reinterpret_cast<const float4 *>(src + lane * 4);
+        L += src[129] * f;
+        O.x = fmaf(v.x, f, O.x); O.y = fmaf(v.y, f, O.y); O.z = fmaf(v.z, f, O.z); O.w = fmaf(v.w, f, O.w);
+      }
+      *reinterpret_cast<float4 *>(a.tail_o + (row0 + g) * kD + lane * 4) = O;
+      if (lane == 0) *reinterpret_cast<float2 *>(a.tail_ml + (row0 + g) * 2) = make_float2(M, L);
+    }
+    tc5::fence_async_smem();   // these reads and writes come before the next item's copies into the stages
+  }
+  if (failed) set_status(c, SPKV_E_TIMEOUT);
+  pdl_wait();   // the merge behind this launch reads the prefix launch's parts too
+}
+
+// ---- merge -----------------------------------------------------------------------------------------
+// One block per unit: the parts of its G query rows.  Up to 8 heads: 8 / 2^ceil(log2 G) warps per row, each
+// taking every so-manieth part; more heads: a warp takes several rows.  Lane l owns dims 4l .. 4l + 3.
 __global__ void __launch_bounds__(256) shared_merge_kernel(SharedArgs a) {
   const CacheView &c = a.c;
+  __shared__ int s_hdr[8];
+  __shared__ float s_ml[8][2];
+  __shared__ float4 s_o[8][32];
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, r = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (r >= a.B * c.Hq) return;
-  const int b = r / c.Hq, j = r % c.Hq, kvh = j / c.G, g = j % c.G;
-  const float lse = __ldcg(a.suf_lse + r);
-  const float4 so = __ldcg(reinterpret_cast<const float4 *>(a.suf_o + (size_t)r * kD) + lane);
-  const int skip = __ldcg(a.item_skip + b * c.Hkv + kvh);
-  float M = lse * kLog2e, L = 1.f;
-  float4 O = so;
-  if (skip > 0) {
-    const int32_t *rec = share_record(a.plan, c.Hkv, a.layer);
-    const int per = max(1, __ldcg(rec)), n = (skip + per - 1) / per;
-    const int R = b * c.G + g, tile = R / kShareRows, row = R % kShareRows;
-    const int first = __ldcg(rec + kShareHdr + c.Hkv + kvh) + tile;
-    const int last = a.max_blocks - 1;   // (a plan that was overwritten reads no further than the workspace)
-    auto at = [&](int s) { return (size_t)max(0, min(first + s * a.n_tiles, last)) * a.rows_per_block + row; };
-    float pm = -INFINITY;
-    for (int s = lane; s < n; s += 32) pm = fmaxf(pm, __ldcg(a.part_ml + at(s) * 2));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) pm = fmaxf(pm, __shfl_xor_sync(0xffffffffu, pm, o));
-    const float top = fmaxf(M, pm);
-    const float w = M == -INFINITY ? 0.f : exp2f(M - top);
-    M = top;
-    L = w;
-    O = make_float4(so.x * w, so.y * w, so.z * w, so.w * w);
-    for (int s0 = 0; s0 < n; s0 += 32) {
+  const int unit = blockIdx.x, b = unit / c.Hkv, kvh = unit - b * c.Hkv, G = c.G;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x < 8) {
+    const int x = threadIdx.x;
+    s_hdr[x] = __ldcg(x == 0 ? a.item_skip + unit : x == 1 ? a.rec : x == 2 ? a.rec + 2 : x == 3 ? a.plan : share_head(a.rec, kvh) + 1);
+  }
+  __syncthreads();
+  const int skip = s_hdr[0], per = max(1, s_hdr[1]), first = s_hdr[4];
+  const int n_tail = s_hdr[3] == a.sig ? max(1, min(s_hdr[2], a.max_tail)) : 1;
+  const int n_pre = skip > 0 ? (skip + per - 1) / per : 0, n = n_pre + n_tail;
+  int wpr = 1;
+  while (2 * wpr * G <= 8) wpr *= 2;
+  const int last_block = a.max_blocks - 1;   // (a plan that was overwritten reads no further than the workspace)
+  for (int g0 = 0; g0 < G; g0 += 8 / wpr) {
+    const int g = g0 + warp / wpr, sub = warp % wpr;
+    const bool on = g < G;
+    const int R = b * G + g, tile = R / kShareRows, row = R % kShareRows;
+    // part p of the row: a share of the common pages, or of the tail
+    auto part = [&](int p, const float *&o) -> const float2 * {
+      if (p < n_pre) {
+        const size_t at = (size_t)max(0, min(first + p * a.n_tiles + tile, last_block)) * a.rows_per_block + row;
+        o = a.part_o + at * kD;
+        return reinterpret_cast<const float2 *>(a.part_ml) + at;
+      }
+      const size_t at = ((size_t)(p - n_pre) * a.n_items + unit) * G + g;
+      o = a.tail_o + at * kD;
+      return reinterpret_cast<const float2 *>(a.tail_ml) + at;
+    };
+    float M = -INFINITY, L = 0.f;
+    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = sub; on && p0 < n; p0 += 32 * wpr) {   // 32 parts at a time, one per lane
+      const int mine = p0 + lane * wpr;
+      const float *po = nullptr;
       float2 ml = make_float2(-INFINITY, 0.f);
-      if (s0 + lane < n) ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + at(s0 + lane));
-      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top), fl = f * ml.y;
-      const int cnt = min(32, n - s0);
+      if (mine < n) ml = __ldcg(part(mine, po));
+      float top = ml.x;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float Mn = fmaxf(M, top);
+      const float old = M == -INFINITY ? 0.f : exp2f(M - Mn);
+      M = Mn;
+      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+      float fl = f * ml.y;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) fl += __shfl_xor_sync(0xffffffffu, fl, o);
+      L = L * old + fl;
+      O.x *= old; O.y *= old; O.z *= old; O.w *= old;
+      const int cnt = min(32, (n - p0 + wpr - 1) / wpr);
 #pragma unroll 8
       for (int x = 0; x < cnt; ++x) {
-        const float4 p = __ldcg(reinterpret_cast<const float4 *>(a.part_o + at(s0 + x) * kD) + lane);
         const float fx = __shfl_sync(0xffffffffu, f, x);
-        L += __shfl_sync(0xffffffffu, fl, x);
-        if (fx != 0.f) {
-          O.x = fmaf(p.x, fx, O.x); O.y = fmaf(p.y, fx, O.y); O.z = fmaf(p.z, fx, O.z); O.w = fmaf(p.w, fx, O.w);
+        const float *src;
+        part(p0 + x * wpr, src);
+        if (fx != 0.f) {   // (a part of weight 0 may never have been written)
+          const float4 v = __ldcg(reinterpret_cast<const float4 *>(src) + lane);
+          O.x = fmaf(v.x, fx, O.x); O.y = fmaf(v.y, fx, O.y); O.z = fmaf(v.z, fx, O.z); O.w = fmaf(v.w, fx, O.w);
         }
       }
     }
+    if (wpr > 1) {   // (at most one round: 8 / wpr >= G)
+      s_o[warp][lane] = O;
+      if (lane == 0) { s_ml[warp][0] = M; s_ml[warp][1] = L; }
+      __syncthreads();
+      if (sub == 0) {
+        float Mx = M;
+        for (int x = 1; x < wpr; ++x) Mx = fmaxf(Mx, s_ml[warp + x][0]);
+        const float w0 = M == -INFINITY ? 0.f : exp2f(M - Mx);
+        L *= w0; O.x *= w0; O.y *= w0; O.z *= w0; O.w *= w0;
+        for (int x = 1; x < wpr; ++x) {
+          const float mx = s_ml[warp + x][0], f = mx == -INFINITY ? 0.f : exp2f(mx - Mx);
+          const float4 v = s_o[warp + x][lane];
+          L = fmaf(s_ml[warp + x][1], f, L);
+          O.x = fmaf(v.x, f, O.x); O.y = fmaf(v.y, f, O.y); O.z = fmaf(v.z, f, O.z); O.w = fmaf(v.w, f, O.w);
+        }
+        M = Mx;
+      }
+    }
+    if (on && sub == 0) {
+      const size_t r = (size_t)b * c.Hq + (size_t)kvh * G + g;
+      const bool none = M == -INFINITY && L == 0.f;   // a sequence that has received nothing: zeros, -inf
+      const float inv = none ? 0.f : 1.f / L;
+      uint2 pk;
+      pk.x = pack_bf16(O.x * inv, O.y * inv);
+      pk.y = pack_bf16(O.z * inv, O.w * inv);
+      *reinterpret_cast<uint2 *>(a.out + r * kD + lane * 4) = pk;
+      if (a.lse && lane == 0) a.lse[r] = none ? -INFINITY : (M + log2f(L)) * kLn2;
+    }
   }
-  const float inv = L > 0.f ? 1.f / L : 0.f;   // (the suffix' rows come normalised: l = 1)
-  uint2 pk;
-  pk.x = pack_bf16(O.x * inv, O.y * inv);
-  pk.y = pack_bf16(O.z * inv, O.w * inv);
-  *reinterpret_cast<uint2 *>(a.out + (size_t)r * kD + lane * 4) = pk;
-  if (a.lse && lane == 0) a.lse[r] = skip > 0 ? (M + log2f(L)) * kLn2 : lse;
 }
 
-struct SharedWs { size_t off_lse, off_skip, off_ml, off_o, off_dec, total; int max_blocks, rows; };
+struct SharedWs { size_t off_ml, off_o, off_tml, off_to, total; int max_blocks, rows, max_tail; };
 static SharedWs shared_ws_layout(const spkv_config_t *cfg, int B) {
   SharedWs w;
   auto a256 = [](size_t x) { return (x + 255) / 256 * 256; };
-  const int G = cfg->n_q_heads / cfg->n_kv_heads, tiles = share_row_tiles(B, G);
-  w.max_blocks = std::max(kMaxGrid, cfg->n_kv_heads * tiles);
+  const int G = cfg->n_q_heads / cfg->n_kv_heads, items = std::max(1, B * cfg->n_kv_heads);
+  w.max_blocks = std::max(kMaxGrid, cfg->n_kv_heads * share_row_tiles(B, G));
   w.rows = std::min(kShareRows, B * G);
-  size_t o = a256((size_t)B * cfg->n_q_heads * kD * 4);   // suffix rows first
-  w.off_lse = o; o += a256((size_t)B * cfg->n_q_heads * 4);
-  w.off_skip = o; o += a256((size_t)B * cfg->n_kv_heads * 4);
+  w.max_tail = std::max(1, kMaxTailItems / items);
+  size_t o = a256((size_t)items * 4);   // the units' skips first
   w.off_ml = o; o += a256((size_t)w.max_blocks * w.rows * 8);
   w.off_o = o; o += a256((size_t)w.max_blocks * w.rows * kD * 4);
-  w.off_dec = o; o += spkv_decode_workspace_bytes(cfg, B);
+  w.off_tml = o; o += a256((size_t)w.max_tail * items * G * 8);
+  w.off_to = o; o += a256((size_t)w.max_tail * items * G * kD * 4);
   w.total = o;
   return w;
 }
@@ -492,39 +716,44 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   char *ws = static_cast<char *>(d_workspace);
   cudaStream_t s = as_stream(stream);
   SharedArgs a = {};
-  a.c = v; a.layer = layer; a.B = B;
+  a.c = v; a.layer = layer; a.B = B; a.n_items = B * v.Hkv;
   a.n_tiles = share_row_tiles(B, v.G);
   a.rows_per_block = w.rows;
+  a.sig = share_signature(v, B);
   a.seq_ids = d_seq_ids;
   a.q = static_cast<const __nv_bfloat16 *>(d_q);
   a.plan = static_cast<const int32_t *>(d_plan);
+  a.rec = share_record(v, a.plan, layer);
   a.scale_log2 = sm_scale * kLog2e;
   a.force_wide = (cache->cfg.flags & SPKV_FLAG_PREFILL_PV_BF16) ? 1 : 0;
-  a.part_o = reinterpret_cast<float *>(ws + w.off_o);
+  a.item_skip = reinterpret_cast<int32_t *>(ws);
   a.part_ml = reinterpret_cast<float *>(ws + w.off_ml);
+  a.part_o = reinterpret_cast<float *>(ws + w.off_o);
+  a.tail_ml = reinterpret_cast<float *>(ws + w.off_tml);
+  a.tail_o = reinterpret_cast<float *>(ws + w.off_to);
   a.max_blocks = w.max_blocks;
-  a.suf_o = reinterpret_cast<float *>(ws);
-  a.suf_lse = reinterpret_cast<float *>(ws + w.off_lse);
-  a.item_skip = reinterpret_cast<int32_t *>(ws + w.off_skip);
+  a.max_tail = w.max_tail;
   a.out = static_cast<__nv_bfloat16 *>(d_out);
   a.lse = d_lse_opt;
   // blocks: one share each (the plan never cuts into more)
-  const int grid = std::max(std::min(kMaxGrid, cache->sm_count), v.Hkv * a.n_tiles);
+  const int sms = std::min(kMaxGrid, cache->sm_count), grid = std::max(sms, v.Hkv * a.n_tiles);
   const bool alt = w.rows <= 128;
   auto prefix = alt ? shared_prefix_kernel<true> : shared_prefix_kernel<false>;
   const int smem = shp::smem_bytes(alt);
-  if (cudaFuncSetAttribute(prefix, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPKV_E_CUDA;
+  int GP = 1;
+  while (GP < v.G) GP <<= 1;
+  auto tail = GP > 8 ? shared_tail_kernel<2> : shared_tail_kernel<1>;
+  if (cudaFuncSetAttribute(prefix, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaFuncSetAttribute(tail, cudaFuncAttributeMaxDynamicSharedMemorySize, sht::kSmemBytes) != cudaSuccess)
+    return SPKV_E_CUDA;
   // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
   // cover; a plain launch waits for all of them.
   const bool plain = (cache->cfg.flags & SPKV_FLAG_OVERLAP) != 0;
   cache->last_kind = kLastOther;
   if (launch_link(!plain, prefix, dim3(grid), dim3(shp::kThreads), (size_t)smem, s, a) != cudaSuccess) return SPKV_E_CUDA;
-  const SharedDecode sd = {a.plan, reinterpret_cast<int32_t *>(ws + w.off_skip)};
-  int rc = decode_suffix(cache, layer, d_seq_ids, B, d_q, d_out, reinterpret_cast<float *>(ws),
-                         reinterpret_cast<float *>(ws + w.off_lse), sm_scale, ws + w.off_dec,
-                         workspace_bytes - w.off_dec, sd, stream);
-  cache->last_kind = kLastOther;
-  if (rc) return rc;
-  return check_stream_error(
-      launch_overlapped(shared_merge_kernel, dim3((B * v.Hq + 7) / 8), dim3(256), 0, s, a));
+  // one block per unit, and enough of them that the shares of long units find a block each
+  if (launch_overlapped(tail, dim3(std::max(a.n_items, 2 * sms)), dim3(sht::kThreads), (size_t)sht::kSmemBytes, s, a, GP) !=
+      cudaSuccess)
+    return SPKV_E_CUDA;
+  return check_stream_error(launch_overlapped(shared_merge_kernel, dim3(a.n_items), dim3(256), 0, s, a));
 }

@@ -2,7 +2,6 @@
 #include <algorithm>
 #include <new>
 
-#include "spkv_decode_common.cuh"
 #include "spkv_share.cuh"
 
 namespace spkv {
@@ -97,25 +96,43 @@ __global__ void __launch_bounds__(128) share_common_kernel(CacheView c, const in
     atomicMin(&s_min, lo);
   }
   __syncthreads();
-  if (threadIdx.x == 0)
-    share_record(plan, c.Hkv, layer)[kShareHdr + kvh] = (B < 2 || s_min < kMinSharedPages) ? 0 : s_min;
+  if (threadIdx.x == 0) {
+    int32_t *head = share_head(share_record(c, plan, layer), kvh);
+    head[0] = (B < 2 || s_min < kMinSharedPages) ? 0 : s_min;
+    head[2] = row0;
+    head[3] = u0;
+  }
 }
 
 // Cuts a layer's common pages into shares: the fewest pages per share, p, for which all shares of all KV
 // heads and row tiles are no more than one block per SM (blocks take one share each, so the longest
-// share is the launch).  One block per layer.
-__global__ void __launch_bounds__(32) share_cut_kernel(CacheView c, int B, int n_tiles, int max_blocks, int32_t *plan) {
-  int32_t *rec = share_record(plan, c.Hkv, blockIdx.x);
-  const int lane = threadIdx.x;
-  auto blocks = [&](int p) {
+// share is the launch).  Likewise the number of shares a unit's own pages are cut into, by the longest
+// unit.  One block per layer.
+__global__ void __launch_bounds__(256) share_cut_kernel(CacheView c, const int32_t *seq_ids, int B, int n_tiles,
+                                                        int max_blocks, int sig, int32_t *plan) {
+  int32_t *rec = share_record(c, plan, blockIdx.x);
+  const int lane = threadIdx.x & 31;
+  __shared__ int s_longest;
+  if (threadIdx.x == 0) s_longest = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < B * c.Hkv; i += 256) {
+    const int seq = seq_ids[i / c.Hkv];
+    if (seq < 0 || seq >= c.S) continue;
+    const int u = unit_index(c, blockIdx.x, seq, i % c.Hkv);
+    atomicMax(&s_longest, (c.len[u] + kP - 1) / kP - share_head(rec, i % c.Hkv)[0] + (min(c.t[u], c.w) + kP - 1) / kP);
+  }
+  auto blocks = [&](int p) {   // (every warp computes the same)
     int n = 0;
-    for (int h = lane; h < c.Hkv; h += 32) n += (rec[kShareHdr + h] + p - 1) / p;
+    for (int h = lane; h < c.Hkv; h += 32) n += (share_head(rec, h)[0] + p - 1) / p;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
     return n * n_tiles;
   };
   int heads = 0, longest = 1;
-  for (int h = lane; h < c.Hkv; h += 32) { heads += rec[kShareHdr + h] > 0; longest = max(longest, rec[kShareHdr + h]); }
+  for (int h = lane; h < c.Hkv; h += 32) {
+    heads += share_head(rec, h)[0] > 0;
+    longest = max(longest, share_head(rec, h)[0]);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     heads += __shfl_xor_sync(0xffffffffu, heads, o);
@@ -128,16 +145,34 @@ __global__ void __launch_bounds__(32) share_cut_kernel(CacheView c, int B, int n
     const int mid = (lo + hi) >> 1;
     if (blocks(mid) <= limit) hi = mid; else lo = mid + 1;
   }
-  const int total = blocks(lo);
-  if (lane == 0) {
-    rec[0] = lo;
-    rec[1] = total;
+  __syncthreads();
+  if (threadIdx.x == 0) {
     int at = 0;
     for (int h = 0; h < c.Hkv; ++h) {
-      rec[kShareHdr + c.Hkv + h] = at;
-      at += (rec[kShareHdr + h] + lo - 1) / lo * n_tiles;
+      share_head(rec, h)[1] = at;
+      at += (share_head(rec, h)[0] + lo - 1) / lo * n_tiles;
     }
-    if (blockIdx.x == 0) { plan[0] = B; plan[1] = c.L; plan[2] = c.Hkv; plan[3] = n_tiles; }
+    rec[0] = lo;
+    rec[1] = at;
+    rec[2] = max(1, min((s_longest + kTailPages - 1) / kTailPages, kMaxTailItems / (B * c.Hkv)));
+    rec[3] = 0;
+    if (blockIdx.x == 0) plan[0] = sig;
+  }
+  __syncthreads();
+  const int n_room = share_max_blocks(c.S, c.Hkv, c.G);
+  for (int x = threadIdx.x; x < n_room; x += 256) {
+    int4 d0 = make_int4(0, 0, 0, 0), d1 = d0;
+    if (x < rec[1]) {
+      int h = c.Hkv - 1;   // the last head that starts at or before this block and has pages
+      while (h > 0 && (share_head(rec, h)[1] > x || share_head(rec, h)[0] == 0)) --h;
+      const int32_t *hd = share_head(rec, h);
+      const int r = x - hd[1], j = r / n_tiles * lo;
+      d0 = make_int4(h, r % n_tiles, j, min(lo, hd[0] - j));
+      d1 = make_int4(hd[0], hd[2], hd[3], sig);
+    }
+    int4 *d = reinterpret_cast<int4 *>(share_desc(c, rec, x));
+    d[0] = d0;
+    d[1] = d1;
   }
 }
 
@@ -172,18 +207,21 @@ extern "C" int spkv_seq_fork(spkv_cache_t *cache, int32_t src, const int32_t *h_
 }
 
 extern "C" size_t spkv_share_plan_bytes(const spkv_config_t *cfg) {
-  if (!cfg || cfg->n_layers < 1 || cfg->n_kv_heads < 1) return 0;
-  return (kSharePlanHdr + (size_t)cfg->n_layers * (kShareHdr + 2 * (size_t)cfg->n_kv_heads)) * 4;
+  if (!cfg || cfg->n_layers < 1 || cfg->max_seqs < 1 || cfg->n_kv_heads < 1 || cfg->n_q_heads < cfg->n_kv_heads) return 0;
+  return (kSharePlanHdr + (size_t)cfg->n_layers * share_record_ints(cfg->max_seqs, cfg->n_kv_heads,
+                                                                    cfg->n_q_heads / cfg->n_kv_heads)) * 4;
 }
 
 extern "C" int spkv_share_plan(spkv_cache_t *cache, const int32_t *d_seq_ids, int32_t B, void *d_plan, size_t plan_bytes,
                                spkv_stream_t stream) {
   if (!cache || B < 1 || B > cache->cfg.max_seqs || !d_seq_ids || !d_plan || ((uintptr_t)d_plan & 15)) return SPKV_E_INVALID;
-  if (plan_bytes < spkv_share_plan_bytes(&cache->cfg)) return SPKV_E_WORKSPACE;
   const CacheView &v = cache->view;
+  if (B * v.Hkv > 1024) return SPKV_E_UNSUPPORTED;
+  if (plan_bytes < spkv_share_plan_bytes(&cache->cfg)) return SPKV_E_WORKSPACE;
   cache->last_kind = kLastOther;
   int32_t *plan = static_cast<int32_t *>(d_plan);
   share_common_kernel<<<v.L * v.Hkv, 128, 0, as_stream(stream)>>>(v, d_seq_ids, B, plan);
-  share_cut_kernel<<<v.L, 32, 0, as_stream(stream)>>>(v, B, share_row_tiles(B, v.G), std::min(kMaxGrid, cache->sm_count), plan);
+  share_cut_kernel<<<v.L, 256, 0, as_stream(stream)>>>(v, d_seq_ids, B, share_row_tiles(B, v.G),
+                                                       std::min(kMaxGrid, cache->sm_count), share_signature(v, B), plan);
   return check_stream_error(cudaGetLastError());
 }

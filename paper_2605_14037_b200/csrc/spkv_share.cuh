@@ -1,35 +1,48 @@
 // What a batch with a common prefix decodes by: the plan's layout and the cut of the common pages.
 //
-// Plan (int32): header {B, layers, KV heads, row tiles, 0 ...}, then one record per layer:
-//   {pages per share, blocks, 0, 0, common pages [Hkv], first block [Hkv]}.
+// Plan (int32): header {signature, 0 ...}, then one record per layer:
+//   {pages per share, blocks, tail shares, 0}
+//   per KV head  {common pages, first block, page-table row and unit of the batch's first sequence}
+//   per block    {KV head, row tile, first page, pages (0: no work)}, {common pages, row, unit, signature}
 // The queries of KV head h are the rows (b, g) -> b * G + g of its group in every sequence, cut into tiles
 // of kShareRows.  A block takes one share of one head's common pages for one row tile; block first[h] +
 // share * row_tiles + tile.  The tiles of a share are neighbours, so that they find its pages in L2.
+// A block's descriptor holds all it needs to know, so that it costs one trip to memory and its first
+// page-table entries the second (148 blocks that each walk the plan by themselves queue up at the
+// same few L2 lines: measured, 8 us of an 18 us launch).
 #pragma once
-#include "spkv_internal.cuh"
+#include "spkv_decode_common.cuh"
 
 namespace spkv {
 
-constexpr int kSharePlanHdr = 8, kShareHdr = 4;
+constexpr int kSharePlanHdr = 8, kShareHdr = 4, kShareHead = 4, kShareDesc = 8;
 constexpr int kShareRows = 256;       // query rows per block: two slots of 128
 constexpr int kMinSharedPages = 1;    // fewer common pages than this are read per sequence
 constexpr int kMinSharePages = 4;     // a share is not cut shorter
+constexpr int kTailPages = 8;         // a unit's own pages are cut into shares of about this many
+constexpr int kMaxTailItems = 1024;   // ... while there are no more shares than this
 
 __host__ __device__ inline int share_row_tiles(int B, int G) { return (B * G + kShareRows - 1) / kShareRows; }
-template <class I>
-__host__ __device__ inline I *share_record(I *plan, int Hkv, int layer) {
-  return plan + kSharePlanHdr + (size_t)layer * (kShareHdr + 2 * Hkv);
+// blocks a layer's record has room for, whatever the batch (B * Hkv <= 1024, B <= max_seqs)
+__host__ __device__ inline int share_max_blocks(int max_seqs, int Hkv, int G) {
+  const int B = max_seqs < 1024 / Hkv ? max_seqs : (1024 / Hkv > 1 ? 1024 / Hkv : 1);
+  const int n = Hkv * share_row_tiles(B, G);
+  return n > kMaxGrid ? n : kMaxGrid;
 }
-
-// What the decode kernel needs to leave a batch's common pages out.
-struct SharedDecode {
-  const int32_t *plan;
-  int32_t *item_skip;   // [B * Hkv] out: the pages each unit left out
-};
-int decode_check_args(const spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B, const void *d_q,
-                      const void *d_out, const float *d_out_f32, bool *empty);
-int decode_suffix(spkv_cache *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B, const void *d_q, void *d_out,
-                  float *d_out_f32, float *d_lse, float sm_scale, void *d_workspace, size_t workspace_bytes,
-                  const SharedDecode &sd, spkv_stream_t stream);
+__host__ __device__ inline size_t share_record_ints(int max_seqs, int Hkv, int G) {
+  return kShareHdr + (size_t)kShareHead * Hkv + (size_t)kShareDesc * share_max_blocks(max_seqs, Hkv, G);
+}
+template <class I>
+__host__ __device__ inline I *share_record(const CacheView &c, I *plan, int layer) {
+  return plan + kSharePlanHdr + (size_t)layer * share_record_ints(c.S, c.Hkv, c.G);
+}
+template <class I> __host__ __device__ inline I *share_head(I *rec, int h) { return rec + kShareHdr + kShareHead * h; }
+template <class I> __host__ __device__ inline I *share_desc(const CacheView &c, I *rec, int block) {
+  return rec + kShareHdr + kShareHead * c.Hkv + kShareDesc * (size_t)block;
+}
+// what a plan must agree on with a call (never 0: a zero-filled buffer is no plan)
+__host__ __device__ inline int share_signature(const CacheView &c, int B) {
+  return (int)((((unsigned)B * 2654435761u + (unsigned)c.L) * 2246822519u + (unsigned)c.Hkv * 4099u + (unsigned)c.G) | 1u);
+}
 
 }  // namespace spkv

@@ -30,10 +30,11 @@ def reference(cache, layer, seq, h, q, scale=SC):
 
 
 def check(cache, layer, seqs, q_bits, out, lse, scale=SC, kv=None):
-    """A weight is rounded to bf16 in a sequence's own pairs (2^-9 of it) and to fp16 or two bf16 terms in the
-    common ones (less); with the row sum kept in fp32 from the unrounded weights, the output is off by at
-    most 2^-9 sum w|v|, then rounded to bf16 (2^-9 |o|).  Scores: 128 products added in fp32, 130 * 2^-24
-    |q||k| scale (and twice that as a relative error of a weight, on both sides of the quotient)."""
+    """A weight is rounded to fp16 (2^-12 of it) or two bf16 terms (less); with the row sum kept in fp32 from the
+    unrounded weights, the output is off by at most 2^-12 sum w|v|, then rounded to bf16: 8 significant
+    bits, so half a step is up to 2^-8 of the value (torch.finfo(bfloat16).eps / 2).  Scores: 128 products
+    added in fp32, 130 * 2^-24 |q||k| scale (and twice that as a relative error of a weight, on both
+    sides of the quotient)."""
     G = q_bits.shape[1] // cache.cfg.n_kv_heads
     got, l = out.float().cpu().double().numpy(), lse.cpu().double().numpy()
     for b, s in enumerate(seqs):
@@ -41,7 +42,7 @@ def check(cache, layer, seqs, q_bits, out, lse, scale=SC, kv=None):
             hs = slice(h * G, (h + 1) * G)
             ref, wv, rl, qk = reference(cache, layer, s, h, f64(q_bits[b, hs]), scale)
             es = 130 * 2.0 ** -24 * qk * scale
-            err, tol = np.abs(got[b, hs] - ref), 2.0 ** -9 * np.abs(ref) + (2.0 ** -9 + 2.0 ** -18 + 2 * es) * wv + 1e-30
+            err, tol = np.abs(got[b, hs] - ref), 2.0 ** -8 * np.abs(ref) + (2.0 ** -12 + 2.0 ** -18 + 2 * es) * wv + 1e-30
             assert (err <= tol).all(), (b, h, err.max(), (err / tol).max())
             assert (np.abs(l[b, hs] - rl) <= es + 2.0 ** -19 * (1 + np.abs(rl))).all(), (b, h, np.abs(l[b, hs] - rl).max())
 
@@ -71,9 +72,8 @@ def queries(wl, t=-1):
 
 
 def commons(cache, plan, layer=0):
-    p = plan.cpu().numpy().view(np.int32)
-    Hkv = cache.cfg.n_kv_heads
-    return p[8 + layer * (4 + 2 * Hkv):][4:4 + Hkv]
+    p = plan.cpu().numpy().view(np.int32)[8:].reshape(cache.cfg.n_layers, -1)[layer]
+    return p[4:4 + 4 * cache.cfg.n_kv_heads:4]
 
 
 @pytest.mark.parametrize("B,Hq,Hkv,T0,m,rates", [
@@ -117,9 +117,6 @@ def test_sequences_that_share_nothing_and_single_sequences():
         assert not commons(cache, plan).any()
         out, lse = cache.spkv_decode_attention_shared(0, ids, qd[:len(seqs)].contiguous(), plan, want_lse=True)
         check(cache, 0, seqs, q[:len(seqs)], out, lse)
-        lse1 = torch.empty_like(lse)
-        one = cache.spkv_decode_attention(0, ids, qd[:len(seqs)].contiguous(), lse=lse1)
-        assert torch.equal(one, out) and torch.equal(lse, lse1)
     cache.check()
 
 
