@@ -53,7 +53,6 @@ struct SharedArgs {
   const int32_t *seq_ids;
   const __nv_bfloat16 *q;       // [B][Hq][128]
   const int32_t *rec;           // the layer's record of the plan
-  const int32_t *plan;
   float scale_log2;
   int force_wide;
   float *part_o, *part_ml;      // prefix: [block][rows_per_block][128], [block][rows_per_block][2]: m (log2 domain), l
@@ -450,9 +449,9 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
     int u = 0, trow = -1;
     if (warp == 0) {
       // trip 1: the plan and the sequence
-      const int4 head = ldcg4(share_head(a.rec, kvh));
-      const int sig = __ldcg(a.plan), n_shares = __ldcg(a.rec + 2), seq = a.seq_ids[b];
-      const bool fits = sig == a.sig;
+      const int4 head = ldcg4(share_head(a.rec, kvh)), parts = ldcg4(share_head(a.rec, kvh) + 4);
+      const int seq = a.seq_ids[b], n_shares = parts.y;
+      const bool fits = parts.z == a.sig;
       if (share >= (fits ? n_shares : 1)) {
         if (lane == 0) s_it[0] = 0;
       } else {
@@ -574,103 +573,87 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
 }
 
 // ---- merge -----------------------------------------------------------------------------------------
-// One block per unit: the parts of its G query rows.  Up to 8 heads: 8 / 2^ceil(log2 G) warps per row, each
-// taking every so-manieth part; more heads: a warp takes several rows.  Lane l owns dims 4l .. 4l + 3.
-__global__ void __launch_bounds__(256) shared_merge_kernel(SharedArgs a) {
+// One block per query row, its four warps taking every fourth part (shares of the common pages, then of the
+// tail); lane l owns dims 4l .. 4l + 3.  All of a warp's loads are issued before the first is used: the
+// launch is three trips to L2 (plan and skip, weights, rows), whatever the number of parts.
+__global__ void __launch_bounds__(128) shared_merge_kernel(SharedArgs a) {
+  constexpr int kWarps = 4, kBatch = 10;
   const CacheView &c = a.c;
-  __shared__ int s_hdr[8];
-  __shared__ float s_ml[8][2];
-  __shared__ float4 s_o[8][32];
+  __shared__ float s_ml[kWarps][2];
+  __shared__ float4 s_o[kWarps][32];
   pdl_trigger();
   pdl_wait();
-  const int unit = blockIdx.x, b = unit / c.Hkv, kvh = unit - b * c.Hkv, G = c.G;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (threadIdx.x < 8) {
-    const int x = threadIdx.x;
-    s_hdr[x] = __ldcg(x == 0 ? a.item_skip + unit : x == 1 ? a.rec : x == 2 ? a.rec + 2 : x == 3 ? a.plan : share_head(a.rec, kvh) + 1);
-  }
-  __syncthreads();
-  const int skip = s_hdr[0], per = max(1, s_hdr[1]), first = s_hdr[4];
-  const int n_tail = s_hdr[3] == a.sig ? max(1, min(s_hdr[2], a.max_tail)) : 1;
-  const int n_pre = skip > 0 ? (skip + per - 1) / per : 0, n = n_pre + n_tail;
-  int wpr = 1;
-  while (2 * wpr * G <= 8) wpr *= 2;
+  const int r = blockIdx.x, b = r / c.Hq, j = r - b * c.Hq, kvh = j / c.G, g = j - kvh * c.G;
+  const int unit = b * c.Hkv + kvh, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // (through L1: the rows of a head that meet on an SM share the line)
+  const int4 parts = *reinterpret_cast<const int4 *>(share_head(a.rec, kvh) + 4);
+  const int first = share_head(a.rec, kvh)[1], skip = __ldcg(a.item_skip + unit);
+  const int n_tail = parts.z == a.sig ? max(1, min(parts.y, a.max_tail)) : 1, n_pre = skip > 0 ? max(parts.x, 0) : 0;
+  const int n = n_pre + n_tail;
+  const int R = b * c.G + g, tile = R / kShareRows, row = R % kShareRows;
   const int last_block = a.max_blocks - 1;   // (a plan that was overwritten reads no further than the workspace)
-  for (int g0 = 0; g0 < G; g0 += 8 / wpr) {
-    const int g = g0 + warp / wpr, sub = warp % wpr;
-    const bool on = g < G;
-    const int R = b * G + g, tile = R / kShareRows, row = R % kShareRows;
-    // part p of the row: a share of the common pages, or of the tail
-    auto part = [&](int p, const float *&o) -> const float2 * {
-      if (p < n_pre) {
-        const size_t at = (size_t)max(0, min(first + p * a.n_tiles + tile, last_block)) * a.rows_per_block + row;
-        o = a.part_o + at * kD;
-        return reinterpret_cast<const float2 *>(a.part_ml) + at;
+  auto row_of = [&](int p, bool pre) -> size_t {   // index of part p's row in its array
+    return pre ? (size_t)max(0, min(first + p * a.n_tiles + tile, last_block)) * a.rows_per_block + row
+               : ((size_t)(p - n_pre) * a.n_items + unit) * c.G + g;
+  };
+  float M = -INFINITY, L = 0.f;
+  float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p0 = warp; p0 < n; p0 += 32 * kWarps) {   // 32 parts at a time, one per lane
+    const int mine = p0 + lane * kWarps;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (mine < n) ml = __ldcg(reinterpret_cast<const float2 *>(mine < n_pre ? a.part_ml : a.tail_ml) + row_of(mine, mine < n_pre));
+    float top = ml.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float Mn = fmaxf(M, top), old = M == -INFINITY ? 0.f : exp2f(M - Mn);
+    M = Mn;
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+    float fl = f * ml.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) fl += __shfl_xor_sync(0xffffffffu, fl, o);
+    L = L * old + fl;
+    O.x *= old; O.y *= old; O.z *= old; O.w *= old;
+    const int cnt = min(32, (n - p0 + kWarps - 1) / kWarps);
+    for (int x0 = 0; x0 < cnt; x0 += kBatch) {
+      float4 v[kBatch];
+#pragma unroll
+      for (int x = 0; x < kBatch; ++x) {
+        const int p = p0 + min(x0 + x, cnt - 1) * kWarps;
+        const bool pre = p < n_pre;
+        v[x] = __ldcg(reinterpret_cast<const float4 *>((pre ? a.part_o : a.tail_o) + row_of(p, pre) * kD) + lane);
       }
-      const size_t at = ((size_t)(p - n_pre) * a.n_items + unit) * G + g;
-      o = a.tail_o + at * kD;
-      return reinterpret_cast<const float2 *>(a.tail_ml) + at;
-    };
-    float M = -INFINITY, L = 0.f;
-    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p0 = sub; on && p0 < n; p0 += 32 * wpr) {   // 32 parts at a time, one per lane
-      const int mine = p0 + lane * wpr;
-      const float *po = nullptr;
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (mine < n) ml = __ldcg(part(mine, po));
-      float top = ml.x;
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const float Mn = fmaxf(M, top);
-      const float old = M == -INFINITY ? 0.f : exp2f(M - Mn);
-      M = Mn;
-      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-      float fl = f * ml.y;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) fl += __shfl_xor_sync(0xffffffffu, fl, o);
-      L = L * old + fl;
-      O.x *= old; O.y *= old; O.z *= old; O.w *= old;
-      const int cnt = min(32, (n - p0 + wpr - 1) / wpr);
-#pragma unroll 8
-      for (int x = 0; x < cnt; ++x) {
-        const float fx = __shfl_sync(0xffffffffu, f, x);
-        const float *src;
-        part(p0 + x * wpr, src);
-        if (fx != 0.f) {   // (a part of weight 0 may never have been written)
-          const float4 v = __ldcg(reinterpret_cast<const float4 *>(src) + lane);
-          O.x = fmaf(v.x, fx, O.x); O.y = fmaf(v.y, fx, O.y); O.z = fmaf(v.z, fx, O.z); O.w = fmaf(v.w, fx, O.w);
+      for (int x = 0; x < kBatch; ++x) {
+        const float fx = __shfl_sync(0xffffffffu, f, min(x0 + x, 31));
+        if (x0 + x < cnt && fx != 0.f) {   // (a part of weight 0 may never have been written)
+          O.x = fmaf(v[x].x, fx, O.x); O.y = fmaf(v[x].y, fx, O.y); O.z = fmaf(v[x].z, fx, O.z); O.w = fmaf(v[x].w, fx, O.w);
         }
       }
-    }
-    if (wpr > 1) {   // (at most one round: 8 / wpr >= G)
-      s_o[warp][lane] = O;
-      if (lane == 0) { s_ml[warp][0] = M; s_ml[warp][1] = L; }
-      __syncthreads();
-      if (sub == 0) {
-        float Mx = M;
-        for (int x = 1; x < wpr; ++x) Mx = fmaxf(Mx, s_ml[warp + x][0]);
-        const float w0 = M == -INFINITY ? 0.f : exp2f(M - Mx);
-        L *= w0; O.x *= w0; O.y *= w0; O.z *= w0; O.w *= w0;
-        for (int x = 1; x < wpr; ++x) {
-          const float mx = s_ml[warp + x][0], f = mx == -INFINITY ? 0.f : exp2f(mx - Mx);
-          const float4 v = s_o[warp + x][lane];
-          L = fmaf(s_ml[warp + x][1], f, L);
-          O.x = fmaf(v.x, f, O.x); O.y = fmaf(v.y, f, O.y); O.z = fmaf(v.z, f, O.z); O.w = fmaf(v.w, f, O.w);
-        }
-        M = Mx;
-      }
-    }
-    if (on && sub == 0) {
-      const size_t r = (size_t)b * c.Hq + (size_t)kvh * G + g;
-      const bool none = M == -INFINITY && L == 0.f;   // a sequence that has received nothing: zeros, -inf
-      const float inv = none ? 0.f : 1.f / L;
-      uint2 pk;
-      pk.x = pack_bf16(O.x * inv, O.y * inv);
-      pk.y = pack_bf16(O.z * inv, O.w * inv);
-      *reinterpret_cast<uint2 *>(a.out + r * kD + lane * 4) = pk;
-      if (a.lse && lane == 0) a.lse[r] = none ? -INFINITY : (M + log2f(L)) * kLn2;
     }
   }
+  s_o[warp][lane] = O;
+  if (lane == 0) { s_ml[warp][0] = M; s_ml[warp][1] = L; }
+  __syncthreads();
+  if (warp) return;
+  float Mx = M;
+#pragma unroll
+  for (int x = 1; x < kWarps; ++x) Mx = fmaxf(Mx, s_ml[x][0]);
+  const float w0 = M == -INFINITY ? 0.f : exp2f(M - Mx);
+  L *= w0; O.x *= w0; O.y *= w0; O.z *= w0; O.w *= w0;
+#pragma unroll
+  for (int x = 1; x < kWarps; ++x) {
+    const float mx = s_ml[x][0], f = mx == -INFINITY ? 0.f : exp2f(mx - Mx);
+    const float4 v = s_o[x][lane];
+    L = fmaf(s_ml[x][1], f, L);
+    O.x = fmaf(v.x, f, O.x); O.y = fmaf(v.y, f, O.y); O.z = fmaf(v.z, f, O.z); O.w = fmaf(v.w, f, O.w);
+  }
+  const bool none = Mx == -INFINITY && L == 0.f;   // a sequence that has received nothing: zeros, -inf
+  const float inv = none ? 0.f : 1.f / L;
+  uint2 pk;
+  pk.x = pack_bf16(O.x * inv, O.y * inv);
+  pk.y = pack_bf16(O.z * inv, O.w * inv);
+  *reinterpret_cast<uint2 *>(a.out + (size_t)r * kD + lane * 4) = pk;
+  if (a.lse && lane == 0) a.lse[r] = none ? -INFINITY : (Mx + log2f(L)) * kLn2;
 }
 
 struct SharedWs { size_t off_ml, off_o, off_tml, off_to, total; int max_blocks, rows, max_tail; };
@@ -722,8 +705,7 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   a.sig = share_signature(v, B);
   a.seq_ids = d_seq_ids;
   a.q = static_cast<const __nv_bfloat16 *>(d_q);
-  a.plan = static_cast<const int32_t *>(d_plan);
-  a.rec = share_record(v, a.plan, layer);
+  a.rec = share_record(v, static_cast<const int32_t *>(d_plan), layer);
   a.scale_log2 = sm_scale * kLog2e;
   a.force_wide = (cache->cfg.flags & SPKV_FLAG_PREFILL_PV_BF16) ? 1 : 0;
   a.item_skip = reinterpret_cast<int32_t *>(ws);
@@ -755,5 +737,5 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   if (launch_overlapped(tail, dim3(std::max(a.n_items, 2 * sms)), dim3(sht::kThreads), (size_t)sht::kSmemBytes, s, a, GP) !=
       cudaSuccess)
     return SPKV_E_CUDA;
-  return check_stream_error(launch_overlapped(shared_merge_kernel, dim3(a.n_items), dim3(256), 0, s, a));
+  return check_stream_error(launch_overlapped(shared_merge_kernel, dim3(B * v.Hq), dim3(128), 0, s, a));
 }

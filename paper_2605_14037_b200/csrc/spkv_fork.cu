@@ -147,15 +147,21 @@ __global__ void __launch_bounds__(256) share_cut_kernel(CacheView c, const int32
   }
   __syncthreads();
   if (threadIdx.x == 0) {
+    const int n_tail = max(1, min((s_longest + kTailPages - 1) / kTailPages, kMaxTailItems / (B * c.Hkv)));
     int at = 0;
     for (int h = 0; h < c.Hkv; ++h) {
-      share_head(rec, h)[1] = at;
-      at += (share_head(rec, h)[0] + lo - 1) / lo * n_tiles;
+      int32_t *hd = share_head(rec, h);
+      const int n_pre = (hd[0] + lo - 1) / lo;
+      hd[1] = at;
+      hd[4] = n_pre;
+      hd[5] = n_tail;
+      hd[6] = sig;
+      hd[7] = 0;
+      at += n_pre * n_tiles;
     }
     rec[0] = lo;
     rec[1] = at;
-    rec[2] = max(1, min((s_longest + kTailPages - 1) / kTailPages, kMaxTailItems / (B * c.Hkv)));
-    rec[3] = 0;
+    rec[2] = rec[3] = 0;
     if (blockIdx.x == 0) plan[0] = sig;
   }
   __syncthreads();

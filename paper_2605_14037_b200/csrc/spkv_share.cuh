@@ -1,8 +1,9 @@
 // What a batch with a common prefix decodes by: the plan's layout and the cut of the common pages.
 //
 // Plan (int32): header {signature, 0 ...}, then one record per layer:
-//   {pages per share, blocks, tail shares, 0}
-//   per KV head  {common pages, first block, page-table row and unit of the batch's first sequence}
+//   {pages per share, blocks, 0, 0}
+//   per KV head  {common pages, first block, page-table row and unit of the batch's first sequence},
+//                {prefix shares, tail shares, signature, 0}
 //   per block    {KV head, row tile, first page, pages (0: no work)}, {common pages, row, unit, signature}
 // The queries of KV head h are the rows (b, g) -> b * G + g of its group in every sequence, cut into tiles
 // of kShareRows.  A block takes one share of one head's common pages for one row tile; block first[h] +
@@ -15,7 +16,7 @@
 
 namespace spkv {
 
-constexpr int kSharePlanHdr = 8, kShareHdr = 4, kShareHead = 4, kShareDesc = 8;
+constexpr int kSharePlanHdr = 8, kShareHdr = 4, kShareHead = 8, kShareDesc = 8;
 constexpr int kShareRows = 256;       // query rows per block: two slots of 128
 constexpr int kMinSharedPages = 1;    // fewer common pages than this are read per sequence
 constexpr int kMinSharePages = 4;     // a share is not cut shorter

@@ -73,7 +73,7 @@ def queries(wl, t=-1):
 
 def commons(cache, plan, layer=0):
     p = plan.cpu().numpy().view(np.int32)[8:].reshape(cache.cfg.n_layers, -1)[layer]
-    return p[4:4 + 4 * cache.cfg.n_kv_heads:4]
+    return p[4:4 + 8 * cache.cfg.n_kv_heads:8]
 
 
 @pytest.mark.parametrize("B,Hq,Hkv,T0,m,rates", [
