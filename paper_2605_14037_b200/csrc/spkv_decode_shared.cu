@@ -15,17 +15,17 @@
 //
 // Prefix kernel.  Per page and 128-row slot: S = Q K^T (8 MMAs M128 N64 K16 into tensor memory), softmax
 // in registers (thread = row = TMEM lane), P in fp16 back over the scores, O += P V with the page's values
-// rescaled to fp16 by two converter warps, or two bf16 terms for a unit of wide-ranging values
+// rescaled to fp16 by a converter warp, or two bf16 terms for a unit of wide-ranging values
 // (value_scale).  No masks: common pages are full and every query sees all of them.
 //   * More than 128 rows in the tile (kAlt = false): slot h holds rows [128 h, 128 h + 128), both walk
 //     every page.  Scores of page j + 2 are issued behind P.V(j), so a slot's next scores are ready.
 //   * At most 128 rows (kAlt): both slots hold the same rows and take alternate pages, which halves the
 //     softmax time per page; scores of a slot's next page are issued behind P.V of its last one.  One of the two
 //     is joined into the other through shared memory at the end.
-// Shared memory: Q (64 KB; kAlt 32 KB) + 5 (4, which leaves room for a tail block) page stages.  Tensor memory: score buffer b of slot h at
+// Shared memory: Q (64 KB; kAlt 32 KB) + 4 (5) page stages, which leaves 34 KB to a tail block.  Tensor memory: score buffer b of slot h at
 // [64 (2h + b), +64), O of slot h at [256 + 128 h, +128).
-// Warps: 0 MMA issue slot 0, 1 page loader, 2-3 value conversion (2: tensor memory), 4-7 / 8-11 softmax of slot 0 / 1,
-// 12 MMA issue slot 1.  All waits are bounded.
+// Warps: 0 / 3 MMA issue of slot 0 / 1, 1 page loader, 2 value conversion and tensor memory, 4-7 / 8-11 softmax
+// of slot 0 / 1.  All waits are bounded.
 #include <algorithm>
 #include <math.h>
 
@@ -35,12 +35,14 @@
 namespace spkv {
 
 namespace shp {
-constexpr int kThreads = 416;
-constexpr int kMmaWarp0 = 0, kMmaWarp1 = 12, kLoaderWarp = 1, kTmemWarp = 2;
-constexpr int kTmemCols = 512, kConvThreads = 64;
+// Twelve warps, three on each of the SM's four register files: at up to 128 registers a thread a tail block of
+// four warps finds room beside them (thirteen warps fill one file, and the tail ran after the prefix).
+constexpr int kThreads = 384;
+constexpr int kMmaWarp0 = 0, kLoaderWarp = 1, kConvWarp = 2, kMmaWarp1 = 3;
+constexpr int kTmemCols = 512;
 constexpr float kPBias = 7.f;   // P is stored as 2^7 p
 enum { B_KV_FULL = 0, B_KV_EMPTY = 8, B_V_READY = 16, B_S_FULL = 24 /* [2h+b] */, B_P_FULL = 28, B_O_DONE = 32, B_COUNT = 36 };
-__host__ __device__ constexpr int stages(bool alt) { return alt ? 4 : 5; }
+__host__ __device__ constexpr int stages(bool alt) { return alt ? 5 : 4; }
 __host__ __device__ constexpr int off_kv(bool alt) { return alt ? 32768 : 65536; }
 __host__ __device__ constexpr int off_bar(bool alt) { return off_kv(alt) + stages(alt) * kPageBytes; }
 __host__ __device__ constexpr int smem_bytes(bool alt) { return off_bar(alt) + 512; }
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
   if (warp == kLoaderWarp && lane == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&bar[B_KV_FULL + i], 1);
-      mbar_init(&bar[B_V_READY + i], kConvThreads);
+      mbar_init(&bar[B_V_READY + i], 32);
     }
     // per slot and parity of the slot's page count: one phase per two of its pages
     for (int i = 0; i < 4; ++i) {
@@ -144,19 +146,29 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
     if (lane == 0) { s_desc[8] = valid; s_desc[9] = (int)vm; }
   } else {
     // Q rows -> two slabs of 128 rows x 128 B per slot, 128-byte swizzle; rows past the last are zero
+    // (six loads in flight per thread: one after the other they took 3 us, 7 for two slots)
     const int qt = warp == 0 ? lane : tid - 32;   // the threads but for the loader warp
-    for (int x = qt; x < (kAlt ? 1 : 2) * 128 * 16; x += kThreads - 32) {
-      const int h = x >> 11, r = (x >> 4) & 127, ch = x & 15;
-      const int R = row_base + h * 128 + r;
-      uint4 val = make_uint4(0, 0, 0, 0);
-      if (h * 128 + r < n_rows) {
-        const int b = R / c.G, g = R - b * c.G;
-        val = *reinterpret_cast<const uint4 *>(a.q + ((size_t)b * c.Hq + kvh * c.G + g) * kD + ch * 8);
+    constexpr int kChunks = (kAlt ? 1 : 2) * 128 * 16, kQThreads = kThreads - 32, kBatch = 6;
+    for (int x0 = qt; x0 < kChunks; x0 += kBatch * kQThreads) {
+      uint4 val[kBatch];
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        const int x = x0 + y * kQThreads, r = x >> 4;   // r: row of the tile (slot 1's follow slot 0's)
+        val[y] = make_uint4(0, 0, 0, 0);
+        if (x < kChunks && r < n_rows) {
+          const int R = row_base + r, b = R / c.G, g = R - b * c.G;
+          val[y] = *reinterpret_cast<const uint4 *>(a.q + ((size_t)b * c.Hq + kvh * c.G + g) * kD + (x & 15) * 8);
+        }
       }
-      *reinterpret_cast<uint4 *>(smem + h * 32768 + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val;
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        const int x = x0 + y * kQThreads, h = x >> 11, r = (x >> 4) & 127, ch = x & 15;
+        if (x < kChunks)
+          *reinterpret_cast<uint4 *>(smem + h * 32768 + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val[y];
+      }
     }
     fence_async_smem();
-    if (warp == kTmemWarp) {
+    if (warp == kConvWarp) {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
                    "n"(kTmemCols) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -199,7 +211,7 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
         mbar_wait_bounded(&bar[B_KV_FULL + (k % kStages)], (k / kStages) & 1);
   } else if (warp == kMmaWarp0 || warp == kMmaWarp1) {
     // ---------------------------------------------------------------- MMA issue (whole warp, one elected lane issues)
-    const int h = warp == kMmaWarp0 ? 0 : 1, n_mine = slot_pages(h);
+    const int h = warp == kMmaWarp1, n_mine = slot_pages(h);
     constexpr uint32_t idesc_qk = instr_desc(128, 64, false), idesc_pv = instr_desc(128, 128, true, true),
                        idesc_pv_bf16 = instr_desc(128, 128, true, false);
     constexpr uint32_t kStageUnits = kPageBytes >> 4;
@@ -226,19 +238,18 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
       if (i + kAhead < n_mine) issue_qk(i + kAhead);   // (behind P.V(i): the pipe runs a thread's instructions in order)
       else umma_commit(&bar[B_O_DONE + 2 * h + b]);
     }
-  } else if (warp == 2 || warp == 3) {
+  } else if (warp == kConvWarp) {
     // ---------------------------------------------------------------- value converter: bf16 -> scaled fp16, in place
-    const int ct = tid - 64;
     for (int j = 0; j < n_pages; ++j) {
       const int s = j % kStages;
       if (!mbar_wait_bounded(&bar[B_KV_FULL + s], (j / kStages) & 1)) { failed = true; break; }
-      uint4 *vb = reinterpret_cast<uint4 *>(smem + kSKV + s * kPageBytes + kBlockElems * 2) + ct;
-#pragma unroll
-      for (int x = 0; x < (wide ? 0 : 1024 / kConvThreads); ++x) {
-        uint4 r = vb[x * kConvThreads];
+      uint4 *vb = reinterpret_cast<uint4 *>(smem + kSKV + s * kPageBytes + kBlockElems * 2) + lane;
+#pragma unroll 8
+      for (int x = 0; x < (wide ? 0 : 32); ++x) {
+        uint4 r = vb[x * 32];
         r.x = bf16x2_to_f16x2(r.x, v_scale); r.y = bf16x2_to_f16x2(r.y, v_scale);
         r.z = bf16x2_to_f16x2(r.z, v_scale); r.w = bf16x2_to_f16x2(r.w, v_scale);
-        vb[x * kConvThreads] = r;
+        vb[x * 32] = r;
       }
       fence_async_smem();
       mbar_arrive(&bar[B_V_READY + s]);
@@ -408,26 +419,28 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
   if (failed) set_status(c, SPKV_E_TIMEOUT);
   fence_before();
   __syncthreads();
-  if (warp == kTmemWarp)
+  if (warp == kConvWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "n"(shp::kTmemCols) : "memory");
 }
 
 // ---- tail ------------------------------------------------------------------------------------------
 namespace sht {
 constexpr int kThreads = 128, kWarps = 4;
-constexpr int off_bar = 2 * kPageBytes, kSmemBytes = off_bar + 128;
+// one page, over which the four warps join their G rows of 132 floats at the end (G = 16: 33 KB)
+__host__ __device__ constexpr int off_bar(int NH) { return NH == 1 ? kPageBytes : kWarps * 16 * 132 * 4; }
+__host__ __device__ constexpr int smem_bytes(int NH) { return off_bar(NH) + 128; }
 }  // namespace sht
 
 // Item = share * n_items + unit.  A unit's pages are what its compact cache holds behind the common pages,
 // then its ring; they are cut into up to `shares` (plan) pieces of at least four.  The four warps take 16
 // pairs each of every page and join at the end through the page stages.
 template <int NH>
-__global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_kernel(SharedArgs a, int GP) {
+__global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_kernel(SharedArgs a) {
   using namespace sht;
   extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = c.G;
-  uint64_t *full = reinterpret_cast<uint64_t *>(smem + off_bar);
+  uint64_t *full = reinterpret_cast<uint64_t *>(smem + off_bar(NH));   // [0] keys, [1] values
   volatile int *s_it = reinterpret_cast<volatile int *>(full + 2);   // share exists, skip, compact pages, length behind
                                                                      // the common pages, ring pairs, first page, pages
   if (tid == 0) {
@@ -439,7 +452,7 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
   // everything before the prefix launch is complete and was written through generic stores
   asm volatile("fence.proxy.async;" ::: "memory");
   const uint64_t pol = l2_evict_first_policy();
-  int loads = 0;        // pages loaded so far: stage loads & 1, phase (loads >> 1) & 1
+  int loads = 0;        // pages loaded so far: their parity is the barriers' phase
   bool failed = false;
   for (int item = blockIdx.x;; item += gridDim.x) {
     const int unit = item % a.n_items, share = item / a.n_items;
@@ -500,18 +513,18 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
         entry = p < nk ? checked_page(c, ldcg_keep(&unit_table(c, trow)[skip + p]), (int)ring_page(c, u, 0))
                        : (int)ring_page(c, u, p - nk);
     };
-    auto load = [&](int i) {            // warp 0
-      if ((i & 31) == 0) fetch_entries(i);
+    auto load = [&](int i, int half) {  // warp 0: keys (half = 0; first) or values of page i
+      if (half == 0 && (i & 31) == 0) fetch_entries(i);
       const int gp = __shfl_sync(0xffffffffu, entry, i & 31);
       if (lane == 0) {
-        uint64_t *bar = &full[(loads + i) & 1];
-        mbar_arrive_expect_tx(bar, kPageBytes);
-        bulk_load_hint(smem + ((loads + i) & 1) * kPageBytes, c.pages + (int64_t)gp * kPageElems, kPageBytes, bar, pol);
+        mbar_arrive_expect_tx(&full[half], kPageBytes / 2);
+        bulk_load_hint(smem + half * (kPageBytes / 2), c.pages + (int64_t)gp * kPageElems + half * kBlockElems,
+                       kPageBytes / 2, &full[half], pol);
       }
     };
     if (warp == 0) {
-      load(0);
-      if (n > 1) load(1);
+      load(0, 0);
+      load(0, 1);
     }
     uint32_t qb[NH][8][2];
     float m[NH][2], l[NH][2], o[NH][8][4];
@@ -525,39 +538,47 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
       for (int mt = 0; mt < 8; ++mt) o[hn][mt][0] = o[hn][mt][1] = o[hn][mt][2] = o[hn][mt][3] = 0.f;
     }
     for (int i = 0; i < n; ++i) {
-      const int st = (loads + i) & 1, p = p0 + i;
+      const int p = p0 + i;
       const int valid = p < nk ? min(kP, len - p * kP) : min(kP, n_ring - (p - nk) * kP);
-      if (!mbar_wait_bounded(&full[st], ((loads + i) >> 1) & 1)) failed = true;
+      const uint32_t ph = (loads + i) & 1;
       const int tok0 = warp * 16;
-      if (!failed && tok0 < valid) {
-        const uint32_t sK = smem_u32(smem + st * kPageBytes), sV = sK + kBlockElems * 2;
-        float s[NH][4];
-        qk_tile_t<NH>(s, qb, sK, tok0, lane);
-        softmax_pv_tile_t<NH>(s, valid, a.scale_log2, m, l, o, sV, tok0, lane);
-      }
-      failed = __syncthreads_or(failed);   // all four warps are done with the stage
+      const uint32_t sK = smem_u32(smem), sV = sK + kBlockElems * 2;
+      float s[NH][4];
+      if (!mbar_wait_bounded(&full[0], ph)) failed = true;
+      if (!failed && tok0 < valid) qk_tile_t<NH>(s, qb, sK, tok0, lane);
+      failed = __syncthreads_or(failed);   // all four warps are done with the keys
       if (failed) {
         // do not leave while copies may still be landing
-        if (tid == 0)
-          for (int k = i; k < min(i + 2, n); ++k) mbar_wait_bounded(&full[(loads + k) & 1], ((loads + k) >> 1) & 1);
+        if (tid == 0) { mbar_wait_bounded(&full[0], ph); mbar_wait_bounded(&full[1], ph); }
         break;
       }
-      if (warp == 0 && i + 2 < n) load(i + 2);
+      if (warp == 0 && i + 1 < n) load(i + 1, 0);
+      if (!mbar_wait_bounded(&full[1], ph)) failed = true;
+      if (!failed && tok0 < valid) softmax_pv_tile_t<NH>(s, valid, a.scale_log2, m, l, o, sV, tok0, lane);
+      failed = __syncthreads_or(failed);   // ... and with the values
+      if (failed) {
+        if (tid == 0) {
+          mbar_wait_bounded(&full[1], ph);
+          if (i + 1 < n) mbar_wait_bounded(&full[0], ph ^ 1);
+        }
+        break;
+      }
+      if (warp == 0 && i + 1 < n) load(i + 1, 1);
     }
     if (failed) break;
     loads += n;
-    // join the four warps: rows [warp][GP][132] over the page stages (every copy of the item has landed)
+    // join the four warps: rows [warp][G][132] over the page (every copy of the item has landed)
     float *red = reinterpret_cast<float *>(smem);
-    segment_hand_over<NH>(red, warp, GP, G, m, l, o, lane);
+    segment_hand_over<NH>(red, warp, G, G, m, l, o, lane);
     __syncthreads();
     for (int g = warp; g < G; g += kWarps) {
       float M = -INFINITY, L = 0.f;
       float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, red[((size_t)w * GP + g) * 132 + 128]);
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, red[((size_t)w * G + g) * 132 + 128]);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float *src = red + ((size_t)w * GP + g) * 132;
+        const float *src = red + ((size_t)w * G + g) * 132;
         const float f = src[128] == -INFINITY ? 0.f : fast_exp2(src[128] - M);
         const float4 v = *reinterpret_cast<const float4 *>(src + lane * 4);
         L += src[129] * f;
@@ -722,11 +743,16 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   const bool alt = w.rows <= 128;
   auto prefix = alt ? shared_prefix_kernel<true> : shared_prefix_kernel<false>;
   const int smem = shp::smem_bytes(alt);
-  int GP = 1;
-  while (GP < v.G) GP <<= 1;
-  auto tail = GP > 8 ? shared_tail_kernel<2> : shared_tail_kernel<1>;
+  auto tail = v.G > 8 ? shared_tail_kernel<2> : shared_tail_kernel<1>;
+  const int tail_smem = sht::smem_bytes(v.G > 8 ? 2 : 1);
+  // (the whole of an SM's shared memory for both: with the default split, which fits one prefix block, a
+  // tail block finds none left beside it)
   if (cudaFuncSetAttribute(prefix, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-      cudaFuncSetAttribute(tail, cudaFuncAttributeMaxDynamicSharedMemorySize, sht::kSmemBytes) != cudaSuccess)
+      cudaFuncSetAttribute(tail, cudaFuncAttributeMaxDynamicSharedMemorySize, tail_smem) != cudaSuccess ||
+      cudaFuncSetAttribute(prefix, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) !=
+          cudaSuccess ||
+      cudaFuncSetAttribute(tail, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) !=
+          cudaSuccess)
     return SPKV_E_CUDA;
   // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
   // cover; a plain launch waits for all of them.
@@ -734,7 +760,7 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   cache->last_kind = kLastOther;
   if (launch_link(!plain, prefix, dim3(grid), dim3(shp::kThreads), (size_t)smem, s, a) != cudaSuccess) return SPKV_E_CUDA;
   // one block per unit, and enough of them that the shares of long units find a block each
-  if (launch_overlapped(tail, dim3(std::max(a.n_items, 2 * sms)), dim3(sht::kThreads), (size_t)sht::kSmemBytes, s, a, GP) !=
+  if (launch_overlapped(tail, dim3(std::max(a.n_items, 2 * sms)), dim3(sht::kThreads), (size_t)tail_smem, s, a) !=
       cudaSuccess)
     return SPKV_E_CUDA;
   return check_stream_error(launch_overlapped(shared_merge_kernel, dim3(B * v.Hq), dim3(128), 0, s, a));
