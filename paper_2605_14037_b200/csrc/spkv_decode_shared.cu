@@ -10,22 +10,22 @@
 // The tail does not depend on the prefix launch.  Its blocks are small (4 warps, two page stages), so that
 // one fits on an SM beside a prefix block of up to 128 rows, and are launched as programmatic
 // dependents: the prefix kernel has waited for everything earlier on the stream before it lets them start.
-// The tail waits for the prefix launch at its own end, so that the merge, which waits for the tail,
-// may read both.
+// The tail's first block waits for the prefix launch at its end, so that the merge, which waits for the
+// tail, may read both.
 //
 // Prefix kernel.  Per page and 128-row slot: S = Q K^T (8 MMAs M128 N64 K16 into tensor memory), softmax
 // in registers (thread = row = TMEM lane), P in fp16 back over the scores, O += P V with the page's values
-// rescaled to fp16 by a converter warp, or two bf16 terms for a unit of wide-ranging values
+// rescaled to fp16 by converter warps, or two bf16 terms for a unit of wide-ranging values
 // (value_scale).  No masks: common pages are full and every query sees all of them.
 //   * More than 128 rows in the tile (kAlt = false): slot h holds rows [128 h, 128 h + 128), both walk
 //     every page.  Scores of page j + 2 are issued behind P.V(j), so a slot's next scores are ready.
 //   * At most 128 rows (kAlt): both slots hold the same rows and take alternate pages, which halves the
 //     softmax time per page; scores of a slot's next page are issued behind P.V of its last one.  One of the two
 //     is joined into the other through shared memory at the end.
-// Shared memory: Q (64 KB; kAlt 32 KB) + 4 (5) page stages, which leaves 34 KB to a tail block.  Tensor memory: score buffer b of slot h at
+// Shared memory: Q (64 KB; kAlt 32 KB) + rings of 4 (5) key and 4 (5) value blocks, which leaves 34 KB to a tail block.  Tensor memory: score buffer b of slot h at
 // [64 (2h + b), +64), O of slot h at [256 + 128 h, +128).
-// Warps: 0 / 3 MMA issue of slot 0 / 1, 1 page loader, 2 value conversion and tensor memory, 4-7 / 8-11 softmax
-// of slot 0 / 1.  All waits are bounded.
+// Warps: 0 / 2 MMA issue of slot 0 / 1, 1 page loader, 3 tensor memory, 4-7 / 8-11 softmax of slot 0 / 1, 12-15 value
+// conversion.  All waits are bounded.
 #include <algorithm>
 #include <math.h>
 
@@ -35,16 +35,26 @@
 namespace spkv {
 
 namespace shp {
-// Twelve warps, three on each of the SM's four register files: at up to 128 registers a thread a tail block of
-// four warps finds room beside them (thirteen warps fill one file, and the tail ran after the prefix).
-constexpr int kThreads = 384;
-constexpr int kMmaWarp0 = 0, kLoaderWarp = 1, kConvWarp = 2, kMmaWarp1 = 3;
+// Sixteen warps, four on each of the SM's register files: at 104 registers a thread a tail block of four warps of
+// 96 finds room beside them (with 13 warps of 128 one file was full, and the tail ran after the prefix).
+// Four warps convert values: one needed 2000 cycles per page and set the pace.
+constexpr int kThreads = 512, kRegs = 104;
+constexpr int kMmaWarp0 = 0, kLoaderWarp = 1, kMmaWarp1 = 2, kTmemWarp = 3;
+constexpr int kConvThreads = 128;   // warps 12-15
 constexpr int kTmemCols = 512;
 constexpr float kPBias = 7.f;   // P is stored as 2^7 p
-enum { B_KV_FULL = 0, B_KV_EMPTY = 8, B_V_READY = 16, B_S_FULL = 24 /* [2h+b] */, B_P_FULL = 28, B_O_DONE = 32, B_COUNT = 36 };
-__host__ __device__ constexpr int stages(bool alt) { return alt ? 5 : 4; }
-__host__ __device__ constexpr int off_kv(bool alt) { return alt ? 32768 : 65536; }
-__host__ __device__ constexpr int off_bar(bool alt) { return off_kv(alt) + stages(alt) * kPageBytes; }
+constexpr int kMaxRing = 5;
+enum { B_K_FULL = 0, B_K_EMPTY = 5, B_V_FULL = 10, B_V_EMPTY = 15, B_V_READY = 20, B_S_FULL = 25 /* [2h+b] */, B_P_FULL = 29,
+       B_O_DONE = 33, B_COUNT = 37 };
+// Key and value blocks travel in rings of their own: a key block is free again as soon as the scores are made, two
+// pages before the values of its page are needed, so nearly every buffer has a copy in flight (a page
+// takes about 2 us to arrive under load; with whole pages in one ring of four, three were in use and
+// one in flight: 2200 cycles per page).
+__host__ __device__ constexpr int ring(bool alt) { return alt ? 5 : 4; }   // key blocks; as many value blocks
+constexpr int kBlockBytes = kPageBytes / 2, kKeyLead = 2;   // keys are loaded two pages ahead of values
+__host__ __device__ constexpr int off_k(bool alt) { return alt ? 32768 : 65536; }
+__host__ __device__ constexpr int off_v(bool alt) { return off_k(alt) + ring(alt) * kBlockBytes; }
+__host__ __device__ constexpr int off_bar(bool alt) { return off_v(alt) + ring(alt) * kBlockBytes; }
 __host__ __device__ constexpr int smem_bytes(bool alt) { return off_bar(alt) + 512; }
 constexpr int kJoinStride = 132;   // floats per row of the hand-over between the slots (kAlt)
 }  // namespace shp
@@ -52,6 +62,7 @@ constexpr int kJoinStride = 132;   // floats per row of the hand-over between th
 struct SharedArgs {
   CacheView c;
   int layer, B, n_items, n_tiles, rows_per_block, sig;
+  unsigned long long g_inv;     // ceil(2^32 / G): row / G as a product and a shift (rows < 2^15, G <= 16)
   const int32_t *seq_ids;
   const __nv_bfloat16 *q;       // [B][Hq][128]
   const int32_t *rec;           // the layer's record of the plan
@@ -61,31 +72,39 @@ struct SharedArgs {
   int max_blocks;
   float *tail_o, *tail_ml;      // tail: [share][item][G][128], [share][item][G][2]
   int max_tail;                 // shares the workspace holds
+  int row_base, row_heads;      // page-table rows of the layer: row_base + seq * row_heads + rank of the KV head
+  unsigned long long local_mask;
   int32_t *item_skip;           // [n_items] common pages the tail left out (0: it read the unit in full)
   __nv_bfloat16 *out;
   float *lse;
 };
 
+// Weight of a part (m, l) against the common maximum M >= m.  A part without a visible key has m = -inf and
+// l = 0; m = -inf with another l means that its scores were NaN (a maximum passes over NaN), which stays NaN.
+__device__ inline float part_weight(float m, float l, float M) {
+  return m == -INFINITY ? (l == 0.f ? 0.f : NAN) : fast_exp2(m - M);
+}
 __device__ inline int4 ldcg4(const int32_t *p) { return __ldcg(reinterpret_cast<const int4 *>(p)); }
 
-// page j of a share into its stage (one thread)
+// key (half = 0) or value block of page j of a share into its ring (one thread)
 template <bool kAlt>
-__device__ inline void load_page(const SharedArgs &a, unsigned char *smem, uint64_t *bar, int j, int gp, uint64_t pol) {
+__device__ inline void load_block(const SharedArgs &a, unsigned char *smem, uint64_t *bar, int half, int j, int gp, uint64_t pol) {
   using namespace shp;
-  const int s = j % stages(kAlt);
-  unsigned char *dst = smem + off_kv(kAlt) + s * kPageBytes;
-  const __nv_bfloat16 *src = a.c.pages + (int64_t)gp * kPageElems;
-  mbar_arrive_expect_tx(&bar[B_KV_FULL + s], kPageBytes);
+  const int s = j % ring(kAlt);
+  unsigned char *dst = smem + (half ? off_v(kAlt) : off_k(kAlt)) + s * kBlockBytes;
+  const __nv_bfloat16 *src = a.c.pages + (int64_t)gp * kPageElems + half * kBlockElems;
+  uint64_t *full = &bar[(half ? B_V_FULL : B_K_FULL) + s];
+  mbar_arrive_expect_tx(full, kBlockBytes);
   // a page that several row tiles read stays in L2 for the others
-  if (a.n_tiles == 1) bulk_load_hint(dst, src, kPageBytes, &bar[B_KV_FULL + s], pol);
-  else bulk_load(dst, src, kPageBytes, &bar[B_KV_FULL + s]);
+  if (a.n_tiles == 1) bulk_load_hint(dst, src, kBlockBytes, full, pol);
+  else bulk_load(dst, src, kBlockBytes, full);
 }
 
 template <bool kAlt>
-__global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedArgs a) {
+__global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
   using namespace tc5;
   using namespace shp;
-  constexpr int kStages = stages(kAlt), kSKV = off_kv(kAlt);
+  constexpr int kRing = ring(kAlt);
   constexpr int kAhead = kAlt ? 1 : 2;       // how many of a slot's pages its scores run ahead of P.V
   extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
@@ -96,9 +115,10 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
   // ---- block-local set-up, then this block's share.  The loader warp goes ahead: descriptor (one trip to
   // memory), page-table entries (the second), first pages; the others load Q meanwhile.
   if (warp == kLoaderWarp && lane == 0) {
-    for (int i = 0; i < kStages; ++i) {
-      mbar_init(&bar[B_KV_FULL + i], 1);
-      mbar_init(&bar[B_V_READY + i], 32);
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&bar[B_K_FULL + i], 1);
+      mbar_init(&bar[B_V_FULL + i], 1);
+      mbar_init(&bar[B_V_READY + i], kConvThreads);
     }
     // per slot and parity of the slot's page count: one phase per two of its pages
     for (int i = 0; i < 4; ++i) {
@@ -116,7 +136,10 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
     // one commit per MMA warp that uses a page
     if (lane == 0) {
       const int left = a.B * c.G - s_desc[1] * kShareRows;
-      for (int i = 0; i < kStages; ++i) mbar_init(&bar[B_KV_EMPTY + i], (!kAlt && left > 128) ? 2 : 1);
+      for (int i = 0; i < kRing; ++i) {
+        mbar_init(&bar[B_K_EMPTY + i], (!kAlt && left > 128) ? 2 : 1);
+        mbar_init(&bar[B_V_EMPTY + i], (!kAlt && left > 128) ? 2 : 1);
+      }
       mbar_fence_init();
     }
   }
@@ -139,36 +162,27 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
     // (stale plan: the unit is shorter by now; the tail sees the same and nobody reads this share's result)
     const bool valid = len / kP >= common;
     if (valid) first_entry = checked_page(c, first_entry, (int)ring_page(c, u, 0));
-    for (int j = 0; j < min(n_pages, kStages) && valid; ++j) {
-      const int gp = __shfl_sync(0xffffffffu, first_entry, j);
-      if (lane == 0) load_page<kAlt>(a, smem, bar, j, gp, pol);
+    for (int j = 0; j < kRing && valid; ++j) {   // the steps of the loop below that find every buffer empty
+      const int gk = __shfl_sync(0xffffffffu, first_entry, j);
+      const int gv = __shfl_sync(0xffffffffu, first_entry, max(j - kKeyLead, 0));
+      if (lane == 0 && j < n_pages) load_block<kAlt>(a, smem, bar, 0, j, gk, pol);
+      if (lane == 0 && j >= kKeyLead && j - kKeyLead < n_pages) load_block<kAlt>(a, smem, bar, 1, j - kKeyLead, gv, pol);
     }
     if (lane == 0) { s_desc[8] = valid; s_desc[9] = (int)vm; }
   } else {
     // Q rows -> two slabs of 128 rows x 128 B per slot, 128-byte swizzle; rows past the last are zero
-    // (six loads in flight per thread: one after the other they took 3 us, 7 for two slots)
+    // (asynchronous copies, all in flight at once: as loads, one after the other, they took 3 us, 7 for two slots)
     const int qt = warp == 0 ? lane : tid - 32;   // the threads but for the loader warp
-    constexpr int kChunks = (kAlt ? 1 : 2) * 128 * 16, kQThreads = kThreads - 32, kBatch = 6;
-    for (int x0 = qt; x0 < kChunks; x0 += kBatch * kQThreads) {
-      uint4 val[kBatch];
-#pragma unroll
-      for (int y = 0; y < kBatch; ++y) {
-        const int x = x0 + y * kQThreads, r = x >> 4;   // r: row of the tile (slot 1's follow slot 0's)
-        val[y] = make_uint4(0, 0, 0, 0);
-        if (x < kChunks && r < n_rows) {
-          const int R = row_base + r, b = R / c.G, g = R - b * c.G;
-          val[y] = *reinterpret_cast<const uint4 *>(a.q + ((size_t)b * c.Hq + kvh * c.G + g) * kD + (x & 15) * 8);
-        }
-      }
-#pragma unroll
-      for (int y = 0; y < kBatch; ++y) {
-        const int x = x0 + y * kQThreads, h = x >> 11, r = (x >> 4) & 127, ch = x & 15;
-        if (x < kChunks)
-          *reinterpret_cast<uint4 *>(smem + h * 32768 + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val[y];
-      }
+    for (int x = qt; x < (kAlt ? 1 : 2) * 128 * 16; x += kThreads - 32) {
+      const int tr = x >> 4, h = x >> 11, r = tr & 127, ch = x & 15;   // row of the tile; slot, row in it, chunk
+      const int R = row_base + min(tr, n_rows - 1), b = (int)(((unsigned long long)R * a.g_inv) >> 32), g = R - b * c.G;
+      const __nv_bfloat16 *src = a.q + ((size_t)b * c.Hq + kvh * c.G + g) * kD + ch * 8;
+      const uint32_t dst = smem_u32(smem + h * 32768 + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(tr < n_rows ? 16 : 0) : "memory");
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     fence_async_smem();
-    if (warp == kConvWarp) {
+    if (warp == kTmemWarp) {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
                    "n"(kTmemCols) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -190,71 +204,85 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
     // nothing to do but to give the tensor memory back
   } else if (warp == kLoaderWarp) {
     // ---------------------------------------------------------------- page loader
-    int j = min(n_pages, kStages);
-    for (int base = 0; base < n_pages && !failed; base += 32) {
-      int page = first_entry;
-      if (base > 0 && base + lane < n_pages)
-        page = checked_page(c, ldcg_keep(&unit_table(c, trow)[j_begin + base + lane]), (int)ring_page(c, u, 0));
-      const int end = min(base + 32, n_pages);
-      for (; j < end; ++j) {
-        const int gp = __shfl_sync(0xffffffffu, page, j - base);
-        if (lane == 0) {
-          if (!mbar_wait_bounded(&bar[B_KV_EMPTY + j % kStages], ((j / kStages) - 1) & 1)) failed = true;
-          if (!failed) load_page<kAlt>(a, smem, bar, j, gp, pol);
-        }
-        failed = __shfl_sync(0xffffffffu, (int)failed, 0) != 0;
-        if (failed) break;
+    // step j: the keys of page j, the values of page j - 2
+    int entry = first_entry, older = 0;   // global page indices of this lane in the current and the previous 32 pages
+    int j = kRing;
+    auto wait_empty = [&](int which, int jj) {
+      return jj < kRing || mbar_wait_bounded(&bar[which + jj % kRing], ((jj / kRing) - 1) & 1);
+    };
+    for (; j < n_pages + kKeyLead; ++j) {
+      if ((j & 31) == 0) {
+        older = entry;
+        if (j + lane < n_pages)
+          entry = checked_page(c, ldcg_keep(&unit_table(c, trow)[j_begin + j + lane]), (int)ring_page(c, u, 0));
       }
+      const int jv = j - kKeyLead;
+      const int gk = __shfl_sync(0xffffffffu, entry, j & 31);
+      const int gv = __shfl_sync(0xffffffffu, (jv >> 5) == (j >> 5) ? entry : older, jv & 31);
+      if (lane == 0) {
+        if (jv >= 0 && jv < n_pages) {
+          failed = !wait_empty(B_V_EMPTY, jv);
+          if (!failed) load_block<kAlt>(a, smem, bar, 1, jv, gv, pol);
+        }
+        if (!failed && j < n_pages) {
+          failed = !wait_empty(B_K_EMPTY, j);
+          if (!failed) load_block<kAlt>(a, smem, bar, 0, j, gk, pol);
+        }
+      }
+      failed = __shfl_sync(0xffffffffu, (int)failed, 0) != 0;
+      if (failed) break;
     }
-    if (failed && lane == 0)   // do not leave while copies may still be landing
-      for (int k = max(0, j - kStages); k < j; ++k)
-        mbar_wait_bounded(&bar[B_KV_FULL + (k % kStages)], (k / kStages) & 1);
+    if (failed && lane == 0) {   // do not leave while copies may still be landing
+      for (int k = max(0, j - kRing); k < min(j, n_pages); ++k) mbar_wait_bounded(&bar[B_K_FULL + (k % kRing)], (k / kRing) & 1);
+      for (int k = max(0, j - kKeyLead - kRing); k < min(j - kKeyLead + 1, n_pages); ++k)
+        mbar_wait_bounded(&bar[B_V_FULL + (k % kRing)], (k / kRing) & 1);
+    }
   } else if (warp == kMmaWarp0 || warp == kMmaWarp1) {
     // ---------------------------------------------------------------- MMA issue (whole warp, one elected lane issues)
     const int h = warp == kMmaWarp1, n_mine = slot_pages(h);
     constexpr uint32_t idesc_qk = instr_desc(128, 64, false), idesc_pv = instr_desc(128, 128, true, true),
                        idesc_pv_bf16 = instr_desc(128, 128, true, false);
-    constexpr uint32_t kStageUnits = kPageBytes >> 4;
-    const uint32_t kv0 = smem_u32(smem + kSKV);
+    constexpr uint32_t kUnits = kBlockBytes >> 4;   // a block in descriptor address units
     const uint64_t dQ = smem_desc(smem_u32(smem + (kAlt ? 0 : h * 32768)), 16, 1024);
-    const uint64_t dK = smem_desc(kv0, 16, 1024), dV = smem_desc(kv0 + kBlockElems * 2, 8192, 1024);
+    const uint64_t dK = smem_desc(smem_u32(smem + off_k(kAlt)), 16, 1024), dV = smem_desc(smem_u32(smem + off_v(kAlt)), 8192, 1024);
     auto issue_qk = [&](int i) {   // S = Q . K^T of the slot's page i into score buffer i & 1, committed at once
-      const int j = page_of(h, i), s = j % kStages, b = i & 1;
-      if (!mbar_wait_bounded(&bar[B_KV_FULL + s], (j / kStages) & 1)) { failed = true; return; }
+      const int j = page_of(h, i), s = j % kRing, b = i & 1;
+      if (!mbar_wait_bounded(&bar[B_K_FULL + s], (j / kRing) & 1)) { failed = true; return; }
       fence_after();
-      umma_qk_page<16384 / 16, 8192 / 16>(tbase + (2 * h + b) * 64, dQ, dK + (uint64_t)s * kStageUnits, idesc_qk);
+      umma_qk_page<16384 / 16, 8192 / 16>(tbase + (2 * h + b) * 64, dQ, dK + (uint64_t)s * kUnits, idesc_qk);
       umma_commit(&bar[B_S_FULL + 2 * h + b]);
+      umma_commit(&bar[B_K_EMPTY + s]);    // this slot has no use for the keys any more
     };
     for (int i = 0; i < min(kAhead, n_mine) && !failed; ++i) issue_qk(i);
     for (int i = 0; i < n_mine && !failed; ++i) {
-      const int j = page_of(h, i), s = j % kStages, b = i & 1;
-      if (!mbar_wait_bounded(&bar[B_V_READY + s], (j / kStages) & 1)) { failed = true; break; }
+      const int j = page_of(h, i), s = j % kRing, b = i & 1;
+      if (!mbar_wait_bounded(&bar[B_V_READY + s], (j / kRing) & 1)) { failed = true; break; }
       if (!mbar_wait_bounded(&bar[B_P_FULL + 2 * h + b], (i >> 1) & 1)) { failed = true; break; }
       fence_after();
       const uint32_t t_p = tbase + (2 * h + b) * 64, t_o = tbase + 256 + h * 128;
-      if (wide) umma_pv_page(t_o, t_p, dV + (uint64_t)s * kStageUnits, idesc_pv_bf16, i > 0 ? 1u : 0u);
-      else umma_pv_page_f16(t_o, t_p, dV + (uint64_t)s * kStageUnits, idesc_pv, i > 0 ? 1u : 0u);
-      umma_commit(&bar[B_KV_EMPTY + s]);   // this slot has no use for the page any more
+      if (wide) umma_pv_page(t_o, t_p, dV + (uint64_t)s * kUnits, idesc_pv_bf16, i > 0 ? 1u : 0u);
+      else umma_pv_page_f16(t_o, t_p, dV + (uint64_t)s * kUnits, idesc_pv, i > 0 ? 1u : 0u);
+      umma_commit(&bar[B_V_EMPTY + s]);    // ... nor for the values
       if (i + kAhead < n_mine) issue_qk(i + kAhead);   // (behind P.V(i): the pipe runs a thread's instructions in order)
       else umma_commit(&bar[B_O_DONE + 2 * h + b]);
     }
-  } else if (warp == kConvWarp) {
+  } else if (warp >= 12) {
     // ---------------------------------------------------------------- value converter: bf16 -> scaled fp16, in place
     for (int j = 0; j < n_pages; ++j) {
-      const int s = j % kStages;
-      if (!mbar_wait_bounded(&bar[B_KV_FULL + s], (j / kStages) & 1)) { failed = true; break; }
-      uint4 *vb = reinterpret_cast<uint4 *>(smem + kSKV + s * kPageBytes + kBlockElems * 2) + lane;
-#pragma unroll 8
-      for (int x = 0; x < (wide ? 0 : 32); ++x) {
-        uint4 r = vb[x * 32];
+      const int s = j % kRing;
+      if (!mbar_wait_bounded(&bar[B_V_FULL + s], (j / kRing) & 1)) { failed = true; break; }
+      uint4 *vb = reinterpret_cast<uint4 *>(smem + off_v(kAlt) + s * kBlockBytes) + (tid - 384);
+#pragma unroll
+      for (int x = 0; x < (wide ? 0 : 1024 / kConvThreads); ++x) {
+        uint4 r = vb[x * kConvThreads];
         r.x = bf16x2_to_f16x2(r.x, v_scale); r.y = bf16x2_to_f16x2(r.y, v_scale);
         r.z = bf16x2_to_f16x2(r.z, v_scale); r.w = bf16x2_to_f16x2(r.w, v_scale);
-        vb[x * 32] = r;
+        vb[x * kConvThreads] = r;
       }
       fence_async_smem();
       mbar_arrive(&bar[B_V_READY + s]);
     }
-  } else {
+  } else if (warp >= 4) {
     // ---------------------------------------------------------------- softmax of slot 0 (warps 4-7) and slot 1 (8-11)
     const int h = (warp >> 2) - 1, row = tid & 127, n_mine = slot_pages(h);
     const uint32_t t_lane = tbase + ((uint32_t)((warp & 3) * 32) << 16);
@@ -362,7 +390,7 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
     const bool have = n_mine > 0;
     if (have && !failed && !mbar_wait_bounded(&bar[B_O_DONE + 2 * h + ((n_mine - 1) & 1)], 0)) failed = true;
     fence_after();
-    float *join = reinterpret_cast<float *>(smem + kSKV);   // kAlt: slot 1's rows, over the page stages
+    float *join = reinterpret_cast<float *>(smem + off_k(kAlt));   // kAlt: slot 1's rows, over the rings
     if (kAlt) {
       // slot 1 hands its rows over; every page has been consumed by both slots before that
       asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -391,7 +419,7 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
       if (kAlt) {
         const float m1 = join[row * kJoinStride + 128], l1 = join[row * kJoinStride + 129];
         M = fmaxf(m_ref, m1);
-        const float w0 = m_ref == -INFINITY ? 0.f : fast_exp2(m_ref - M), w1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - M);
+        const float w0 = part_weight(m_ref, l, M), w1 = part_weight(m1, l1, M);
         l = l * w0 + l1 * l_scale * w1;
         f0 = o_scale * w0;
         f1 = o_scale * w1;
@@ -419,7 +447,7 @@ __global__ void __launch_bounds__(shp::kThreads, 1) shared_prefix_kernel(SharedA
   if (failed) set_status(c, SPKV_E_TIMEOUT);
   fence_before();
   __syncthreads();
-  if (warp == kConvWarp)
+  if (warp == kTmemWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "n"(shp::kTmemCols) : "memory");
 }
 
@@ -442,7 +470,7 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = c.G;
   uint64_t *full = reinterpret_cast<uint64_t *>(smem + off_bar(NH));   // [0] keys, [1] values
   volatile int *s_it = reinterpret_cast<volatile int *>(full + 2);   // share exists, skip, compact pages, length behind
-                                                                     // the common pages, ring pairs, first page, pages
+                                                                     // the common pages, ring pairs, first page, pages, `ahead` holds
   if (tid == 0) {
     mbar_init(&full[0], 1);
     mbar_init(&full[1], 1);
@@ -459,7 +487,7 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
     const int b = unit / c.Hkv, kvh = unit - b * c.Hkv;
     __syncthreads();    // the previous item's stages and s_it have been read
     if (share >= a.max_tail) break;
-    int u = 0, trow = -1;
+    int u = 0, trow = -1, ahead = 0;   // ahead: page-table entry common + lane, fetched before it is known to be needed
     if (warp == 0) {
       // trip 1: the plan and the sequence
       const int4 head = ldcg4(share_head(a.rec, kvh)), parts = ldcg4(share_head(a.rec, kvh) + 4);
@@ -474,25 +502,29 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
         const bool ok = seq >= 0 && seq < c.S;
         if (!ok && lane == 0 && share == 0) set_status(c, SPKV_E_BOUNDS);
         u = unit_index(c, a.layer, ok ? seq : 0, kvh);
-        // trip 2: the unit; does the batch's first sequence still hold the common pages, and which is their last
-        trow = unit_table_row(c, u);
+        // the unit's page-table row as spkv_cache_create laid the rows out: no trip for it
+        const bool local = kvh < 64 && ((a.local_mask >> kvh) & 1);
+        const int below = kvh < 64 ? __popcll(a.local_mask & ((1ULL << kvh) - 1ULL)) : 0;
+        trow = local ? -1 : a.row_base + (ok ? seq : 0) * a.row_heads + kvh - below;
+        // trip 2: the unit; do it and the batch's first sequence still hold the common pages (the last one names
+        // them all); the unit's own first pages
         int len = ldcg_keep(&c.len[u]), n_ring = min(ldcg_keep(&c.t[u]), c.w);
+        if (trow >= 0 && common + lane < c.max_pages) ahead = ldcg_keep(&unit_table(c, trow)[common + lane]);
         int skip = 0;
-        if (common > 0) {
-          const int len0 = ldcg_keep(&c.len[u0]), last0 = ldcg_keep(&unit_table(c, row0)[common - 1]);
-          // trip 3: does the unit hold that same page (then it holds all before it)
-          if (trow >= 0 && len / kP >= common && len0 / kP >= common &&
-              ldcg_keep(&unit_table(c, trow)[common - 1]) == last0)
-            skip = common;
+        if (common > 0 && trow >= 0) {
+          const int len0 = ldcg_keep(&c.len[u0]), last0 = ldcg_keep(&unit_table(c, row0)[common - 1]),
+                    last = ldcg_keep(&unit_table(c, trow)[common - 1]);
+          if (len / kP >= common && len0 / kP >= common && last == last0) skip = common;
         }
         if (!ok) { len = 0; n_ring = 0; skip = 0; }
         len -= skip * kP;
         const int nk = (len + kP - 1) / kP, np = nk + (n_ring + kP - 1) / kP;
-        const int ku = max(1, min(np / 4, fits ? n_shares : 1));
+        const int ku = max(1, min(np / kTailMinPages, fits ? n_shares : 1));
         const int p0 = share < ku ? (int)((long long)np * share / ku) : 0;
         const int p1 = share < ku ? (int)((long long)np * (share + 1) / ku) : 0;
         if (lane == 0) {
           s_it[0] = 1; s_it[1] = skip; s_it[2] = nk; s_it[3] = len; s_it[4] = n_ring; s_it[5] = p0; s_it[6] = p1 - p0;
+          s_it[7] = skip == common && p0 == 0;
           if (share == 0) a.item_skip[unit] = skip;
         }
         __syncwarp();
@@ -510,7 +542,8 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
     auto fetch_entries = [&](int i) {   // warp 0: global page indices of the share's pages i .. i + 31, one per lane
       const int p = p0 + i + lane;
       if (i + lane < n)
-        entry = p < nk ? checked_page(c, ldcg_keep(&unit_table(c, trow)[skip + p]), (int)ring_page(c, u, 0))
+        entry = p < nk ? checked_page(c, i == 0 && s_it[7] ? ahead : ldcg_keep(&unit_table(c, trow)[skip + p]),
+                                      (int)ring_page(c, u, 0))
                        : (int)ring_page(c, u, p - nk);
     };
     auto load = [&](int i, int half) {  // warp 0: keys (half = 0; first) or values of page i
@@ -579,7 +612,7 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float *src = red + ((size_t)w * G + g) * 132;
-        const float f = src[128] == -INFINITY ? 0.f : fast_exp2(src[128] - M);
+        const float f = part_weight(src[128], src[129], M);
         const float4 v = *reinterpret_cast<const float4 *>(src + lane * 4);
         L += src[129] * f;
         O.x = fmaf(v.x, f, O.x); O.y = fmaf(v.y, f, O.y); O.z = fmaf(v.z, f, O.z); O.w = fmaf(v.w, f, O.w);
@@ -590,65 +623,68 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
     tc5::fence_async_smem();   // these reads and writes come before the next item's copies into the stages
   }
   if (failed) set_status(c, SPKV_E_TIMEOUT);
-  pdl_wait();   // the merge behind this launch reads the prefix launch's parts too
+  // The merge behind this launch reads the prefix launch's parts too: one block stays until that is complete
+  // (all of them would keep the blocks behind them out while the prefix runs).
+  if (blockIdx.x == 0) pdl_wait();
 }
 
 // ---- merge -----------------------------------------------------------------------------------------
 // One block per query row, its four warps taking every fourth part (shares of the common pages, then of the
-// tail); lane l owns dims 4l .. 4l + 3.  All of a warp's loads are issued before the first is used: the
-// launch is three trips to L2 (plan and skip, weights, rows), whatever the number of parts.
+// tail); lane l owns dims 4l .. 4l + 3.  The plan's line is read before the launch waits for the tail (it was
+// complete before the prefix launch let anything start); everything behind the wait -- did the unit leave
+// the common pages out, the parts' weights, the parts -- is loaded at once: one trip to L2.
 __global__ void __launch_bounds__(128) shared_merge_kernel(SharedArgs a) {
-  constexpr int kWarps = 4, kBatch = 10;
+  constexpr int kWarps = 4, kBatch = 8;
   const CacheView &c = a.c;
   __shared__ float s_ml[kWarps][2];
   __shared__ float4 s_o[kWarps][32];
   pdl_trigger();
-  pdl_wait();
   const int r = blockIdx.x, b = r / c.Hq, j = r - b * c.Hq, kvh = j / c.G, g = j - kvh * c.G;
   const int unit = b * c.Hkv + kvh, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // (through L1: the rows of a head that meet on an SM share the line)
   const int4 parts = *reinterpret_cast<const int4 *>(share_head(a.rec, kvh) + 4);
-  const int first = share_head(a.rec, kvh)[1], skip = __ldcg(a.item_skip + unit);
-  const int n_tail = parts.z == a.sig ? max(1, min(parts.y, a.max_tail)) : 1, n_pre = skip > 0 ? max(parts.x, 0) : 0;
-  const int n = n_pre + n_tail;
+  const int first = share_head(a.rec, kvh)[1];
+  const bool fits = parts.z == a.sig;
+  const int n_pre = fits ? max(parts.x, 0) : 0, n = n_pre + (fits ? max(1, min(parts.y, a.max_tail)) : 1);
   const int R = b * c.G + g, tile = R / kShareRows, row = R % kShareRows;
   const int last_block = a.max_blocks - 1;   // (a plan that was overwritten reads no further than the workspace)
   auto row_of = [&](int p, bool pre) -> size_t {   // index of part p's row in its array
     return pre ? (size_t)max(0, min(first + p * a.n_tiles + tile, last_block)) * a.rows_per_block + row
                : ((size_t)(p - n_pre) * a.n_items + unit) * c.G + g;
   };
+  pdl_wait();
+  const int skip = __ldcg(a.item_skip + unit);
   float M = -INFINITY, L = 0.f;
   float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p0 = warp; p0 < n; p0 += 32 * kWarps) {   // 32 parts at a time, one per lane
+  for (int p0 = warp; p0 < n; p0 += kBatch * kWarps) {   // kBatch parts at a time; lane x holds part x's weight
     const int mine = p0 + lane * kWarps;
+    const bool have = lane < kBatch && mine < n;
     float2 ml = make_float2(-INFINITY, 0.f);
-    if (mine < n) ml = __ldcg(reinterpret_cast<const float2 *>(mine < n_pre ? a.part_ml : a.tail_ml) + row_of(mine, mine < n_pre));
+    if (have) ml = __ldcg(reinterpret_cast<const float2 *>(mine < n_pre ? a.part_ml : a.tail_ml) + row_of(mine, mine < n_pre));
+    float4 v[kBatch];
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      const int p = min(p0 + x * kWarps, n - 1);
+      const bool pre = p < n_pre;
+      v[x] = __ldcg(reinterpret_cast<const float4 *>((pre ? a.part_o : a.tail_o) + row_of(p, pre) * kD) + lane);
+    }
+    if (mine < n_pre && skip == 0) ml = make_float2(-INFINITY, 0.f);   // the tail read this unit in full
     float top = ml.x;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float Mn = fmaxf(M, top), old = M == -INFINITY ? 0.f : exp2f(M - Mn);
+    const float Mn = fmaxf(M, top), old = part_weight(M, L, Mn);
     M = Mn;
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-    float fl = f * ml.y;
+    const float f = part_weight(ml.x, ml.y, M);
+    float fl = f == 0.f ? 0.f : f * ml.y;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) fl += __shfl_xor_sync(0xffffffffu, fl, o);
     L = L * old + fl;
     O.x *= old; O.y *= old; O.z *= old; O.w *= old;
-    const int cnt = min(32, (n - p0 + kWarps - 1) / kWarps);
-    for (int x0 = 0; x0 < cnt; x0 += kBatch) {
-      float4 v[kBatch];
 #pragma unroll
-      for (int x = 0; x < kBatch; ++x) {
-        const int p = p0 + min(x0 + x, cnt - 1) * kWarps;
-        const bool pre = p < n_pre;
-        v[x] = __ldcg(reinterpret_cast<const float4 *>((pre ? a.part_o : a.tail_o) + row_of(p, pre) * kD) + lane);
-      }
-#pragma unroll
-      for (int x = 0; x < kBatch; ++x) {
-        const float fx = __shfl_sync(0xffffffffu, f, min(x0 + x, 31));
-        if (x0 + x < cnt && fx != 0.f) {   // (a part of weight 0 may never have been written)
-          O.x = fmaf(v[x].x, fx, O.x); O.y = fmaf(v[x].y, fx, O.y); O.z = fmaf(v[x].z, fx, O.z); O.w = fmaf(v[x].w, fx, O.w);
-        }
+    for (int x = 0; x < kBatch; ++x) {
+      const float fx = __shfl_sync(0xffffffffu, f, x);
+      if (fx != 0.f) {   // (a part of weight 0 may never have been written)
+        O.x = fmaf(v[x].x, fx, O.x); O.y = fmaf(v[x].y, fx, O.y); O.z = fmaf(v[x].z, fx, O.z); O.w = fmaf(v[x].w, fx, O.w);
       }
     }
   }
@@ -659,11 +695,11 @@ __global__ void __launch_bounds__(128) shared_merge_kernel(SharedArgs a) {
   float Mx = M;
 #pragma unroll
   for (int x = 1; x < kWarps; ++x) Mx = fmaxf(Mx, s_ml[x][0]);
-  const float w0 = M == -INFINITY ? 0.f : exp2f(M - Mx);
+  const float w0 = part_weight(M, L, Mx);
   L *= w0; O.x *= w0; O.y *= w0; O.z *= w0; O.w *= w0;
 #pragma unroll
   for (int x = 1; x < kWarps; ++x) {
-    const float mx = s_ml[x][0], f = mx == -INFINITY ? 0.f : exp2f(mx - Mx);
+    const float f = part_weight(s_ml[x][0], s_ml[x][1], Mx);
     const float4 v = s_o[x][lane];
     L = fmaf(s_ml[x][1], f, L);
     O.x = fmaf(v.x, f, O.x); O.y = fmaf(v.y, f, O.y); O.z = fmaf(v.z, f, O.z); O.w = fmaf(v.w, f, O.w);
@@ -724,6 +760,7 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   a.n_tiles = share_row_tiles(B, v.G);
   a.rows_per_block = w.rows;
   a.sig = share_signature(v, B);
+  a.g_inv = ((1ULL << 32) + v.G - 1) / v.G;
   a.seq_ids = d_seq_ids;
   a.q = static_cast<const __nv_bfloat16 *>(d_q);
   a.rec = share_record(v, static_cast<const int32_t *>(d_plan), layer);
@@ -736,6 +773,9 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   a.tail_o = reinterpret_cast<float *>(ws + w.off_to);
   a.max_blocks = w.max_blocks;
   a.max_tail = w.max_tail;
+  for (int l = 0; l < layer; ++l) a.row_base += (v.Hkv - __builtin_popcountll(cache->local_mask[l])) * v.S;
+  a.row_heads = v.Hkv - __builtin_popcountll(cache->local_mask[layer]);
+  a.local_mask = cache->local_mask[layer];
   a.out = static_cast<__nv_bfloat16 *>(d_out);
   a.lse = d_lse_opt;
   // blocks: one share each (the plan never cuts into more)

@@ -21,6 +21,7 @@ constexpr int kShareRows = 256;       // query rows per block: two slots of 128
 constexpr int kMinSharedPages = 1;    // fewer common pages than this are read per sequence
 constexpr int kMinSharePages = 4;     // a share is not cut shorter
 constexpr int kTailPages = 8;         // a unit's own pages are cut into shares of about this many
+constexpr int kTailMinPages = 4;     // ... and no piece is shorter than half of that
 constexpr int kMaxTailItems = 1024;   // ... while there are no more shares than this
 
 __host__ __device__ inline int share_row_tiles(int B, int G) { return (B * G + kShareRows - 1) / kShareRows; }
