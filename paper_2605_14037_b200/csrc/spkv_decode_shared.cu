@@ -27,6 +27,7 @@
 // Warps: 0 / 2 MMA issue of slot 0 / 1, 1 page loader, 3 tensor memory, 4-7 / 8-11 softmax of slot 0 / 1, 12-15 value
 // conversion.  All waits are bounded.
 #include <algorithm>
+#include <atomic>
 #include <math.h>
 
 #include "spkv_share.cuh"
@@ -734,6 +735,25 @@ static SharedWs shared_ws_layout(const spkv_config_t *cfg, int B) {
 
 using namespace spkv;
 
+namespace {
+// Attributes of the two kernels, set once per device (a bit each).
+std::atomic<unsigned long long> g_ready[2][2];
+
+// The kernel may use `smem` bytes and gets the whole of an SM's shared memory to share out: with the default
+// split, which fits one prefix block, a tail block finds none left beside it.
+int whole_shared_memory(const void *kernel, int smem, std::atomic<unsigned long long> *ready) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return SPKV_E_CUDA;
+  const unsigned long long bit = dev < 64 ? 1ULL << dev : 0;
+  if (bit & ready->load(std::memory_order_acquire)) return SPKV_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
+    return SPKV_E_CUDA;
+  ready->fetch_or(bit, std::memory_order_release);
+  return SPKV_OK;
+}
+}  // namespace
+
 extern "C" size_t spkv_decode_shared_workspace_bytes(const spkv_config_t *cfg, int32_t B) {
   if (!cfg || B < 0 || cfg->n_kv_heads < 1 || cfg->n_q_heads < cfg->n_kv_heads) return 0;
   return shared_ws_layout(cfg, B).total;
@@ -785,15 +805,8 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   const int smem = shp::smem_bytes(alt);
   auto tail = v.G > 8 ? shared_tail_kernel<2> : shared_tail_kernel<1>;
   const int tail_smem = sht::smem_bytes(v.G > 8 ? 2 : 1);
-  // (the whole of an SM's shared memory for both: with the default split, which fits one prefix block, a
-  // tail block finds none left beside it)
-  if (cudaFuncSetAttribute(prefix, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-      cudaFuncSetAttribute(tail, cudaFuncAttributeMaxDynamicSharedMemorySize, tail_smem) != cudaSuccess ||
-      cudaFuncSetAttribute(prefix, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) !=
-          cudaSuccess ||
-      cudaFuncSetAttribute(tail, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) !=
-          cudaSuccess)
-    return SPKV_E_CUDA;
+  if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(prefix), smem, &g_ready[0][alt])) return rc;
+  if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(tail), tail_smem, &g_ready[1][v.G > 8])) return rc;
   // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
   // cover; a plain launch waits for all of them.
   const bool plain = (cache->cfg.flags & SPKV_FLAG_OVERLAP) != 0;

@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 
 import torch
 
@@ -163,6 +164,19 @@ def _stream(stream=None):
     return C.c_void_p(s.cuda_stream)
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _on_device(dev, stream, fn, *args):
+    """fn(*args, stream) with `dev` current (the caller's current device is put back)"""
+    if dev == _current_device():
+        return fn(*args, _raw_stream(dev) if stream is None else stream.cuda_stream)
+    with torch.cuda.device(dev):
+        return fn(*args, _raw_stream(dev) if stream is None else stream.cuda_stream)
+
+
 def _ptr(t, dtype=None):
     if t is None:
         return None
@@ -218,7 +232,7 @@ class Cache:
             _check(lib().spkv_cache_create(C.byref(self.cfg), _ptr(self.arena), self.arena_bytes,
                                            _stream(), C.byref(h)), "spkv_cache_create")
         self._h = h
-        self._ws = {}
+        self._ws, self._shared_bytes = {}, {}
         self.G = n_q_heads // n_kv_heads
         self.default_scale = 1.0 / math.sqrt(head_dim)
 
@@ -245,7 +259,7 @@ class Cache:
         with torch.cuda.device(self.device):
             _check(lib().spkv_cache_attach(C.byref(self.cfg), _ptr(arena), arena.numel(), _stream(), C.byref(h)),
                    "spkv_cache_attach")
-        self._h, self._ws = h, {}
+        self._h, self._ws, self._shared_bytes = h, {}, {}
         self.G = self.cfg.n_q_heads // self.cfg.n_kv_heads
         self.default_scale = 1.0 / math.sqrt(self.cfg.head_dim)
         return self
@@ -375,16 +389,40 @@ class Cache:
                                      stream=None):
         """spkv_decode_attention with the pages that all sequences have in common read once for the batch.
         Returns out, or (out, lse) with want_lse."""
-        B = seq_ids.numel()
+        B, cfg = seq_ids.shape[0], self.cfg
+        shape = (B, cfg.n_q_heads, cfg.head_dim)
+        dev = q.get_device()
+
+        def check(t, dtype, want):
+            if t.dtype is not dtype or t.shape != want or t.get_device() != dev or not t.is_contiguous():
+                raise ValueError(f"expected a contiguous {dtype} tensor {tuple(want)} on the cache's device, got "
+                                 f"{t.dtype} {tuple(t.shape)} on {t.device}")
+
+        check(q, torch.bfloat16, shape)
+        check(seq_ids, torch.int32, (B,))
+        check(plan, torch.uint8, plan.shape)
         if out is None:
             out = torch.empty_like(q)
-        if want_lse and lse is None:
-            lse = torch.empty((B, self.cfg.n_q_heads), dtype=torch.float32, device=q.device)
-        ws = self._workspace("decode_shared", lib().spkv_decode_shared_workspace_bytes(C.byref(self.cfg), B))
-        _check(lib().spkv_decode_attention_shared(
-            self._h, layer, _ptr(seq_ids, torch.int32), B, _ptr(q, torch.bfloat16), _ptr(out, torch.bfloat16),
-            _ptr(lse, torch.float32), self.default_scale if sm_scale is None else sm_scale, _ptr(plan, torch.uint8),
-            plan.numel(), _ptr(ws), ws.numel(), _stream(stream)), "spkv_decode_attention_shared")
+        else:
+            check(out, torch.bfloat16, shape)
+        if lse is not None:
+            check(lse, torch.float32, shape[:2])
+        elif want_lse:
+            lse = q.new_empty(shape[:2], dtype=torch.float32)
+        if dev < 0 or dev != self.arena.get_device():
+            raise ValueError("all tensors of a call live on the cache's device")
+        nbytes = self._shared_bytes.get(B)
+        if nbytes is None:
+            nbytes = self._shared_bytes[B] = lib().spkv_decode_shared_workspace_bytes(C.byref(cfg), B)
+        ws = self._ws.get("decode_shared")
+        if ws is None or ws.numel() < nbytes:
+            ws = self._workspace("decode_shared", nbytes)
+        rc = _on_device(dev, stream, lib().spkv_decode_attention_shared, self._h, layer, seq_ids.data_ptr(), B, q.data_ptr(),
+                        out.data_ptr(), None if lse is None else lse.data_ptr(),
+                        self.default_scale if sm_scale is None else sm_scale, plan.data_ptr(), plan.numel(), ws.data_ptr(),
+                        ws.numel())
+        if rc:
+            raise SpkvError(rc, "spkv_decode_attention_shared")
         return (out, lse) if want_lse else out
 
     def spkv_prefill(self, layer, seq, k, v, logits, q=None, out=None, sm_scale=None, stream=None):
@@ -559,7 +597,9 @@ class NormRope:
     def __init__(self, norm, rope, dtype, keep):
         self.norm, self.rope, self.dtype, self._keep = norm, rope, dtype, keep
         self._n, self._r = C.addressof(norm), C.addressof(rope)
-        self.heads, self.head_dim = (norm.n_q_heads, norm.n_kv_heads), norm.head_dim
+        self.heads, self.head_dim, self.n_axes = (norm.n_q_heads, norm.n_kv_heads), norm.head_dim, rope.n_axes
+        self.weights_on = next((w.get_device() for w in keep if w is not None), None)
+        self.forward, self.backward = lib().spkv_norm_rope, lib().spkv_norm_rope_backward
         self.workspace_bytes = lib().spkv_norm_rope_workspace_bytes(self._n)
         self._ws = {}
 
@@ -589,55 +629,75 @@ def make_norm_rope(n_q_heads, n_kv_heads, head_dim=128, dtype=torch.bfloat16, wq
     for w in (wq, wk):
         if w is not None and (w.shape != (head_dim,) or (wq is not None and w.dtype != wq.dtype)):
             raise ValueError("norm weights are [head_dim] tensors of one type")
+    if wq is not None and wk is not None and wq.device != wk.device:
+        raise ValueError("norm weights live on one device")
     wd = next((w.dtype for w in (wq, wk) if w is not None), torch.float32)
     which = {True: NORM_Q | NORM_K, False: 0, "q": NORM_Q, "k": NORM_K}[norm]
     d = QkNorm(_DTYPE[dtype], _DTYPE[wd], head_dim, n_q_heads, n_kv_heads, which, eps, _ptr(wq), _ptr(wk))
     return NormRope(d, rope, dtype, (wq, wk))
 
 
-def _rows(nr, t, heads, n, what):
-    """spkv_rows_t of a [n, heads, head_dim] tensor of any token and head stride."""
-    if t.dtype != nr.dtype or t.dim() != 3 or t.shape[0] != n or t.shape[1] != heads or t.shape[2] != nr.head_dim:
-        raise ValueError(f"{what}: expected {nr.dtype} [{n}, {heads}, {nr.head_dim}], got {t.dtype} {tuple(t.shape)}")
-    st = t.stride()
-    if (st[2] != 1 and nr.head_dim > 1) or not t.is_cuda:
-        raise ValueError(f"{what}: a device tensor whose rows are contiguous")
-    return Rows(t.data_ptr(), st[0] if n > 1 else 0, st[1] if heads > 1 else 0)   # (the stride of a single entry says nothing)
+# The row calls are made once per layer and token batch, often for a handful of rows: what the binding does
+# around the launch is kept to a few microseconds (one check per tensor, all views packed at once).
+_SIX_ROWS, _EIGHT_ROWS = struct.Struct("Qqq" * 6), struct.Struct("Qqq" * 8)
+_ROW = C.sizeof(Rows)
 
 
-def _positions(nr, pos):
-    """n_tok of an int32 [n_tok] or [n_axes, n_tok] device tensor"""
-    n = pos.shape[-1]
-    if pos.dtype != torch.int32 or not pos.is_cuda or not pos.is_contiguous() or pos.numel() != nr.rope.n_axes * n:
-        raise ValueError(f"positions: contiguous int32 [{nr.rope.n_axes}, n_tok] on the device")
-    return n
-
-
-def _same_device(first, *others):
-    if any(t is not None and t.device != first.device for t in others):
+def _row(nr, t, heads, n, dev, what):
+    """(pointer, token stride, head stride) of a [n, heads, head_dim] tensor of any token and head stride."""
+    D = nr.head_dim
+    if t.dtype is not nr.dtype or t.shape != (n, heads, D):
+        raise ValueError(f"{what}: expected {nr.dtype} [{n}, {heads}, {D}], got {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != dev:
         raise ValueError("all tensors of a call live on one device")
+    st = t.stride()
+    if st[2] != 1 or dev < 0:
+        raise ValueError(f"{what}: a device tensor whose rows are contiguous")
+    return t.data_ptr(), st[0] if n > 1 else 0, st[1] if heads > 1 else 0   # (the stride of a single entry says nothing)
+
+
+def _row_out(nr, like, t, heads, n, dev, what):
+    """(tensor, its row view) of a result: the caller's, or a contiguous one made here"""
+    if t is not None:
+        return t, _row(nr, t, heads, n, dev, what)
+    D = nr.head_dim
+    t = like.new_empty((n, heads, D))
+    return t, (t.data_ptr(), heads * D, D)
+
+
+def _positions(nr, pos, dev):
+    """(n_tok, pointer) of an int32 [n_tok] or [n_axes, n_tok] device tensor"""
+    n = pos.shape[-1]
+    if pos.dtype is not torch.int32 or not pos.is_contiguous() or pos.numel() != nr.n_axes * n:
+        raise ValueError(f"positions: contiguous int32 [{nr.n_axes}, n_tok] on the device")
+    if pos.get_device() != dev or (nr.weights_on is not None and nr.weights_on != dev):
+        raise ValueError("all tensors of a call live on one device")
+    return n, pos.data_ptr()
 
 
 def spkv_norm_rope(nr, positions, q, k, v=None, q_out=None, k_out=None, v_out=None, stream=None):
     """Norm + rotation of q [n_tok, n_q_heads, head_dim] and k [n_tok, n_kv_heads, head_dim] (any strides;
     e.g. views of one fused projection), v handed on.  Returns (q_out, k_out, v_out), contiguous
     tensors unless given; v_out is None without v."""
-    n = _positions(nr, positions)
+    dev = q.get_device()
+    n, pos = _positions(nr, positions, dev)
     hq, hkv = nr.heads
-    shape_k = (n, hkv, nr.head_dim)
-    if q_out is None:
-        q_out = torch.empty((n, hq, nr.head_dim), dtype=nr.dtype, device=q.device)
-    if k_out is None:
-        k_out = torch.empty(shape_k, dtype=nr.dtype, device=q.device)
-    if v is not None and v_out is None:
-        v_out = torch.empty(shape_k, dtype=nr.dtype, device=q.device)
-    _same_device(q, k, v, q_out, k_out, v_out, positions, *nr._keep)
-    a = [C.byref(_rows(nr, t, h, n, w)) for t, h, w in ((q, hq, "q"), (k, hkv, "k"))]
-    a.append(None if v is None else C.byref(_rows(nr, v, hkv, n, "v")))
-    a += [C.byref(_rows(nr, t, h, n, w)) for t, h, w in ((q_out, hq, "q_out"), (k_out, hkv, "k_out"))]
-    a.append(None if v is None else C.byref(_rows(nr, v_out, hkv, n, "v_out")))
-    with torch.cuda.device(q.device):
-        _check(lib().spkv_norm_rope(nr._n, nr._r, n, positions.data_ptr(), *a, _stream(stream)), "spkv_norm_rope")
+    rq, rk = _row(nr, q, hq, n, dev, "q"), _row(nr, k, hkv, n, dev, "k")
+    q_out, oq = _row_out(nr, q, q_out, hq, n, dev, "q_out")
+    k_out, ok = _row_out(nr, q, k_out, hkv, n, dev, "k_out")
+    io = (Rows * 6)()
+    at = C.addressof(io)
+    if v is None:
+        v_out = None
+        _SIX_ROWS.pack_into(io, 0, *rq, *rk, 0, 0, 0, *oq, *ok, 0, 0, 0)
+        av = av_out = None
+    else:
+        v_out, ov = _row_out(nr, q, v_out, hkv, n, dev, "v_out")
+        _SIX_ROWS.pack_into(io, 0, *rq, *rk, *_row(nr, v, hkv, n, dev, "v"), *oq, *ok, *ov)
+        av, av_out = at + 2 * _ROW, at + 5 * _ROW
+    rc = _on_device(dev, stream, nr.forward, nr._n, nr._r, n, pos, at, at + _ROW, av, at + 3 * _ROW, at + 4 * _ROW, av_out)
+    if rc:
+        raise SpkvError(rc, "spkv_norm_rope")
     return q_out, k_out, v_out
 
 
@@ -646,33 +706,37 @@ def spkv_norm_rope_backward(nr, positions, q, k, q_grad, k_grad, v_grad=None, dq
     """Gradients of spkv_norm_rope: q, k its input rows (None for a side without norm), q_grad, k_grad,
     v_grad those of its outputs.  Returns (dq, dk, dv, dwq, dwk); dwq, dwk float32, None for a
     side without norm or weight_grads=False; dv None without v_grad."""
-    n = _positions(nr, positions)
-    hq, hkv = nr.heads
-    dev, D = q_grad.device, nr.head_dim
-    if dq is None:
-        dq = torch.empty((n, hq, D), dtype=nr.dtype, device=dev)
-    if dk is None:
-        dk = torch.empty((n, hkv, D), dtype=nr.dtype, device=dev)
-    if v_grad is not None and dv is None:
-        dv = torch.empty((n, hkv, D), dtype=nr.dtype, device=dev)
-    normed = nr.norm.norm
-    dwq = torch.empty(D, dtype=torch.float32, device=dev) if weight_grads and normed & NORM_Q else None
-    dwk = torch.empty(D, dtype=torch.float32, device=dev) if weight_grads and normed & NORM_K else None
-    _same_device(q_grad, q, k, k_grad, v_grad, dq, dk, dv, positions, *nr._keep)
-
-    def rows(t, h, what):
-        return None if t is None else C.byref(_rows(nr, t, h, n, what))
-
-    with torch.cuda.device(dev):
-        st = _stream(stream)
-        ws = nr.workspace(dev, st.value) if dwq is not None or dwk is not None else None
-        _check(lib().spkv_norm_rope_backward(
-            nr._n, nr._r, n, positions.data_ptr(), rows(q, hq, "q"), rows(k, hkv, "k"), rows(q_grad, hq, "q_grad"),
-            rows(k_grad, hkv, "k_grad"), rows(v_grad, hkv, "v_grad"), rows(dq, hq, "dq"), rows(dk, hkv, "dk"),
-            rows(dv if v_grad is not None else None, hkv, "dv"), None if dwq is None else dwq.data_ptr(),
-            None if dwk is None else dwk.data_ptr(), None if ws is None else ws.data_ptr(),
-            0 if ws is None else ws.numel(), st), "spkv_norm_rope_backward")
-    return dq, dk, dv if v_grad is not None else None, dwq, dwk
+    dev = q_grad.get_device()
+    n, pos = _positions(nr, positions, dev)
+    (hq, hkv), D, normed = nr.heads, nr.head_dim, nr.norm.norm
+    none = (0, 0, 0)
+    xq = _row(nr, q, hq, n, dev, "q") if normed & NORM_Q else none
+    xk = _row(nr, k, hkv, n, dev, "k") if normed & NORM_K else none
+    gq, gk = _row(nr, q_grad, hq, n, dev, "q_grad"), _row(nr, k_grad, hkv, n, dev, "k_grad")
+    dq, yq = _row_out(nr, q_grad, dq, hq, n, dev, "dq")
+    dk, yk = _row_out(nr, q_grad, dk, hkv, n, dev, "dk")
+    gv = yv = none
+    if v_grad is None:
+        dv = None
+    else:
+        gv = _row(nr, v_grad, hkv, n, dev, "v_grad")
+        dv, yv = _row_out(nr, q_grad, dv, hkv, n, dev, "dv")
+    dwq = q_grad.new_empty(D, dtype=torch.float32) if weight_grads and normed & NORM_Q else None
+    dwk = q_grad.new_empty(D, dtype=torch.float32) if weight_grads and normed & NORM_K else None
+    ws, ws_bytes = None, 0
+    if dwq is not None or dwk is not None:
+        ws_bytes = nr.workspace_bytes
+        ws = nr.workspace(q_grad.device, _raw_stream(dev) if stream is None else stream.cuda_stream).data_ptr()
+    io = (Rows * 8)()
+    at = C.addressof(io)
+    _EIGHT_ROWS.pack_into(io, 0, *xq, *xk, *gq, *gk, *gv, *yq, *yk, *yv)
+    rc = _on_device(dev, stream, nr.backward, nr._n, nr._r, n, pos, at, at + _ROW, at + 2 * _ROW, at + 3 * _ROW,
+                    at + 4 * _ROW if v_grad is not None else None, at + 5 * _ROW, at + 6 * _ROW,
+                    at + 7 * _ROW if v_grad is not None else None, None if dwq is None else dwq.data_ptr(),
+                    None if dwk is None else dwk.data_ptr(), ws, ws_bytes)
+    if rc:
+        raise SpkvError(rc, "spkv_norm_rope_backward")
+    return dq, dk, dv, dwq, dwk
 
 
 _softgate_ws = {}
