@@ -16,8 +16,8 @@
 //
 // Angles.  A frequency is held as a fraction of a turn per position in 64-bit fixed point, so that
 // position * frequency modulo one turn is one exact integer product; what is left -- 32 bits of a turn -- goes
-// through sincospif.  Far positions lose nothing (in fp32 a position of 10^6 is 0.06 rad off).  A block
-// computes the sines and cosines of its tokens once, into shared memory, for all its heads: no table
+// through sincospif.  Far positions lose nothing (in fp32 a position of 10^6 is 0.06 rad off).  A warp
+// computes the sines and cosines of a token once, through shared memory, for all its heads: no table
 // in memory, no position limit.
 //
 // What bounds it: bytes.  Each row is read and written once; about 35 issue slots per 512 B moved.
@@ -31,13 +31,15 @@
 
 namespace spkv {
 
-constexpr int kRowThreads = 256;
-constexpr int kMaxTile = 8;         // tokens per block and pass
-constexpr int kMaxBwdBlocks = 2048; // partial sums of the weight gradients the workspace holds
+constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
+constexpr int kFwdBlocks = 2, kBwdBlocks = 2;   // blocks per SM (registers)
+constexpr int kAhead = 3;                       // passes of rows loaded ahead (forward)
+constexpr int kMaxBwdBlocks = 512;              // partial sums of the weight gradients the workspace holds
 
 struct RowArgs {
   spkv_rope_t rope;
-  int n_tok, Hq, Hkv, Hv, D, tile;
+  int n_tok, Hq, Hkv, Hv, D;
+  int wpt;                     // warps per token: 1, 2, 4 or 8
   int norm;                    // bit 0: queries, bit 1: keys
   int w_dtype;
   float eps, inv_d;
@@ -47,49 +49,78 @@ struct RowArgs {
   float *part;                 // backward: [gridDim.x][2][D] partial sums of g u, or null
 };
 
+// ---- two floats per instruction (packed fp32 arithmetic of sm_100), in one 64-bit register pair
+typedef uint64_t f2;
+__device__ inline f2 pk(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ inline float2 up(f2 r) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
+  return v;
+}
+__device__ inline f2 mul(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ inline f2 fma(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ inline f2 sub(f2 a, f2 b) {
+  f2 r;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// A 16-byte chunk as pairs of neighbouring elements.
 template <class T> struct Elem;
 template <> struct Elem<__nv_bfloat16> {
   static constexpr int kChunk = 8;
-  static __device__ inline void unpack(const uint4 &v, float (&f)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-  }
-  static __device__ inline uint32_t pack2(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  static __device__ inline f2 pair(uint32_t w) { return pk(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+  static __device__ inline uint32_t word(f2 v) {
+    const float2 f = up(v);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
     return *reinterpret_cast<const uint32_t *>(&h);
-  }
-  static __device__ inline uint4 pack(const float (&f)[8]) {
-    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
   }
 };
 template <> struct Elem<__half> {
   static constexpr int kChunk = 8;
-  static __device__ inline void unpack(const uint4 &v, float (&f)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-      f[2 * i] = p.x; f[2 * i + 1] = p.y;
-    }
+  static __device__ inline f2 pair(uint32_t w) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    return pk(f.x, f.y);
   }
-  static __device__ inline uint32_t pack2(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
+  static __device__ inline uint32_t word(f2 v) {
+    const float2 f = up(v);
+    const __half2 h = __floats2half2_rn(f.x, f.y);
     return *reinterpret_cast<const uint32_t *>(&h);
-  }
-  static __device__ inline uint4 pack(const float (&f)[8]) {
-    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
   }
 };
 template <> struct Elem<float> {
   static constexpr int kChunk = 4;
-  static __device__ inline void unpack(const uint4 &v, float (&f)[4]) {
-    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
-  }
-  static __device__ inline uint4 pack(const float (&f)[4]) {
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-  }
 };
+template <class T>
+__device__ inline void unpack(const uint4 &v, f2 (&f)[Elem<T>::kChunk / 2]) {
+  if constexpr (Elem<T>::kChunk == 4) {
+    f[0] = pk(__uint_as_float(v.x), __uint_as_float(v.y));
+    f[1] = pk(__uint_as_float(v.z), __uint_as_float(v.w));
+  } else {
+    f[0] = Elem<T>::pair(v.x); f[1] = Elem<T>::pair(v.y); f[2] = Elem<T>::pair(v.z); f[3] = Elem<T>::pair(v.w);
+  }
+}
+template <class T>
+__device__ inline uint4 pack(const f2 (&f)[Elem<T>::kChunk / 2]) {
+  if constexpr (Elem<T>::kChunk == 4) {
+    const float2 a = up(f[0]), b = up(f[1]);
+    return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+  } else {
+    return make_uint4(Elem<T>::word(f[0]), Elem<T>::word(f[1]), Elem<T>::word(f[2]), Elem<T>::word(f[3]));
+  }
+}
 
 __device__ inline float load_weight(const void *w, int dtype, int i) {
   if (!w) return 1.f;
@@ -111,78 +142,95 @@ __device__ inline LaneChunks lane_chunks(const RowArgs &a, int j) {
   return l;
 }
 
-// Element e of a lane's chunk 0 / 1 is half of the lane's pair pair_of(e): (i, i + rot/2): lo of pair e and
-// hi of pair e; adjacent pairs: chunk 0 holds pairs 0 .. CE/2-1, chunk 1 the others.
-// Rotates the CE pairs of a lane in place; cs holds (cos, sin) of its pairs, sgn = -1 for the transpose.
-template <int CE>
-__device__ inline void rotate(float (&f0)[CE], float (&f1)[CE], const float2 (&cs)[CE], bool interleaved, float sgn) {
-  if (!interleaved) {
+// A lane's CE pairs: pair e is (f0[e], f1[e]), or with adjacent pairs the two elements of f2 number e of chunk 0,
+// then of chunk 1.  Angles as the rotation wants them: cosines c and sines s of pairs (2i, 2i + 1), or
+// with adjacent pairs of pair i alone (c = (cos, cos), s = (sin, sin)).
+template <int CE, bool kAdjacent> struct Angles { f2 c[kAdjacent ? CE : CE / 2], s[kAdjacent ? CE : CE / 2]; };
+
+// Rotates a lane's pairs in place; kBack: by the opposite angle (the transpose).
+template <int CE, bool kAdjacent, bool kBack>
+__device__ inline void rotate(f2 (&f0)[CE / 2], f2 (&f1)[CE / 2], const Angles<CE, kAdjacent> &a) {
+  if constexpr (!kAdjacent) {
 #pragma unroll
-    for (int e = 0; e < CE; ++e) {
-      const float c = cs[e].x, s = sgn * cs[e].y, lo = f0[e], hi = f1[e];
-      f0[e] = lo * c - hi * s;
-      f1[e] = hi * c + lo * s;
+    for (int i = 0; i < CE / 2; ++i) {
+      const f2 lo = f0[i], hi = f1[i];
+      f0[i] = kBack ? fma(lo, a.c[i], mul(hi, a.s[i])) : sub(mul(lo, a.c[i]), mul(hi, a.s[i]));
+      f1[i] = kBack ? sub(mul(hi, a.c[i]), mul(lo, a.s[i])) : fma(hi, a.c[i], mul(lo, a.s[i]));
     }
   } else {
+    auto turn = [](f2 v, f2 c, f2 s) {   // (lo, hi) -> (lo c - hi s, hi c + lo s)
+      const float2 x = up(v), cc = up(c), ss = up(s);
+      const float sn = kBack ? -ss.x : ss.x;
+      return pk(x.x * cc.x - x.y * sn, x.y * cc.x + x.x * sn);
+    };
 #pragma unroll
-    for (int e = 0; e < CE / 2; ++e) {
-      const float c = cs[e].x, s = sgn * cs[e].y, lo = f0[2 * e], hi = f0[2 * e + 1];
-      f0[2 * e] = lo * c - hi * s;
-      f0[2 * e + 1] = hi * c + lo * s;
-      const float c2 = cs[CE / 2 + e].x, s2 = sgn * cs[CE / 2 + e].y, lo2 = f1[2 * e], hi2 = f1[2 * e + 1];
-      f1[2 * e] = lo2 * c2 - hi2 * s2;
-      f1[2 * e + 1] = hi2 * c2 + lo2 * s2;
+    for (int i = 0; i < CE / 2; ++i) {
+      f0[i] = turn(f0[i], a.c[i], a.s[i]);
+      f1[i] = turn(f1[i], a.c[CE / 2 + i], a.s[CE / 2 + i]);
     }
   }
 }
 
-// Shared memory of a block: (cos, sin) of [tile][pairs] and the two weights as floats, both ordered so that
-// the lanes of a row read neighbouring 16-byte vectors: vector i of lane j at (i * TPR + j).
+// ---- shared memory of a block: the frequencies, the two weights as floats, and a table of (cos, sin) per warp.
+// Weights and angles are ordered so that the lanes of a row read neighbouring 16-byte vectors.
 template <int CE, int TPR>
-__device__ inline int cs_slot(int pair) {   // pair -> float2 index inside a token's table
-  const int j = pair / CE, e = pair % CE;
-  return ((e >> 1) * TPR + j) * 2 + (e & 1);
+struct Tables {
+  uint64_t turn[SPKV_MAX_ROW_DIM / 2];
+  int32_t axis[SPKV_MAX_ROW_DIM / 2];
+  alignas(16) float w[2][2 * CE * TPR];             // element e of lane j at ((e / 4) TPR + j) 4 + e % 4
+  alignas(16) float2 cs[kRowWarps][CE * TPR];       // pair e of lane j at ((e / 2) TPR + j) 2 + e % 2
+};
+template <int CE, int TPR>
+__device__ inline void fill_tables(const RowArgs &a, Tables<CE, TPR> &t) {   // the whole block; ends with a barrier
+  for (int p = threadIdx.x; p < a.rope.rot_dim / 2; p += kRowThreads) {
+    t.turn[p] = a.rope.turn[p];
+    t.axis[p] = a.rope.axis[p];
+  }
+  if (a.norm)
+    for (int x = threadIdx.x; x < 2 * 2 * CE * TPR; x += kRowThreads) {
+      const int side = x / (2 * CE * TPR), r = x % (2 * CE * TPR), j = r / (2 * CE), e = r % (2 * CE);
+      const LaneChunks l = lane_chunks<CE>(a, j);
+      const int d = e < CE ? l.c0 + e : l.c1 + e - CE;
+      t.w[side][((e >> 2) * TPR + j) * 4 + (e & 3)] = l.live ? load_weight(side ? a.wk : a.wq, a.w_dtype, d) : 0.f;
+    }
+  __syncthreads();
 }
-template <int CE, int TPR>
-__device__ inline void load_cs(const float2 *tab, int j, float2 (&cs)[CE]) {
+// Sines and cosines of one token, by one warp, and this lane's share of them ((1, 0) where nothing is rotated).
+template <int CE, int TPR, bool kAdjacent>
+__device__ inline void token_angles(const RowArgs &a, Tables<CE, TPR> &t, int tok, bool rot, Angles<CE, kAdjacent> &out) {
+  const int lane = threadIdx.x & 31, j = threadIdx.x % TPR;
+  float2 *tab = t.cs[threadIdx.x >> 5];
+  __syncwarp();    // the previous token's angles have been read
+  for (int p = lane; p < a.rope.rot_dim / 2; p += 32) {
+    const int pos = __ldg(&a.pos[(size_t)t.axis[p] * a.n_tok + tok]);
+    // turns modulo one, 64-bit fixed point; the upper 32 bits as half turns in [-1, 1)
+    const uint64_t turns = (uint64_t)(int64_t)pos * t.turn[p];
+    float sn, cn;
+    sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f, &sn, &cn);
+    tab[((p % CE >> 1) * TPR + p / CE) * 2 + (p & 1)] = make_float2(cn * a.rope.scale, sn * a.rope.scale);
+  }
+  __syncwarp();
 #pragma unroll
   for (int i = 0; i < CE / 2; ++i) {
-    const float4 v = *reinterpret_cast<const float4 *>(tab + (i * TPR + j) * 2);
-    cs[2 * i] = make_float2(v.x, v.y);
-    cs[2 * i + 1] = make_float2(v.z, v.w);
+    float4 v = make_float4(1.f, 0.f, 1.f, 0.f);
+    if (rot) v = *reinterpret_cast<const float4 *>(tab + (i * TPR + j) * 2);
+    if constexpr (kAdjacent) {
+      out.c[2 * i] = pk(v.x, v.x); out.s[2 * i] = pk(v.y, v.y);
+      out.c[2 * i + 1] = pk(v.z, v.z); out.s[2 * i + 1] = pk(v.w, v.w);
+    } else {
+      out.c[i] = pk(v.x, v.z);
+      out.s[i] = pk(v.y, v.w);
+    }
   }
 }
 template <int CE, int TPR>
-__device__ inline void fill_cs(const RowArgs &a, float2 *s_cs, int tok0, int n_here) {
-  const int P = a.rope.rot_dim / 2;
-  for (int x = threadIdx.x; x < n_here * P; x += kRowThreads) {
-    const int t = x / P, p = x % P;
-    const int pos = a.pos[(size_t)a.rope.axis[p] * a.n_tok + tok0 + t];
-    // turns modulo one, 64-bit fixed point; the upper 32 bits as half turns in [-1, 1)
-    const uint64_t turns = (uint64_t)(int64_t)pos * a.rope.turn[p];
-    float s, c;
-    sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f, &s, &c);
-    s_cs[t * (CE * TPR) + cs_slot<CE, TPR>(p)] = make_float2(c * a.rope.scale, s * a.rope.scale);
-  }
-}
-template <int CE, int TPR>
-__device__ inline void fill_weights(const RowArgs &a, float *s_w) {   // [2][2 chunks * CE * TPR]
-  for (int x = threadIdx.x; x < 2 * TPR * 2 * CE; x += kRowThreads) {
-    const int side = x / (2 * CE * TPR), r = x % (2 * CE * TPR), j = r / (2 * CE), e = r % (2 * CE);
-    const LaneChunks l = lane_chunks<CE>(a, j);
-    const int d = e < CE ? l.c0 + e : l.c1 + e - CE;
-    const float w = l.live ? load_weight(side ? a.wk : a.wq, a.w_dtype, d) : 0.f;
-    s_w[side * 2 * CE * TPR + ((e >> 2) * TPR + j) * 4 + (e & 3)] = w;
-  }
-}
-template <int CE, int TPR>
-__device__ inline void load_w(const float *s_w, int j, float (&w0)[CE], float (&w1)[CE]) {
+__device__ inline void lane_weights(const float *w, int j, f2 (&w0)[CE / 2], f2 (&w1)[CE / 2]) {
 #pragma unroll
   for (int i = 0; i < CE / 4; ++i) {
-    const float4 v = *reinterpret_cast<const float4 *>(s_w + (i * TPR + j) * 4);
-    w0[4 * i] = v.x; w0[4 * i + 1] = v.y; w0[4 * i + 2] = v.z; w0[4 * i + 3] = v.w;
-    const float4 u = *reinterpret_cast<const float4 *>(s_w + ((i + CE / 4) * TPR + j) * 4);
-    w1[4 * i] = u.x; w1[4 * i + 1] = u.y; w1[4 * i + 2] = u.z; w1[4 * i + 3] = u.w;
+    const float4 v = *reinterpret_cast<const float4 *>(w + (i * TPR + j) * 4);
+    w0[2 * i] = pk(v.x, v.y); w0[2 * i + 1] = pk(v.z, v.w);
+    const float4 u = *reinterpret_cast<const float4 *>(w + ((i + CE / 4) * TPR + j) * 4);
+    w1[2 * i] = pk(u.x, u.y); w1[2 * i + 1] = pk(u.z, u.w);
   }
 }
 
@@ -192,191 +240,218 @@ __device__ inline float row_sum(float v) {
   for (int o = TPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-
-// row r of a tile -> side (0 q, 1 k, 2 v), token of the tile, head
-struct RowAt { int side, tok, head; };
-__device__ inline RowAt row_at(const RowArgs &a, int r, int n_here) {
-  RowAt w;
-  int H = a.Hq;
-  w.side = 0;
-  if (r >= n_here * a.Hq) {
-    r -= n_here * a.Hq; H = a.Hkv; w.side = 1;
-    if (r >= n_here * a.Hkv) { r -= n_here * a.Hkv; H = a.Hv; w.side = 2; }
-  }
-  w.tok = r / H;
-  w.head = r - w.tok * H;
-  return w;
+// sum over a lane's elements of a * b
+template <int CE>
+__device__ inline float dot(const f2 (&a0)[CE / 2], const f2 (&b0)[CE / 2], const f2 (&a1)[CE / 2], const f2 (&b1)[CE / 2]) {
+  f2 s = mul(a0[0], b0[0]), t = mul(a1[0], b1[0]);
+#pragma unroll
+  for (int i = 1; i < CE / 2; ++i) { s = fma(a0[i], b0[i], s); t = fma(a1[i], b1[i], t); }
+  const float2 x = up(s), y = up(t);
+  return (x.x + x.y) + (y.x + y.y);
 }
+
 template <class T>
 __device__ inline T *row_ptr(const spkv_rows_t &v, int tok, int head) {
   return static_cast<T *>(v.ptr) + (int64_t)tok * v.token_stride + (int64_t)head * v.head_stride;
 }
-__device__ inline const spkv_rows_t &side_of(const spkv_rows_t (&v)[3], int side) {
-  return side == 0 ? v[0] : side == 1 ? v[1] : v[2];
+template <class T>
+__device__ inline void load_row(uint4 (&r)[2], const T *p, const LaneChunks &l, bool on) {
+  r[0] = r[1] = make_uint4(0, 0, 0, 0);
+  if (on) {
+    r[0] = __ldcs(reinterpret_cast<const uint4 *>(p + l.c0));
+    r[1] = __ldcs(reinterpret_cast<const uint4 *>(p + l.c1));
+  }
+}
+template <class T>
+__device__ inline void store_row(T *p, const LaneChunks &l, bool on, const uint4 &r0, const uint4 &r1) {
+  if (on) {
+    *reinterpret_cast<uint4 *>(p + l.c0) = r0;
+    *reinterpret_cast<uint4 *>(p + l.c1) = r1;
+  }
 }
 
-template <class T, int TPR>
-__global__ void __launch_bounds__(kRowThreads) norm_rope_kernel(const __grid_constant__ RowArgs a) {
-  constexpr int CE = Elem<T>::kChunk, kRowsPerPass = kRowThreads / TPR;
-  extern __shared__ __align__(16) unsigned char smem[];
-  float2 *s_cs = reinterpret_cast<float2 *>(smem);
-  float *s_w = reinterpret_cast<float *>(s_cs + a.tile * CE * TPR);
-  pdl_trigger();
-  const int tok0 = blockIdx.x * a.tile, n_here = min(a.tile, a.n_tok - tok0);
-  fill_cs<CE, TPR>(a, s_cs, tok0, n_here);
-  if (a.norm) fill_weights<CE, TPR>(a, s_w);
-  __syncthreads();
-  const int j = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  const LaneChunks l = lane_chunks<CE>(a, j);
-  const int n_rows = n_here * (a.Hq + a.Hkv + a.Hv);
-  for (int base = 0; base < n_rows; base += kRowsPerPass) {
-    // (every lane takes part in the shuffles; lanes past the last row or the row's end hold zeros)
-    const int r = base + sub;
-    const bool on = r < n_rows && l.live;
-    const RowAt w = row_at(a, min(r, n_rows - 1), n_here);
-    const T *src = row_ptr<const T>(side_of(a.x, w.side), tok0 + w.tok, w.head);
-    uint4 r0 = make_uint4(0, 0, 0, 0), r1 = r0;
-    if (on) {
-      r0 = __ldcs(reinterpret_cast<const uint4 *>(src + l.c0));
-      r1 = __ldcs(reinterpret_cast<const uint4 *>(src + l.c1));
-    }
-    float f0[CE], f1[CE];
-    Elem<T>::unpack(r0, f0);
-    Elem<T>::unpack(r1, f1);
-    float rr = 1.f;
-    if (a.norm) {   // (uniform; a warp's rows may lie on several sides, all lanes shuffle)
-      float ss = 0.f;
+// Work split.  A token belongs to one warp, or to 2, 4 or 8 of a block's warps when there are too few tokens to
+// give every warp one; a warp's lanes take 32 / TPR heads at a time.  The token's sines and cosines
+// stay in registers for all its heads, a row costs no index arithmetic but an addition, and the next rows
+// are loaded before the current ones are worked on.
+template <int TPR> struct WarpWork {
+  int first, stride, head0, step;   // first token, tokens between two of this warp; first head, heads per pass
+  __device__ WarpWork(const RowArgs &a) {
+    const int w = blockIdx.x * kRowWarps + (threadIdx.x >> 5), part = w & (a.wpt - 1), rows = 32 / TPR;
+    first = w / a.wpt;
+    stride = gridDim.x * kRowWarps / a.wpt;
+    head0 = part * rows;
+    step = a.wpt * rows;
+  }
+};
+
+// One side's heads of a warp's token.
+template <class T, int TPR, bool kAdjacent, bool kCopy>
+__device__ inline void forward_side(const RowArgs &a, const spkv_rows_t &x, const spkv_rows_t &y, int H, bool normed,
+                                    const float *s_w, const Angles<Elem<T>::kChunk, kAdjacent> &ang, int tok,
+                                    const WarpWork<TPR> &work, const LaneChunks &l) {
+  constexpr int CE = Elem<T>::kChunk;
+  const int sub = (threadIdx.x & 31) / TPR, j = threadIdx.x % TPR, head0 = work.head0, step = work.step;
+  if (head0 >= H) return;   // (warp-uniform, as is the loop: all lanes shuffle)
+  f2 w0[CE / 2], w1[CE / 2];
+  if (!kCopy && normed) lane_weights<CE, TPR>(s_w, j, w0, w1);
+  const T *src = row_ptr<const T>(x, tok, head0 + sub);
+  T *dst = row_ptr<T>(y, tok, head0 + sub);
+  const int64_t in_step = step * x.head_stride, out_step = step * y.head_stride;
+  uint4 nxt[kAhead][2];
 #pragma unroll
-      for (int e = 0; e < CE; ++e) { ss = fmaf(f0[e], f0[e], ss); ss = fmaf(f1[e], f1[e], ss); }
-      rr = rsqrtf(row_sum<TPR>(ss) * a.inv_d + a.eps);
-    }
-    if (w.side < 2) {
-      if ((a.norm >> w.side) & 1) {
-        float w0[CE], w1[CE];
-        load_w<CE, TPR>(s_w + w.side * 2 * CE * TPR, j, w0, w1);
+  for (int u = 0; u < kAhead; ++u, src += in_step) load_row(nxt[u], src, l, l.live && head0 + u * step + sub < H);
+  for (int h0 = head0; h0 < H; h0 += kAhead * step) {
+    uint4 cur[kAhead][2];
 #pragma unroll
-        for (int e = 0; e < CE; ++e) { f0[e] *= rr * w0[e]; f1[e] *= rr * w1[e]; }
+    for (int u = 0; u < kAhead; ++u) { cur[u][0] = nxt[u][0]; cur[u][1] = nxt[u][1]; }
+    if (h0 + kAhead * step < H)
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u, src += in_step)
+        load_row(nxt[u], src, l, l.live && h0 + (kAhead + u) * step + sub < H);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (!kCopy) {
+        f2 f0[CE / 2], f1[CE / 2];
+        unpack<T>(cur[u][0], f0);
+        unpack<T>(cur[u][1], f1);
+        if (normed) {
+          const float r = rsqrtf(row_sum<TPR>(dot<CE>(f0, f0, f1, f1)) * a.inv_d + a.eps);
+          const f2 rr = pk(r, r);
+#pragma unroll
+          for (int i = 0; i < CE / 2; ++i) { f0[i] = mul(f0[i], mul(rr, w0[i])); f1[i] = mul(f1[i], mul(rr, w1[i])); }
+        }
+        rotate<CE, kAdjacent, false>(f0, f1, ang);
+        cur[u][0] = pack<T>(f0);
+        cur[u][1] = pack<T>(f1);
       }
-      if (l.rot) {
-        float2 cs[CE];
-        load_cs<CE, TPR>(s_cs + w.tok * CE * TPR, j, cs);
-        rotate<CE>(f0, f1, cs, a.rope.interleaved != 0, 1.f);
-      }
-      r0 = Elem<T>::pack(f0);
-      r1 = Elem<T>::pack(f1);
-    }
-    if (on) {
-      T *dst = row_ptr<T>(side_of(a.y, w.side), tok0 + w.tok, w.head);
-      *reinterpret_cast<uint4 *>(dst + l.c0) = r0;
-      *reinterpret_cast<uint4 *>(dst + l.c1) = r1;
+      store_row(dst, l, l.live && h0 + u * step + sub < H, cur[u][0], cur[u][1]);
+      dst += out_step;
     }
   }
 }
 
-// Backward.  Blocks walk the token tiles with a stride of the grid, so that the partial sums of the weight
-// gradients are a fixed split of the rows whatever the timing: the result is the same every time.  A
-// lane keeps the sums of its 2 CE columns for both sides in registers over all its rows; at the end the
-// lanes that share columns are added up, first through shuffles, then through shared memory in warp order.
-template <class T, int TPR>
-__global__ void __launch_bounds__(kRowThreads) norm_rope_backward_kernel(const __grid_constant__ RowArgs a) {
-  constexpr int CE = Elem<T>::kChunk, kRowsPerPass = kRowThreads / TPR, kWarps = kRowThreads / 32;
-  extern __shared__ __align__(16) unsigned char smem[];
-  float2 *s_cs = reinterpret_cast<float2 *>(smem);
-  float *s_w = reinterpret_cast<float *>(s_cs + a.tile * CE * TPR);
-  float *s_dw = s_w + 2 * 2 * CE * TPR;   // [warp][2 CE * TPR], one side at a time
+template <class T, int TPR, bool kAdjacent>
+__global__ void __launch_bounds__(kRowThreads, 2) norm_rope_kernel(const __grid_constant__ RowArgs a) {
+  constexpr int CE = Elem<T>::kChunk;
+  __shared__ Tables<CE, TPR> tables;
   pdl_trigger();
-  if (a.norm) fill_weights<CE, TPR>(a, s_w);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int j = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  const LaneChunks l = lane_chunks<CE>(a, j);
-  float dw[2][2 * CE];
-#pragma unroll
-  for (int e = 0; e < 2 * CE; ++e) dw[0][e] = dw[1][e] = 0.f;
-  const int n_tiles = (a.n_tok + a.tile - 1) / a.tile;
-  for (int tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
-    const int tok0 = tile * a.tile, n_here = min(a.tile, a.n_tok - tok0);
-    __syncthreads();   // the previous tile's table has been read
-    fill_cs<CE, TPR>(a, s_cs, tok0, n_here);
-    __syncthreads();
-    // one side after the other, so that the rows of a pass all add to the same sums
-#pragma unroll
-    for (int side = 0; side < 3; ++side) {
-      const int H = side == 0 ? a.Hq : side == 1 ? a.Hkv : a.Hv, n_rows = n_here * H;
-      const bool normed = side < 2 && ((a.norm >> side) & 1);
-      for (int base = 0; base < n_rows; base += kRowsPerPass) {
-        const int r = base + sub, rc = min(r, n_rows - 1);
-        const bool on = r < n_rows && l.live;
-        const int tok = rc / H, head = rc - tok * H;
-        uint4 g0 = make_uint4(0, 0, 0, 0), g1 = g0, x0 = g0, x1 = g0;
-        if (on) {
-          const T *gp = row_ptr<const T>(a.g[side], tok0 + tok, head);
-          g0 = __ldcs(reinterpret_cast<const uint4 *>(gp + l.c0));
-          g1 = __ldcs(reinterpret_cast<const uint4 *>(gp + l.c1));
-          if (normed) {
-            const T *xp = row_ptr<const T>(a.x[side], tok0 + tok, head);
-            x0 = __ldcs(reinterpret_cast<const uint4 *>(xp + l.c0));
-            x1 = __ldcs(reinterpret_cast<const uint4 *>(xp + l.c1));
-          }
-        }
-        if (side < 2) {
-          float f0[CE], f1[CE];
-          Elem<T>::unpack(g0, f0);
-          Elem<T>::unpack(g1, f1);
-          if (l.rot) {
-            float2 cs[CE];
-            load_cs<CE, TPR>(s_cs + tok * CE * TPR, j, cs);
-            rotate<CE>(f0, f1, cs, a.rope.interleaved != 0, -1.f);
-          }
-          if (normed) {
-            float u0[CE], u1[CE], w0[CE], w1[CE];
-            Elem<T>::unpack(x0, u0);
-            Elem<T>::unpack(x1, u1);
-            load_w<CE, TPR>(s_w + side * 2 * CE * TPR, j, w0, w1);
-            // sum x^2 and sum (w g) x in one pass: the mean of w g u is r times the latter's
-            float ss = 0.f, gx = 0.f;
-#pragma unroll
-            for (int e = 0; e < CE; ++e) {
-              ss = fmaf(u0[e], u0[e], ss);
-              ss = fmaf(u1[e], u1[e], ss);
-            }
-            const float rr = rsqrtf(row_sum<TPR>(ss) * a.inv_d + a.eps);
-#pragma unroll
-            for (int e = 0; e < CE; ++e) {
-              u0[e] *= rr; u1[e] *= rr;
-              dw[side][e] = fmaf(f0[e], u0[e], dw[side][e]);
-              dw[side][CE + e] = fmaf(f1[e], u1[e], dw[side][CE + e]);
-              f0[e] *= w0[e]; f1[e] *= w1[e];
-              gx = fmaf(f0[e], u0[e], gx);
-              gx = fmaf(f1[e], u1[e], gx);
-            }
-            const float mean = row_sum<TPR>(gx) * a.inv_d;
-#pragma unroll
-            for (int e = 0; e < CE; ++e) {
-              f0[e] = rr * (f0[e] - u0[e] * mean);
-              f1[e] = rr * (f1[e] - u1[e] * mean);
-            }
-          }
-          g0 = Elem<T>::pack(f0);
-          g1 = Elem<T>::pack(f1);
-        }
-        if (on) {
-          T *dst = row_ptr<T>(a.y[side], tok0 + tok, head);
-          *reinterpret_cast<uint4 *>(dst + l.c0) = g0;
-          *reinterpret_cast<uint4 *>(dst + l.c1) = g1;
-        }
-      }
-    }
+  fill_tables<CE, TPR>(a, tables);
+  const WarpWork<TPR> work(a);
+  const LaneChunks l = lane_chunks<CE>(a, threadIdx.x % TPR);
+  for (int64_t tok = work.first; tok < a.n_tok; tok += work.stride) {
+    Angles<CE, kAdjacent> ang;
+    token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l.rot, ang);
+    forward_side<T, TPR, kAdjacent, false>(a, a.x[0], a.y[0], a.Hq, a.norm & 1, tables.w[0], ang, (int)tok, work, l);
+    forward_side<T, TPR, kAdjacent, false>(a, a.x[1], a.y[1], a.Hkv, (a.norm >> 1) & 1, tables.w[1], ang, (int)tok, work, l);
+    forward_side<T, TPR, kAdjacent, true>(a, a.x[2], a.y[2], a.Hv, false, tables.w[0], ang, (int)tok, work, l);
   }
-  if (!a.part) return;
+}
+
+// One side's heads of a warp's token, backward: dx rows out, this lane's columns of g u added to dw.
+template <class T, int TPR, bool kAdjacent, bool kCopy>
+__device__ inline void backward_side(const RowArgs &a, const spkv_rows_t &x, const spkv_rows_t &g, const spkv_rows_t &y,
+                                     int H, bool normed, const float *s_w, const Angles<Elem<T>::kChunk, kAdjacent> &ang,
+                                     int tok, const WarpWork<TPR> &work, const LaneChunks &l,
+                                     f2 (&dw0)[Elem<T>::kChunk / 2], f2 (&dw1)[Elem<T>::kChunk / 2]) {
+  constexpr int CE = Elem<T>::kChunk;
+  const int sub = (threadIdx.x & 31) / TPR, j = threadIdx.x % TPR, head0 = work.head0, step = work.step;
+  if (head0 >= H) return;
+  const T *gp = row_ptr<const T>(g, tok, head0 + sub);
+  const T *xp = normed ? row_ptr<const T>(x, tok, head0 + sub) : nullptr;
+  T *dst = row_ptr<T>(y, tok, head0 + sub);
+  const int64_t g_step = step * g.head_stride, x_step = normed ? step * x.head_stride : 0, y_step = step * y.head_stride;
+  uint4 gn[2], xn[2];
+  load_row(gn, gp, l, l.live && head0 + sub < H);
+  load_row(xn, xp, l, normed && l.live && head0 + sub < H);
+  for (int h = head0; h < H; h += step) {
+    uint4 gc[2] = {gn[0], gn[1]};
+    const uint4 xc[2] = {xn[0], xn[1]};
+    const bool on = l.live && h + sub < H;
+    gp += g_step;
+    xp += x_step;
+    if (h + step < H) {
+      const bool more = l.live && h + step + sub < H;
+      load_row(gn, gp, l, more);
+      load_row(xn, xp, l, normed && more);
+    }
+    if (!kCopy) {
+      f2 f0[CE / 2], f1[CE / 2];
+      unpack<T>(gc[0], f0);
+      unpack<T>(gc[1], f1);
+      rotate<CE, kAdjacent, true>(f0, f1, ang);
+      if (normed) {
+        f2 u0[CE / 2], u1[CE / 2], w0[CE / 2], w1[CE / 2];
+        unpack<T>(xc[0], u0);
+        unpack<T>(xc[1], u1);
+        lane_weights<CE, TPR>(s_w, j, w0, w1);
+        const float r = rsqrtf(row_sum<TPR>(dot<CE>(u0, u0, u1, u1)) * a.inv_d + a.eps);
+        const f2 rr = pk(r, r);
+#pragma unroll
+        for (int i = 0; i < CE / 2; ++i) {
+          u0[i] = mul(u0[i], rr);
+          u1[i] = mul(u1[i], rr);
+          dw0[i] = fma(f0[i], u0[i], dw0[i]);
+          dw1[i] = fma(f1[i], u1[i], dw1[i]);
+          f0[i] = mul(f0[i], w0[i]);
+          f1[i] = mul(f1[i], w1[i]);
+        }
+        const float m = -row_sum<TPR>(dot<CE>(f0, u0, f1, u1)) * a.inv_d;
+        const f2 mean = pk(m, m);
+#pragma unroll
+        for (int i = 0; i < CE / 2; ++i) { f0[i] = mul(rr, fma(u0[i], mean, f0[i])); f1[i] = mul(rr, fma(u1[i], mean, f1[i])); }
+      }
+      gc[0] = pack<T>(f0);
+      gc[1] = pack<T>(f1);
+    }
+    store_row(dst, l, on, gc[0], gc[1]);
+    dst += y_step;
+  }
+}
+
+// Backward.  A warp goes over its tokens once for the queries and once for keys and values, so that the sums of one
+// side's weight gradient are all a lane has to keep.  Which rows a lane adds up is fixed by the launch
+// alone: the result is the same every time.  Lanes that share columns are added up at the end, first
+// through shuffles, then through shared memory in warp order.
+template <class T, int TPR, bool kAdjacent>
+__global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(const __grid_constant__ RowArgs a) {
+  constexpr int CE = Elem<T>::kChunk;
+  __shared__ Tables<CE, TPR> tables;
+  __shared__ float s_dw[kRowWarps][2 * CE * TPR];
+  pdl_trigger();
+  fill_tables<CE, TPR>(a, tables);
+  const WarpWork<TPR> work(a);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = threadIdx.x % TPR;
+  const LaneChunks l = lane_chunks<CE>(a, j);
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
-    __syncthreads();
+    const int H = side ? a.Hkv : a.Hq;
+    f2 dw0[CE / 2], dw1[CE / 2];
 #pragma unroll
-    for (int e = 0; e < 2 * CE; ++e) {
-      float v = dw[side][e];
+    for (int i = 0; i < CE / 2; ++i) dw0[i] = dw1[i] = pk(0.f, 0.f);
+    if (H > 0)
+      for (int64_t tok = work.first; tok < a.n_tok; tok += work.stride) {
+        Angles<CE, kAdjacent> ang;
+        token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l.rot, ang);
+        backward_side<T, TPR, kAdjacent, false>(a, a.x[side], a.g[side], a.y[side], H, (a.norm >> side) & 1, tables.w[side],
+                                                ang, (int)tok, work, l, dw0, dw1);
+        if (side == 1)
+          backward_side<T, TPR, kAdjacent, true>(a, a.x[2], a.g[2], a.y[2], a.Hv, false, tables.w[0], ang, (int)tok, work, l,
+                                                 dw0, dw1);
+      }
+    if (!a.part) continue;
 #pragma unroll
-      for (int o = TPR; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (lane < TPR) s_dw[(warp * 2 * CE + e) * TPR + j] = v;
+    for (int i = 0; i < CE; ++i) {
+      float2 v = up(i < CE / 2 ? dw0[i % (CE / 2)] : dw1[i % (CE / 2)]);
+#pragma unroll
+      for (int o = TPR; o < 32; o <<= 1) {
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+      }
+      if (lane < TPR) {
+        s_dw[warp][(2 * i) * TPR + j] = v.x;
+        s_dw[warp][(2 * i + 1) * TPR + j] = v.y;
+      }
     }
     __syncthreads();
     for (int x = threadIdx.x; x < 2 * CE * TPR; x += kRowThreads) {
@@ -384,9 +459,10 @@ __global__ void __launch_bounds__(kRowThreads) norm_rope_backward_kernel(const _
       const LaneChunks ll = lane_chunks<CE>(a, jj);
       float v = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) v += s_dw[(w * 2 * CE + e) * TPR + jj];
+      for (int w = 0; w < kRowWarps; ++w) v += s_dw[w][e * TPR + jj];
       if (ll.live) a.part[((size_t)blockIdx.x * 2 + side) * a.D + (e < CE ? ll.c0 + e : ll.c1 + e - CE)] = v;
     }
+    __syncthreads();
   }
 }
 
@@ -453,17 +529,29 @@ static int device_sms(int *sms) {
   return check_stream_error(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
 }
 
+// Warps per token, and blocks: one warp per token once that fills the GPU, more of them for fewer tokens.
+static int split_rows(RowArgs &a, int sms, int blocks_per_sm) {
+  const int64_t fill = (int64_t)sms * blocks_per_sm * kRowWarps;
+  a.wpt = 1;
+  while (a.wpt < kRowWarps && (int64_t)a.n_tok * a.wpt < fill) a.wpt *= 2;
+  return (int)std::min<int64_t>((int64_t)sms * blocks_per_sm, ((int64_t)a.n_tok * a.wpt + kRowWarps - 1) / kRowWarps);
+}
+
 template <class T, int TPR>
-static int launch_rows(RowArgs &a, bool backward, int grid, float *dwq, float *dwk, cudaStream_t s) {
-  constexpr int CE = Elem<T>::kChunk;
-  const size_t smem = (size_t)a.tile * CE * TPR * 8 + 2 * 2 * CE * TPR * 4 +
-                      (backward ? (size_t)(kRowThreads / 32) * 2 * CE * TPR * 4 : 0);
+static int launch_rows(RowArgs &a, bool backward, int sms, float *dwq, float *dwk, cudaStream_t s) {
+  const bool adjacent = a.rope.interleaved != 0;
   if (!backward) {
-    norm_rope_kernel<T, TPR><<<grid, kRowThreads, smem, s>>>(a);
+    const int grid = split_rows(a, sms, kFwdBlocks);
+    if (adjacent) norm_rope_kernel<T, TPR, true><<<grid, kRowThreads, 0, s>>>(a);
+    else norm_rope_kernel<T, TPR, false><<<grid, kRowThreads, 0, s>>>(a);
     return check_stream_error(cudaGetLastError());
   }
-  if (grid) norm_rope_backward_kernel<T, TPR><<<grid, kRowThreads, smem, s>>>(a);
-  if (cudaGetLastError() != cudaSuccess) return SPKV_E_CUDA;
+  const int grid = a.Hq + a.Hkv ? std::min(kMaxBwdBlocks, split_rows(a, sms, kBwdBlocks)) : 0;
+  if (grid) {
+    if (adjacent) norm_rope_backward_kernel<T, TPR, true><<<grid, kRowThreads, 0, s>>>(a);
+    else norm_rope_backward_kernel<T, TPR, false><<<grid, kRowThreads, 0, s>>>(a);
+    if (cudaGetLastError() != cudaSuccess) return SPKV_E_CUDA;
+  }
   if (!a.part) return SPKV_OK;
   if (!grid) {   // no rows: the sums are zero
     norm_weight_grad_kernel<<<dim3(a.D / 16, 2), 256, 0, s>>>(a.part, 0, a.D, dwq, dwk);
@@ -474,12 +562,12 @@ static int launch_rows(RowArgs &a, bool backward, int grid, float *dwq, float *d
 }
 
 // lanes per row: two 16-byte chunks each, rounded up to a power of two
-static int dispatch_rows(RowArgs &a, int dtype, bool backward, int grid, float *dwq, float *dwk, cudaStream_t s) {
+static int dispatch_rows(RowArgs &a, int dtype, bool backward, int sms, float *dwq, float *dwk, cudaStream_t s) {
   const int lanes = a.D * elem_bytes(dtype) / 32;
-#define SPKV_ROWS(T)                                                                            if (lanes <= 4) return launch_rows<T, 4>(a, backward, grid, dwq, dwk, s);                      if (lanes <= 8) return launch_rows<T, 8>(a, backward, grid, dwq, dwk, s);                      if (lanes <= 16) return launch_rows<T, 16>(a, backward, grid, dwq, dwk, s);
+#define SPKV_ROWS(T)                                                                            if (lanes <= 4) return launch_rows<T, 4>(a, backward, sms, dwq, dwk, s);                      if (lanes <= 8) return launch_rows<T, 8>(a, backward, sms, dwq, dwk, s);                      if (lanes <= 16) return launch_rows<T, 16>(a, backward, sms, dwq, dwk, s);
   if (dtype == SPKV_F32) {
     SPKV_ROWS(float)
-    return launch_rows<float, 32>(a, backward, grid, dwq, dwk, s);
+    return launch_rows<float, 32>(a, backward, sms, dwq, dwk, s);
   }
   if (dtype == SPKV_F16) {
     SPKV_ROWS(__half)
@@ -538,9 +626,7 @@ extern "C" int spkv_norm_rope(const spkv_qk_norm_t *norm, const spkv_rope_t *rop
   }
   int sms = 0;
   if ((rc = device_sms(&sms))) return rc;
-  // tokens per block: enough blocks to fill the GPU four times over first, then fewer tables of angles
-  a.tile = std::max(1, std::min(kMaxTile, n_tok / (4 * sms)));
-  return dispatch_rows(a, norm->dtype, false, (int)(((int64_t)n_tok + a.tile - 1) / a.tile), nullptr, nullptr, as_stream(stream));
+  return dispatch_rows(a, norm->dtype, false, sms, nullptr, nullptr, as_stream(stream));
 }
 
 extern "C" size_t spkv_norm_rope_workspace_bytes(const spkv_qk_norm_t *norm) {
@@ -577,9 +663,7 @@ extern "C" int spkv_norm_rope_backward(const spkv_qk_norm_t *norm, const spkv_ro
   }
   int sms = 0;
   if ((rc = device_sms(&sms))) return rc;
-  a.tile = std::max(1, std::min(kMaxTile, n_tok / (4 * sms)));
   a.part = weights ? static_cast<float *>(d_workspace) : nullptr;
-  const int n_tiles = (int)(((int64_t)n_tok + a.tile - 1) / a.tile);
-  const int grid = rows ? std::min(n_tiles, std::min(kMaxBwdBlocks, 4 * sms)) : 0;
-  return dispatch_rows(a, norm->dtype, true, grid, d_dwq, d_dwk, as_stream(stream));
+  if (!rows) a.Hq = a.Hkv = a.Hv = 0;
+  return dispatch_rows(a, norm->dtype, true, sms, d_dwq, d_dwk, as_stream(stream));
 }
