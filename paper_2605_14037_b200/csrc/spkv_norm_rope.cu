@@ -181,35 +181,33 @@ struct Tables {
   alignas(16) float2 cs[kRowWarps][CE * TPR];       // pair e of lane j at ((e / 2) TPR + j) 2 + e % 2
 };
 template <int CE, int TPR>
+__device__ inline void fill_weights(const RowArgs &a, float (&w)[2][2 * CE * TPR]) {
+  for (int x = threadIdx.x; x < 2 * 2 * CE * TPR; x += kRowThreads) {
+    const int side = x / (2 * CE * TPR), r = x % (2 * CE * TPR), j = r / (2 * CE), e = r % (2 * CE);
+    const LaneChunks l = lane_chunks<CE>(a, j);
+    const int d = e < CE ? l.c0 + e : l.c1 + e - CE;
+    w[side][((e >> 2) * TPR + j) * 4 + (e & 3)] = l.live ? load_weight(side ? a.wk : a.wq, a.w_dtype, d) : 0.f;
+  }
+}
+template <int CE, int TPR>
 __device__ inline void fill_tables(const RowArgs &a, Tables<CE, TPR> &t) {   // the whole block; ends with a barrier
   for (int p = threadIdx.x; p < a.rope.rot_dim / 2; p += kRowThreads) {
     t.turn[p] = a.rope.turn[p];
     t.axis[p] = a.rope.axis[p];
   }
-  if (a.norm)
-    for (int x = threadIdx.x; x < 2 * 2 * CE * TPR; x += kRowThreads) {
-      const int side = x / (2 * CE * TPR), r = x % (2 * CE * TPR), j = r / (2 * CE), e = r % (2 * CE);
-      const LaneChunks l = lane_chunks<CE>(a, j);
-      const int d = e < CE ? l.c0 + e : l.c1 + e - CE;
-      t.w[side][((e >> 2) * TPR + j) * 4 + (e & 3)] = l.live ? load_weight(side ? a.wk : a.wq, a.w_dtype, d) : 0.f;
-    }
+  if (a.norm) fill_weights<CE, TPR>(a, t.w);
   __syncthreads();
 }
-// Sines and cosines of one token, by one warp, and this lane's share of them ((1, 0) where nothing is rotated).
+// (cos, sin) of one pair: turns modulo one as a 64-bit fixed-point product, its upper 32 bits as half turns in [-1, 1)
+__device__ inline float2 pair_angle(const RowArgs &a, int pos, uint64_t turn) {
+  const uint64_t turns = (uint64_t)(int64_t)pos * turn;
+  float sn, cn;
+  sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f, &sn, &cn);
+  return make_float2(cn * a.rope.scale, sn * a.rope.scale);
+}
+// A lane's share of a token's table; (1, 0) where nothing is rotated.
 template <int CE, int TPR, bool kAdjacent>
-__device__ inline void token_angles(const RowArgs &a, Tables<CE, TPR> &t, int tok, bool rot, Angles<CE, kAdjacent> &out) {
-  const int lane = threadIdx.x & 31, j = threadIdx.x % TPR;
-  float2 *tab = t.cs[threadIdx.x >> 5];
-  __syncwarp();    // the previous token's angles have been read
-  for (int p = lane; p < a.rope.rot_dim / 2; p += 32) {
-    const int pos = __ldg(&a.pos[(size_t)t.axis[p] * a.n_tok + tok]);
-    // turns modulo one, 64-bit fixed point; the upper 32 bits as half turns in [-1, 1)
-    const uint64_t turns = (uint64_t)(int64_t)pos * t.turn[p];
-    float sn, cn;
-    sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f, &sn, &cn);
-    tab[((p % CE >> 1) * TPR + p / CE) * 2 + (p & 1)] = make_float2(cn * a.rope.scale, sn * a.rope.scale);
-  }
-  __syncwarp();
+__device__ inline void lane_angles(const float2 *tab, int j, bool rot, Angles<CE, kAdjacent> &out) {
 #pragma unroll
   for (int i = 0; i < CE / 2; ++i) {
     float4 v = make_float4(1.f, 0.f, 1.f, 0.f);
@@ -222,6 +220,19 @@ __device__ inline void token_angles(const RowArgs &a, Tables<CE, TPR> &t, int to
       out.s[i] = pk(v.y, v.w);
     }
   }
+}
+// Sines and cosines of one token, by one warp, and this lane's share of them.
+template <int CE, int TPR, bool kAdjacent>
+__device__ inline void token_angles(const RowArgs &a, Tables<CE, TPR> &t, int tok, bool rot, Angles<CE, kAdjacent> &out) {
+  const int lane = threadIdx.x & 31, j = threadIdx.x % TPR;
+  float2 *tab = t.cs[threadIdx.x >> 5];
+  __syncwarp();    // the previous token's angles have been read
+  for (int p = lane; p < a.rope.rot_dim / 2; p += 32) {
+    tab[((p % CE >> 1) * TPR + p / CE) * 2 + (p & 1)] =
+        pair_angle(a, __ldg(&a.pos[(size_t)t.axis[p] * a.n_tok + tok]), t.turn[p]);
+  }
+  __syncwarp();
+  lane_angles<CE, TPR, kAdjacent>(tab, j, rot, out);
 }
 template <int CE, int TPR>
 __device__ inline void lane_weights(const float *w, int j, f2 (&w0)[CE / 2], f2 (&w1)[CE / 2]) {
@@ -348,6 +359,65 @@ __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_kernel(const __grid_
   }
 }
 
+// Forward for few tokens (a decode step): a block per token, its rows of all sides in one short loop.  Such a launch
+// is a chain of waits -- instructions, positions and weights, rows -- so the code is small (the kernel above spends
+// more on fetching its instructions than on a token: 4.1 against 2.7 us for one token), and the first rows
+// are on their way while the angles are computed.
+template <class T, int TPR, bool kAdjacent>
+__global__ void __launch_bounds__(kRowThreads) norm_rope_few_kernel(const __grid_constant__ RowArgs a) {
+  constexpr int CE = Elem<T>::kChunk, kRows = kRowThreads / TPR;
+  __shared__ alignas(16) float2 s_cs[CE * TPR];
+  __shared__ alignas(16) float s_w[2][2 * CE * TPR];
+  pdl_trigger();
+  const int tok = blockIdx.x, j = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const LaneChunks l = lane_chunks<CE>(a, j);
+  const int n_rows = a.Hq + a.Hkv + a.Hv;
+  // row r of the token: side and head (a warp's rows may lie on several sides)
+  auto side_of = [&](int r) { return (r >= a.Hq) + (r >= a.Hq + a.Hkv); };
+  auto head_of = [&](int r, int side) { return r - (side ? a.Hq : 0) - (side == 2 ? a.Hkv : 0); };
+  uint4 nxt[2];
+  auto fetch = [&](int r) {
+    const bool on = l.live && r < n_rows;
+    const int side = on ? side_of(r) : 0;
+    load_row(nxt, row_ptr<const T>(side == 0 ? a.x[0] : side == 1 ? a.x[1] : a.x[2], tok, on ? head_of(r, side) : 0), l, on);
+  };
+  fetch(sub);
+  for (int p = threadIdx.x; p < a.rope.rot_dim / 2; p += kRowThreads)
+    s_cs[((p % CE >> 1) * TPR + p / CE) * 2 + (p & 1)] = pair_angle(a, __ldg(&a.pos[(size_t)a.rope.axis[p] * a.n_tok + tok]), a.rope.turn[p]);
+  if (a.norm) fill_weights<CE, TPR>(a, s_w);
+  __syncthreads();
+  Angles<CE, kAdjacent> ang;
+  lane_angles<CE, TPR, kAdjacent>(s_cs, j, l.rot, ang);
+#pragma unroll 1
+  for (int base = 0; base < n_rows; base += kRows) {
+    const int r = base + sub, side = side_of(r);
+    uint4 cur[2] = {nxt[0], nxt[1]};
+    fetch(r + kRows);
+    if (__any_sync(0xffffffffu, side < 2)) {
+      f2 f0[CE / 2], f1[CE / 2];
+      unpack<T>(cur[0], f0);
+      unpack<T>(cur[1], f1);
+      if (a.norm) {
+        const float q = rsqrtf(row_sum<TPR>(dot<CE>(f0, f0, f1, f1)) * a.inv_d + a.eps);
+        if (side < 2 && ((a.norm >> side) & 1)) {
+          f2 w0[CE / 2], w1[CE / 2];
+          lane_weights<CE, TPR>(s_w[side], j, w0, w1);
+          const f2 rr = pk(q, q);
+#pragma unroll
+          for (int i = 0; i < CE / 2; ++i) { f0[i] = mul(f0[i], mul(rr, w0[i])); f1[i] = mul(f1[i], mul(rr, w1[i])); }
+        }
+      }
+      if (side < 2) {
+        rotate<CE, kAdjacent, false>(f0, f1, ang);
+        cur[0] = pack<T>(f0);
+        cur[1] = pack<T>(f1);
+      }
+    }
+    const bool on = l.live && r < n_rows;
+    store_row(row_ptr<T>(side == 0 ? a.y[0] : side == 1 ? a.y[1] : a.y[2], tok, on ? head_of(r, side) : 0), l, on, cur[0], cur[1]);
+  }
+}
+
 // One side's heads of a warp's token, backward: dx rows out, this lane's columns of g u added to dw.
 template <class T, int TPR, bool kAdjacent, bool kCopy>
 __device__ inline void backward_side(const RowArgs &a, const spkv_rows_t &x, const spkv_rows_t &g, const spkv_rows_t &y,
@@ -466,19 +536,23 @@ __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(cons
   }
 }
 
-// Sums the blocks' partial weight gradients, in a fixed order: grid (D / 16, 2 sides), 256 threads = 16 columns x 16 slices.
-__global__ void __launch_bounds__(256) norm_weight_grad_kernel(const float *part, int n_blocks, int D, float *dwq, float *dwk) {
-  __shared__ float s[16][17];
+// Sums the blocks' partial weight gradients, in a fixed order: grid (D / 16, 2 sides), 512 threads = 16 columns x 32
+// slices of the blocks.
+constexpr int kGradSlices = 32;
+__global__ void __launch_bounds__(16 * kGradSlices) norm_weight_grad_kernel(const float *part, int n_blocks, int D, float *dwq,
+                                                                           float *dwk) {
+  __shared__ float s[kGradSlices][17];
   const int col = blockIdx.x * 16 + (threadIdx.x & 15), slice = threadIdx.x >> 4, side = blockIdx.y;
   pdl_wait();
   float v = 0.f;
-  for (int b = slice; b < n_blocks; b += 16) v += part[((size_t)b * 2 + side) * D + col];
+#pragma unroll 8
+  for (int b = slice; b < n_blocks; b += kGradSlices) v += __ldcg(&part[((size_t)b * 2 + side) * D + col]);
   s[slice][threadIdx.x & 15] = v;
   __syncthreads();
   if (threadIdx.x < 16) {
     float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += s[i][threadIdx.x];
+    for (int i = 0; i < kGradSlices; ++i) t += s[i][threadIdx.x];
     float *out = side ? dwk : dwq;
     if (out) out[col] = t;
   }
@@ -540,6 +614,11 @@ static int split_rows(RowArgs &a, int sms, int blocks_per_sm) {
 template <class T, int TPR>
 static int launch_rows(RowArgs &a, bool backward, int sms, float *dwq, float *dwk, cudaStream_t s) {
   const bool adjacent = a.rope.interleaved != 0;
+  if (!backward && a.n_tok <= 2 * sms) {
+    if (adjacent) norm_rope_few_kernel<T, TPR, true><<<a.n_tok, kRowThreads, 0, s>>>(a);
+    else norm_rope_few_kernel<T, TPR, false><<<a.n_tok, kRowThreads, 0, s>>>(a);
+    return check_stream_error(cudaGetLastError());
+  }
   if (!backward) {
     const int grid = split_rows(a, sms, kFwdBlocks);
     if (adjacent) norm_rope_kernel<T, TPR, true><<<grid, kRowThreads, 0, s>>>(a);
@@ -554,10 +633,10 @@ static int launch_rows(RowArgs &a, bool backward, int sms, float *dwq, float *dw
   }
   if (!a.part) return SPKV_OK;
   if (!grid) {   // no rows: the sums are zero
-    norm_weight_grad_kernel<<<dim3(a.D / 16, 2), 256, 0, s>>>(a.part, 0, a.D, dwq, dwk);
+    norm_weight_grad_kernel<<<dim3(a.D / 16, 2), 16 * kGradSlices, 0, s>>>(a.part, 0, a.D, dwq, dwk);
     return check_stream_error(cudaGetLastError());
   }
-  return check_stream_error(launch_overlapped(norm_weight_grad_kernel, dim3(a.D / 16, 2), dim3(256), 0, s, a.part, grid,
+  return check_stream_error(launch_overlapped(norm_weight_grad_kernel, dim3(a.D / 16, 2), dim3(16 * kGradSlices), 0, s, a.part, grid,
                                               a.D, dwq, dwk));
 }
 
