@@ -22,7 +22,8 @@
 //   * At most 128 rows (kAlt): both slots hold the same rows and take alternate pages, which halves the
 //     softmax time per page; scores of a slot's next page are issued behind P.V of its last one.  One of the two
 //     is joined into the other through shared memory at the end.
-// Shared memory: Q (64 KB; kAlt 32 KB) + rings of 4 (5) key and 4 (5) value blocks, which leaves 34 KB to a tail block.  Tensor memory: score buffer b of slot h at
+// Shared memory: Q (64 KB; kAlt 32 KB) + rings of 3 (4) key and 3 (4) value blocks, which leaves 66 KB to a tail
+// block.  Tensor memory: score buffer b of slot h at
 // [64 (2h + b), +64), O of slot h at [256 + 128 h, +128).
 // Warps: 0 / 2 MMA issue of slot 0 / 1, 1 page loader, 3 tensor memory, 4-7 / 8-11 softmax of slot 0 / 1, 12-15 value
 // conversion.  All waits are bounded.
@@ -44,14 +45,12 @@ constexpr int kMmaWarp0 = 0, kLoaderWarp = 1, kMmaWarp1 = 2, kTmemWarp = 3;
 constexpr int kConvThreads = 128;   // warps 12-15
 constexpr int kTmemCols = 512;
 constexpr float kPBias = 7.f;   // P is stored as 2^7 p
-constexpr int kMaxRing = 5;
-enum { B_K_FULL = 0, B_K_EMPTY = 5, B_V_FULL = 10, B_V_EMPTY = 15, B_V_READY = 20, B_S_FULL = 25 /* [2h+b] */, B_P_FULL = 29,
-       B_O_DONE = 33, B_COUNT = 37 };
+enum { B_K_FULL = 0, B_K_EMPTY = 4, B_V_FULL = 8, B_V_EMPTY = 12, B_V_READY = 16, B_S_FULL = 20 /* [2h+b] */, B_P_FULL = 24,
+       B_O_DONE = 28, B_COUNT = 32 };
 // Key and value blocks travel in rings of their own: a key block is free again as soon as the scores are made, two
 // pages before the values of its page are needed, so nearly every buffer has a copy in flight (a page
-// takes about 2 us to arrive under load; with whole pages in one ring of four, three were in use and
-// one in flight: 2200 cycles per page).
-__host__ __device__ constexpr int ring(bool alt) { return alt ? 5 : 4; }   // key blocks; as many value blocks
+// takes about 2 us to arrive under load; in one ring of four whole pages three were in use, one in flight).
+__host__ __device__ constexpr int ring(bool alt) { return alt ? 4 : 3; }   // key blocks; as many value blocks
 constexpr int kBlockBytes = kPageBytes / 2, kKeyLead = 2;   // keys are loaded two pages ahead of values
 __host__ __device__ constexpr int off_k(bool alt) { return alt ? 32768 : 65536; }
 __host__ __device__ constexpr int off_v(bool alt) { return off_k(alt) + ring(alt) * kBlockBytes; }
@@ -163,11 +162,11 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
     // (stale plan: the unit is shorter by now; the tail sees the same and nobody reads this share's result)
     const bool valid = len / kP >= common;
     if (valid) first_entry = checked_page(c, first_entry, (int)ring_page(c, u, 0));
-    for (int j = 0; j < kRing && valid; ++j) {   // the steps of the loop below that find every buffer empty
+    // the keys of the first two pages; the rest follows when Q is in place (every block's rings at once are 20 MB
+    // of requests, behind which the tail's first look at its units would wait 3 us)
+    for (int j = 0; j < kKeyLead && valid; ++j) {
       const int gk = __shfl_sync(0xffffffffu, first_entry, j);
-      const int gv = __shfl_sync(0xffffffffu, first_entry, max(j - kKeyLead, 0));
       if (lane == 0 && j < n_pages) load_block<kAlt>(a, smem, bar, 0, j, gk, pol);
-      if (lane == 0 && j >= kKeyLead && j - kKeyLead < n_pages) load_block<kAlt>(a, smem, bar, 1, j - kKeyLead, gv, pol);
     }
     if (lane == 0) { s_desc[8] = valid; s_desc[9] = (int)vm; }
   } else {
@@ -207,7 +206,7 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
     // ---------------------------------------------------------------- page loader
     // step j: the keys of page j, the values of page j - 2
     int entry = first_entry, older = 0;   // global page indices of this lane in the current and the previous 32 pages
-    int j = kRing;
+    int j = kKeyLead;
     auto wait_empty = [&](int which, int jj) {
       return jj < kRing || mbar_wait_bounded(&bar[which + jj % kRing], ((jj / kRing) - 1) & 1);
     };
@@ -455,9 +454,8 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
 // ---- tail ------------------------------------------------------------------------------------------
 namespace sht {
 constexpr int kThreads = 128, kWarps = 4;
-// one page, over which the four warps join their G rows of 132 floats at the end (G = 16: 33 KB)
-__host__ __device__ constexpr int off_bar(int NH) { return NH == 1 ? kPageBytes : kWarps * 16 * 132 * 4; }
-__host__ __device__ constexpr int smem_bytes(int NH) { return off_bar(NH) + 128; }
+// two pages, over which the four warps join their G rows of 132 floats at the end (33 KB at G = 16)
+constexpr int off_bar = 2 * kPageBytes, kSmemBytes = off_bar + 128;
 }  // namespace sht
 
 // Item = share * n_items + unit.  A unit's pages are what its compact cache holds behind the common pages,
@@ -469,19 +467,18 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
   extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = c.G;
-  uint64_t *full = reinterpret_cast<uint64_t *>(smem + off_bar(NH));   // [0] keys, [1] values
-  volatile int *s_it = reinterpret_cast<volatile int *>(full + 2);   // share exists, skip, compact pages, length behind
+  uint64_t *full = reinterpret_cast<uint64_t *>(smem + off_bar);   // [2 buffer + half]: keys, values
+  volatile int *s_it = reinterpret_cast<volatile int *>(full + 4);   // share exists, skip, compact pages, length behind
                                                                      // the common pages, ring pairs, first page, pages, `ahead` holds
   if (tid == 0) {
-    mbar_init(&full[0], 1);
-    mbar_init(&full[1], 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&full[i], 1);
     mbar_fence_init();
   }
   pdl_trigger();
   // everything before the prefix launch is complete and was written through generic stores
   asm volatile("fence.proxy.async;" ::: "memory");
   const uint64_t pol = l2_evict_first_policy();
-  int loads = 0;        // pages loaded so far: their parity is the barriers' phase
+  int loads = 0;        // pages of the items before: page i of this one is in buffer (loads + i) & 1, phase (loads + i) >> 1 & 1
   bool failed = false;
   for (int item = blockIdx.x;; item += gridDim.x) {
     const int unit = item % a.n_items, share = item / a.n_items;
@@ -551,14 +548,20 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
       if (half == 0 && (i & 31) == 0) fetch_entries(i);
       const int gp = __shfl_sync(0xffffffffu, entry, i & 31);
       if (lane == 0) {
-        mbar_arrive_expect_tx(&full[half], kPageBytes / 2);
-        bulk_load_hint(smem + half * (kPageBytes / 2), c.pages + (int64_t)gp * kPageElems + half * kBlockElems,
-                       kPageBytes / 2, &full[half], pol);
+        const int bf = (loads + i) & 1;
+        uint64_t *bar = &full[2 * bf + half];
+        mbar_arrive_expect_tx(bar, kPageBytes / 2);
+        bulk_load_hint(smem + bf * kPageBytes + half * (kPageBytes / 2), c.pages + (int64_t)gp * kPageElems + half * kBlockElems,
+                       kPageBytes / 2, bar, pol);
       }
     };
     if (warp == 0) {
       load(0, 0);
       load(0, 1);
+      if (n > 1) {
+        load(1, 0);
+        load(1, 1);
+      }
     }
     uint32_t qb[NH][8][2];
     float m[NH][2], l[NH][2], o[NH][8][4];
@@ -574,34 +577,33 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
     for (int i = 0; i < n; ++i) {
       const int p = p0 + i;
       const int valid = p < nk ? min(kP, len - p * kP) : min(kP, n_ring - (p - nk) * kP);
-      const uint32_t ph = (loads + i) & 1;
+      const int bf = (loads + i) & 1;
+      const uint32_t ph = ((loads + i) >> 1) & 1;
       const int tok0 = warp * 16;
-      const uint32_t sK = smem_u32(smem), sV = sK + kBlockElems * 2;
+      const uint32_t sK = smem_u32(smem + bf * kPageBytes), sV = sK + kBlockElems * 2;
       float s[NH][4];
-      if (!mbar_wait_bounded(&full[0], ph)) failed = true;
+      if (!mbar_wait_bounded(&full[2 * bf], ph)) failed = true;
       if (!failed && tok0 < valid) qk_tile_t<NH>(s, qb, sK, tok0, lane);
       failed = __syncthreads_or(failed);   // all four warps are done with the keys
+      if (!failed) {
+        if (warp == 0 && i + 2 < n) load(i + 2, 0);
+        if (!mbar_wait_bounded(&full[2 * bf + 1], ph)) failed = true;
+        if (!failed && tok0 < valid) softmax_pv_tile_t<NH>(s, valid, a.scale_log2, m, l, o, sV, tok0, lane);
+        failed = __syncthreads_or(failed);   // ... and with the values
+      }
       if (failed) {
-        // do not leave while copies may still be landing
-        if (tid == 0) { mbar_wait_bounded(&full[0], ph); mbar_wait_bounded(&full[1], ph); }
+        // do not leave while copies may still be landing (keys up to page i + 2, values up to i + 1)
+        if (tid == 0)
+          for (int k = i; k < min(i + 3, n); ++k)
+            for (int half = 0; half < 2; ++half)
+              mbar_wait_bounded(&full[2 * ((loads + k) & 1) + half], ((loads + k) >> 1) & 1);
         break;
       }
-      if (warp == 0 && i + 1 < n) load(i + 1, 0);
-      if (!mbar_wait_bounded(&full[1], ph)) failed = true;
-      if (!failed && tok0 < valid) softmax_pv_tile_t<NH>(s, valid, a.scale_log2, m, l, o, sV, tok0, lane);
-      failed = __syncthreads_or(failed);   // ... and with the values
-      if (failed) {
-        if (tid == 0) {
-          mbar_wait_bounded(&full[1], ph);
-          if (i + 1 < n) mbar_wait_bounded(&full[0], ph ^ 1);
-        }
-        break;
-      }
-      if (warp == 0 && i + 1 < n) load(i + 1, 1);
+      if (warp == 0 && i + 2 < n) load(i + 2, 1);
     }
     if (failed) break;
     loads += n;
-    // join the four warps: rows [warp][G][132] over the page (every copy of the item has landed)
+    // join the four warps: rows [warp][G][132] over the pages (every copy of the item has landed)
     float *red = reinterpret_cast<float *>(smem);
     segment_hand_over<NH>(red, warp, G, G, m, l, o, lane);
     __syncthreads();
@@ -804,7 +806,7 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   auto prefix = alt ? shared_prefix_kernel<true> : shared_prefix_kernel<false>;
   const int smem = shp::smem_bytes(alt);
   auto tail = v.G > 8 ? shared_tail_kernel<2> : shared_tail_kernel<1>;
-  const int tail_smem = sht::smem_bytes(v.G > 8 ? 2 : 1);
+  const int tail_smem = sht::kSmemBytes;
   if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(prefix), smem, &g_ready[0][alt])) return rc;
   if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(tail), tail_smem, &g_ready[1][v.G > 8])) return rc;
   // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
