@@ -18,10 +18,9 @@
 // rescaled to fp16 by converter warps, or two bf16 terms for a unit of wide-ranging values
 // (value_scale).  No masks: common pages are full and every query sees all of them.
 //   * More than 128 rows in the tile (kAlt = false): slot h holds rows [128 h, 128 h + 128), both walk
-//     every page.  Scores of page j + 2 are issued behind P.V(j), so a slot's next scores are ready.
+//     every page.
 //   * At most 128 rows (kAlt): both slots hold the same rows and take alternate pages, which halves the
-//     softmax time per page; scores of a slot's next page are issued behind P.V of its last one.  One of the two
-//     is joined into the other through shared memory at the end.
+//     softmax time per page.  One of the two is joined into the other through shared memory at the end.
 // Shared memory: Q (64 KB; kAlt 32 KB) + rings of 3 (4) key and 3 (4) value blocks, which leaves 66 KB to a tail
 // block.  Tensor memory: score buffer b of slot h at
 // [64 (2h + b), +64), O of slot h at [256 + 128 h, +128).
@@ -51,7 +50,9 @@ enum { B_K_FULL = 0, B_K_EMPTY = 4, B_V_FULL = 8, B_V_EMPTY = 12, B_V_READY = 16
 // pages before the values of its page are needed, so nearly every buffer has a copy in flight (a page
 // takes about 2 us to arrive under load; in one ring of four whole pages three were in use, one in flight).
 __host__ __device__ constexpr int ring(bool alt) { return alt ? 4 : 3; }   // key blocks; as many value blocks
-constexpr int kBlockBytes = kPageBytes / 2, kKeyLead = 2;   // keys are loaded two pages ahead of values
+constexpr int kBlockBytes = kPageBytes / 2;
+// keys are loaded this many pages ahead of values: as far as a slot's scores run ahead of its P.V
+__host__ __device__ constexpr int key_lead(bool alt) { return alt ? 4 : 2; }
 __host__ __device__ constexpr int off_k(bool alt) { return alt ? 32768 : 65536; }
 __host__ __device__ constexpr int off_v(bool alt) { return off_k(alt) + ring(alt) * kBlockBytes; }
 __host__ __device__ constexpr int off_bar(bool alt) { return off_v(alt) + ring(alt) * kBlockBytes; }
@@ -104,8 +105,8 @@ template <bool kAlt>
 __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
   using namespace tc5;
   using namespace shp;
-  constexpr int kRing = ring(kAlt);
-  constexpr int kAhead = kAlt ? 1 : 2;       // how many of a slot's pages its scores run ahead of P.V
+  constexpr int kRing = ring(kAlt), kKeyLead = key_lead(kAlt);
+  constexpr int kAhead = 2;                  // how many of a slot's pages its scores run ahead of P.V
   extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
   uint64_t *bar = reinterpret_cast<uint64_t *>(smem + off_bar(kAlt));
@@ -162,7 +163,7 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
     // (stale plan: the unit is shorter by now; the tail sees the same and nobody reads this share's result)
     const bool valid = len / kP >= common;
     if (valid) first_entry = checked_page(c, first_entry, (int)ring_page(c, u, 0));
-    // the keys of the first two pages; the rest follows when Q is in place (every block's rings at once are 20 MB
+    // the keys that the first scores need; the rest follows when Q is in place (every block's rings at once are 20 MB
     // of requests, behind which the tail's first look at its units would wait 3 us)
     for (int j = 0; j < kKeyLead && valid; ++j) {
       const int gk = __shfl_sync(0xffffffffu, first_entry, j);
@@ -204,7 +205,7 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
     // nothing to do but to give the tensor memory back
   } else if (warp == kLoaderWarp) {
     // ---------------------------------------------------------------- page loader
-    // step j: the keys of page j, the values of page j - 2
+    // step j: the keys of page j, the values of page j - kKeyLead
     int entry = first_entry, older = 0;   // global page indices of this lane in the current and the previous 32 pages
     int j = kKeyLead;
     auto wait_empty = [&](int which, int jj) {
@@ -318,11 +319,10 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
       const bool grow = mx > m_ref + 8.f;
       const float m_new = grow ? mx : m_ref;
       if (i > 0 && __any_sync(0xffffffffu, grow)) {
-        // O is stable between the completion of P.V(i-1) and the hand-over of P(i).  kAlt: the scores of
-        // this page were issued behind P.V(i-1).  Otherwise those of the next page were; the last page
-        // has a barrier of its own.
-        if (!kAlt && !(i + 1 < n_mine ? mbar_wait_bounded(&bar[B_S_FULL + 2 * h + (b ^ 1)], ((i + 1) >> 1) & 1)
-                                      : mbar_wait_bounded(&bar[B_O_DONE + 2 * h + (b ^ 1)], 0))) {
+        // O is stable between the completion of P.V(i-1) and the hand-over of P(i).  The scores of the slot's next page
+        // were issued behind P.V(i-1); its last page has a barrier of its own.
+        if (!(i + 1 < n_mine ? mbar_wait_bounded(&bar[B_S_FULL + 2 * h + (b ^ 1)], ((i + 1) >> 1) & 1)
+                             : mbar_wait_bounded(&bar[B_O_DONE + 2 * h + (b ^ 1)], 0))) {
           failed = true;
           break;
         }
