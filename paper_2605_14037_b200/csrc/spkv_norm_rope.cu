@@ -24,6 +24,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include <cuda_fp16.h>
 
@@ -129,18 +130,38 @@ __device__ inline float load_weight(const void *w, int dtype, int i) {
   return static_cast<const float *>(w)[i];
 }
 
-// Where lane j of a row finds its two chunks (element offsets), and whether its pairs are rotated.
+// Where lane j of a row finds its two chunks (element offsets).  Neighbouring lanes always read neighbouring chunks
+// (a lane with two chunks side by side would make every 32-byte sector two requests).  Pairs (i, i + rot/2):
+// chunks j and j + rot/2 of the rotated dims, the others in two halves likewise, rot = false; adjacent
+// pairs lie within a chunk, the row goes in two halves.
 struct LaneChunks { int c0, c1; bool live, rot; };
 template <int CE>
 __device__ inline LaneChunks lane_chunks(const RowArgs &a, int j) {
   LaneChunks l;
-  const int n_rot = a.rope.rot_dim / (2 * CE);   // lanes whose pairs are rotated
-  l.live = j < a.D / (2 * CE);
+  const int lanes = a.D / (2 * CE), n_rot = a.rope.interleaved ? lanes : a.rope.rot_dim / (2 * CE);
+  l.live = j < lanes;
   l.rot = j < n_rot;
-  if (l.rot && !a.rope.interleaved) { l.c0 = j * CE; l.c1 = a.rope.rot_dim / 2 + j * CE; }
-  else { l.c0 = 2 * j * CE; l.c1 = l.c0 + CE; }
+  if (l.rot) { l.c0 = j * CE; l.c1 = l.c0 + n_rot * CE; }
+  else { l.c0 = (n_rot + j) * CE; l.c1 = l.c0 + (lanes - n_rot) * CE; }
   return l;
 }
+// Place of pair p in a token's table of (cos, sin): pair e of lane j at ((e / 2) TPR + j) 2 + e % 2.
+template <int CE, int TPR, bool kAdjacent>
+__device__ inline int pair_slot(const RowArgs &a, int p) {
+  int j, e;
+  if (kAdjacent) {
+    const int chunk = p / (CE / 2), lanes = a.D / (2 * CE);
+    j = chunk < lanes ? chunk : chunk - lanes;
+    e = p % (CE / 2) + (chunk < lanes ? 0 : CE / 2);
+  } else {
+    j = p / CE;
+    e = p % CE;
+  }
+  return ((e >> 1) * TPR + j) * 2 + (e & 1);
+}
+// Pairs that the table holds: the rotated ones; with adjacent pairs every one, since a lane may have both kinds.
+template <bool kAdjacent>
+__device__ inline int table_pairs(const RowArgs &a) { return kAdjacent ? a.D / 2 : a.rope.rot_dim / 2; }
 
 // A lane's CE pairs: pair e is (f0[e], f1[e]), or with adjacent pairs the two elements of f2 number e of chunk 0,
 // then of chunk 1.  Angles as the rotation wants them: cosines c and sines s of pairs (2i, 2i + 1), or
@@ -227,9 +248,9 @@ __device__ inline void token_angles(const RowArgs &a, Tables<CE, TPR> &t, int to
   const int lane = threadIdx.x & 31, j = threadIdx.x % TPR;
   float2 *tab = t.cs[threadIdx.x >> 5];
   __syncwarp();    // the previous token's angles have been read
-  for (int p = lane; p < a.rope.rot_dim / 2; p += 32) {
-    tab[((p % CE >> 1) * TPR + p / CE) * 2 + (p & 1)] =
-        pair_angle(a, __ldg(&a.pos[(size_t)t.axis[p] * a.n_tok + tok]), t.turn[p]);
+  for (int p = lane; p < table_pairs<kAdjacent>(a); p += 32) {
+    tab[pair_slot<CE, TPR, kAdjacent>(a, p)] =
+        p < a.rope.rot_dim / 2 ? pair_angle(a, __ldg(&a.pos[(size_t)t.axis[p] * a.n_tok + tok]), t.turn[p]) : make_float2(1.f, 0.f);
   }
   __syncwarp();
   lane_angles<CE, TPR, kAdjacent>(tab, j, rot, out);
@@ -262,8 +283,8 @@ __device__ inline float dot(const f2 (&a0)[CE / 2], const f2 (&b0)[CE / 2], cons
 }
 
 template <class T>
-__device__ inline T *row_ptr(const spkv_rows_t &v, int tok, int head) {
-  return static_cast<T *>(v.ptr) + (int64_t)tok * v.token_stride + (int64_t)head * v.head_stride;
+__device__ inline T *row_ptr(const spkv_rows_t &v, int64_t tok, int head) {
+  return static_cast<T *>(v.ptr) + tok * v.token_stride + (int64_t)head * v.head_stride;
 }
 template <class T>
 __device__ inline void load_row(uint4 (&r)[2], const T *p, const LaneChunks &l, bool on) {
@@ -296,66 +317,133 @@ template <int TPR> struct WarpWork {
   }
 };
 
+// A warp's rows are one stream -- token after token, query, key and value heads, `step` heads a pass -- that runs
+// kDepth passes ahead through shared memory: a lane copies its own 32 bytes of a pass there
+// asynchronously and reads them back, so that what is on its way costs no registers (2 KB per warp in
+// registers left memory waiting: 40 us for 8192 tokens of 32/8 heads; see the figures at the head).
+template <class T, int TPR, int kStreams>
+struct RowStream {
+  static constexpr int kDepth = 4;
+  const RowArgs &a;
+  const WarpWork<TPR> &work;
+  const LaneChunks &l;
+  uint4 *ring;                  // this lane's first chunk of pass 0; chunk k of stream s of pass d at ((d kStreams + s) 2 + k) 32
+  int64_t tok;                  // next pass to ask for
+  int pass, slot;               // ... of the token; ring slot of the next pass to take (= to ask for, once the ring is full)
+  int n_pass[3];                // passes of the warp per side
+  __device__ RowStream(const RowArgs &a_, const WarpWork<TPR> &w, const LaneChunks &l_, uint4 *warp_ring, int first_side,
+                       int last_side)
+      : a(a_), work(w), l(l_), ring(warp_ring + (threadIdx.x & 31)), tok(w.first), pass(0), slot(0) {
+    const int H[3] = {a.Hq, a.Hkv, a.Hv};
+#pragma unroll
+    for (int s = 0; s < 3; ++s)
+      n_pass[s] = s < first_side || s > last_side || H[s] <= w.head0 ? 0 : (H[s] - w.head0 + w.step - 1) / w.step;
+  }
+  __device__ bool any() const { return n_pass[0] + n_pass[1] + n_pass[2] > 0; }
+  // asks for the next pass, into the current slot
+  __device__ void ask() {
+    if (tok < a.n_tok && any()) {
+      const int side = (pass >= n_pass[0]) + (pass >= n_pass[0] + n_pass[1]);
+      const int i = pass - (side ? n_pass[0] : 0) - (side == 2 ? n_pass[1] : 0);
+      const int h = work.head0 + i * work.step + (threadIdx.x & 31) / TPR;
+      const bool on = l.live && h < (side ? a.Hkv : a.Hq);
+#pragma unroll
+      for (int s = 0; s < kStreams; ++s) {
+        // stream 0 of the backward pass: upstream gradients; stream 1: the inputs of a normed side
+        const spkv_rows_t &v = kStreams == 1 ? (side == 0 ? a.x[0] : side == 1 ? a.x[1] : a.x[2])
+                               : s == 0      ? (side == 0 ? a.g[0] : side == 1 ? a.g[1] : a.g[2])
+                                             : (side == 0 ? a.x[0] : a.x[1]);
+        const bool use = on && (s == 0 || (side < 2 && ((a.norm >> side) & 1)));
+        const T *src = use ? row_ptr<const T>(v, tok, h) : static_cast<const T *>(v.ptr);
+        uint4 *dst = ring + (slot * kStreams + s) * 64;
+        copy16(dst, src + l.c0, use);
+        copy16(dst + 32, src + l.c1, use);
+      }
+      if (++pass == n_pass[0] + n_pass[1] + n_pass[2]) {
+        pass = 0;
+        tok += work.stride;
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  static __device__ void copy16(uint4 *dst, const T *src, bool on) {   // zeros where a lane has no row
+    if (!on) { *dst = make_uint4(0, 0, 0, 0); return; }
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                 ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src) : "memory");
+  }
+  __device__ void start() {
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) {
+      slot = d;
+      ask();
+    }
+    slot = 0;
+  }
+  // the oldest pass; then asks for one more
+  __device__ void take(uint4 (&r)[kStreams][2]) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+#pragma unroll
+    for (int s = 0; s < kStreams; ++s) {
+      r[s][0] = ring[(slot * kStreams + s) * 64];
+      r[s][1] = ring[(slot * kStreams + s) * 64 + 32];
+    }
+    ask();
+    slot = slot + 1 == kDepth ? 0 : slot + 1;
+  }
+};
+
 // One side's heads of a warp's token.
 template <class T, int TPR, bool kAdjacent, bool kCopy>
-__device__ inline void forward_side(const RowArgs &a, const spkv_rows_t &x, const spkv_rows_t &y, int H, bool normed,
-                                    const float *s_w, const Angles<Elem<T>::kChunk, kAdjacent> &ang, int tok,
-                                    const WarpWork<TPR> &work, const LaneChunks &l) {
+__device__ inline void forward_side(const RowArgs &a, const spkv_rows_t &y, int H, int n_pass, bool normed, const float *s_w,
+                                    const Angles<Elem<T>::kChunk, kAdjacent> &ang, int64_t tok, const WarpWork<TPR> &work,
+                                    const LaneChunks &l, RowStream<T, TPR, 1> &stream) {
   constexpr int CE = Elem<T>::kChunk;
-  const int sub = (threadIdx.x & 31) / TPR, j = threadIdx.x % TPR, head0 = work.head0, step = work.step;
-  if (head0 >= H) return;   // (warp-uniform, as is the loop: all lanes shuffle)
+  if (n_pass == 0) return;   // (warp-uniform, as is the loop: all lanes shuffle)
+  const int sub = (threadIdx.x & 31) / TPR, j = threadIdx.x % TPR;
   f2 w0[CE / 2], w1[CE / 2];
   if (!kCopy && normed) lane_weights<CE, TPR>(s_w, j, w0, w1);
-  const T *src = row_ptr<const T>(x, tok, head0 + sub);
-  T *dst = row_ptr<T>(y, tok, head0 + sub);
-  const int64_t in_step = step * x.head_stride, out_step = step * y.head_stride;
-  uint4 nxt[kAhead][2];
+  T *dst = row_ptr<T>(y, tok, work.head0 + sub);
+  const int64_t out_step = work.step * y.head_stride;
+  int h = work.head0 + sub;
+#pragma unroll 2
+  for (int i = 0; i < n_pass; ++i, h += work.step, dst += out_step) {
+    uint4 cur[1][2];
+    stream.take(cur);
+    if (!kCopy) {
+      f2 f0[CE / 2], f1[CE / 2];
+      unpack<T>(cur[0][0], f0);
+      unpack<T>(cur[0][1], f1);
+      if (normed) {
+        const float r = rsqrtf(row_sum<TPR>(dot<CE>(f0, f0, f1, f1)) * a.inv_d + a.eps);
+        const f2 rr = pk(r, r);
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u, src += in_step) load_row(nxt[u], src, l, l.live && head0 + u * step + sub < H);
-  for (int h0 = head0; h0 < H; h0 += kAhead * step) {
-    uint4 cur[kAhead][2];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) { cur[u][0] = nxt[u][0]; cur[u][1] = nxt[u][1]; }
-    if (h0 + kAhead * step < H)
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u, src += in_step)
-        load_row(nxt[u], src, l, l.live && h0 + (kAhead + u) * step + sub < H);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (!kCopy) {
-        f2 f0[CE / 2], f1[CE / 2];
-        unpack<T>(cur[u][0], f0);
-        unpack<T>(cur[u][1], f1);
-        if (normed) {
-          const float r = rsqrtf(row_sum<TPR>(dot<CE>(f0, f0, f1, f1)) * a.inv_d + a.eps);
-          const f2 rr = pk(r, r);
-#pragma unroll
-          for (int i = 0; i < CE / 2; ++i) { f0[i] = mul(f0[i], mul(rr, w0[i])); f1[i] = mul(f1[i], mul(rr, w1[i])); }
-        }
-        rotate<CE, kAdjacent, false>(f0, f1, ang);
-        cur[u][0] = pack<T>(f0);
-        cur[u][1] = pack<T>(f1);
+        for (int e = 0; e < CE / 2; ++e) { f0[e] = mul(f0[e], mul(rr, w0[e])); f1[e] = mul(f1[e], mul(rr, w1[e])); }
       }
-      store_row(dst, l, l.live && h0 + u * step + sub < H, cur[u][0], cur[u][1]);
-      dst += out_step;
+      rotate<CE, kAdjacent, false>(f0, f1, ang);
+      cur[0][0] = pack<T>(f0);
+      cur[0][1] = pack<T>(f1);
     }
+    store_row(dst, l, l.live && h < H, cur[0][0], cur[0][1]);
   }
 }
 
 template <class T, int TPR, bool kAdjacent>
-__global__ void __launch_bounds__(kRowThreads, 2) norm_rope_kernel(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__(kRowThreads, kFwdBlocks) norm_rope_kernel(const __grid_constant__ RowArgs a) {
   constexpr int CE = Elem<T>::kChunk;
   __shared__ Tables<CE, TPR> tables;
+  __shared__ uint4 s_ring[kRowWarps][RowStream<T, TPR, 1>::kDepth * 64];
   pdl_trigger();
-  fill_tables<CE, TPR>(a, tables);
   const WarpWork<TPR> work(a);
   const LaneChunks l = lane_chunks<CE>(a, threadIdx.x % TPR);
+  RowStream<T, TPR, 1> stream(a, work, l, s_ring[threadIdx.x >> 5], 0, 2);
+  stream.start();
+  fill_tables<CE, TPR>(a, tables);
   for (int64_t tok = work.first; tok < a.n_tok; tok += work.stride) {
     Angles<CE, kAdjacent> ang;
     token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l.rot, ang);
-    forward_side<T, TPR, kAdjacent, false>(a, a.x[0], a.y[0], a.Hq, a.norm & 1, tables.w[0], ang, (int)tok, work, l);
-    forward_side<T, TPR, kAdjacent, false>(a, a.x[1], a.y[1], a.Hkv, (a.norm >> 1) & 1, tables.w[1], ang, (int)tok, work, l);
-    forward_side<T, TPR, kAdjacent, true>(a, a.x[2], a.y[2], a.Hv, false, tables.w[0], ang, (int)tok, work, l);
+    forward_side<T, TPR, kAdjacent, false>(a, a.y[0], a.Hq, stream.n_pass[0], a.norm & 1, tables.w[0], ang, tok, work, l, stream);
+    forward_side<T, TPR, kAdjacent, false>(a, a.y[1], a.Hkv, stream.n_pass[1], (a.norm >> 1) & 1, tables.w[1], ang, tok, work, l, stream);
+    forward_side<T, TPR, kAdjacent, true>(a, a.y[2], a.Hv, stream.n_pass[2], false, tables.w[0], ang, tok, work, l, stream);
   }
 }
 
@@ -382,8 +470,10 @@ __global__ void __launch_bounds__(kRowThreads) norm_rope_few_kernel(const __grid
     load_row(nxt, row_ptr<const T>(side == 0 ? a.x[0] : side == 1 ? a.x[1] : a.x[2], tok, on ? head_of(r, side) : 0), l, on);
   };
   fetch(sub);
-  for (int p = threadIdx.x; p < a.rope.rot_dim / 2; p += kRowThreads)
-    s_cs[((p % CE >> 1) * TPR + p / CE) * 2 + (p & 1)] = pair_angle(a, __ldg(&a.pos[(size_t)a.rope.axis[p] * a.n_tok + tok]), a.rope.turn[p]);
+  for (int p = threadIdx.x; p < table_pairs<kAdjacent>(a); p += kRowThreads)
+    s_cs[pair_slot<CE, TPR, kAdjacent>(a, p)] =
+        p < a.rope.rot_dim / 2 ? pair_angle(a, __ldg(&a.pos[(size_t)a.rope.axis[p] * a.n_tok + tok]), a.rope.turn[p])
+                               : make_float2(1.f, 0.f);
   if (a.norm) fill_weights<CE, TPR>(a, s_w);
   __syncthreads();
   Angles<CE, kAdjacent> ang;
@@ -597,10 +687,15 @@ static RowArgs row_args(const spkv_qk_norm_t *n, const spkv_rope_t *rope, int n_
   return a;
 }
 
+// SMs of the current device, asked for once per device.
 static int device_sms(int *sms) {
+  static std::atomic<int> known[64];
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return SPKV_E_CUDA;
-  return check_stream_error(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return SPKV_E_CUDA;
+  if (dev < 64 && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return SPKV_OK;
+  if (cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return SPKV_E_CUDA;
+  if (dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
+  return SPKV_OK;
 }
 
 // Warps per token, and blocks: one warp per token once that fills the GPU, more of them for fewer tokens.
