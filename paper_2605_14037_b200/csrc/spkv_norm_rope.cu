@@ -323,7 +323,7 @@ template <int TPR> struct WarpWork {
 // registers left memory waiting: 40 us for 8192 tokens of 32/8 heads; see the figures at the head).
 template <class T, int TPR, int kStreams>
 struct RowStream {
-  static constexpr int kDepth = 4;
+  static constexpr int kDepth = 4 / kStreams;
   const RowArgs &a;
   const WarpWork<TPR> &work;
   const LaneChunks &l;
@@ -510,62 +510,49 @@ __global__ void __launch_bounds__(kRowThreads) norm_rope_few_kernel(const __grid
 
 // One side's heads of a warp's token, backward: dx rows out, this lane's columns of g u added to dw.
 template <class T, int TPR, bool kAdjacent, bool kCopy>
-__device__ inline void backward_side(const RowArgs &a, const spkv_rows_t &x, const spkv_rows_t &g, const spkv_rows_t &y,
-                                     int H, bool normed, const float *s_w, const Angles<Elem<T>::kChunk, kAdjacent> &ang,
-                                     int tok, const WarpWork<TPR> &work, const LaneChunks &l,
-                                     f2 (&dw0)[Elem<T>::kChunk / 2], f2 (&dw1)[Elem<T>::kChunk / 2]) {
+__device__ inline void backward_side(const RowArgs &a, const spkv_rows_t &y, int H, int n_pass, bool normed, const float *s_w,
+                                     const Angles<Elem<T>::kChunk, kAdjacent> &ang, int64_t tok, const WarpWork<TPR> &work,
+                                     const LaneChunks &l, RowStream<T, TPR, 2> &stream, f2 (&dw0)[Elem<T>::kChunk / 2],
+                                     f2 (&dw1)[Elem<T>::kChunk / 2]) {
   constexpr int CE = Elem<T>::kChunk;
-  const int sub = (threadIdx.x & 31) / TPR, j = threadIdx.x % TPR, head0 = work.head0, step = work.step;
-  if (head0 >= H) return;
-  const T *gp = row_ptr<const T>(g, tok, head0 + sub);
-  const T *xp = normed ? row_ptr<const T>(x, tok, head0 + sub) : nullptr;
-  T *dst = row_ptr<T>(y, tok, head0 + sub);
-  const int64_t g_step = step * g.head_stride, x_step = normed ? step * x.head_stride : 0, y_step = step * y.head_stride;
-  uint4 gn[2], xn[2];
-  load_row(gn, gp, l, l.live && head0 + sub < H);
-  load_row(xn, xp, l, normed && l.live && head0 + sub < H);
-  for (int h = head0; h < H; h += step) {
-    uint4 gc[2] = {gn[0], gn[1]};
-    const uint4 xc[2] = {xn[0], xn[1]};
-    const bool on = l.live && h + sub < H;
-    gp += g_step;
-    xp += x_step;
-    if (h + step < H) {
-      const bool more = l.live && h + step + sub < H;
-      load_row(gn, gp, l, more);
-      load_row(xn, xp, l, normed && more);
-    }
+  if (n_pass == 0) return;
+  const int sub = (threadIdx.x & 31) / TPR, j = threadIdx.x % TPR;
+  T *dst = row_ptr<T>(y, tok, work.head0 + sub);
+  const int64_t out_step = work.step * y.head_stride;
+  int h = work.head0 + sub;
+  for (int i = 0; i < n_pass; ++i, h += work.step, dst += out_step) {
+    uint4 cur[2][2];   // upstream gradients, inputs
+    stream.take(cur);
     if (!kCopy) {
       f2 f0[CE / 2], f1[CE / 2];
-      unpack<T>(gc[0], f0);
-      unpack<T>(gc[1], f1);
+      unpack<T>(cur[0][0], f0);
+      unpack<T>(cur[0][1], f1);
       rotate<CE, kAdjacent, true>(f0, f1, ang);
       if (normed) {
         f2 u0[CE / 2], u1[CE / 2], w0[CE / 2], w1[CE / 2];
-        unpack<T>(xc[0], u0);
-        unpack<T>(xc[1], u1);
+        unpack<T>(cur[1][0], u0);
+        unpack<T>(cur[1][1], u1);
         lane_weights<CE, TPR>(s_w, j, w0, w1);
         const float r = rsqrtf(row_sum<TPR>(dot<CE>(u0, u0, u1, u1)) * a.inv_d + a.eps);
         const f2 rr = pk(r, r);
 #pragma unroll
-        for (int i = 0; i < CE / 2; ++i) {
-          u0[i] = mul(u0[i], rr);
-          u1[i] = mul(u1[i], rr);
-          dw0[i] = fma(f0[i], u0[i], dw0[i]);
-          dw1[i] = fma(f1[i], u1[i], dw1[i]);
-          f0[i] = mul(f0[i], w0[i]);
-          f1[i] = mul(f1[i], w1[i]);
+        for (int e = 0; e < CE / 2; ++e) {
+          u0[e] = mul(u0[e], rr);
+          u1[e] = mul(u1[e], rr);
+          dw0[e] = fma(f0[e], u0[e], dw0[e]);
+          dw1[e] = fma(f1[e], u1[e], dw1[e]);
+          f0[e] = mul(f0[e], w0[e]);
+          f1[e] = mul(f1[e], w1[e]);
         }
         const float m = -row_sum<TPR>(dot<CE>(f0, u0, f1, u1)) * a.inv_d;
         const f2 mean = pk(m, m);
 #pragma unroll
-        for (int i = 0; i < CE / 2; ++i) { f0[i] = mul(rr, fma(u0[i], mean, f0[i])); f1[i] = mul(rr, fma(u1[i], mean, f1[i])); }
+        for (int e = 0; e < CE / 2; ++e) { f0[e] = mul(rr, fma(u0[e], mean, f0[e])); f1[e] = mul(rr, fma(u1[e], mean, f1[e])); }
       }
-      gc[0] = pack<T>(f0);
-      gc[1] = pack<T>(f1);
+      cur[0][0] = pack<T>(f0);
+      cur[0][1] = pack<T>(f1);
     }
-    store_row(dst, l, on, gc[0], gc[1]);
-    dst += y_step;
+    store_row(dst, l, l.live && h < H, cur[0][0], cur[0][1]);
   }
 }
 
@@ -577,7 +564,10 @@ template <class T, int TPR, bool kAdjacent>
 __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(const __grid_constant__ RowArgs a) {
   constexpr int CE = Elem<T>::kChunk;
   __shared__ Tables<CE, TPR> tables;
-  __shared__ float s_dw[kRowWarps][2 * CE * TPR];
+  // rows on their way; at the end of a side its sums, [warp][2 CE * TPR]
+  __shared__ uint4 s_ring[kRowWarps][RowStream<T, TPR, 2>::kDepth * 128];
+  float *s_dw = reinterpret_cast<float *>(s_ring);
+  static_assert(sizeof(s_ring) >= kRowWarps * 2 * CE * TPR * 4, "room for the sums");
   pdl_trigger();
   fill_tables<CE, TPR>(a, tables);
   const WarpWork<TPR> work(a);
@@ -589,17 +579,21 @@ __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(cons
     f2 dw0[CE / 2], dw1[CE / 2];
 #pragma unroll
     for (int i = 0; i < CE / 2; ++i) dw0[i] = dw1[i] = pk(0.f, 0.f);
-    if (H > 0)
+    RowStream<T, TPR, 2> stream(a, work, l, s_ring[warp], side, 2 * side);
+    if (stream.any()) {
+      stream.start();
       for (int64_t tok = work.first; tok < a.n_tok; tok += work.stride) {
         Angles<CE, kAdjacent> ang;
         token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l.rot, ang);
-        backward_side<T, TPR, kAdjacent, false>(a, a.x[side], a.g[side], a.y[side], H, (a.norm >> side) & 1, tables.w[side],
-                                                ang, (int)tok, work, l, dw0, dw1);
+        backward_side<T, TPR, kAdjacent, false>(a, a.y[side], H, stream.n_pass[side], (a.norm >> side) & 1, tables.w[side], ang,
+                                                tok, work, l, stream, dw0, dw1);
         if (side == 1)
-          backward_side<T, TPR, kAdjacent, true>(a, a.x[2], a.g[2], a.y[2], a.Hv, false, tables.w[0], ang, (int)tok, work, l,
+          backward_side<T, TPR, kAdjacent, true>(a, a.y[2], a.Hv, stream.n_pass[2], false, tables.w[0], ang, tok, work, l, stream,
                                                  dw0, dw1);
       }
+    }
     if (!a.part) continue;
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < CE; ++i) {
       float2 v = up(i < CE / 2 ? dw0[i % (CE / 2)] : dw1[i % (CE / 2)]);
@@ -609,8 +603,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(cons
         v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
       }
       if (lane < TPR) {
-        s_dw[warp][(2 * i) * TPR + j] = v.x;
-        s_dw[warp][(2 * i + 1) * TPR + j] = v.y;
+        s_dw[(warp * 2 * CE + 2 * i) * TPR + j] = v.x;
+        s_dw[(warp * 2 * CE + 2 * i + 1) * TPR + j] = v.y;
       }
     }
     __syncthreads();
@@ -619,7 +613,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(cons
       const LaneChunks ll = lane_chunks<CE>(a, jj);
       float v = 0.f;
 #pragma unroll
-      for (int w = 0; w < kRowWarps; ++w) v += s_dw[w][e * TPR + jj];
+      for (int w = 0; w < kRowWarps; ++w) v += s_dw[(w * 2 * CE + e) * TPR + jj];
       if (ll.live) a.part[((size_t)blockIdx.x * 2 + side) * a.D + (e < CE ? ll.c0 + e : ll.c1 + e - CE)] = v;
     }
     __syncthreads();
