@@ -147,7 +147,8 @@ __global__ void __launch_bounds__(256) share_cut_kernel(CacheView c, const int32
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    const int n_tail = max(1, min((s_longest + kTailPages - 1) / kTailPages, kMaxTailItems / (B * c.Hkv)));
+    const int units = B * c.Hkv;
+    const int n_tail = max(1, min(max((s_longest + kTailPages - 1) / kTailPages, max_blocks / units), kMaxTailItems / units));
     int at = 0;
     for (int h = 0; h < c.Hkv; ++h) {
       int32_t *hd = share_head(rec, h);

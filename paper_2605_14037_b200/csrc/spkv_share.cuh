@@ -20,9 +20,9 @@ constexpr int kSharePlanHdr = 8, kShareHdr = 4, kShareHead = 8, kShareDesc = 8;
 constexpr int kShareRows = 256;       // query rows per block: two slots of 128
 constexpr int kMinSharedPages = 1;    // fewer common pages than this are read per sequence
 constexpr int kMinSharePages = 4;     // a share is not cut shorter
-constexpr int kTailPages = 8;         // a unit's own pages are cut into shares of about this many
-constexpr int kTailMinPages = 4;     // ... and no piece is shorter than half of that
-constexpr int kMaxTailItems = 1024;   // ... while there are no more shares than this
+constexpr int kTailPages = 8;         // a unit's own pages are cut into pieces of about this many, more while SMs are left
+constexpr int kTailMinPages = 2;      // ... not into shorter ones than this
+constexpr int kMaxTailItems = 1024;   // ... and not into more pieces than this, all units together
 
 __host__ __device__ inline int share_row_tiles(int B, int G) { return (B * G + kShareRows - 1) / kShareRows; }
 // blocks a layer's record has room for, whatever the batch (B * Hkv <= 1024, B <= max_seqs)
