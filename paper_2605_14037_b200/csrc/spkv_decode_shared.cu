@@ -819,7 +819,7 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
       cudaSuccess)
     return SPKV_E_CUDA;
   // up to 40 parts in one round of loads; few rows: eight warps each (8 sequences of 64 heads: 20.4 -> 19.2 us a call),
-  // many: four, so that all rows are on the GPU at once (64 sequences of 32 heads: 43 against 45 us)
+  // many: two, so that all rows are on the GPU at once (64 sequences of 32 heads: 42 against 45 us)
   if (B * v.Hq <= 8 * sms) return check_stream_error(launch_overlapped(shared_merge_kernel<8, 5>, dim3(B * v.Hq), dim3(256), 0, s, a));
-  return check_stream_error(launch_overlapped(shared_merge_kernel<4, 8>, dim3(B * v.Hq), dim3(128), 0, s, a));
+  return check_stream_error(launch_overlapped(shared_merge_kernel<2, 10>, dim3(B * v.Hq), dim3(64), 0, s, a));
 }
