@@ -197,8 +197,8 @@ int spkv_cache_attach(const spkv_config_t *cfg, void *d_arena, size_t arena_byte
 
 /* Checkpoint / rollback of a live cache without copying its pool: saves (restores) the metadata
  * and the ring pages -- everything appends and prefill chunks change IN PLACE; the pairs they add
- * to the pool land behind the saved lengths and are simply forgotten by a rollback.  Valid as long
- * as no spkv_cache_reset_seq came between the two (it hands pages to other units).  Use: replaying
+ * to the pool land behind the saved lengths and are simply forgotten by a rollback, as is a fork.  Valid as
+ * long as no spkv_cache_reset_seq came between the two (it hands pages to other units).  Use: replaying
  * the same decode steps (benchmark repeats, speculative tokens that were rejected).
  *   d_buf: device, >= spkv_cache_checkpoint_bytes(cache) bytes.  Asynchronous on `stream`; a full
  *   synchronisation point for SPKV_FLAG_OVERLAP. */
@@ -437,7 +437,7 @@ int spkv_decode_attention_static(spkv_cache_t *cache, int32_t layer, const int32
  * The attention call checks each unit against the page tables as they are: where a unit no longer
  * starts with the plan's pages (a sequence was reset, rolled back or replaced) that unit is read in
  * full, as is everything when the plan was made for another B -- a stale plan costs time, never the
- * result.  After sequences changed, make a new one.
+ * result (so does one of another cache).  After sequences changed, make a new one.
  *   d_plan: spkv_share_plan_bytes(cfg) bytes of device memory, 16-byte aligned, filled by spkv_share_plan
  *   and otherwise left alone (the attention call only reads it: several calls and graphs may share it). */
 size_t spkv_share_plan_bytes(const spkv_config_t *cfg);
@@ -445,10 +445,9 @@ int spkv_share_plan(spkv_cache_t *cache, const int32_t *d_seq_ids, int32_t B, vo
                     spkv_stream_t stream);
 
 /* Arguments as spkv_decode_attention.  d_workspace: >= spkv_decode_shared_workspace_bytes(cfg, B) bytes, 256-byte
- * aligned, used by this entry point of this cache only, zero-filled once before its first use; calls
- * that share it must not overlap on the GPU.  Always ordered after everything earlier on `stream`, also under
+ * aligned, whatever it holds; calls that share it must not overlap on the GPU.  Always ordered after everything earlier on `stream`, also under
  * SPKV_FLAG_OVERLAP.  Weights times values as in spkv_prefill for the shared pages (SPKV_FLAG_PREFILL_PV_BF16
- * included), sm_scale positive and finite. */
+ * included), sm_scale positive and finite, B * n_kv_heads <= 1024 as in every decode call. */
 size_t spkv_decode_shared_workspace_bytes(const spkv_config_t *cfg, int32_t B);
 int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B,
                                  const void *d_q, void *d_out, float *d_lse_opt, float sm_scale, const void *d_plan,

@@ -199,6 +199,8 @@ static int make_handle(const spkv_config_t *cfg, void *d_arena, const Layout &l,
     for (int l2 = 0; l2 < cfg->n_layers; ++l2)
       for (int h = 0; h < cfg->n_kv_heads; ++h)
         if (cfg->h_local_only[l2 * cfg->n_kv_heads + h]) c->local_mask[l2] |= 1ULL << h;
+  const uint64_t h = layout_hash(cfg);
+  c->share_salt = (uint32_t)(h ^ (h >> 32));
   c->cfg.h_local_only = nullptr;   // the caller's array is read during this call only
   c->host_ready = false;
   c->stack_ready = false;

@@ -781,7 +781,7 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   a.c = v; a.layer = layer; a.B = B; a.n_items = B * v.Hkv;
   a.n_tiles = share_row_tiles(B, v.G);
   a.rows_per_block = w.rows;
-  a.sig = share_signature(v, B);
+  a.sig = share_signature(cache, B);
   a.g_inv = ((1ULL << 32) + v.G - 1) / v.G;
   a.seq_ids = d_seq_ids;
   a.q = static_cast<const __nv_bfloat16 *>(d_q);

@@ -229,6 +229,6 @@ extern "C" int spkv_share_plan(spkv_cache_t *cache, const int32_t *d_seq_ids, in
   int32_t *plan = static_cast<int32_t *>(d_plan);
   share_common_kernel<<<v.L * v.Hkv, 128, 0, as_stream(stream)>>>(v, d_seq_ids, B, plan);
   share_cut_kernel<<<v.L, 256, 0, as_stream(stream)>>>(v, d_seq_ids, B, share_row_tiles(B, v.G),
-                                                       std::min(kMaxGrid, cache->sm_count), share_signature(v, B), plan);
+                                                       std::min(kMaxGrid, cache->sm_count), share_signature(cache, B), plan);
   return check_stream_error(cudaGetLastError());
 }

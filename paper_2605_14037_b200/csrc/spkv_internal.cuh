@@ -282,6 +282,7 @@ struct spkv_cache {
   int last_decode_items;    // units of the previous decode launch (the workspace halves depend on it)
   void *last_decode_ws;     // and its workspace
   int *appends_pending;     // [n_layers] appends since the layer's last decode launch
+  uint32_t share_salt;      // layout hash folded to 32 bits: what a share plan has to agree on with the cache
   unsigned long long *local_mask;   // [n_layers] bit h set: KV head h of the layer was declared local-only
   // spkv_decode_step_host: copy streams and events of its two-slot pipeline (made on first use)
   cudaStream_t copy_in, copy_out;

@@ -42,9 +42,10 @@ template <class I> __host__ __device__ inline I *share_head(I *rec, int h) { ret
 template <class I> __host__ __device__ inline I *share_desc(const CacheView &c, I *rec, int block) {
   return rec + kShareHdr + kShareHead * c.Hkv + kShareDesc * (size_t)block;
 }
-// what a plan must agree on with a call (never 0: a zero-filled buffer is no plan)
-__host__ __device__ inline int share_signature(const CacheView &c, int B) {
-  return (int)((((unsigned)B * 2654435761u + (unsigned)c.L) * 2246822519u + (unsigned)c.Hkv * 4099u + (unsigned)c.G) | 1u);
+// What a plan must agree on with a call: the batch size and the cache's layout, which fixes where units and page tables
+// lie (never 0: a zero-filled buffer is no plan).
+inline int share_signature(const spkv_cache *cache, int B) {
+  return (int)(((uint32_t)B * 2654435761u ^ cache->share_salt) | 1u);
 }
 
 }  // namespace spkv

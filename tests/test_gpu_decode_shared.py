@@ -348,3 +348,124 @@ def test_refusals():
     o, lse = cache.spkv_decode_attention_shared(0, bad, qd, plan, want_lse=True)
     assert cache.spkv_status() == -9
     assert (o[1] == 0).all() and (lse[1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("B,Hq", [(2, 8), (33, 32)])
+def test_long_shares(B, Hq):
+    """More pages per block than the page-table entries a warp holds at once (32): 8 dense heads of 47000 tokens
+    are 5900 pages, 40 and more per block; one and two slots of query rows."""
+    spkv = load()
+    cache = make(spkv, n_seqs=B + 1, Hq=Hq, Hkv=8, pool=8 * 740 + B * 8 * 4, max_context=48000)
+    wl = Workload(21, 47000, 1, Hq, 8, (1.0,) * 8, cache.spkv_tau_logit(), with_q=False)
+    feed(cache, wl, 0, 0, 0, 0, 47000, 8192)
+    cache.spkv_seq_fork(0, range(1, B + 1))
+    ids = torch.arange(1, B + 1, dtype=torch.int32, device=dev())
+    plan = cache.spkv_share_plan(ids)
+    rec = plan.cpu().numpy().view(np.int32)[8:]
+    assert rec[0] > 32 and rec[1] <= 256
+    q = synth.normal_bf16(np.random.default_rng(3), (B, Hq, D))
+    out, lse = cache.spkv_decode_attention_shared(0, ids, to_dev_bf16(q), plan, want_lse=True)
+    cache.check()
+    for b in {0, B // 2, B - 1}:
+        check(cache, 0, [b + 1], q[b:b + 1], out[b:b + 1], lse[b:b + 1])
+
+
+@pytest.mark.parametrize("planned", [True, False])
+def test_long_pieces_of_a_sequences_own(planned):
+    """Sequences that share nothing and are long: with a plan their pages go in pieces, without one a block walks
+    all 300 of a unit."""
+    spkv = load()
+    cache = make(spkv, n_seqs=2, Hq=4, Hkv=2, pool=1300, max_context=20000, flags=0)
+    wl = Workload(22, 19000, 2, 4, 2, (1.0, 0.3), cache.spkv_tau_logit(), with_q=False)
+    for j in range(2):
+        feed(cache, wl, 0, j, j, 0, 19000, 8192)
+    ids = torch.arange(2, dtype=torch.int32, device=dev())
+    plan = cache.spkv_share_plan(ids)
+    if not planned:
+        plan.zero_()
+    q = synth.normal_bf16(np.random.default_rng(4), (2, 4, D))
+    out, lse = cache.spkv_decode_attention_shared(0, ids, to_dev_bf16(q), plan, want_lse=True)
+    cache.check()
+    check(cache, 0, [0, 1], q, out, lse)
+
+
+@pytest.mark.parametrize("w", [1, 64, 65, 200])
+@pytest.mark.parametrize("sinks", [0, 5])
+def test_windows_and_sinks(w, sinks):
+    spkv = load()
+    cache, wl, ids = build(spkv, 4, 8, 2, 1000, 30, (0.4, 1.0), w=w, sink_tokens=sinks)
+    q, qd = queries(wl)
+    out, lse = cache.spkv_decode_attention_shared(0, ids, qd, cache.spkv_share_plan(ids), want_lse=True)
+    cache.check()
+    check(cache, 0, range(1, 5), q, out, lse)
+
+
+def test_two_term_product_with_alternating_slots():
+    """Values past 2^20 with at most 128 query rows: both slots of a block hold the same rows."""
+    spkv = load()
+    cache, wl, ids = build(spkv, 3, 8, 2, 1500, 30, (0.5, 1.0), gain=2.0 ** 21)
+    q, qd = queries(wl)
+    out, lse = cache.spkv_decode_attention_shared(0, ids, qd, cache.spkv_share_plan(ids), want_lse=True)
+    cache.check()
+    check(cache, 0, range(1, 4), q, out, lse)
+
+
+def test_a_plan_of_another_cache():
+    """Another layout's plan (heads without page tables) does not fit; the same layout's is checked like a stale one."""
+    spkv = load()
+    a, wl, ids = build(spkv, 3, 8, 2, 1500, 5, (0.5, 1.0), pool=300)
+    b, _, _ = build(spkv, 3, 8, 2, 1500, 5, (0.5, 1.0), pool=300, local_only=[[1, 0]])
+    c = make(spkv, n_seqs=4, Hq=8, Hkv=2, pool=300, max_context=1569)
+    for j in range(3):
+        feed(c, wl, 0, j + 1, j, 0, 900)
+    q, qd = queries(wl)
+    for cache in (b, c):
+        out, lse = cache.spkv_decode_attention_shared(0, ids, qd, a.spkv_share_plan(ids), want_lse=True)
+        cache.check()
+        check(cache, 0, range(1, 4), q, out, lse)
+
+
+def test_two_streams_in_turn():
+    """Calls on two streams, ordered by events, on one cache and workspace."""
+    spkv = load()
+    cache, wl, ids = build(spkv, 6, 8, 2, 1200, 20, (0.5, 1.0))
+    plan = cache.spkv_share_plan(ids)
+    q, qd = queries(wl)
+    want = cache.spkv_decode_attention_shared(0, ids, qd, plan)
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = []
+    for i in range(6):
+        with torch.cuda.stream(s[i & 1]):
+            s[i & 1].wait_stream(s[1 - (i & 1)])
+            outs.append(cache.spkv_decode_attention_shared(0, ids, qd, plan))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    cache.check()
+
+
+def test_output_over_the_queries():
+    spkv = load()
+    cache, wl, ids = build(spkv, 6, 8, 2, 1200, 20, (0.5, 1.0))
+    plan = cache.spkv_share_plan(ids)
+    _, qd = queries(wl)
+    want = cache.spkv_decode_attention_shared(0, ids, qd, plan)
+    buf = qd.clone()
+    cache.spkv_decode_attention_shared(0, ids, buf, plan, out=buf)
+    assert torch.equal(buf, want)
+    cache.check()
+
+
+def test_binding_refusals():
+    spkv = load()
+    cache, wl, ids = build(spkv, 2, 4, 2, 300, 1, (0.5, 1.0))
+    _, qd = queries(wl)
+    plan = cache.spkv_share_plan(ids)
+    for args in ((0, ids.long(), qd, plan), (0, ids, qd[:1], plan), (0, ids, qd.float(), plan), (0, ids[:1], qd, plan),
+                 (0, ids, qd.transpose(0, 1).contiguous().transpose(0, 1), plan), (0, ids, qd, plan.view(torch.int32)),
+                 (0, ids.cpu(), qd, plan), (0, ids, qd.cpu(), plan)):
+        with pytest.raises(ValueError):
+            cache.spkv_decode_attention_shared(*args)
+    for kw in (dict(out=torch.empty_like(qd)[:1]), dict(lse=torch.empty((2, 4), device=dev(), dtype=torch.float64))):
+        with pytest.raises(ValueError):
+            cache.spkv_decode_attention_shared(0, ids, qd, plan, **kw)

@@ -137,6 +137,10 @@ CASES = [
     dict(n=5000, hq=8, hkv=2, norm=False), dict(n=30, hq=4, hkv=2, norm="q", wdtype="f32"),
     dict(n=30, hq=4, hkv=2, norm="k", weights=False, scale=1.25), dict(n=30, hq=4, hkv=2, rot=0),
     dict(n=77, hq=4, hkv=2, D=96, rot=96, dtype="f32", wdtype="bf16"), dict(n=9, hq=64, hkv=8, dtype="f16", rot=16),
+    # from a block per token to a warp per token: eight, four, two warps a token, with and without heads for each
+    dict(n=297, hq=3, hkv=1), dict(n=500, hq=40, hkv=5, interleaved=True, rot=64), dict(n=900, hq=17, hkv=2, dtype="f16", D=64),
+    dict(n=2400, hq=5, hkv=3, D=32, dtype="f32"), dict(n=310, hq=2, hkv=2, D=240, rot=48, axes=2, interleaved=True),
+    dict(n=1, hq=6, hkv=2, D=176, rot=96, interleaved=True, dtype="f16"),
 ]
 
 
