@@ -57,7 +57,7 @@ __host__ __device__ constexpr int off_k(bool alt) { return alt ? 32768 : 65536; 
 __host__ __device__ constexpr int off_v(bool alt) { return off_k(alt) + ring(alt) * kBlockBytes; }
 __host__ __device__ constexpr int off_bar(bool alt) { return off_v(alt) + ring(alt) * kBlockBytes; }
 __host__ __device__ constexpr int smem_bytes(bool alt) { return off_bar(alt) + 512; }
-constexpr int kJoinStride = 132;   // floats per row of the hand-over between the slots (kAlt)
+constexpr int kRowStride = 132;   // floats per row of the results in shared memory
 }  // namespace shp
 
 struct SharedArgs {
@@ -390,10 +390,12 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
     const bool have = n_mine > 0;
     if (have && !failed && !mbar_wait_bounded(&bar[B_O_DONE + 2 * h + ((n_mine - 1) & 1)], 0)) failed = true;
     fence_after();
-    float *join = reinterpret_cast<float *>(smem + off_k(kAlt));   // kAlt: slot 1's rows, over the rings
-    if (kAlt) {
-      // slot 1 hands its rows over; every page has been consumed by both slots before that
-      asm volatile("bar.sync 1, 256;" ::: "memory");
+    // Both slots are through with Q, keys and values before their shared memory is written to.
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    float *stage = reinterpret_cast<float *>(smem);          // [row][132]: a row's O, and (m, l) of slot 1
+    float *mine = stage + (size_t)((kAlt ? 0 : h * 128) + row) * kRowStride;
+    float M = m_ref, f0 = o_scale, f1 = 0.f;
+    if (kAlt) {   // slot 1 hands its rows over
       if (h == 1) {
         if (have && live && !failed) {
 #pragma unroll
@@ -403,29 +405,25 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
             tmem_ld_wait();
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-              *reinterpret_cast<float4 *>(join + row * kJoinStride + q8 * 16 + 4 * x) =
+              *reinterpret_cast<float4 *>(mine + q8 * 16 + 4 * x) =
                   make_float4(t16[4 * x], t16[4 * x + 1], t16[4 * x + 2], t16[4 * x + 3]);
           }
         }
-        join[row * kJoinStride + 128] = have ? m_ref : -INFINITY;
-        join[row * kJoinStride + 129] = l;
+        mine[128] = have ? m_ref : -INFINITY;
+        mine[129] = l;
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
     }
-    const int r_out = (kAlt ? 0 : h * 128) + row;
     if (have && !failed && live && (!kAlt || h == 0)) {
-      float f0 = o_scale, f1 = 0.f, M = m_ref;
       l *= l_scale;
       if (kAlt) {
-        const float m1 = join[row * kJoinStride + 128], l1 = join[row * kJoinStride + 129];
+        const float m1 = mine[128], l1 = mine[129];
         M = fmaxf(m_ref, m1);
         const float w0 = part_weight(m_ref, l, M), w1 = part_weight(m1, l1, M);
         l = l * w0 + l1 * l_scale * w1;
         f0 = o_scale * w0;
         f1 = o_scale * w1;
       }
-      const size_t at = (size_t)blockIdx.x * a.rows_per_block + r_out;
-      const bool write = r_out < n_rows;
 #pragma unroll
       for (int q8 = 0; q8 < 8; ++q8) {
         float t16[16];
@@ -434,14 +432,24 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           float4 o = make_float4(t16[4 * x] * f0, t16[4 * x + 1] * f0, t16[4 * x + 2] * f0, t16[4 * x + 3] * f0);
+          float4 *at = reinterpret_cast<float4 *>(mine + q8 * 16 + 4 * x);
           if (kAlt && f1 != 0.f) {
-            const float4 p = *reinterpret_cast<const float4 *>(join + row * kJoinStride + q8 * 16 + 4 * x);
+            const float4 p = *at;
             o.x = fmaf(p.x, f1, o.x); o.y = fmaf(p.y, f1, o.y); o.z = fmaf(p.z, f1, o.z); o.w = fmaf(p.w, f1, o.w);
           }
-          if (write) *reinterpret_cast<float4 *>(a.part_o + at * kD + q8 * 16 + 4 * x) = o;
+          *at = o;
         }
       }
-      if (write) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(M, l);
+      // out row by row, 512 bytes at a time (a thread per row would write 32 rows' sixteenths at once: 19 MB of
+      // parts took 5 us to drain, and no tail block could start before)
+      __syncwarp();
+      const int r0 = (kAlt ? 0 : h * 128) + (row & ~31);
+      const size_t at = (size_t)blockIdx.x * a.rows_per_block + r0;
+#pragma unroll 4
+      for (int r = 0; r < min(32, n_rows - r0); ++r)
+        *reinterpret_cast<float4 *>(a.part_o + (at + r) * kD + lane * 4) =
+            *reinterpret_cast<const float4 *>(stage + (size_t)(r0 + r) * kRowStride + lane * 4);
+      if (r0 + lane < n_rows) *reinterpret_cast<float2 *>(a.part_ml + (at + lane) * 2) = make_float2(M, l);
     }
   }
   if (failed) set_status(c, SPKV_E_TIMEOUT);
