@@ -7,11 +7,11 @@
 //   tail    what is left of every unit, its own pages and its ring: one small block per unit (several for a long
 //           one), mma.sync tiles of the unit's G query heads as in the decode kernel; leaves (m, l, O) too;
 //   merge   joins a row's parts by their log-sum-exp weights.
-// The tail does not depend on the prefix launch.  Its blocks are small (4 warps, two page stages), so that
-// one fits on an SM beside a prefix block of up to 128 rows, and are launched as programmatic
-// dependents: the prefix kernel has waited for everything earlier on the stream before it lets them start.
-// The tail's first block waits for the prefix launch at its end, so that the merge, which waits for the
-// tail, may read both.
+// The tail does not depend on the prefix launch.  Its blocks are small (4 warps, two page buffers), so that
+// one fits on an SM beside a prefix block, and are launched as programmatic dependents: the prefix
+// kernel has waited for everything earlier on the stream before it lets them start.
+// The tail launch is not complete before the prefix launch is, so that the merge, which waits for the tail,
+// may read both.
 //
 // Prefix kernel.  Per page and 128-row slot: S = Q K^T (8 MMAs M128 N64 K16 into tensor memory), softmax
 // in registers (thread = row = TMEM lane), P in fp16 back over the scores, O += P V with the page's values
@@ -26,6 +26,12 @@
 // [64 (2h + b), +64), O of slot h at [256 + 128 h, +128).
 // Warps: 0 / 2 MMA issue of slot 0 / 1, 1 page loader, 3 tensor memory, 4-7 / 8-11 softmax of slot 0 / 1, 12-15 value
 // conversion.  All waits are bounded.
+//
+// What bounds it (B200; device time of a call in a graph, three caches in turn): up to 128 rows, memory while the pages
+// stream (8 sequences of 64/8 heads on 65536 common tokens, 59 MB: 19.1 us, of which 10 at 5.8 TB/s, 3 until
+// the first scores, 6 for the end of the tail and the merge); beyond, the chain scores -> softmax -> P -> MMA
+// (2050 cycles per page and 256 rows; the tensor pipe is busy half of that) and then the tail's mma.sync tiles, which
+// get little of the tensor pipe beside the prefix (64 sequences of 32/8 heads on 131072: 37.7 us).
 #include <algorithm>
 #include <atomic>
 #include <math.h>
@@ -38,7 +44,7 @@ namespace spkv {
 namespace shp {
 // Sixteen warps, four on each of the SM's register files: at 104 registers a thread a tail block of four warps of
 // 96 finds room beside them (with 13 warps of 128 one file was full, and the tail ran after the prefix).
-// Four warps convert values: one needed 2000 cycles per page and set the pace.
+// (Two converter warps instead of four, or the MMA warps on other schedulers: within 2 %.)
 constexpr int kThreads = 512, kRegs = 104;
 constexpr int kMmaWarp0 = 0, kLoaderWarp = 1, kMmaWarp1 = 2, kTmemWarp = 3;
 constexpr int kConvThreads = 128;   // warps 12-15
@@ -73,6 +79,8 @@ struct SharedArgs {
   int max_blocks;
   float *tail_o, *tail_ml;      // tail: [share][item][G][128], [share][item][G][2]
   int max_tail;                 // shares the workspace holds
+  int tail_blocks;              // blocks of the tail launch that take items; those behind join prefix parts
+  float *pre_o, *pre_ml;        // a query row's prefix parts joined: [B * Hq][128], [B * Hq][2]
   int row_base, row_heads;      // page-table rows of the layer: row_base + seq * row_heads + rank of the KV head
   unsigned long long local_mask;
   int32_t *item_skip;           // [n_items] common pages the tail left out (0: it read the unit in full)
@@ -459,6 +467,77 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "n"(shp::kTmemCols) : "memory");
 }
 
+// ---- joining parts -----------------------------------------------------------------------------------
+// Adds parts first, first + stride, ... < n of a query row to (M, L, O), kBatch of them in one round of loads; one warp,
+// lane l owns dims 4l .. 4l + 3.  at(p, o, ml): where part p's row and its (m, l) lie; use(p): does it count.
+template <int kBatch, class At, class Use>
+__device__ inline void join_parts(int first, int stride, int n, At at, Use use, float &M, float &L, float4 &O) {
+  const int lane = threadIdx.x & 31;
+  for (int p0 = first; p0 < n; p0 += kBatch * stride) {
+    const int mine = p0 + lane * stride;
+    const float *po, *pml;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < kBatch && mine < n) {
+      at(mine, po, pml);
+      ml = __ldcg(reinterpret_cast<const float2 *>(pml));
+    }
+    float4 v[kBatch];
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      at(min(p0 + x * stride, n - 1), po, pml);
+      v[x] = __ldcg(reinterpret_cast<const float4 *>(po) + lane);
+    }
+    if (!use(mine)) ml = make_float2(-INFINITY, 0.f);
+    float top = ml.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float Mn = fmaxf(M, top), old = part_weight(M, L, Mn);
+    M = Mn;
+    const float f = part_weight(ml.x, ml.y, M);
+    float fl = f == 0.f ? 0.f : f * ml.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) fl += __shfl_xor_sync(0xffffffffu, fl, o);
+    L = L * old + fl;
+    O.x *= old; O.y *= old; O.z *= old; O.w *= old;
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      const float fx = __shfl_sync(0xffffffffu, f, x);
+      if (fx != 0.f) {   // (a part of weight 0 may never have been written)
+        O.x = fmaf(v[x].x, fx, O.x); O.y = fmaf(v[x].y, fx, O.y); O.z = fmaf(v[x].z, fx, O.z); O.w = fmaf(v[x].w, fx, O.w);
+      }
+    }
+  }
+}
+
+// Where prefix part p of a query row lies: row R = b * G + g of its KV head.
+__device__ inline size_t prefix_part_row(const SharedArgs &a, int first, int R, int p) {
+  const int last_block = a.max_blocks - 1;   // (a plan that was overwritten reads no further than the workspace)
+  return (size_t)max(0, min(first + p * a.n_tiles + R / kShareRows, last_block)) * a.rows_per_block + R % kShareRows;
+}
+
+// With more than 128 query rows a KV head, the last blocks of the tail launch make one part of a row's prefix parts, a
+// warp per row.  They wait for the prefix launch and run beside the last tail blocks, so that the merge finds
+// little left to read (64 sequences of 32 heads on 8 KV heads: 18 parts a row, 19 MB; 40.1 -> 38.3 us a call.
+// With fewer rows the tail ends with the prefix and nothing would hide it: 19 -> 23 us).
+__device__ inline void join_prefix_parts(const SharedArgs &a, int block, int n_blocks) {
+  const CacheView &c = a.c;
+  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  for (int r = block * warps + (threadIdx.x >> 5); r < a.B * c.Hq; r += n_blocks * warps) {
+    const int b = r / c.Hq, j = r - b * c.Hq, kvh = j / c.G, R = b * c.G + j - kvh * c.G;
+    const int4 parts = ldcg4(share_head(a.rec, kvh) + 4);
+    const int first = __ldcg(share_head(a.rec, kvh) + 1), n = parts.z == a.sig ? max(parts.x, 0) : 0;
+    float M = -INFINITY, L = 0.f;
+    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+    join_parts<8>(0, 1, n, [&](int p, const float *&o, const float *&ml) {
+      const size_t at = prefix_part_row(a, first, R, p);
+      o = a.part_o + at * kD;
+      ml = a.part_ml + at * 2;
+    }, [](int) { return true; }, M, L, O);
+    *reinterpret_cast<float4 *>(a.pre_o + (size_t)r * kD + lane * 4) = O;
+    if (lane == 0) *reinterpret_cast<float2 *>(a.pre_ml + (size_t)r * 2) = make_float2(M, L);
+  }
+}
+
 // ---- tail ------------------------------------------------------------------------------------------
 namespace sht {
 constexpr int kThreads = 128, kWarps = 4;
@@ -483,12 +562,17 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
     mbar_fence_init();
   }
   pdl_trigger();
+  if ((int)blockIdx.x >= a.tail_blocks) {
+    pdl_wait();
+    join_prefix_parts(a, (int)blockIdx.x - a.tail_blocks, (int)gridDim.x - a.tail_blocks);
+    return;
+  }
   // everything before the prefix launch is complete and was written through generic stores
   asm volatile("fence.proxy.async;" ::: "memory");
   const uint64_t pol = l2_evict_first_policy();
   int loads = 0;        // pages of the items before: page i of this one is in buffer (loads + i) & 1, phase (loads + i) >> 1 & 1
   bool failed = false;
-  for (int item = blockIdx.x;; item += gridDim.x) {
+  for (int item = blockIdx.x;; item += a.tail_blocks) {
     const int unit = item % a.n_items, share = item / a.n_items;
     const int b = unit / c.Hkv, kvh = unit - b * c.Hkv;
     __syncthreads();    // the previous item's stages and s_it have been read
@@ -634,17 +718,16 @@ __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_ke
     tc5::fence_async_smem();   // these reads and writes come before the next item's copies into the stages
   }
   if (failed) set_status(c, SPKV_E_TIMEOUT);
-  // The merge behind this launch reads the prefix launch's parts too: one block stays until that is complete
-  // (all of them would keep the blocks behind them out while the prefix runs).
+  // The merge reads the prefix launch's parts too: this launch is not complete before that one is (its joining blocks
+  // wait for it, or else its first block, at its end: all of them would keep others out while the prefix runs).
   if (blockIdx.x == 0) pdl_wait();
 }
 
 // ---- merge -----------------------------------------------------------------------------------------
-// One block per query row, its kWarps warps taking every kWarps-th part (shares of the common pages, then of the
-// tail); lane l owns dims 4l .. 4l + 3.  The plan's line is read before the launch waits for the tail (it was
-// complete before the prefix launch let anything start); everything behind the wait -- did the unit leave
-// the common pages out, the parts' weights, the parts -- is loaded at once: one trip to L2.
-template <int kWarps, int kBatch>
+// One block per query row: its prefix parts (kJoined: one, made by the tail launch) and the parts of the tail, kWarps warps
+// taking every kWarps-th.  The plan's line is read before the launch waits for the tail (it was complete
+// before the prefix launch let anything start); everything behind the wait is loaded at once: one trip to L2.
+template <int kWarps, int kBatch, bool kJoined>
 __global__ void __launch_bounds__(32 * kWarps) shared_merge_kernel(SharedArgs a) {
   const CacheView &c = a.c;
   __shared__ float s_ml[kWarps][2];
@@ -656,75 +739,47 @@ __global__ void __launch_bounds__(32 * kWarps) shared_merge_kernel(SharedArgs a)
   const int4 parts = *reinterpret_cast<const int4 *>(share_head(a.rec, kvh) + 4);
   const int first = share_head(a.rec, kvh)[1];
   const bool fits = parts.z == a.sig;
-  const int n_pre = fits ? max(parts.x, 0) : 0, n = n_pre + (fits ? max(1, min(parts.y, a.max_tail)) : 1);
-  const int R = b * c.G + g, tile = R / kShareRows, row = R % kShareRows;
-  const int last_block = a.max_blocks - 1;   // (a plan that was overwritten reads no further than the workspace)
-  auto row_of = [&](int p, bool pre) -> size_t {   // index of part p's row in its array
-    return pre ? (size_t)max(0, min(first + p * a.n_tiles + tile, last_block)) * a.rows_per_block + row
-               : ((size_t)(p - n_pre) * a.n_items + unit) * c.G + g;
-  };
+  const int n_pre = kJoined ? 1 : fits ? max(parts.x, 0) : 0, n = n_pre + (fits ? max(1, min(parts.y, a.max_tail)) : 1);
   pdl_wait();
   const int skip = __ldcg(a.item_skip + unit);
   float M = -INFINITY, L = 0.f;
   float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p0 = warp; p0 < n; p0 += kBatch * kWarps) {   // kBatch parts at a time; lane x holds part x's weight
-    const int mine = p0 + lane * kWarps;
-    const bool have = lane < kBatch && mine < n;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (have) ml = __ldcg(reinterpret_cast<const float2 *>(mine < n_pre ? a.part_ml : a.tail_ml) + row_of(mine, mine < n_pre));
-    float4 v[kBatch];
+  join_parts<kBatch>(warp, kWarps, n, [&](int p, const float *&o, const float *&ml) {
+    const bool pre = p < n_pre;
+    const size_t at = !pre ? ((size_t)(p - n_pre) * a.n_items + unit) * c.G + g
+                           : kJoined ? (size_t)r : prefix_part_row(a, first, b * c.G + g, p);
+    o = (!pre ? a.tail_o : kJoined ? a.pre_o : a.part_o) + at * kD;
+    ml = (!pre ? a.tail_ml : kJoined ? a.pre_ml : a.part_ml) + at * 2;
+  }, [&](int p) { return p >= n_pre || skip > 0; /* otherwise the tail read this unit in full */ }, M, L, O);
+  if (kWarps > 1) {
+    s_o[warp][lane] = O;
+    if (lane == 0) { s_ml[warp][0] = M; s_ml[warp][1] = L; }
+    __syncthreads();
+    if (warp) return;
+    float Mx = M;
 #pragma unroll
-    for (int x = 0; x < kBatch; ++x) {
-      const int p = min(p0 + x * kWarps, n - 1);
-      const bool pre = p < n_pre;
-      v[x] = __ldcg(reinterpret_cast<const float4 *>((pre ? a.part_o : a.tail_o) + row_of(p, pre) * kD) + lane);
+    for (int x = 1; x < kWarps; ++x) Mx = fmaxf(Mx, s_ml[x][0]);
+    const float w0 = part_weight(M, L, Mx);
+    L *= w0; O.x *= w0; O.y *= w0; O.z *= w0; O.w *= w0;
+#pragma unroll
+    for (int x = 1; x < kWarps; ++x) {
+      const float f = part_weight(s_ml[x][0], s_ml[x][1], Mx);
+      const float4 v = s_o[x][lane];
+      L = fmaf(s_ml[x][1], f, L);
+      O.x = fmaf(v.x, f, O.x); O.y = fmaf(v.y, f, O.y); O.z = fmaf(v.z, f, O.z); O.w = fmaf(v.w, f, O.w);
     }
-    if (mine < n_pre && skip == 0) ml = make_float2(-INFINITY, 0.f);   // the tail read this unit in full
-    float top = ml.x;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float Mn = fmaxf(M, top), old = part_weight(M, L, Mn);
-    M = Mn;
-    const float f = part_weight(ml.x, ml.y, M);
-    float fl = f == 0.f ? 0.f : f * ml.y;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) fl += __shfl_xor_sync(0xffffffffu, fl, o);
-    L = L * old + fl;
-    O.x *= old; O.y *= old; O.z *= old; O.w *= old;
-#pragma unroll
-    for (int x = 0; x < kBatch; ++x) {
-      const float fx = __shfl_sync(0xffffffffu, f, x);
-      if (fx != 0.f) {   // (a part of weight 0 may never have been written)
-        O.x = fmaf(v[x].x, fx, O.x); O.y = fmaf(v[x].y, fx, O.y); O.z = fmaf(v[x].z, fx, O.z); O.w = fmaf(v[x].w, fx, O.w);
-      }
-    }
+    M = Mx;
   }
-  s_o[warp][lane] = O;
-  if (lane == 0) { s_ml[warp][0] = M; s_ml[warp][1] = L; }
-  __syncthreads();
-  if (warp) return;
-  float Mx = M;
-#pragma unroll
-  for (int x = 1; x < kWarps; ++x) Mx = fmaxf(Mx, s_ml[x][0]);
-  const float w0 = part_weight(M, L, Mx);
-  L *= w0; O.x *= w0; O.y *= w0; O.z *= w0; O.w *= w0;
-#pragma unroll
-  for (int x = 1; x < kWarps; ++x) {
-    const float f = part_weight(s_ml[x][0], s_ml[x][1], Mx);
-    const float4 v = s_o[x][lane];
-    L = fmaf(s_ml[x][1], f, L);
-    O.x = fmaf(v.x, f, O.x); O.y = fmaf(v.y, f, O.y); O.z = fmaf(v.z, f, O.z); O.w = fmaf(v.w, f, O.w);
-  }
-  const bool none = Mx == -INFINITY && L == 0.f;   // a sequence that has received nothing: zeros, -inf
+  const bool none = M == -INFINITY && L == 0.f;   // a sequence that has received nothing: zeros, -inf
   const float inv = none ? 0.f : 1.f / L;
   uint2 pk;
   pk.x = pack_bf16(O.x * inv, O.y * inv);
   pk.y = pack_bf16(O.z * inv, O.w * inv);
   *reinterpret_cast<uint2 *>(a.out + (size_t)r * kD + lane * 4) = pk;
-  if (a.lse && lane == 0) a.lse[r] = none ? -INFINITY : (Mx + log2f(L)) * kLn2;
+  if (a.lse && lane == 0) a.lse[r] = none ? -INFINITY : (M + log2f(L)) * kLn2;
 }
 
-struct SharedWs { size_t off_ml, off_o, off_tml, off_to, total; int max_blocks, rows, max_tail; };
+struct SharedWs { size_t off_ml, off_o, off_tml, off_to, off_pml, off_po, total; int max_blocks, rows, max_tail; };
 static SharedWs shared_ws_layout(const spkv_config_t *cfg, int B) {
   SharedWs w;
   auto a256 = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -737,6 +792,8 @@ static SharedWs shared_ws_layout(const spkv_config_t *cfg, int B) {
   w.off_o = o; o += a256((size_t)w.max_blocks * w.rows * kD * 4);
   w.off_tml = o; o += a256((size_t)w.max_tail * items * G * 8);
   w.off_to = o; o += a256((size_t)w.max_tail * items * G * kD * 4);
+  w.off_pml = o; o += a256((size_t)items * G * 8);
+  w.off_po = o; o += a256((size_t)items * G * kD * 4);
   w.total = o;
   return w;
 }
@@ -801,6 +858,8 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   a.part_o = reinterpret_cast<float *>(ws + w.off_o);
   a.tail_ml = reinterpret_cast<float *>(ws + w.off_tml);
   a.tail_o = reinterpret_cast<float *>(ws + w.off_to);
+  a.pre_ml = reinterpret_cast<float *>(ws + w.off_pml);
+  a.pre_o = reinterpret_cast<float *>(ws + w.off_po);
   a.max_blocks = w.max_blocks;
   a.max_tail = w.max_tail;
   for (int l = 0; l < layer; ++l) a.row_base += (v.Hkv - __builtin_popcountll(cache->local_mask[l])) * v.S;
@@ -822,12 +881,13 @@ extern "C" int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, 
   const bool plain = (cache->cfg.flags & SPKV_FLAG_OVERLAP) != 0;
   cache->last_kind = kLastOther;
   if (launch_link(!plain, prefix, dim3(grid), dim3(shp::kThreads), (size_t)smem, s, a) != cudaSuccess) return SPKV_E_CUDA;
-  // one block per unit, and enough of them that the shares of long units find a block each
-  if (launch_overlapped(tail, dim3(std::max(a.n_items, 2 * sms)), dim3(sht::kThreads), (size_t)tail_smem, s, a) !=
-      cudaSuccess)
+  // one block per unit, and enough of them that the pieces of long units find a block each; behind them, with many query
+  // rows, the blocks that join the prefix parts: a warp per row up to two blocks per SM
+  a.tail_blocks = std::max(a.n_items, 2 * sms);
+  const int joiners = alt ? 0 : std::min((B * v.Hq + sht::kWarps - 1) / sht::kWarps, 2 * sms);
+  if (launch_overlapped(tail, dim3(a.tail_blocks + joiners), dim3(sht::kThreads), (size_t)tail_smem, s, a) != cudaSuccess)
     return SPKV_E_CUDA;
-  // up to 40 parts in one round of loads; few rows: eight warps each (8 sequences of 64 heads: 20.4 -> 19.2 us a call),
-  // many: two, so that all rows are on the GPU at once (64 sequences of 32 heads: 42 against 45 us)
-  if (B * v.Hq <= 8 * sms) return check_stream_error(launch_overlapped(shared_merge_kernel<8, 5>, dim3(B * v.Hq), dim3(256), 0, s, a));
-  return check_stream_error(launch_overlapped(shared_merge_kernel<2, 10>, dim3(B * v.Hq), dim3(64), 0, s, a));
+  // With the prefix parts joined few parts are left; otherwise up to 40 go in one round of loads.
+  auto merge = joiners ? shared_merge_kernel<1, 4, true> : shared_merge_kernel<8, 5, false>;
+  return check_stream_error(launch_overlapped(merge, dim3(B * v.Hq), dim3(joiners ? 32 : 256), 0, s, a));
 }

@@ -8,11 +8,11 @@
 // and, for g = the rotation's transpose applied to the upstream gradient,
 //   dx = r (w g - u mean(w g u)),  r = 1 / sqrt(mean(x^2) + eps),   dw = sum over rows of g u.
 //
-// A row of head_dim elements belongs to TPR neighbouring lanes; a lane holds two 16-byte chunks of it,
-// chosen so that both halves of every rotated pair are in the same lane: with pairs (i, i + rot/2)
-// chunks j and j + rot/2, with pairs (2i, 2i + 1) two chunks side by side.  The row is read
-// once, its sum of squares goes through log2(TPR) shuffles, everything else stays in registers, all in
-// fp32, and is rounded once on the way out.
+// A row of head_dim elements belongs to TPR neighbouring lanes; a lane holds two 16-byte chunks of it, chosen so
+// that both halves of every rotated pair are in the same lane: with pairs (i, i + rot/2) chunks j and j + rot/2,
+// with pairs (2i, 2i + 1) chunks that hold whole pairs.  The row is read once, its sum of squares goes
+// through log2(TPR) shuffles, everything else stays in registers, all in fp32 (two elements per
+// instruction), and is rounded once on the way out.
 //
 // Angles.  A frequency is held as a fraction of a turn per position in 64-bit fixed point, so that
 // position * frequency modulo one turn is one exact integer product; what is left -- 32 bits of a turn -- goes
@@ -20,7 +20,10 @@
 // computes the sines and cosines of a token once, through shared memory, for all its heads: no table
 // in memory, no position limit.
 //
-// What bounds it: bytes.  Each row is read and written once; about 35 issue slots per 512 B moved.
+// What bounds it: bytes; each row is read and written once.  B200, device time: 8192 tokens of 32/8 heads, bf16, 201 MB:
+// 37.3 us = 5.4 TB/s (0.84 of the measured copy rate); backward of 32768 tokens, 1.14 GB: 191 us = 6.0 TB/s
+// (0.93).  With rows held in registers on their way 50 and 271 us: too few bytes in flight.  One token: 2.5 us,
+// a launch and three trips to memory.
 #include <math.h>
 
 #include <algorithm>
