@@ -139,6 +139,8 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
   pdl_wait();
   pdl_trigger();   // (only now: what follows may then rely on everything before this launch)
   if (warp == kLoaderWarp) {
+    // (pages were written through generic stores)
+    asm volatile("fence.proxy.async;" ::: "memory");
     const int32_t *dp = share_desc(c, a.rec, blockIdx.x);
     if (lane < 8) s_desc[lane] = __ldcg(dp + lane);
     __syncwarp();
@@ -517,7 +519,7 @@ __device__ inline size_t prefix_part_row(const SharedArgs &a, int first, int R, 
 
 // With more than 128 query rows a KV head, the last blocks of the tail launch make one part of a row's prefix parts, a
 // warp per row.  They wait for the prefix launch and run beside the last tail blocks, so that the merge finds
-// little left to read (64 sequences of 32 heads on 8 KV heads: 18 parts a row, 19 MB; 40.1 -> 38.3 us a call.
+// little left to read (64 sequences of 32 heads on 8 KV heads: 18 parts a row, 19 MB; 40.1 -> 37.7 us a call.
 // With fewer rows the tail ends with the prefix and nothing would hide it: 19 -> 23 us).
 __device__ inline void join_prefix_parts(const SharedArgs &a, int block, int n_blocks) {
   const CacheView &c = a.c;
@@ -546,8 +548,10 @@ constexpr int off_bar = 2 * kPageBytes, kSmemBytes = off_bar + 128;
 }  // namespace sht
 
 // Item = share * n_items + unit.  A unit's pages are what its compact cache holds behind the common pages,
-// then its ring; they are cut into up to `shares` (plan) pieces of at least four.  The four warps take 16
-// pairs each of every page and join at the end through the page stages.
+// then its ring; they are cut into up to `shares` (plan) pieces of at least kTailMinPages.  The four warps take 16
+// pairs each of every page and join at the end through the page buffers.  64 sequences of 32/8
+// heads with a page of their own and a ring of two: 50 MB, 7.8 us at the copy rate, which the prefix launch hides but for
+// some 3 us.
 template <int NH>
 __global__ void __launch_bounds__(sht::kThreads, NH == 1 ? 5 : 3) shared_tail_kernel(SharedArgs a) {
   using namespace sht;

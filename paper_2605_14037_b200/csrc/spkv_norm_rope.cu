@@ -37,7 +37,6 @@ namespace spkv {
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 constexpr int kFwdBlocks = 2, kBwdBlocks = 2;   // blocks per SM (registers)
-constexpr int kAhead = 3;                       // passes of rows loaded ahead (forward)
 constexpr int kMaxBwdBlocks = 512;              // partial sums of the weight gradients the workspace holds
 
 struct RowArgs {
@@ -322,8 +321,8 @@ template <int TPR> struct WarpWork {
 
 // A warp's rows are one stream -- token after token, query, key and value heads, `step` heads a pass -- that runs
 // kDepth passes ahead through shared memory: a lane copies its own 32 bytes of a pass there
-// asynchronously and reads them back, so that what is on its way costs no registers (2 KB per warp in
-// registers left memory waiting: 40 us for 8192 tokens of 32/8 heads; see the figures at the head).
+// asynchronously and reads them back, so that what is on its way costs no registers (a warp's 2 KB in registers
+// left memory waiting: 40 us for 8192 tokens of 32/8 heads, 37.3 this way).
 template <class T, int TPR, int kStreams>
 struct RowStream {
   static constexpr int kDepth = 4 / kStreams;
@@ -647,12 +646,11 @@ __global__ void __launch_bounds__(16 * kGradSlices) norm_weight_grad_kernel(cons
 
 static int elem_bytes(int dtype) { return dtype == SPKV_F32 ? 4 : 2; }
 
-static int check_rows(const spkv_rows_t *r, int heads, int n_tok, int dtype) {
+static int check_rows(const spkv_rows_t *r, int heads, int dtype) {
   if (heads == 0) return SPKV_OK;
   if (!r || !r->ptr) return SPKV_E_INVALID;
   const int64_t per16 = 16 / elem_bytes(dtype);
   if (((uintptr_t)r->ptr & 15) || r->head_stride % per16 || r->token_stride % per16) return SPKV_E_INVALID;
-  (void)n_tok;
   return SPKV_OK;
 }
 
@@ -735,7 +733,10 @@ static int launch_rows(RowArgs &a, bool backward, int sms, float *dwq, float *dw
 // lanes per row: two 16-byte chunks each, rounded up to a power of two
 static int dispatch_rows(RowArgs &a, int dtype, bool backward, int sms, float *dwq, float *dwk, cudaStream_t s) {
   const int lanes = a.D * elem_bytes(dtype) / 32;
-#define SPKV_ROWS(T)                                                                            if (lanes <= 4) return launch_rows<T, 4>(a, backward, sms, dwq, dwk, s);                      if (lanes <= 8) return launch_rows<T, 8>(a, backward, sms, dwq, dwk, s);                      if (lanes <= 16) return launch_rows<T, 16>(a, backward, sms, dwq, dwk, s);
+#define SPKV_ROWS(T)                                                       \
+  if (lanes <= 4) return launch_rows<T, 4>(a, backward, sms, dwq, dwk, s); \
+  if (lanes <= 8) return launch_rows<T, 8>(a, backward, sms, dwq, dwk, s); \
+  if (lanes <= 16) return launch_rows<T, 16>(a, backward, sms, dwq, dwk, s);
   if (dtype == SPKV_F32) {
     SPKV_ROWS(float)
     return launch_rows<float, 32>(a, backward, sms, dwq, dwk, s);
@@ -791,7 +792,7 @@ extern "C" int spkv_norm_rope(const spkv_qk_norm_t *norm, const spkv_rope_t *rop
   const spkv_rows_t *in[3] = {q, k, v}, *out[3] = {q_out, k_out, v_out};
   const int heads[3] = {a.Hq, a.Hkv, a.Hv};
   for (int i = 0; i < 3; ++i) {
-    if ((rc = check_rows(in[i], heads[i], n_tok, norm->dtype)) || (rc = check_rows(out[i], heads[i], n_tok, norm->dtype)))
+    if ((rc = check_rows(in[i], heads[i], norm->dtype)) || (rc = check_rows(out[i], heads[i], norm->dtype)))
       return rc;
     if (heads[i]) { a.x[i] = *in[i]; a.y[i] = *out[i]; }
   }
@@ -826,8 +827,8 @@ extern "C" int spkv_norm_rope_backward(const spkv_qk_norm_t *norm, const spkv_ro
   const int heads[3] = {a.Hq, a.Hkv, a.Hv};
   for (int i = 0; rows && i < 3; ++i) {
     const bool normed = i < 2 && ((a.norm >> i) & 1);
-    if ((rc = check_rows(g[i], heads[i], n_tok, norm->dtype)) || (rc = check_rows(y[i], heads[i], n_tok, norm->dtype)) ||
-        (rc = check_rows(x[i], normed ? heads[i] : 0, n_tok, norm->dtype)))
+    if ((rc = check_rows(g[i], heads[i], norm->dtype)) || (rc = check_rows(y[i], heads[i], norm->dtype)) ||
+        (rc = check_rows(x[i], normed ? heads[i] : 0, norm->dtype)))
       return rc;
     if (heads[i]) { a.g[i] = *g[i]; a.y[i] = *y[i]; }
     if (heads[i] && normed) a.x[i] = *x[i];

@@ -42,10 +42,10 @@ template <class I> __host__ __device__ inline I *share_head(I *rec, int h) { ret
 template <class I> __host__ __device__ inline I *share_desc(const CacheView &c, I *rec, int block) {
   return rec + kShareHdr + kShareHead * c.Hkv + kShareDesc * (size_t)block;
 }
-// What a plan must agree on with a call: the batch size and the cache's layout, which fixes where units and page tables
-// lie (never 0: a zero-filled buffer is no plan).
+// What a plan must agree on with a call: the batch size, the cache's layout, which fixes where units and page tables
+// lie, and the number of SMs the shares were cut for (never 0: a zero-filled buffer is no plan).
 inline int share_signature(const spkv_cache *cache, int B) {
-  return (int)(((uint32_t)B * 2654435761u ^ cache->share_salt) | 1u);
+  return (int)(((uint32_t)B * 2654435761u ^ cache->share_salt ^ (uint32_t)cache->sm_count * 0x9e3779b1u << 1) | 1u);
 }
 
 }  // namespace spkv

@@ -177,6 +177,25 @@ def _on_device(dev, stream, fn, *args):
         return fn(*args, _raw_stream(dev) if stream is None else stream.cuda_stream)
 
 
+_capturing = torch.cuda.is_current_stream_capturing
+
+
+def _scratch(store, nbytes, dev, stream):
+    """Workspace of one call on `dev`: kept in `store` per stream (calls on two streams may run at once), replaced
+    when it is too small.  A call that is being captured gets one from its graph's memory pool, which no other
+    graph and no eager call uses."""
+    if stream is not None or dev != _current_device():
+        with torch.cuda.device(dev), torch.cuda.stream(stream):
+            return _scratch(store, nbytes, dev, None)
+    if _capturing():
+        return torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
+    key = (dev, _raw_stream(dev))
+    ws = store.get(key)
+    if ws is None or ws.numel() < nbytes:
+        ws = store[key] = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
+    return ws
+
+
 def _ptr(t, dtype=None):
     if t is None:
         return None
@@ -232,7 +251,7 @@ class Cache:
             _check(lib().spkv_cache_create(C.byref(self.cfg), _ptr(self.arena), self.arena_bytes,
                                            _stream(), C.byref(h)), "spkv_cache_create")
         self._h = h
-        self._ws, self._shared_bytes = {}, {}
+        self._ws, self._shared_ws, self._shared_bytes = {}, {}, {}
         self.G = n_q_heads // n_kv_heads
         self.default_scale = 1.0 / math.sqrt(head_dim)
 
@@ -259,7 +278,7 @@ class Cache:
         with torch.cuda.device(self.device):
             _check(lib().spkv_cache_attach(C.byref(self.cfg), _ptr(arena), arena.numel(), _stream(), C.byref(h)),
                    "spkv_cache_attach")
-        self._h, self._ws, self._shared_bytes = h, {}, {}
+        self._h, self._ws, self._shared_ws, self._shared_bytes = h, {}, {}, {}
         self.G = self.cfg.n_q_heads // self.cfg.n_kv_heads
         self.default_scale = 1.0 / math.sqrt(self.cfg.head_dim)
         return self
@@ -414,9 +433,7 @@ class Cache:
         nbytes = self._shared_bytes.get(B)
         if nbytes is None:
             nbytes = self._shared_bytes[B] = lib().spkv_decode_shared_workspace_bytes(C.byref(cfg), B)
-        ws = self._ws.get("decode_shared")
-        if ws is None or ws.numel() < nbytes:
-            ws = self._workspace("decode_shared", nbytes)
+        ws = _scratch(self._shared_ws, nbytes, dev, stream)
         rc = _on_device(dev, stream, lib().spkv_decode_attention_shared, self._h, layer, seq_ids.data_ptr(), B, q.data_ptr(),
                         out.data_ptr(), None if lse is None else lse.data_ptr(),
                         self.default_scale if sm_scale is None else sm_scale, plan.data_ptr(), plan.numel(), ws.data_ptr(),
@@ -603,13 +620,6 @@ class NormRope:
         self.workspace_bytes = lib().spkv_norm_rope_workspace_bytes(self._n)
         self._ws = {}
 
-    def workspace(self, device, stream):
-        """Scratch of the weight gradients: one per stream, so that calls on two streams do not share it."""
-        ws = self._ws.get((device, stream))
-        if ws is None:
-            ws = self._ws[device, stream] = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
-        return ws
-
 
 def make_norm_rope(n_q_heads, n_kv_heads, head_dim=128, dtype=torch.bfloat16, wq=None, wk=None, norm=True, eps=1e-6,
                    rot_dim=None, theta=10000.0, inv_freq=None, axis=None, n_axes=1, interleaved=False, scale=1.0):
@@ -726,7 +736,8 @@ def spkv_norm_rope_backward(nr, positions, q, k, q_grad, k_grad, v_grad=None, dq
     ws, ws_bytes = None, 0
     if dwq is not None or dwk is not None:
         ws_bytes = nr.workspace_bytes
-        ws = nr.workspace(q_grad.device, _raw_stream(dev) if stream is None else stream.cuda_stream).data_ptr()
+        scratch = _scratch(nr._ws, ws_bytes, dev, stream)   # (alive until the launch is made)
+        ws = scratch.data_ptr()
     io = (Rows * 8)()
     at = C.addressof(io)
     _EIGHT_ROWS.pack_into(io, 0, *xq, *xk, *gq, *gk, *gv, *yq, *yk, *yv)

@@ -275,9 +275,8 @@ def test_decode_steps_in_a_graph_beside_the_per_sequence_call(overlap):
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
         want = [torch.empty_like(o) for o in outs]
-        step(twin, want)                                # (also allocates the workspaces outside the capture)
+        step(twin, want)
         pos.sub_(1)
-        cache._workspace("decode_shared", twin._ws["decode_shared"].numel())
         s.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=s):
@@ -441,6 +440,43 @@ def test_two_streams_in_turn():
             outs.append(cache.spkv_decode_attention_shared(0, ids, qd, plan))
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+    cache.check()
+
+
+def test_graphs_and_eager_calls_on_streams_of_their_own():
+    """Graphs of a small batch captured on one stream, replayed at the same time on two, while eager calls of the whole
+    batch make a larger workspace: nobody writes over anybody's parts."""
+    spkv = load()
+    cache, wl, ids = build(spkv, 24, 32, 2, 6000, 5, (0.8, 0.3))
+    q, qd = queries(wl)
+    plan, whole = cache.spkv_share_plan(ids[:4].contiguous()), cache.spkv_share_plan(ids)
+    qs = [qd[:4].contiguous(), (qd[:4] * 0.5).contiguous()]
+    few = ids[:4].contiguous()
+    want = [cache.spkv_decode_attention_shared(0, few, x, plan) for x in qs]
+    want_all = cache.spkv_decode_attention_shared(0, ids, qd, whole)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for x in qs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            o = x
+            for _ in range(8):
+                o = cache.spkv_decode_attention_shared(0, few, x, plan)
+        graphs.append(g)
+        outs.append(o)
+    s = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(10):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, s):
+            with torch.cuda.stream(st):
+                g.replay()
+        eager = [cache.spkv_decode_attention_shared(0, ids, qd, whole, stream=s[2]) for _ in range(4)]
+        here = [cache.spkv_decode_attention_shared(0, few, x, plan) for x in qs]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs + here, want + want))
+        assert all(torch.equal(e, want_all) for e in eager)
     cache.check()
 
 

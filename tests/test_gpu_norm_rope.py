@@ -318,6 +318,35 @@ def test_another_stream_and_a_captured_graph():
     assert all(torch.equal(a, b) for a, b in zip(out, want)) and all(torch.equal(a, b) for a, b in zip(res, ref))
 
 
+def test_captured_backward_passes_replayed_at_the_same_time():
+    """Two graphs of one descriptor, captured on one stream and replayed on two beside eager calls on a third: the
+    weight gradients' partial sums of each are its own."""
+    c, d = Case(21, n=3000, hq=8, hkv=2), Case(22, n=2500, hq=8, hkv=2)
+    calls = [lambda c=c: c.spkv.spkv_norm_rope_backward(c.nr, c.pos_d, c.x[0], c.x[1], *c.g),
+             lambda: c.spkv.spkv_norm_rope_backward(c.nr, d.pos_d, d.x[0], d.x[1], *d.g)]
+    want = [f() for f in calls]
+    graphs, res = [], []
+    for f in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            r = f()
+        graphs.append(graph)
+        res.append(r)
+    s = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(20):
+        for r in res:
+            for t in r:
+                t.zero_()
+        torch.cuda.synchronize()
+        for graph, st in zip(graphs, s):
+            with torch.cuda.stream(st):
+                graph.replay()
+        eager = [f() for f in calls]
+        torch.cuda.synchronize()
+        for a, b, w in zip(res, eager, want):
+            assert all(torch.equal(x, z) and torch.equal(y, z) for x, y, z in zip(a, b, w))
+
+
 def test_binding_refusals():
     spkv = load()
     nr = spkv.make_norm_rope(4, 2)
