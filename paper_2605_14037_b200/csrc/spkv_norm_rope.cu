@@ -28,6 +28,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include <cuda_fp16.h>
 
@@ -566,35 +567,32 @@ template <class T, int TPR, bool kAdjacent>
 __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(const __grid_constant__ RowArgs a) {
   constexpr int CE = Elem<T>::kChunk;
   __shared__ Tables<CE, TPR> tables;
-  // rows on their way; at the end of a side its sums, [warp][2 CE * TPR]
   __shared__ uint4 s_ring[kRowWarps][RowStream<T, TPR, 2>::kDepth * 128];
-  float *s_dw = reinterpret_cast<float *>(s_ring);
-  static_assert(sizeof(s_ring) >= kRowWarps * 2 * CE * TPR * 4, "room for the sums");
+  // a side's sums at its end, [warp][2 CE * TPR], over the angles (nobody needs them then)
+  float *s_dw = reinterpret_cast<float *>(tables.cs);
+  static_assert(sizeof(tables.cs) >= kRowWarps * 2 * CE * TPR * 4, "room for the sums");
   pdl_trigger();
-  fill_tables<CE, TPR>(a, tables);
   const WarpWork<TPR> work(a);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = threadIdx.x % TPR;
   const LaneChunks l = lane_chunks<CE>(a, j);
-#pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const int H = side ? a.Hkv : a.Hq;
-    f2 dw0[CE / 2], dw1[CE / 2];
+  f2 dw0[CE / 2], dw1[CE / 2];
+  auto walk = [&](auto side_c, RowStream<T, TPR, 2> &stream) {
+    constexpr int side = decltype(side_c)::value;
 #pragma unroll
     for (int i = 0; i < CE / 2; ++i) dw0[i] = dw1[i] = pk(0.f, 0.f);
-    RowStream<T, TPR, 2> stream(a, work, l, s_ring[warp], side, 2 * side);
-    if (stream.any()) {
-      stream.start();
-      for (int64_t tok = work.first; tok < a.n_tok; tok += work.stride) {
-        Angles<CE, kAdjacent> ang;
-        token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l.rot, ang);
-        backward_side<T, TPR, kAdjacent, false>(a, a.y[side], H, stream.n_pass[side], (a.norm >> side) & 1, tables.w[side], ang,
-                                                tok, work, l, stream, dw0, dw1);
-        if (side == 1)
-          backward_side<T, TPR, kAdjacent, true>(a, a.y[2], a.Hv, stream.n_pass[2], false, tables.w[0], ang, tok, work, l, stream,
-                                                 dw0, dw1);
-      }
+    if (!stream.any()) return;
+    for (int64_t tok = work.first; tok < a.n_tok; tok += work.stride) {
+      Angles<CE, kAdjacent> ang;
+      token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l.rot, ang);
+      backward_side<T, TPR, kAdjacent, false>(a, a.y[side], side ? a.Hkv : a.Hq, stream.n_pass[side], (a.norm >> side) & 1,
+                                              tables.w[side], ang, tok, work, l, stream, dw0, dw1);
+      if (side == 1)
+        backward_side<T, TPR, kAdjacent, true>(a, a.y[2], a.Hv, stream.n_pass[2], false, tables.w[0], ang, tok, work, l, stream,
+                                               dw0, dw1);
     }
-    if (!a.part) continue;
+  };
+  auto sum = [&](int side) {
+    if (!a.part) return;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < CE; ++i) {
@@ -619,7 +617,17 @@ __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(cons
       if (ll.live) a.part[((size_t)blockIdx.x * 2 + side) * a.D + (e < CE ? ll.c0 + e : ll.c1 + e - CE)] = v;
     }
     __syncthreads();
-  }
+  };
+  // each side's first rows are on their way while the tables are filled, or the other side's sums made
+  RowStream<T, TPR, 2> queries(a, work, l, s_ring[warp], 0, 0);
+  queries.start();
+  fill_tables<CE, TPR>(a, tables);
+  walk(std::integral_constant<int, 0>(), queries);
+  RowStream<T, TPR, 2> keys_values(a, work, l, s_ring[warp], 1, 2);
+  keys_values.start();
+  sum(0);
+  walk(std::integral_constant<int, 1>(), keys_values);
+  sum(1);
 }
 
 // Sums the blocks' partial weight gradients, in a fixed order: grid (D / 16, 2 sides), 512 threads = 16 columns x 32
