@@ -38,6 +38,7 @@ namespace spkv {
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 constexpr int kFwdBlocks = 2, kBwdBlocks = 2;   // blocks per SM (registers)
+constexpr int kFewBlocks = 4;                   // blocks per SM up to which the kernel for few tokens is the faster one
 constexpr int kMaxBwdBlocks = 512;              // partial sums of the weight gradients the workspace holds
 
 struct RowArgs {
@@ -449,12 +450,13 @@ __global__ void __launch_bounds__(kRowThreads, kFwdBlocks) norm_rope_kernel(cons
   }
 }
 
-// Forward for few tokens (a decode step): a block per token, its rows of all sides in one short loop.  Such a launch
-// is a chain of waits -- instructions, positions and weights, rows -- so the code is small (the kernel above spends
-// more on fetching its instructions than on a token: 4.1 against 2.7 us for one token), and the first rows
-// are on their way while the angles are computed.
+// Forward for few tokens (a decode step): a block per token, or several that share its rows (gridDim.y) while there
+// is room for them; the rows of all sides in one short loop.  Such a launch is a chain of waits -- instructions,
+// positions and weights, rows -- so the code is small (the kernel above spends more on fetching its
+// instructions than on a token) and the first rows are on their way while the angles are computed.  One token of
+// 32/8 heads 3.0 us a launch (4.3 above; 2.9 and 5.1 with 24/24 fp32 heads), 592 tokens 5.7 (6.3).
 template <class T, int TPR, bool kAdjacent>
-__global__ void __launch_bounds__(kRowThreads) norm_rope_few_kernel(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__(kRowThreads, kFewBlocks) norm_rope_few_kernel(const __grid_constant__ RowArgs a) {
   constexpr int CE = Elem<T>::kChunk, kRows = kRowThreads / TPR;
   __shared__ alignas(16) float2 s_cs[CE * TPR];
   __shared__ alignas(16) float s_w[2][2 * CE * TPR];
@@ -471,7 +473,8 @@ __global__ void __launch_bounds__(kRowThreads) norm_rope_few_kernel(const __grid
     const int side = on ? side_of(r) : 0;
     load_row(nxt, row_ptr<const T>(side == 0 ? a.x[0] : side == 1 ? a.x[1] : a.x[2], tok, on ? head_of(r, side) : 0), l, on);
   };
-  fetch(sub);
+  const int first = blockIdx.y * kRows + sub, step = gridDim.y * kRows;
+  fetch(first);
   for (int p = threadIdx.x; p < table_pairs<kAdjacent>(a); p += kRowThreads)
     s_cs[pair_slot<CE, TPR, kAdjacent>(a, p)] =
         p < a.rope.rot_dim / 2 ? pair_angle(a, __ldg(&a.pos[(size_t)a.rope.axis[p] * a.n_tok + tok]), a.rope.turn[p])
@@ -481,10 +484,10 @@ __global__ void __launch_bounds__(kRowThreads) norm_rope_few_kernel(const __grid
   Angles<CE, kAdjacent> ang;
   lane_angles<CE, TPR, kAdjacent>(s_cs, j, l.rot, ang);
 #pragma unroll 1
-  for (int base = 0; base < n_rows; base += kRows) {
-    const int r = base + sub, side = side_of(r);
+  for (int r = first; r - sub < n_rows; r += step) {   // (the same passes for all lanes: they shuffle)
+    const int side = side_of(r);
     uint4 cur[2] = {nxt[0], nxt[1]};
-    fetch(r + kRows);
+    fetch(r + step);
     if (__any_sync(0xffffffffu, side < 2)) {
       f2 f0[CE / 2], f1[CE / 2];
       unpack<T>(cur[0], f0);
@@ -721,9 +724,11 @@ static int split_rows(RowArgs &a, int sms, int blocks_per_sm, int rows_per_pass,
 template <class T, int TPR>
 static int launch_rows(RowArgs &a, bool backward, int sms, float *dwq, float *dwk, cudaStream_t s) {
   const bool adjacent = a.rope.interleaved != 0;
-  if (!backward && a.n_tok <= 2 * sms) {
-    if (adjacent) norm_rope_few_kernel<T, TPR, true><<<a.n_tok, kRowThreads, 0, s>>>(a);
-    else norm_rope_few_kernel<T, TPR, false><<<a.n_tok, kRowThreads, 0, s>>>(a);
+  if (!backward && a.n_tok <= kFewBlocks * sms) {
+    const int passes = ((a.Hq + a.Hkv + a.Hv) * TPR + kRowThreads - 1) / kRowThreads;
+    const dim3 grid(a.n_tok, std::max(1, std::min(passes, kFewBlocks * sms / a.n_tok)));
+    if (adjacent) norm_rope_few_kernel<T, TPR, true><<<grid, kRowThreads, 0, s>>>(a);
+    else norm_rope_few_kernel<T, TPR, false><<<grid, kRowThreads, 0, s>>>(a);
     return check_stream_error(cudaGetLastError());
   }
   if (!backward) {

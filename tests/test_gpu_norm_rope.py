@@ -141,6 +141,11 @@ CASES = [
     dict(n=297, hq=3, hkv=1), dict(n=500, hq=40, hkv=5, interleaved=True, rot=64), dict(n=900, hq=17, hkv=2, dtype="f16", D=64),
     dict(n=2400, hq=5, hkv=3, D=32, dtype="f32"), dict(n=310, hq=2, hkv=2, D=240, rot=48, axes=2, interleaved=True),
     dict(n=1, hq=6, hkv=2, D=176, rot=96, interleaved=True, dtype="f16"),
+    # several blocks a token, the last of them in part; a block a token with many heads
+    dict(n=2, hq=64, hkv=63, dtype="f32"), dict(n=150, hq=37, hkv=7), dict(n=592, hq=19, hkv=9, D=80, rot=48, dtype="f16"),
+    # two, four and eight warps a token
+    dict(n=601, hq=40, hkv=5, interleaved=True, rot=64), dict(n=1200, hq=24, hkv=23, dtype="f32"),
+    dict(n=888, hq=64, hkv=61, dtype="f32", D=112, rot=96),
 ]
 
 
