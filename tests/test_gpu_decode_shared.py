@@ -104,6 +104,23 @@ def test_against_the_formula(B, Hq, Hkv, T0, m, rates):
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("B,Hq,Hkv", [(1024, 1, 1), (512, 4, 2), (64, 16, 16), (341, 48, 3)])
+def test_the_largest_batches(B, Hq, Hkv):
+    """1024 units (one piece of its own each), more query rows than a block of any KV head takes"""
+    spkv = load()
+    cache, wl, ids = build(spkv, B, Hq, Hkv, 700, 3, tuple(0.2 + 0.8 * (i % 2) for i in range(Hkv)), seed=B)
+    q, qd = queries(wl)
+    plan = cache.spkv_share_plan(ids)
+    out, lse = cache.spkv_decode_attention_shared(0, ids, qd, plan, want_lse=True)
+    cache.check()
+    some = sorted({0, 1, B // 2, B - 2, B - 1, *range(0, B, max(1, B // 12))})
+    check(cache, 0, [b + 1 for b in some], q[some], out[some], lse[some])
+    lone = torch.empty_like(lse[some])   # (the per-sequence call takes fewer sequences at once)
+    cache.spkv_decode_attention(0, ids[some].contiguous(), qd[some].contiguous(), lse=lone)
+    # (each within 130 * 2^-24 |q| |k| scale of the formula, as in `check`; |q| |k| scale stays below 50 here)
+    assert torch.isfinite(lse).all() and (lse[some] - lone).abs().max() < 2 * 130 * 2.0 ** -24 * 50 + 2.0 ** -17
+
+
 def test_sequences_that_share_nothing_and_single_sequences():
     spkv = load()
     cache = make(spkv, n_seqs=4, flags=0)              # also without SPKV_FLAG_FORK
