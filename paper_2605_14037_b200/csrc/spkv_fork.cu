@@ -16,7 +16,9 @@ __global__ void __launch_bounds__(256) seq_fork_kernel(CacheView c, int src, For
   const int layer = blockIdx.x / c.Hkv, kvh = blockIdx.x % c.Hkv;
   const int us = unit_index(c, layer, src, kvh), ud = unit_index(c, layer, dst.id[blockIdx.y], kvh);
   const int tid = threadIdx.x;
-  if (c.t[ud] != 0 || c.len[ud] != 0) {
+  // The whole block decides, behind a barrier: thread 0 writes these two words at the end, and a warp that came to them
+  // later would take the finished unit for one that was not empty and leave its part uncopied.
+  if (__syncthreads_or(c.t[ud] != 0 || c.len[ud] != 0)) {
     if (tid == 0) set_status(c, SPKV_E_FORK);
     return;
   }

@@ -242,3 +242,45 @@ def test_fork_in_a_captured_graph():
             compare_state(cache, 0, 1, h, unit(wl, [(0, 0, 300 if hi == 340 else 340)], h, tl))
         feed(cache, wl, 0, 0, 0, 300 if hi == 340 else 340, hi)
     cache.check()
+
+
+@pytest.mark.parametrize("T0,rates,w,local", [
+    (100, (1.0, 0.5), 128, None),             # within the window: nothing kept yet
+    (640, (0.0, 0.0), 512, None),             # nothing ever kept, a long ring
+    (128 + 128 * 64, (1.0, 1.0), 128, None),  # 128 whole pages: more table entries than a warp takes
+    (700, (1.0, 1.0), 128, [[1, 1]]),         # no page tables at all
+    (1, (1.0, 1.0), 1, None),
+])
+def test_units_without_a_partly_filled_page(T0, rates, w, local):
+    """No page is copied, so nothing but the block's own barrier stands between the look at the destination and its
+    last write: every destination's ring, logits, table and owner counts are complete, time after time."""
+    spkv = load()
+    n = 64
+    cache = make(spkv, n_seqs=n + 1, pool=2 * (T0 // 64 + 2), max_context=T0 + 64, w=w, local_only=local)
+    tl = cache.spkv_tau_logit()
+    wl = Workload(T0, T0, 1, 4, 2, rates, tl)
+    feed(cache, wl, 0, 0, 0, 0, T0)
+    ref = [unit(wl, [(0, 0, T0)], h, tl, w) for h in range(2)]
+    pages = used(cache)
+    assert pages == (0 if local else sum(len(u) // 64 for u in ref))
+    kept, ring = ([read(0, 0, h) for h in range(2)] for read in (cache.spkv_read_kept, cache.spkv_read_window))
+    for _ in range(5):
+        cache.spkv_seq_fork(0, range(1, n + 1))
+        cache.check()
+        assert used(cache) == pages
+        ln, t = cache.spkv_read_lengths(0)
+        assert (t == T0).all() and (ln == ln[0]).all()
+        for s in range(1, n + 1, 7):
+            for h in range(2):
+                for got, want in ((cache.spkv_read_kept(0, s, h), kept[h]), (cache.spkv_read_window(0, s, h), ring[h])):
+                    assert all(np.array_equal(x, y) for x, y in zip(got, want))
+        for s in range(1, n + 1):               # each counted itself in: no page goes back before the last of them
+            cache.spkv_cache_reset_seq(s)
+            if s % 16 == 0:
+                assert used(cache) == pages
+    if not local:
+        for h in range(2):
+            compare_state(cache, 0, 0, h, ref[h])
+    cache.spkv_cache_reset_seq(0)
+    assert used(cache) == 0
+    cache.check()
