@@ -113,7 +113,10 @@ typedef struct {
  * earlier work, as any stream-ordered kernel does; the library still issues its hot-path kernels
  * as programmatic dependent launches, so their block-local set-up runs under the tail of the
  * previous kernel, but they execute griddepcontrol.wait before touching an input or the cache).  Any other call of the library (prefill,
- * score, reset, ...) is a full synchronisation point either way. */
+ * score, reset, ..., and the calls that take no cache: spkv_norm_rope, spkv_softgate_forward, ...) is a full
+ * synchronisation point either way: the next append or decode waits for everything earlier on the stream.  Rows
+ * that spkv_norm_rope writes may therefore go straight into the next append or decode; what another library's kernels
+ * write may not (spkv_note_foreign_work). */
 #define SPKV_FLAG_OVERLAP 1
 
 /* SPKV_FLAG_PREFILL_PV_BF16 (off by default): the chunk attention of spkv_prefill multiplies the
@@ -315,7 +318,8 @@ typedef struct {
 
 /* d_pos [n_axes, n_tok] int32 device (may be NULL when rot_dim is 0).  v and v_out both NULL or both given.
  * An output may be its own input (same pointer and strides); any other overlap is not allowed.
- * Asynchronous on `stream`; n_tok = 0 does nothing. */
+ * Asynchronous on `stream`; n_tok = 0 does nothing.  A full synchronisation point for SPKV_FLAG_OVERLAP, as is the
+ * backward pass. */
 int spkv_norm_rope(const spkv_qk_norm_t *norm, const spkv_rope_t *rope, int32_t n_tok, const int32_t *d_pos,
                    const spkv_rows_t *q, const spkv_rows_t *k, const spkv_rows_t *v, const spkv_rows_t *q_out,
                    const spkv_rows_t *k_out, const spkv_rows_t *v_out, spkv_stream_t stream);

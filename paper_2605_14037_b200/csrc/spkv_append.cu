@@ -193,6 +193,7 @@ using namespace spkv;
 // was a decode/append of a different layer of this cache on the same stream and no other append
 // of this layer is outstanding: the kernel then waits for its own layer's decode launches only.
 static int append_must_wait(spkv_cache *cache, int layer, cudaStream_t s) {
+  look_for_cacheless_calls(cache);
   const bool independent = (cache->cfg.flags & SPKV_FLAG_OVERLAP) &&
                            (cache->last_kind == kLastDecode || cache->last_kind == kLastAppend) &&
                            cache->last_layer != layer && cache->last_stream == s &&

@@ -13,6 +13,8 @@ namespace spkv {
 
 static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+std::atomic<unsigned long long> cacheless_calls{0};
+
 int check_stream_error(cudaError_t e) { return e == cudaSuccess ? SPKV_OK : SPKV_E_CUDA; }
 
 // Eq. 2 moved to logit space: u >= tau  <=>  logit >= log(tau / (1 - tau)).
@@ -185,6 +187,7 @@ static int make_handle(const spkv_config_t *cfg, void *d_arena, const Layout &l,
   c->last_kind = kLastOther;
   c->last_layer = -1;
   c->last_stream = nullptr;
+  c->cacheless_seen = cacheless_calls.load(std::memory_order_relaxed);
   c->ws_toggle = 0;
   c->half_last_layer[0] = c->half_last_layer[1] = -1;
   c->last_decode_items = -1;

@@ -456,6 +456,7 @@ static int decode_attention_impl(spkv_cache_t *cache, int32_t layer, const int32
   // for the append covers it: the append, launched after that decode, itself waited for every
   // decode launch of its layer before it touched the cache.  (The kernel could not wait for it
   // directly: a block cannot tell its own launch's count from older ones.)
+  look_for_cacheless_calls(cache);
   a.wait_mode = ((cache->cfg.flags & SPKV_FLAG_OVERLAP) && cache->last_kind == kLastAppend &&
                  cache->last_layer == layer && cache->last_stream == as_stream(stream) &&
                  // same workspace, cut into the same halves, as the launch it may run beside

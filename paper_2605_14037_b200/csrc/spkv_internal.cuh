@@ -29,6 +29,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/spkv.h"
 
 namespace spkv {
@@ -277,6 +279,7 @@ struct spkv_cache {
   int last_kind;        // 0 other, 1 append, 2 decode
   int last_layer;
   cudaStream_t last_stream;
+  unsigned long long cacheless_seen;   // cacheless calls of the process when this cache last looked (cacheless_calls)
   int ws_toggle;        // decode workspace half used by the next decode launch
   int half_last_layer[2];   // layer of the decode launch that last used each workspace half (-1: none)
   int last_decode_items;    // units of the previous decode launch (the workspace halves depend on it)
@@ -296,6 +299,16 @@ struct spkv_cache {
 
 namespace spkv {
 int check_stream_error(cudaError_t e);
+// Calls that take no cache (norm + rotation of rows, soft-gated forward, stream read) enqueue kernels that no cache's
+// last_kind knows of, and some of them let dependents launch early.  Each counts itself here, and a cache that finds the
+// count moved treats its own previous launch as "other": its next append or decode waits for the whole
+// stream.  (Calls on other streams and for other caches cost an overlap, nothing else.)
+extern std::atomic<unsigned long long> cacheless_calls;
+inline void note_cacheless_call() { cacheless_calls.fetch_add(1, std::memory_order_relaxed); }
+inline void look_for_cacheless_calls(spkv_cache *c) {
+  const unsigned long long n = cacheless_calls.load(std::memory_order_relaxed);
+  if (n != c->cacheless_seen) { c->cacheless_seen = n; c->last_kind = kLastOther; }
+}
 inline cudaStream_t as_stream(spkv_stream_t s) { return reinterpret_cast<cudaStream_t>(s); }
 float tau_to_logit(float tau);
 // per-layer linear predictors and local-only masks of a stack step, passed to kernels by value

@@ -820,6 +820,7 @@ extern "C" int spkv_norm_rope(const spkv_qk_norm_t *norm, const spkv_rope_t *rop
   }
   int sms = 0;
   if ((rc = device_sms(&sms))) return rc;
+  note_cacheless_call();
   return dispatch_rows(a, norm->dtype, false, sms, nullptr, nullptr, as_stream(stream));
 }
 
@@ -859,5 +860,6 @@ extern "C" int spkv_norm_rope_backward(const spkv_qk_norm_t *norm, const spkv_ro
   if ((rc = device_sms(&sms))) return rc;
   a.part = weights ? static_cast<float *>(d_workspace) : nullptr;
   if (!rows) a.Hq = a.Hkv = a.Hv = 0;
+  note_cacheless_call();
   return dispatch_rows(a, norm->dtype, true, sms, d_dwq, d_dwk, as_stream(stream));
 }

@@ -105,6 +105,7 @@ extern "C" int spkv_softgate_forward(int32_t T, int32_t n_q_heads, int32_t n_kv_
   a.gate2 = reinterpret_cast<const float *>(ws + w.off_gate);
   a.lse = d_lse_opt;
   cudaStream_t s = as_stream(stream);
+  note_cacheless_call();
   a.chained = T < 64;
   int rc = check_stream_error(launch_link(a.chained != 0, softgate_prepare_kernel, dim3(w.n_pages, n_kv_heads), dim3(64), 0, s,
                                           a, reinterpret_cast<float *>(ws + w.off_gate), alpha));

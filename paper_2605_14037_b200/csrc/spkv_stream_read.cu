@@ -95,6 +95,7 @@ extern "C" int spkv_wait_selftest(const void *d_buf, long long limit_clocks, int
   if (cudaFuncSetAttribute(wait_selftest_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageBytes + 64) !=
       cudaSuccess)
     return SPKV_E_CUDA;
+  note_cacheless_call();
   wait_selftest_kernel<<<1, 32, kPageBytes + 64, as_stream(stream)>>>(static_cast<const unsigned char *>(d_buf),
                                                                      limit_clocks, d_status);
   return check_stream_error(cudaGetLastError());
@@ -111,6 +112,7 @@ extern "C" int spkv_stream_read(const void *d_buf, size_t bytes, unsigned long l
     return SPKV_E_CUDA;
   if (cudaFuncSetAttribute(stream_read_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kReadSmem) != cudaSuccess)
     return SPKV_E_CUDA;
+  note_cacheless_call();
   stream_read_kernel<<<sms, 32, kReadSmem, as_stream(stream)>>>(static_cast<const unsigned char *>(d_buf), n_pages,
                                                                d_sink, d_status);
   return check_stream_error(cudaGetLastError());

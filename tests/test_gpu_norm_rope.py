@@ -366,3 +366,69 @@ def test_binding_refusals():
         spkv.spkv_norm_rope(nr, pos, odd, k)
     with pytest.raises(ValueError):
         spkv.make_norm_rope(4, 2, inv_freq=np.ones(3))
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_rows_go_straight_into_an_overlapping_cache(graph):
+    """SPKV_FLAG_OVERLAP: an append or decode behind the row call that writes its inputs waits for it.  All rows go
+    through the same three buffers, the batch's own last among 9000, so that a launch which did not wait would
+    find an earlier call's.  Against a twin that waits for the device between any two calls."""
+    spkv = load()
+    L, B, n, hq, hkv, T0 = 4, 8, 9000, 16, 4, 300
+    gen = torch.Generator(device=dev()).manual_seed(5)
+    rnd = lambda *shape: torch.randn(shape, generator=gen, device=dev())
+    caches = [spkv.Cache(L, B, hq, hkv, 1024, L * B * hkv * 8, window=64, tau=0.5, device=dev(), flags=spkv.FLAG_OVERLAP)
+              for _ in range(2)]
+    for l in range(L):
+        for s in range(B):
+            k, v, lg = rnd(T0, hkv, 128).bfloat16(), rnd(T0, hkv, 128).bfloat16(), rnd(T0, hkv)
+            for c in caches:
+                c.spkv_prefill(l, s, k, v, lg)
+    nr = spkv.make_norm_rope(hq, hkv)
+    qkv = [rnd(n, hq + 2 * hkv, 128).bfloat16() for _ in range(L + 1)]
+    lg = rnd(L, B, hkv)
+    pos = torch.arange(n, dtype=torch.int32, device=dev())
+    ids = torch.arange(B, dtype=torch.int32, device=dev())
+
+    def step(c, q, k, v, outs, between):
+        rows = lambda x: spkv.spkv_norm_rope(nr, pos, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], q, k, v)
+        for l in range(L):
+            rows(qkv[l])
+            between()
+            c.spkv_append_evict(l, ids, k[-B:], v[-B:], lg[l])
+            between()
+            rows(qkv[l + 1])
+            between()
+            c.spkv_decode_attention(l, ids, q[-B:], out=outs[l])
+            between()
+
+    results = []
+    for c, wait in zip(caches, (False, True)):
+        bufs = [torch.zeros((n, h, 128), dtype=torch.bfloat16, device=dev()) for h in (hq, hkv, hkv)]
+        once = torch.zeros((L, B, hq, 128), dtype=torch.bfloat16, device=dev())
+        c.decode_workspace(B)
+        torch.cuda.synchronize()
+        if graph and not wait:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                step(c, *bufs, once, lambda: None)
+        outs = []
+        for i in range(3):
+            if wait:
+                step(c, *bufs, once, torch.cuda.synchronize)
+            elif graph:
+                g.replay()
+            else:
+                step(c, *bufs, once, lambda: None)
+            outs.append(once.clone())
+            c.spkv_note_foreign_work()      # (the copy of the results)
+        c.check()
+        results.append(torch.stack(outs))
+    assert torch.equal(*results) and results[0].abs().max() > 0
+    for l in range(L):
+        assert np.array_equal(caches[0].spkv_read_lengths(l)[0], caches[1].spkv_read_lengths(l)[0])
+        for s in range(B):
+            for h in range(hkv):
+                for read in ("spkv_read_kept", "spkv_read_window"):
+                    a, b = (getattr(c, read)(l, s, h) for c in caches)
+                    assert all(np.array_equal(x, y) for x, y in zip(a, b))
