@@ -136,17 +136,19 @@ __device__ inline float load_weight(const void *w, int dtype, int i) {
 
 // Where lane j of a row finds its two chunks (element offsets).  Neighbouring lanes always read neighbouring chunks
 // (a lane with two chunks side by side would make every 32-byte sector two requests).  Pairs (i, i + rot/2):
-// chunks j and j + rot/2 of the rotated dims, the others in two halves likewise, rot = false; adjacent
-// pairs lie within a chunk, the row goes in two halves.
-struct LaneChunks { int c0, c1; bool live, rot; };
+// chunks j and j + rot/2 of the rotated dims, the others in two halves likewise, not rotated; adjacent
+// pairs lie within a chunk, the row goes in two halves.  A chunk is rotated as a whole or not at all (rot_dim is a
+// multiple of 16), and what is not rotated is not touched: times (1, 0) an infinity would reach its neighbour as NaN.
+struct LaneChunks { int c0, c1; bool live, rot0, rot1; };   // rot0, rot1: is the chunk rotated
 template <int CE>
 __device__ inline LaneChunks lane_chunks(const RowArgs &a, int j) {
   LaneChunks l;
   const int lanes = a.D / (2 * CE), n_rot = a.rope.interleaved ? lanes : a.rope.rot_dim / (2 * CE);
   l.live = j < lanes;
-  l.rot = j < n_rot;
-  if (l.rot) { l.c0 = j * CE; l.c1 = l.c0 + n_rot * CE; }
+  if (j < n_rot) { l.c0 = j * CE; l.c1 = l.c0 + n_rot * CE; }
   else { l.c0 = (n_rot + j) * CE; l.c1 = l.c0 + (lanes - n_rot) * CE; }
+  l.rot0 = l.c0 < a.rope.rot_dim;
+  l.rot1 = l.c1 < a.rope.rot_dim;
   return l;
 }
 // Place of pair p in a token's table of (cos, sin): pair e of lane j at ((e / 2) TPR + j) 2 + e % 2.
@@ -163,19 +165,17 @@ __device__ inline int pair_slot(const RowArgs &a, int p) {
   }
   return ((e >> 1) * TPR + j) * 2 + (e & 1);
 }
-// Pairs that the table holds: the rotated ones; with adjacent pairs every one, since a lane may have both kinds.
-template <bool kAdjacent>
-__device__ inline int table_pairs(const RowArgs &a) { return kAdjacent ? a.D / 2 : a.rope.rot_dim / 2; }
-
 // A lane's CE pairs: pair e is (f0[e], f1[e]), or with adjacent pairs the two elements of f2 number e of chunk 0,
 // then of chunk 1.  Angles as the rotation wants them: cosines c and sines s of pairs (2i, 2i + 1), or
 // with adjacent pairs of pair i alone (c = (cos, cos), s = (sin, sin)).
 template <int CE, bool kAdjacent> struct Angles { f2 c[kAdjacent ? CE : CE / 2], s[kAdjacent ? CE : CE / 2]; };
 
-// Rotates a lane's pairs in place; kBack: by the opposite angle (the transpose).
-template <int CE, bool kAdjacent, bool kBack>
-__device__ inline void rotate(f2 (&f0)[CE / 2], f2 (&f1)[CE / 2], const Angles<CE, kAdjacent> &a) {
+// Rotates the pairs of a lane's rotated chunks in place; kBack: by the opposite angle (the transpose); kAll: every
+// dim of the head is rotated (without the branches 8192 tokens take 39.3 us a call, with them 40.8).
+template <int CE, bool kAdjacent, bool kBack, bool kAll>
+__device__ inline void rotate(f2 (&f0)[CE / 2], f2 (&f1)[CE / 2], const Angles<CE, kAdjacent> &a, const LaneChunks &l) {
   if constexpr (!kAdjacent) {
+    if (!kAll && !l.rot0) return;   // (as rot1: the two chunks are each other's halves)
 #pragma unroll
     for (int i = 0; i < CE / 2; ++i) {
       const f2 lo = f0[i], hi = f1[i];
@@ -188,10 +188,13 @@ __device__ inline void rotate(f2 (&f0)[CE / 2], f2 (&f1)[CE / 2], const Angles<C
       const float sn = kBack ? -ss.x : ss.x;
       return pk(x.x * cc.x - x.y * sn, x.y * cc.x + x.x * sn);
     };
+    if (kAll || l.rot0) {
 #pragma unroll
-    for (int i = 0; i < CE / 2; ++i) {
-      f0[i] = turn(f0[i], a.c[i], a.s[i]);
-      f1[i] = turn(f1[i], a.c[CE / 2 + i], a.s[CE / 2 + i]);
+      for (int i = 0; i < CE / 2; ++i) f0[i] = turn(f0[i], a.c[i], a.s[i]);
+    }
+    if (kAll || l.rot1) {
+#pragma unroll
+      for (int i = 0; i < CE / 2; ++i) f1[i] = turn(f1[i], a.c[CE / 2 + i], a.s[CE / 2 + i]);
     }
   }
 }
@@ -230,13 +233,13 @@ __device__ inline float2 pair_angle(const RowArgs &a, int pos, uint64_t turn) {
   sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f, &sn, &cn);
   return make_float2(cn * a.rope.scale, sn * a.rope.scale);
 }
-// A lane's share of a token's table; (1, 0) where nothing is rotated.
+// A lane's share of a token's table (of its rotated chunks; the table holds no other pairs).
 template <int CE, int TPR, bool kAdjacent>
-__device__ inline void lane_angles(const float2 *tab, int j, bool rot, Angles<CE, kAdjacent> &out) {
+__device__ inline void lane_angles(const float2 *tab, int j, const LaneChunks &l, Angles<CE, kAdjacent> &out) {
 #pragma unroll
   for (int i = 0; i < CE / 2; ++i) {
     float4 v = make_float4(1.f, 0.f, 1.f, 0.f);
-    if (rot) v = *reinterpret_cast<const float4 *>(tab + (i * TPR + j) * 2);
+    if (!kAdjacent || i < CE / 4 ? l.rot0 : l.rot1) v = *reinterpret_cast<const float4 *>(tab + (i * TPR + j) * 2);
     if constexpr (kAdjacent) {
       out.c[2 * i] = pk(v.x, v.x); out.s[2 * i] = pk(v.y, v.y);
       out.c[2 * i + 1] = pk(v.z, v.z); out.s[2 * i + 1] = pk(v.w, v.w);
@@ -248,16 +251,14 @@ __device__ inline void lane_angles(const float2 *tab, int j, bool rot, Angles<CE
 }
 // Sines and cosines of one token, by one warp, and this lane's share of them.
 template <int CE, int TPR, bool kAdjacent>
-__device__ inline void token_angles(const RowArgs &a, Tables<CE, TPR> &t, int tok, bool rot, Angles<CE, kAdjacent> &out) {
+__device__ inline void token_angles(const RowArgs &a, Tables<CE, TPR> &t, int tok, const LaneChunks &l, Angles<CE, kAdjacent> &out) {
   const int lane = threadIdx.x & 31, j = threadIdx.x % TPR;
   float2 *tab = t.cs[threadIdx.x >> 5];
   __syncwarp();    // the previous token's angles have been read
-  for (int p = lane; p < table_pairs<kAdjacent>(a); p += 32) {
-    tab[pair_slot<CE, TPR, kAdjacent>(a, p)] =
-        p < a.rope.rot_dim / 2 ? pair_angle(a, __ldg(&a.pos[(size_t)t.axis[p] * a.n_tok + tok]), t.turn[p]) : make_float2(1.f, 0.f);
-  }
+  for (int p = lane; p < a.rope.rot_dim / 2; p += 32)
+    tab[pair_slot<CE, TPR, kAdjacent>(a, p)] = pair_angle(a, __ldg(&a.pos[(size_t)t.axis[p] * a.n_tok + tok]), t.turn[p]);
   __syncwarp();
-  lane_angles<CE, TPR, kAdjacent>(tab, j, rot, out);
+  lane_angles<CE, TPR, kAdjacent>(tab, j, l, out);
 }
 template <int CE, int TPR>
 __device__ inline void lane_weights(const float *w, int j, f2 (&w0)[CE / 2], f2 (&w1)[CE / 2]) {
@@ -408,26 +409,29 @@ __device__ inline void forward_side(const RowArgs &a, const spkv_rows_t &y, int 
   T *dst = row_ptr<T>(y, tok, work.head0 + sub);
   const int64_t out_step = work.step * y.head_stride;
   int h = work.head0 + sub;
+  auto passes = [&](auto all) {
 #pragma unroll 2
-  for (int i = 0; i < n_pass; ++i, h += work.step, dst += out_step) {
-    uint4 cur[1][2];
-    stream.take(cur);
-    if (!kCopy) {
-      f2 f0[CE / 2], f1[CE / 2];
-      unpack<T>(cur[0][0], f0);
-      unpack<T>(cur[0][1], f1);
-      if (normed) {
-        const float r = rsqrtf(row_sum<TPR>(dot<CE>(f0, f0, f1, f1)) * a.inv_d + a.eps);
-        const f2 rr = pk(r, r);
+    for (int i = 0; i < n_pass; ++i, h += work.step, dst += out_step) {
+      uint4 cur[1][2];
+      stream.take(cur);
+      if (!kCopy) {
+        f2 f0[CE / 2], f1[CE / 2];
+        unpack<T>(cur[0][0], f0);
+        unpack<T>(cur[0][1], f1);
+        if (normed) {
+          const float r = rsqrtf(row_sum<TPR>(dot<CE>(f0, f0, f1, f1)) * a.inv_d + a.eps);
+          const f2 rr = pk(r, r);
 #pragma unroll
-        for (int e = 0; e < CE / 2; ++e) { f0[e] = mul(f0[e], mul(rr, w0[e])); f1[e] = mul(f1[e], mul(rr, w1[e])); }
+          for (int e = 0; e < CE / 2; ++e) { f0[e] = mul(f0[e], mul(rr, w0[e])); f1[e] = mul(f1[e], mul(rr, w1[e])); }
+        }
+        rotate<CE, kAdjacent, false, decltype(all)::value>(f0, f1, ang, l);
+        cur[0][0] = pack<T>(f0);
+        cur[0][1] = pack<T>(f1);
       }
-      rotate<CE, kAdjacent, false>(f0, f1, ang);
-      cur[0][0] = pack<T>(f0);
-      cur[0][1] = pack<T>(f1);
+      store_row(dst, l, l.live && h < H, cur[0][0], cur[0][1]);
     }
-    store_row(dst, l, l.live && h < H, cur[0][0], cur[0][1]);
-  }
+  };
+  if (kCopy || a.rope.rot_dim == a.D) passes(std::true_type()); else passes(std::false_type());
 }
 
 template <class T, int TPR, bool kAdjacent>
@@ -443,7 +447,7 @@ __global__ void __launch_bounds__(kRowThreads, kFwdBlocks) norm_rope_kernel(cons
   fill_tables<CE, TPR>(a, tables);
   for (int64_t tok = work.first; tok < a.n_tok; tok += work.stride) {
     Angles<CE, kAdjacent> ang;
-    token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l.rot, ang);
+    token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l, ang);
     forward_side<T, TPR, kAdjacent, false>(a, a.y[0], a.Hq, stream.n_pass[0], a.norm & 1, tables.w[0], ang, tok, work, l, stream);
     forward_side<T, TPR, kAdjacent, false>(a, a.y[1], a.Hkv, stream.n_pass[1], (a.norm >> 1) & 1, tables.w[1], ang, tok, work, l, stream);
     forward_side<T, TPR, kAdjacent, true>(a, a.y[2], a.Hv, stream.n_pass[2], false, tables.w[0], ang, tok, work, l, stream);
@@ -475,14 +479,12 @@ __global__ void __launch_bounds__(kRowThreads, kFewBlocks) norm_rope_few_kernel(
   };
   const int first = blockIdx.y * kRows + sub, step = gridDim.y * kRows;
   fetch(first);
-  for (int p = threadIdx.x; p < table_pairs<kAdjacent>(a); p += kRowThreads)
-    s_cs[pair_slot<CE, TPR, kAdjacent>(a, p)] =
-        p < a.rope.rot_dim / 2 ? pair_angle(a, __ldg(&a.pos[(size_t)a.rope.axis[p] * a.n_tok + tok]), a.rope.turn[p])
-                               : make_float2(1.f, 0.f);
+  for (int p = threadIdx.x; p < a.rope.rot_dim / 2; p += kRowThreads)
+    s_cs[pair_slot<CE, TPR, kAdjacent>(a, p)] = pair_angle(a, __ldg(&a.pos[(size_t)a.rope.axis[p] * a.n_tok + tok]), a.rope.turn[p]);
   if (a.norm) fill_weights<CE, TPR>(a, s_w);
   __syncthreads();
   Angles<CE, kAdjacent> ang;
-  lane_angles<CE, TPR, kAdjacent>(s_cs, j, l.rot, ang);
+  lane_angles<CE, TPR, kAdjacent>(s_cs, j, l, ang);
 #pragma unroll 1
   for (int r = first; r - sub < n_rows; r += step) {   // (the same passes for all lanes: they shuffle)
     const int side = side_of(r);
@@ -503,7 +505,7 @@ __global__ void __launch_bounds__(kRowThreads, kFewBlocks) norm_rope_few_kernel(
         }
       }
       if (side < 2) {
-        rotate<CE, kAdjacent, false>(f0, f1, ang);
+        rotate<CE, kAdjacent, false, false>(f0, f1, ang, l);
         cur[0] = pack<T>(f0);
         cur[1] = pack<T>(f1);
       }
@@ -525,40 +527,43 @@ __device__ inline void backward_side(const RowArgs &a, const spkv_rows_t &y, int
   T *dst = row_ptr<T>(y, tok, work.head0 + sub);
   const int64_t out_step = work.step * y.head_stride;
   int h = work.head0 + sub;
-  for (int i = 0; i < n_pass; ++i, h += work.step, dst += out_step) {
-    uint4 cur[2][2];   // upstream gradients, inputs
-    stream.take(cur);
-    if (!kCopy) {
-      f2 f0[CE / 2], f1[CE / 2];
-      unpack<T>(cur[0][0], f0);
-      unpack<T>(cur[0][1], f1);
-      rotate<CE, kAdjacent, true>(f0, f1, ang);
-      if (normed) {
-        f2 u0[CE / 2], u1[CE / 2], w0[CE / 2], w1[CE / 2];
-        unpack<T>(cur[1][0], u0);
-        unpack<T>(cur[1][1], u1);
-        lane_weights<CE, TPR>(s_w, j, w0, w1);
-        const float r = rsqrtf(row_sum<TPR>(dot<CE>(u0, u0, u1, u1)) * a.inv_d + a.eps);
-        const f2 rr = pk(r, r);
+  auto passes = [&](auto all) {
+    for (int i = 0; i < n_pass; ++i, h += work.step, dst += out_step) {
+      uint4 cur[2][2];   // upstream gradients, inputs
+      stream.take(cur);
+      if (!kCopy) {
+        f2 f0[CE / 2], f1[CE / 2];
+        unpack<T>(cur[0][0], f0);
+        unpack<T>(cur[0][1], f1);
+        rotate<CE, kAdjacent, true, decltype(all)::value>(f0, f1, ang, l);
+        if (normed) {
+          f2 u0[CE / 2], u1[CE / 2], w0[CE / 2], w1[CE / 2];
+          unpack<T>(cur[1][0], u0);
+          unpack<T>(cur[1][1], u1);
+          lane_weights<CE, TPR>(s_w, j, w0, w1);
+          const float r = rsqrtf(row_sum<TPR>(dot<CE>(u0, u0, u1, u1)) * a.inv_d + a.eps);
+          const f2 rr = pk(r, r);
 #pragma unroll
-        for (int e = 0; e < CE / 2; ++e) {
-          u0[e] = mul(u0[e], rr);
-          u1[e] = mul(u1[e], rr);
-          dw0[e] = fma(f0[e], u0[e], dw0[e]);
-          dw1[e] = fma(f1[e], u1[e], dw1[e]);
-          f0[e] = mul(f0[e], w0[e]);
-          f1[e] = mul(f1[e], w1[e]);
+          for (int e = 0; e < CE / 2; ++e) {
+            u0[e] = mul(u0[e], rr);
+            u1[e] = mul(u1[e], rr);
+            dw0[e] = fma(f0[e], u0[e], dw0[e]);
+            dw1[e] = fma(f1[e], u1[e], dw1[e]);
+            f0[e] = mul(f0[e], w0[e]);
+            f1[e] = mul(f1[e], w1[e]);
+          }
+          const float m = -row_sum<TPR>(dot<CE>(f0, u0, f1, u1)) * a.inv_d;
+          const f2 mean = pk(m, m);
+#pragma unroll
+          for (int e = 0; e < CE / 2; ++e) { f0[e] = mul(rr, fma(u0[e], mean, f0[e])); f1[e] = mul(rr, fma(u1[e], mean, f1[e])); }
         }
-        const float m = -row_sum<TPR>(dot<CE>(f0, u0, f1, u1)) * a.inv_d;
-        const f2 mean = pk(m, m);
-#pragma unroll
-        for (int e = 0; e < CE / 2; ++e) { f0[e] = mul(rr, fma(u0[e], mean, f0[e])); f1[e] = mul(rr, fma(u1[e], mean, f1[e])); }
+        cur[0][0] = pack<T>(f0);
+        cur[0][1] = pack<T>(f1);
       }
-      cur[0][0] = pack<T>(f0);
-      cur[0][1] = pack<T>(f1);
+      store_row(dst, l, l.live && h < H, cur[0][0], cur[0][1]);
     }
-    store_row(dst, l, l.live && h < H, cur[0][0], cur[0][1]);
-  }
+  };
+  if (kCopy || a.rope.rot_dim == a.D) passes(std::true_type()); else passes(std::false_type());
 }
 
 // Backward.  A warp goes over its tokens once for the queries and once for keys and values, so that the sums of one
@@ -585,7 +590,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(cons
     if (!stream.any()) return;
     for (int64_t tok = work.first; tok < a.n_tok; tok += work.stride) {
       Angles<CE, kAdjacent> ang;
-      token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l.rot, ang);
+      token_angles<CE, TPR, kAdjacent>(a, tables, (int)tok, l, ang);
       backward_side<T, TPR, kAdjacent, false>(a, a.y[side], side ? a.Hkv : a.Hq, stream.n_pass[side], (a.norm >> side) & 1,
                                               tables.w[side], ang, tok, work, l, stream, dw0, dw1);
       if (side == 1)

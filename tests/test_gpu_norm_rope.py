@@ -432,3 +432,46 @@ def test_rows_go_straight_into_an_overlapping_cache(graph):
                 for read in ("spkv_read_kept", "spkv_read_window"):
                     a, b = (getattr(c, read)(l, s, h) for c in caches)
                     assert all(np.array_equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("n", [3, 700])          # both forward kernels
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype,D,rot", [("bf16", 128, 64), ("f32", 64, 16), ("f16", 96, 80), ("bf16", 48, 16), ("f32", 256, 0),
+                                         ("bf16", 128, 128)])
+def test_infinities_and_nans_stay_in_their_pair(n, interleaved, dtype, D, rot):
+    """Dims from rot_dim on are not rotated: what is there neither reaches another dim nor changes; a rotated dim
+    reaches its partner only.  Without norm, forward and backward, and values that are infinite in a normed row."""
+    spkv, dt = load(), DT[dtype]
+    gen = torch.Generator().manual_seed(D + rot)
+    x = torch.randn((n, 5, D), generator=gen).to(dt).to(dev())
+    pos = torch.arange(n, dtype=torch.int32, device=dev()) * 37 + 1
+    partner = lambda d: d if d >= rot else d ^ 1 if interleaved else (d + rot // 2) % rot
+    bad = x.clone()
+    hit = torch.zeros(x.shape, dtype=torch.bool, device=dev())
+    plant = [float("inf"), float("-inf"), float("nan"), -0.0]
+    for i, d in enumerate(sorted({0, rot // 2, rot - 1, rot, rot + 1, rot + (D - rot) // 2, D - 1, D - 2})):
+        if 0 <= d < D:
+            t, h = i % n, i % 5
+            bad[t, h, d] = plant[i % 4]
+            hit[t, h, d] = hit[t, h, partner(d)] = True
+    nr = spkv.make_norm_rope(4, 1, D, dt, norm=False, rot_dim=rot, interleaved=interleaved)
+    calls = (lambda y: spkv.spkv_norm_rope(nr, pos, y[:, :4], y[:, 4:]),
+             lambda y: spkv.spkv_norm_rope_backward(nr, pos, None, None, y[:, :4], y[:, 4:]))
+    for call in calls:
+        clean, got = (torch.cat(call(y)[:2], 1) for y in (x, bad))
+        assert torch.equal(got[~hit], clean[~hit])
+        bits = torch.int32 if dtype == "f32" else torch.int16
+        rest, want = got[..., rot:].contiguous(), bad[..., rot:].contiguous()
+        nan = want.isnan()
+        assert torch.equal(rest.isnan(), nan)
+        assert torch.equal(rest.view(bits)[~nan], want.view(bits)[~nan])        # bit for bit, -0 too
+        assert (torch.isnan(got) | torch.isinf(got))[..., :rot].sum() <= 2 * (~torch.isfinite(bad))[..., :rot].sum()
+    # an infinity in a normed row: 1 / sqrt(inf) = 0, so the row's other dims are zeros
+    d = D - 1
+    y = x.clone()
+    y[n - 1, 2, d] = float("inf")
+    nr = spkv.make_norm_rope(4, 1, D, dt, rot_dim=rot, interleaved=interleaved)
+    got = spkv.spkv_norm_rope(nr, pos, y[:, :4], y[:, 4:])[0][n - 1, 2]
+    others = torch.ones(D, dtype=torch.bool, device=dev())
+    others[d] = others[partner(d)] = False
+    assert got[d].isnan() and (got[others] == 0).all()
