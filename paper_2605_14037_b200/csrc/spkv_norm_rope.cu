@@ -541,7 +541,8 @@ __device__ inline void backward_side(const RowArgs &a, const spkv_rows_t &y, int
           unpack<T>(cur[1][0], u0);
           unpack<T>(cur[1][1], u1);
           lane_weights<CE, TPR>(s_w, j, w0, w1);
-          const float r = rsqrtf(row_sum<TPR>(dot<CE>(u0, u0, u1, u1)) * a.inv_d + a.eps);
+          const float r0 = rsqrtf(row_sum<TPR>(dot<CE>(u0, u0, u1, u1)) * a.inv_d + a.eps);
+          const float r = h < H ? r0 : 0.f;   // (lanes without a row hold zeros: with eps = 0 infinity times zero in dw)
           const f2 rr = pk(r, r);
 #pragma unroll
           for (int e = 0; e < CE / 2; ++e) {

@@ -475,3 +475,14 @@ def test_infinities_and_nans_stay_in_their_pair(n, interleaved, dtype, D, rot):
     others = torch.ones(D, dtype=torch.bool, device=dev())
     others[d] = others[partner(d)] = False
     assert got[d].isnan() and (got[others] == 0).all()
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (5, 1), (1, 1), (37, 7), (16, 16)])
+@pytest.mark.parametrize("dtype,n", [("bf16", 9), ("f32", 1), ("f16", 900), ("bf16", 3000)])
+def test_no_eps_and_head_counts_that_leave_lanes_idle(monkeypatch, hq, hkv, dtype, n):
+    """eps = 0: a lane without a row must not bring 0 * (1 / 0) into the weight gradients of the rows there are."""
+    monkeypatch.setitem(globals(), "EPS", 0.0)      # of the descriptor and of the formulas
+    c = Case(hq + n, n, hq, hkv, dtype=dtype)
+    assert c.nr.norm.eps == 0.0
+    check_forward(c, c.spkv.spkv_norm_rope(c.nr, c.pos_d, *c.x))
+    check_backward(c, c.spkv.spkv_norm_rope_backward(c.nr, c.pos_d, c.x[0], c.x[1], *c.g))
