@@ -398,10 +398,13 @@ class Cache:
     def spkv_share_plan(self, seq_ids, plan=None, stream=None):
         """The plan a batch with a common prefix decodes by (a device tensor; one for all layers and steps of
         the same sequences)."""
+        dev = self.arena.get_device()
         if plan is None:
-            plan = torch.zeros(lib().spkv_share_plan_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=self.device)
-        _check(lib().spkv_share_plan(self._h, _ptr(seq_ids, torch.int32), seq_ids.numel(), _ptr(plan, torch.uint8),
-                                     plan.numel(), _stream(stream)), "spkv_share_plan")
+            plan = torch.zeros(lib().spkv_share_plan_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=f"cuda:{dev}")
+        if seq_ids.get_device() != dev or plan.get_device() != dev:
+            raise ValueError("all tensors of a call live on the cache's device")
+        _check(_on_device(dev, stream, lib().spkv_share_plan, self._h, _ptr(seq_ids, torch.int32), seq_ids.numel(),
+                          _ptr(plan, torch.uint8), plan.numel()), "spkv_share_plan")
         return plan
 
     def spkv_decode_attention_shared(self, layer, seq_ids, q, plan, out=None, lse=None, sm_scale=None, want_lse=False,
@@ -522,8 +525,8 @@ class Cache:
         """Makes the empty sequences `dst` (host ints) continuations of sequence src (FLAG_FORK caches)."""
         import numpy as np
         ids = np.ascontiguousarray(np.asarray(list(dst), dtype=np.int32))
-        _check(lib().spkv_seq_fork(self._h, int(src), ids.ctypes.data if ids.size else None, int(ids.size),
-                                   _stream(stream)), "spkv_seq_fork")
+        _check(_on_device(self.arena.get_device(), stream, lib().spkv_seq_fork, self._h, int(src),
+                          ids.ctypes.data if ids.size else None, int(ids.size)), "spkv_seq_fork")
 
     def spkv_set_tau(self, tau):
         _check(lib().spkv_set_tau(self._h, tau), "spkv_set_tau")
