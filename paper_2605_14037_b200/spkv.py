@@ -169,24 +169,33 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _on_device(dev, stream, fn, *args):
-    """fn(*args, stream) with `dev` current (the caller's current device is put back)"""
+def _on_device(dev, fn, *args):
+    """fn(*args, dev's current stream) with `dev` current (the caller's current device is put back)"""
     if dev == _current_device():
-        return fn(*args, _raw_stream(dev) if stream is None else stream.cuda_stream)
+        return fn(*args, _raw_stream(dev))
     with torch.cuda.device(dev):
-        return fn(*args, _raw_stream(dev) if stream is None else stream.cuda_stream)
+        return fn(*args, _raw_stream(dev))
+
+
+def _under(stream, dev, call, *args):
+    """call(*args) with `stream` current: what the call allocates -- results, plan, workspace -- then comes from that
+    stream's memory.  (A block of another stream's may still have work in flight there.)"""
+    if stream.device_index != dev:
+        raise ValueError("the stream is on another device than the call's tensors")
+    with torch.cuda.stream(stream):
+        return call(*args)
 
 
 _capturing = torch.cuda.is_current_stream_capturing
 
 
-def _scratch(store, nbytes, dev, stream):
-    """Workspace of one call on `dev`: kept in `store` per stream (calls on two streams may run at once), replaced
-    when it is too small.  A call that is being captured gets one from its graph's memory pool, which no other
-    graph and no eager call uses."""
-    if stream is not None or dev != _current_device():
-        with torch.cuda.device(dev), torch.cuda.stream(stream):
-            return _scratch(store, nbytes, dev, None)
+def _scratch(store, nbytes, dev):
+    """Workspace of one call on `dev`'s current stream: kept in `store` per stream (calls on two streams may run at
+    once), replaced when it is too small.  A call that is being captured gets one from its graph's memory pool, which
+    no other graph and no eager call uses."""
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return _scratch(store, nbytes, dev)
     if _capturing():
         return torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
     key = (dev, _raw_stream(dev))
@@ -399,11 +408,13 @@ class Cache:
         """The plan a batch with a common prefix decodes by (a device tensor; one for all layers and steps of
         the same sequences)."""
         dev = self.arena.get_device()
+        if stream is not None:
+            return _under(stream, dev, self.spkv_share_plan, seq_ids, plan)
         if plan is None:
-            plan = torch.zeros(lib().spkv_share_plan_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=f"cuda:{dev}")
+            plan = torch.empty(lib().spkv_share_plan_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=f"cuda:{dev}")
         if seq_ids.get_device() != dev or plan.get_device() != dev:
             raise ValueError("all tensors of a call live on the cache's device")
-        _check(_on_device(dev, stream, lib().spkv_share_plan, self._h, _ptr(seq_ids, torch.int32), seq_ids.numel(),
+        _check(_on_device(dev, lib().spkv_share_plan, self._h, _ptr(seq_ids, torch.int32), seq_ids.numel(),
                           _ptr(plan, torch.uint8), plan.numel()), "spkv_share_plan")
         return plan
 
@@ -414,6 +425,8 @@ class Cache:
         B, cfg = seq_ids.shape[0], self.cfg
         shape = (B, cfg.n_q_heads, cfg.head_dim)
         dev = q.get_device()
+        if stream is not None:
+            return _under(stream, dev, self.spkv_decode_attention_shared, layer, seq_ids, q, plan, out, lse, sm_scale, want_lse)
 
         def check(t, dtype, want):
             if t.dtype is not dtype or t.shape != want or t.get_device() != dev or not t.is_contiguous():
@@ -436,8 +449,8 @@ class Cache:
         nbytes = self._shared_bytes.get(B)
         if nbytes is None:
             nbytes = self._shared_bytes[B] = lib().spkv_decode_shared_workspace_bytes(C.byref(cfg), B)
-        ws = _scratch(self._shared_ws, nbytes, dev, stream)
-        rc = _on_device(dev, stream, lib().spkv_decode_attention_shared, self._h, layer, seq_ids.data_ptr(), B, q.data_ptr(),
+        ws = _scratch(self._shared_ws, nbytes, dev)
+        rc = _on_device(dev, lib().spkv_decode_attention_shared, self._h, layer, seq_ids.data_ptr(), B, q.data_ptr(),
                         out.data_ptr(), None if lse is None else lse.data_ptr(),
                         self.default_scale if sm_scale is None else sm_scale, plan.data_ptr(), plan.numel(), ws.data_ptr(),
                         ws.numel())
@@ -524,9 +537,12 @@ class Cache:
     def spkv_seq_fork(self, src, dst, stream=None):
         """Makes the empty sequences `dst` (host ints) continuations of sequence src (FLAG_FORK caches)."""
         import numpy as np
+        dev = self.arena.get_device()
+        if stream is not None:
+            return _under(stream, dev, self.spkv_seq_fork, src, dst)
         ids = np.ascontiguousarray(np.asarray(list(dst), dtype=np.int32))
-        _check(_on_device(self.arena.get_device(), stream, lib().spkv_seq_fork, self._h, int(src),
-                          ids.ctypes.data if ids.size else None, int(ids.size)), "spkv_seq_fork")
+        _check(_on_device(dev, lib().spkv_seq_fork, self._h, int(src), ids.ctypes.data if ids.size else None, int(ids.size)),
+               "spkv_seq_fork")
 
     def spkv_set_tau(self, tau):
         _check(lib().spkv_set_tau(self._h, tau), "spkv_set_tau")
@@ -693,6 +709,8 @@ def spkv_norm_rope(nr, positions, q, k, v=None, q_out=None, k_out=None, v_out=No
     e.g. views of one fused projection), v handed on.  Returns (q_out, k_out, v_out), contiguous
     tensors unless given; v_out is None without v."""
     dev = q.get_device()
+    if stream is not None:
+        return _under(stream, dev, spkv_norm_rope, nr, positions, q, k, v, q_out, k_out, v_out)
     n, pos = _positions(nr, positions, dev)
     hq, hkv = nr.heads
     rq, rk = _row(nr, q, hq, n, dev, "q"), _row(nr, k, hkv, n, dev, "k")
@@ -708,7 +726,7 @@ def spkv_norm_rope(nr, positions, q, k, v=None, q_out=None, k_out=None, v_out=No
         v_out, ov = _row_out(nr, q, v_out, hkv, n, dev, "v_out")
         _SIX_ROWS.pack_into(io, 0, *rq, *rk, *_row(nr, v, hkv, n, dev, "v"), *oq, *ok, *ov)
         av, av_out = at + 2 * _ROW, at + 5 * _ROW
-    rc = _on_device(dev, stream, nr.forward, nr._n, nr._r, n, pos, at, at + _ROW, av, at + 3 * _ROW, at + 4 * _ROW, av_out)
+    rc = _on_device(dev, nr.forward, nr._n, nr._r, n, pos, at, at + _ROW, av, at + 3 * _ROW, at + 4 * _ROW, av_out)
     if rc:
         raise SpkvError(rc, "spkv_norm_rope")
     return q_out, k_out, v_out
@@ -720,6 +738,8 @@ def spkv_norm_rope_backward(nr, positions, q, k, q_grad, k_grad, v_grad=None, dq
     v_grad those of its outputs.  Returns (dq, dk, dv, dwq, dwk); dwq, dwk float32, None for a
     side without norm or weight_grads=False; dv None without v_grad."""
     dev = q_grad.get_device()
+    if stream is not None:
+        return _under(stream, dev, spkv_norm_rope_backward, nr, positions, q, k, q_grad, k_grad, v_grad, dq, dk, dv, weight_grads)
     n, pos = _positions(nr, positions, dev)
     (hq, hkv), D, normed = nr.heads, nr.head_dim, nr.norm.norm
     none = (0, 0, 0)
@@ -739,12 +759,12 @@ def spkv_norm_rope_backward(nr, positions, q, k, q_grad, k_grad, v_grad=None, dq
     ws, ws_bytes = None, 0
     if dwq is not None or dwk is not None:
         ws_bytes = nr.workspace_bytes
-        scratch = _scratch(nr._ws, ws_bytes, dev, stream)   # (alive until the launch is made)
+        scratch = _scratch(nr._ws, ws_bytes, dev)   # (alive until the launch is made)
         ws = scratch.data_ptr()
     io = (Rows * 8)()
     at = C.addressof(io)
     _EIGHT_ROWS.pack_into(io, 0, *xq, *xk, *gq, *gk, *gv, *yq, *yk, *yv)
-    rc = _on_device(dev, stream, nr.backward, nr._n, nr._r, n, pos, at, at + _ROW, at + 2 * _ROW, at + 3 * _ROW,
+    rc = _on_device(dev, nr.backward, nr._n, nr._r, n, pos, at, at + _ROW, at + 2 * _ROW, at + 3 * _ROW,
                     at + 4 * _ROW if v_grad is not None else None, at + 5 * _ROW, at + 6 * _ROW,
                     at + 7 * _ROW if v_grad is not None else None, None if dwq is None else dwq.data_ptr(),
                     None if dwk is None else dwk.data_ptr(), ws, ws_bytes)

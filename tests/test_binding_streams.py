@@ -1,8 +1,9 @@
-"""Which device the binding's calls run on when it is not the current one.  No GPU is needed: the library and
-CUDA's current device are stand-ins."""
+"""Where the binding's calls run and where their results come from: another device than the current one, another
+stream than the current one.  The device tests need no GPU (the library and CUDA's current device are stand-ins)."""
 import contextlib
 import ctypes as C
 
+import numpy as np
 import pytest
 import torch
 
@@ -88,3 +89,74 @@ def test_a_plan_of_another_devices_tensors_is_refused(spkv, two_devices):
         with pytest.raises(ValueError):
             cache.spkv_share_plan(ids, plan)
     assert not two_devices
+
+
+def test_a_stream_of_another_device_is_refused(spkv, two_devices):
+    cache, stream = a_cache(spkv, 1), type("S", (), dict(device_index=0, cuda_stream=7))()
+    ids, plan = Tensor((2,), torch.int32, 1, 4096), Tensor((1 << 16,), torch.uint8, 1, 8192)
+    q = Tensor((2, 4, 128), torch.bfloat16, 1, 4096)
+    nr = type("N", (), {})()
+    for call in (lambda: cache.spkv_share_plan(ids, plan, stream=stream), lambda: cache.spkv_seq_fork(0, [1], stream=stream),
+                 lambda: cache.spkv_decode_attention_shared(0, ids, q, plan, stream=stream),
+                 lambda: spkv.spkv_norm_rope(nr, ids, q, q, stream=stream),
+                 lambda: spkv.spkv_norm_rope_backward(nr, ids, q, q, q, q, stream=stream)):
+        with pytest.raises(ValueError):
+            call()
+    assert not two_devices
+
+
+# ---- on the GPU --------------------------------------------------------------------------------------
+def pool_of(t):
+    """The stream whose memory the tensor lies in."""
+    at = t.data_ptr()
+    return next(s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"])
+
+
+def forked(spkv, B=3, T0=900):
+    from gpu_util import Workload
+    from test_gpu_fork import feed, make
+    cache = make(spkv, n_seqs=B + 1, max_context=2048)
+    wl = Workload(2, T0, 1, 4, 2, (0.6, 1.0), cache.spkv_tau_logit())
+    feed(cache, wl, 0, 0, 0, 0, T0)
+    cache.spkv_seq_fork(0, range(1, B + 1))
+    cache.check()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    return cache, torch.arange(1, B + 1, dtype=torch.int32, device="cuda"), torch.randn((B, 4, 128), generator=gen, device="cuda").bfloat16()
+
+
+@pytest.mark.gpu
+def test_results_come_from_the_memory_of_the_calls_stream(spkv):
+    cache, ids, q = forked(spkv)
+    plan = cache.spkv_share_plan(ids)
+    w = torch.ones(128, device="cuda")
+    nr = spkv.make_norm_rope(4, 2, wq=w, wk=w)
+    pos = torch.arange(3, dtype=torch.int32, device="cuda")
+    k = q[:, :2].contiguous()
+    keep = [q.clone() for _ in range(8)]       # ... and the current stream has blocks of these sizes to give away
+    del keep
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    res = [cache.spkv_share_plan(ids, stream=s), *cache.spkv_decode_attention_shared(0, ids, q, plan, want_lse=True, stream=s),
+           *spkv.spkv_norm_rope(nr, pos, q, k, k, stream=s), *spkv.spkv_norm_rope_backward(nr, pos, q, k, q, k, k, stream=s)]
+    s.synchronize()
+    assert len(res) == 11 and all(pool_of(t) == s.cuda_stream for t in res)
+    ref = [*cache.spkv_decode_attention_shared(0, ids, q, plan, want_lse=True),
+           *spkv.spkv_norm_rope(nr, pos, q, k, k), *spkv.spkv_norm_rope_backward(nr, pos, q, k, q, k, k)]
+    assert all(torch.equal(a, b) for a, b in zip(res[1:], ref))
+    cache.check()
+
+
+@pytest.mark.gpu
+def test_a_plan_made_on_another_stream_is_not_cleared_behind_its_back(spkv):
+    """The current stream is busy while another makes the plan: nothing the binding puts on the current one may
+    reach the plan afterwards."""
+    cache, ids, q = forked(spkv)
+    want = cache.spkv_share_plan(ids).cpu().numpy().view(np.int32)[8:]
+    assert want.any()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    plan = cache.spkv_share_plan(ids, stream=s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert np.array_equal(plan.cpu().numpy().view(np.int32)[8:], want)
