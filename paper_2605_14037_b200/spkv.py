@@ -11,6 +11,8 @@ High level: ``Cache`` owns an arena tensor and workspaces and forwards to them.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import inspect
 import math
 import os
 import struct
@@ -186,6 +188,20 @@ def _under(stream, dev, call, *args):
         return call(*args)
 
 
+def _on_its_stream(call):
+    """A call that allocates results or workspaces, with the stream given to it made current (see _under)."""
+    at = list(inspect.signature(call).parameters).index("stream")
+
+    @functools.wraps(call)
+    def run(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            return call(*args, **kw)
+    return run
+
+
 _capturing = torch.cuda.is_current_stream_capturing
 
 
@@ -292,6 +308,7 @@ class Cache:
         self.default_scale = 1.0 / math.sqrt(self.cfg.head_dim)
         return self
 
+    @_on_its_stream
     def spkv_cache_checkpoint(self, buf=None, stream=None):
         """Saves metadata + ring pages into `buf` (allocated when None); returns the buffer."""
         n = lib().spkv_cache_checkpoint_bytes(self._h)
@@ -339,6 +356,7 @@ class Cache:
         return self._workspace("decode", lib().spkv_decode_workspace_bytes(C.byref(self.cfg), B))
 
     # -- hot path -----------------------------------------------------------------------
+    @_on_its_stream
     def spkv_score(self, pred, x, logits=None, flags=None, stream=None):
         n_tok = x.shape[0]
         if logits is None:
@@ -360,6 +378,7 @@ class Cache:
             _ptr(x, torch.bfloat16), _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16),
             _ptr(logits_out, torch.float32), _stream(stream)), "spkv_score_append_evict")
 
+    @_on_its_stream
     def spkv_decode_attention(self, layer, seq_ids, q, out=None, lse=None, sm_scale=None,
                               stream=None):
         B = seq_ids.numel()
@@ -373,6 +392,7 @@ class Cache:
             _stream(stream)), "spkv_decode_attention")
         return out
 
+    @_on_its_stream
     def spkv_decode_attention_f32(self, layer, seq_ids, q, out=None, out_f32=None, lse=None, sm_scale=None,
                                   stream=None):
         """spkv_decode_attention that also returns the rows before their rounding to bf16;
@@ -390,6 +410,7 @@ class Cache:
             _stream(stream)), "spkv_decode_attention_f32")
         return out, out_f32
 
+    @_on_its_stream
     def spkv_decode_attention_static(self, layer, seq_ids, q, out=None, lse=None, sm_scale=None,
                                      stream=None):
         """Same result as spkv_decode_attention, for callers that may not allocate device
@@ -458,6 +479,7 @@ class Cache:
             raise SpkvError(rc, "spkv_decode_attention_shared")
         return (out, lse) if want_lse else out
 
+    @_on_its_stream
     def spkv_prefill(self, layer, seq, k, v, logits, q=None, out=None, sm_scale=None, stream=None):
         Cn = k.shape[0]
         if q is not None and out is None:
@@ -470,6 +492,7 @@ class Cache:
             _stream(stream)), "spkv_prefill")
         return out
 
+    @_on_its_stream
     def spkv_decode_step_host(self, layer, pred, seq_ids, h_x, h_q, h_k, h_v, h_out, sm_scale=None,
                               stream=None):
         """Host (pinned) tensors in, host tensor out; enqueues the copies (on the cache's own
@@ -491,6 +514,7 @@ class Cache:
             self.default_scale if sm_scale is None else sm_scale, _ptr(st), st.numel(),
             _stream(stream)), "spkv_decode_step_host")
 
+    @_on_its_stream
     def spkv_decode_stack(self, preds, seq_ids, x, q, k, v, out=None, logits_out=None, lse=None, sm_scale=None,
                           stream=None):
         """One decode step of all layers from device tensors [L, B, ...]: the appends of every layer in
@@ -509,6 +533,7 @@ class Cache:
             "spkv_decode_stack")
         return out
 
+    @_on_its_stream
     def spkv_decode_stack_host(self, preds, seq_ids, h_x, h_q, h_k, h_v, h_out, sm_scale=None, stream=None):
         """One decode step of all layers from host (pinned) tensors [L, B, ...]; enqueues four
         copies in, the 2 L kernels and one copy out on the stream."""
@@ -607,6 +632,7 @@ class Cache:
         return pos[:n], k[:n], v[:n], lg[:n]
 
 
+@_on_its_stream
 def spkv_stream_read(buf, passes=5, stream=None):
     """Read-only HBM rate in GB/s: streams the uint8 tensor `buf` through spkv_stream_read
     `passes` times (after one warm-up pass), timed with CUDA events on the launching stream."""
@@ -776,6 +802,7 @@ def spkv_norm_rope_backward(nr, positions, q, k, q_grad, k_grad, v_grad=None, dq
 _softgate_ws = {}
 
 
+@_on_its_stream
 def spkv_softgate_forward(q, k, v, logits, window=128, alpha=0.0, tau=0.5, sm_scale=None, flags=0, out=None,
                           want_lse=False, stream=None, status=None):
     """Soft-gated whole-sequence forward (Eq. 6 / Eq. 7; see spkv.h).  q [T,Hq,128], k, v [T,Hkv,128]
@@ -805,6 +832,7 @@ def spkv_softgate_forward(q, k, v, logits, window=128, alpha=0.0, tau=0.5, sm_sc
     return (out, lse) if want_lse else out
 
 
+@_on_its_stream
 def spkv_wait_selftest(buf, limit_clocks, stream=None):
     """Runs the library's bounded-wait error path once (see spkv.h); returns the four status
     words [code, drained, clocks waited, data in place] as a list."""

@@ -160,3 +160,48 @@ def test_a_plan_made_on_another_stream_is_not_cleared_behind_its_back(spkv):
     s.synchronize()
     torch.cuda.synchronize()
     assert np.array_equal(plan.cpu().numpy().view(np.int32)[8:], want)
+
+
+@pytest.mark.gpu
+def test_the_other_calls_results_too(spkv):
+    cache, ids, q = forked(spkv)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    rnd = lambda *shape: torch.randn(shape, generator=gen, device="cuda").bfloat16()
+    T = 300
+    k, v, qs, lg = rnd(T, 2, 128), rnd(T, 2, 128), rnd(T, 4, 128), torch.randn((T, 2), generator=gen, device="cuda")
+    x, pred = rnd(3, 64), spkv.make_predictor(rnd(2, 64), torch.zeros(2, device="cuda"))
+    keep = [torch.empty_like(t) for t in (q, qs, x) for _ in range(4)]     # blocks the current stream can give away
+    del keep
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def results(stream):
+        r = [cache.spkv_score(pred, x, stream=stream), cache.spkv_decode_attention(0, ids, q, stream=stream),
+             *cache.spkv_decode_attention_f32(0, ids, q, None, None, None, None, stream),
+             cache.spkv_decode_attention_static(0, ids, q, stream=stream),
+             spkv.spkv_softgate_forward(qs, k, v, lg, stream=stream),
+             cache.spkv_cache_checkpoint(stream=stream), cache.spkv_prefill(0, 1, k, v, lg, qs, stream=stream)]
+        cache.spkv_cache_rollback(r[-2], stream=stream)
+        r.append(cache.spkv_decode_stack([pred], ids, x[None], q[None], k[None, :3], v[None, :3], stream=stream))
+        cache.spkv_cache_rollback(r[-3], stream=stream)
+        (stream or torch.cuda.current_stream()).synchronize()
+        return r
+
+    got = results(s)
+    assert all(pool_of(t) == s.cuda_stream for t in got)
+    assert all(torch.equal(a, b) for i, (a, b) in enumerate(zip(got, results(None))) if i != 6)
+    cache.check()
+
+
+@pytest.mark.gpu
+def test_soft_gated_forward_waits_for_its_own_stream(spkv):
+    """The device-side verdict is read behind the kernels of the stream the call was given."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    rnd = lambda *shape: torch.randn(shape, generator=gen, device="cuda").bfloat16()
+    q, k, v, lg = rnd(500, 4, 128), rnd(500, 2, 128), rnd(500, 2, 128), torch.randn((500, 2), generator=gen, device="cuda")
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+    spkv.spkv_softgate_forward(q, k, v, lg, stream=s)
+    assert s.query(), "the call returned before its kernels had run"
