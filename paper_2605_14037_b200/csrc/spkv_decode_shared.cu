@@ -172,7 +172,7 @@ __global__ void __maxnreg__(shp::kRegs) shared_prefix_kernel(SharedArgs a) {
     if (lane < n_pages) first_entry = ldcg_keep(&unit_table(c, trow)[j_begin + lane]);
     // (stale plan: the unit is shorter by now; the tail sees the same and nobody reads this share's result)
     const bool valid = len / kP >= common;
-    if (valid) first_entry = checked_page(c, first_entry, (int)ring_page(c, u, 0));
+    if (valid && lane < n_pages) first_entry = checked_page(c, first_entry, (int)ring_page(c, u, 0));   // (the others hold none)
     // the keys that the first scores need; the rest follows when Q is in place (every block's rings at once are 20 MB
     // of requests, behind which the tail's first look at its units would wait 3 us)
     for (int j = 0; j < kKeyLead && valid; ++j) {

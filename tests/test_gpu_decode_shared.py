@@ -522,3 +522,18 @@ def test_binding_refusals():
     for kw in (dict(out=torch.empty_like(qd)[:1]), dict(lse=torch.empty((2, 4), device=dev(), dtype=torch.float64))):
         with pytest.raises(ValueError):
             cache.spkv_decode_attention_shared(0, ids, qd, plan, **kw)
+
+
+@pytest.mark.parametrize("B,T0,m", [(2, 300, 1), (3, 1200, 40), (20, 4000, 3), (4, 100, 0)])
+def test_range_checks_find_nothing_in_a_sound_cache(B, T0, m):
+    """SPKV_FLAG_DEBUG_BOUNDS: shares of fewer pages than a warp has lanes, pieces of a unit's own pages, units without
+    any -- no index that nobody uses is reported, and the results are those without the flag."""
+    spkv = load()
+    outs = []
+    for flags in (0, spkv.FLAG_DEBUG_BOUNDS):
+        cache, wl, ids = build(spkv, B, 16, 2, T0, m, (0.4, 1.0), seed=B, flags=flags)
+        q, qd = queries(wl)
+        plan = cache.spkv_share_plan(ids)
+        outs.append(cache.spkv_decode_attention_shared(0, ids, qd, plan, want_lse=True))
+        assert cache.spkv_status() == 0
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
