@@ -537,3 +537,39 @@ def test_range_checks_find_nothing_in_a_sound_cache(B, T0, m):
         outs.append(cache.spkv_decode_attention_shared(0, ids, qd, plan, want_lse=True))
         assert cache.spkv_status() == 0
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+@pytest.mark.parametrize("B", [3, 20])
+@pytest.mark.parametrize("wide", [False, True])
+def test_roundings_of_weights_that_do_not_average_out(B, wide):
+    """Keys of three scores, so that all weights of a kind are rounded alike: the largest, whose weight is exact, with
+    values of zero, and two kinds whose fp16 weights are off by -1.87 and +1.80 times 2^-12 and whose values cancel.
+    fp16 has 11 significant bits: a weight is off by up to 2^-11 of itself (finfo.eps / 2), hence the output by up
+    to 2^-11 sum w|v|.  Two bf16 terms leave 2^-8 of 2^-8 of a weight.  A score is one exact product times
+    log2(e) / sqrt(128), 3 roundings of 2^-24 of at most 2; exponential 2^-22, sums 2^-20: below 2^-18 together."""
+    spkv = load()
+    T0, big, plus, minus = 6000, 1.0, 0.486328125, 0.515625
+    cache = make(spkv, n_seqs=B + 1, Hq=16, Hkv=2, pool=2 * (T0 // 64 + 2) + B * 8, max_context=T0 + 64,
+                 flags=spkv.FLAG_FORK | (spkv.FLAG_PREFILL_PV_BF16 if wide else 0))
+    wl = Workload(1, T0, 1, 16, 2, (1.0, 1.0), cache.spkv_tau_logit(), with_q=False)
+    kind = np.arange(T0) % 64
+    k = np.where(kind == 5, big, np.where(kind % 2 == 0, plus, minus)).astype(np.float32)
+    n_plus, n_minus = (kind % 2 == 0).sum(), ((kind % 2 == 1) & (kind != 5)).sum()
+    w = lambda x: np.exp(15.0 * (x - big) / math.sqrt(D))
+    v = np.where(kind == 5, 0.0, np.where(kind % 2 == 0, 1.0, -n_plus * w(plus) / (n_minus * w(minus)))).astype(np.float32)
+    keys = np.zeros((T0, 1, 2, D), np.float32)
+    keys[..., 0] = k[:, None, None]
+    wl.K, wl.V = synth.to_bf16_bits(keys), synth.to_bf16_bits(np.broadcast_to(v[:, None, None, None], keys.shape).copy())
+    feed(cache, wl, 0, 0, 0, 0, T0)
+    cache.spkv_seq_fork(0, range(1, B + 1))
+    ids = torch.arange(1, B + 1, dtype=torch.int32, device=dev())
+    q = np.zeros((B, 16, D), np.float32)
+    q[..., 0] = 15.0
+    q = synth.to_bf16_bits(q)
+    out = cache.spkv_decode_attention_shared(0, ids, to_dev_bf16(q), cache.spkv_share_plan(ids))
+    cache.check()
+    ref, wv, _, _ = reference(cache, 0, 1, 0, f64(q[0, :8]))
+    tol = 2.0 ** -8 * np.abs(ref) + ((2.0 ** -16 if wide else 2.0 ** -11) + 2.0 ** -18) * wv
+    err = np.abs(out.double().cpu().numpy().reshape(B, 2, 8, D) - ref)
+    assert np.abs(ref).max() < 2.0 ** -8 * wv.min(), "the values cancel"
+    assert (err <= tol).all(), (err / wv).max() * 2 ** 12
