@@ -165,7 +165,6 @@ __global__ void __launch_bounds__(256) share_cut_kernel(CacheView c, const int32
     rec[0] = lo;
     rec[1] = at;
     rec[2] = rec[3] = 0;
-    if (blockIdx.x == 0) plan[0] = sig;
   }
   __syncthreads();
   const int n_room = share_max_blocks(c.S, c.Hkv, c.G);

@@ -572,7 +572,7 @@ __device__ inline void backward_side(const RowArgs &a, const spkv_rows_t &y, int
 // alone: the result is the same every time.  Lanes that share columns are added up at the end, first
 // through shuffles, then through shared memory in warp order.
 template <class T, int TPR, bool kAdjacent>
-__global__ void __launch_bounds__(kRowThreads, 2) norm_rope_backward_kernel(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__(kRowThreads, kBwdBlocks) norm_rope_backward_kernel(const __grid_constant__ RowArgs a) {
   constexpr int CE = Elem<T>::kChunk;
   __shared__ Tables<CE, TPR> tables;
   __shared__ uint4 s_ring[kRowWarps][RowStream<T, TPR, 2>::kDepth * 128];

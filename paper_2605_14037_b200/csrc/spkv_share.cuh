@@ -1,6 +1,6 @@
 // What a batch with a common prefix decodes by: the plan's layout and the cut of the common pages.
 //
-// Plan (int32): header {signature, 0 ...}, then one record per layer:
+// Plan (int32): kSharePlanHdr words that nobody reads (records start at a multiple of 32 bytes), then one record per layer:
 //   {pages per share, blocks, 0, 0}
 //   per KV head  {common pages, first block, page-table row and unit of the batch's first sequence},
 //                {prefix shares, tail shares, signature, 0}
