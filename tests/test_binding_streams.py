@@ -205,3 +205,33 @@ def test_soft_gated_forward_waits_for_its_own_stream(spkv):
         torch.cuda._sleep(200_000_000)
     spkv.spkv_softgate_forward(q, k, v, lg, stream=s)
     assert s.query(), "the call returned before its kernels had run"
+
+
+@pytest.mark.gpu
+def test_calls_with_results_given_do_not_reach_the_allocator(spkv):
+    """Once a stream has its workspaces: row calls without weight gradients, plan, fork, reset and the shared-prefix call."""
+    cache, ids, q = forked(spkv)
+    nr = spkv.make_norm_rope(4, 2)
+    pos = torch.arange(3, dtype=torch.int32, device="cuda")
+    k = q[:, :2].contiguous()
+    qo, out = torch.empty_like(q), torch.empty_like(q)
+    ko, vo, lse = torch.empty_like(k), torch.empty_like(k), torch.empty(3, 4, device="cuda")
+    plan = cache.spkv_share_plan(ids)
+
+    def calls():
+        spkv.spkv_norm_rope(nr, pos, q, k, k, qo, ko, vo)
+        spkv.spkv_norm_rope_backward(nr, pos, q, k, q, k, k, qo, ko, vo, weight_grads=False)
+        cache.spkv_cache_reset_seq(2)
+        cache.spkv_seq_fork(0, [2])
+        cache.spkv_share_plan(ids, plan)
+        cache.spkv_decode_attention_shared(0, ids, q, plan, out=out, lse=lse)
+
+    calls()
+    torch.cuda.synchronize()
+    count = lambda: (torch.cuda.memory_stats()["allocation.all.allocated"], torch.cuda.mem_get_info()[0])
+    before = count()
+    for _ in range(5):
+        calls()
+    torch.cuda.synchronize()
+    assert count() == before
+    cache.check()

@@ -486,3 +486,25 @@ def test_no_eps_and_head_counts_that_leave_lanes_idle(monkeypatch, hq, hkv, dtyp
     assert c.nr.norm.eps == 0.0
     check_forward(c, c.spkv.spkv_norm_rope(c.nr, c.pos_d, *c.x))
     check_backward(c, c.spkv.spkv_norm_rope_backward(c.nr, c.pos_d, c.x[0], c.x[1], *c.g))
+
+
+@pytest.mark.parametrize("n", [5, 1500])         # both forward kernels
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_broadcast_rows(n, dtype):
+    """Rows that several tokens or heads share (stride 0), as inputs and as upstream gradients: the bits of the rows
+    written out; a gradient is one per token and head."""
+    c = Case(30 + n, n, 6, 2, dtype=dtype)
+    x, g = [t[:1, :1] for t in c.x], [t[:, :1] for t in c.g]
+    wide = lambda t, h: t.expand(n, h, c.D)
+    for i, form in enumerate((lambda t, h: wide(t, h), lambda t, h: wide(t[:, :1], h) if t.shape[0] > 1 else wide(t, h))):
+        xs, gs = [[form(t, h) for t, h in zip(ts, (6, 2, 2))] for ts in (x if i == 0 else [t[:, :1] for t in c.x], g)]
+        full = [[t.contiguous() for t in ts] for ts in (xs, gs)]
+        assert any(0 in t.stride() for t in xs) and any(0 in t.stride() for t in gs)
+        a, b = c.spkv.spkv_norm_rope(c.nr, c.pos_d, *xs), c.spkv.spkv_norm_rope(c.nr, c.pos_d, *full[0])
+        assert all(torch.equal(s, t) for s, t in zip(a, b))
+        a = c.spkv.spkv_norm_rope_backward(c.nr, c.pos_d, xs[0], xs[1], *gs)
+        b = c.spkv.spkv_norm_rope_backward(c.nr, c.pos_d, full[0][0], full[0][1], *full[1])
+        assert all(torch.equal(s, t) for s, t in zip(a, b))
+        c2 = Case(30 + n, n, 6, 2, dtype=dtype)      # ... and the formulas
+        c2.x, c2.g = tuple(full[0]), tuple(full[1])
+        check_backward(c2, a)
