@@ -15,14 +15,16 @@
 // instruction), and is rounded once on the way out.
 //
 // Angles.  A frequency is held as a fraction of a turn per position in 64-bit fixed point, so that
-// position * frequency modulo one turn is one exact integer product; what is left -- 32 bits of a turn -- goes
-// through sincospif.  Far positions lose nothing (in fp32 a position of 10^6 is 0.06 rad off).  A warp
+// position * frequency modulo one turn is one integer product without rounding; the upper 32 bits of that turn go
+// through sincospif as a float.  That float's rounding, 2^-25 of a half turn or 9.4e-8 rad, is the angle's error at every
+// position; the fraction's own (2^-64 turn, for |inv_freq| > 2 pi that many times more) times 2^31 positions and the bits
+// cut off add 3e-9 (in fp32 a position of 10^6 is 0.06 rad off).  A warp
 // computes the sines and cosines of a token once, through shared memory, for all its heads: no table
 // in memory, no position limit.
 //
 // What bounds it: bytes; each row is read and written once.  B200, device time: 8192 tokens of 32/8 heads, bf16, 201 MB:
-// 37.3 us = 5.4 TB/s (0.84 of the measured copy rate); backward of 32768 tokens, 1.14 GB: 191 us = 6.0 TB/s
-// (0.93).  With rows held in registers on their way 50 and 271 us: too few bytes in flight.  One token: 2.5 us,
+// 37.6 us = 5.4 TB/s (0.83 of the measured copy rate); backward of 32768 tokens, 1.14 GB: 181 us = 6.3 TB/s
+// (0.98).  With rows held in registers on their way 50 and 271 us: too few bytes in flight.  One token: 3.1 us,
 // a launch and three trips to memory.
 #include <math.h>
 
@@ -171,16 +173,18 @@ __device__ inline int pair_slot(const RowArgs &a, int p) {
 template <int CE, bool kAdjacent> struct Angles { f2 c[kAdjacent ? CE : CE / 2], s[kAdjacent ? CE : CE / 2]; };
 
 // Rotates the pairs of a lane's rotated chunks in place; kBack: by the opposite angle (the transpose); kAll: every
-// dim of the head is rotated (without the branches 8192 tokens take 39.3 us a call, with them 40.8).
+// dim of the head is rotated, nothing to select (8192 tokens of 32/8 heads 37.7 us on the device; half of the dims
+// rotated 42.0, the selects take 2.6 of it; with a branch in their place the same, and 1001 fp32 tokens 10.1 instead of 9.9).
 template <int CE, bool kAdjacent, bool kBack, bool kAll>
 __device__ inline void rotate(f2 (&f0)[CE / 2], f2 (&f1)[CE / 2], const Angles<CE, kAdjacent> &a, const LaneChunks &l) {
   if constexpr (!kAdjacent) {
-    if (!kAll && !l.rot0) return;   // (as rot1: the two chunks are each other's halves)
 #pragma unroll
     for (int i = 0; i < CE / 2; ++i) {
       const f2 lo = f0[i], hi = f1[i];
-      f0[i] = kBack ? fma(lo, a.c[i], mul(hi, a.s[i])) : sub(mul(lo, a.c[i]), mul(hi, a.s[i]));
-      f1[i] = kBack ? sub(mul(hi, a.c[i]), mul(lo, a.s[i])) : fma(hi, a.c[i], mul(lo, a.s[i]));
+      const f2 x = kBack ? fma(lo, a.c[i], mul(hi, a.s[i])) : sub(mul(lo, a.c[i]), mul(hi, a.s[i]));
+      const f2 y = kBack ? sub(mul(hi, a.c[i]), mul(lo, a.s[i])) : fma(hi, a.c[i], mul(lo, a.s[i]));
+      f0[i] = kAll || l.rot0 ? x : lo;   // (rot0 as rot1: the two chunks are each other's halves)
+      f1[i] = kAll || l.rot0 ? y : hi;
     }
   } else {
     auto turn = [](f2 v, f2 c, f2 s) {   // (lo, hi) -> (lo c - hi s, hi c + lo s)
