@@ -275,8 +275,9 @@ int spkv_set_head_tau(spkv_cache_t *cache, int32_t layer, int32_t kv_head, float
  *     (y_lo, y_hi) -> scale * (y_lo cos t - y_hi sin t,  y_hi cos t + y_lo sin t)
  * for each rotated pair, t = position[axis of the pair][token] * inv_freq[pair]; dims from rot_dim on
  * are not rotated, value rows are handed on unchanged.  Sums and products are float32, each result is
- * rounded once.  Angles are exact for every int32 position (negative ones too): a frequency is held
- * as a 64-bit fraction of a turn and the product is taken modulo one turn. */
+ * rounded once.  Far positions cost no accuracy: a frequency is held as a 64-bit fraction of a turn and its product
+ * with the position is taken modulo one turn, so at every int32 position (negative ones too) an angle is off by at most
+ * 1e-7 + 2e-10 |inv_freq| radians.  What is not rotated is not touched (infinities, NaN and -0 included). */
 enum { SPKV_BF16 = 0, SPKV_F16 = 1, SPKV_F32 = 2 };
 enum { SPKV_NORM_Q = 1, SPKV_NORM_K = 2 };
 #define SPKV_MAX_ROW_DIM 256
@@ -312,7 +313,7 @@ typedef struct {
   int32_t head_dim;           /* a multiple of 16 up to SPKV_MAX_ROW_DIM (the cache itself takes 128)    */
   int32_t n_q_heads, n_kv_heads;   /* either may be 0: that side's tensors are then ignored              */
   int32_t norm;               /* OR of SPKV_NORM_Q, SPKV_NORM_K; 0 = rotation only                       */
-  float eps;
+  float eps;                  /* >= 0; with 0 a row of zeros becomes NaN, as 0 / 0 does                  */
   const void *d_wq, *d_wk;    /* [head_dim] device, NULL = ones                                          */
 } spkv_qk_norm_t;
 

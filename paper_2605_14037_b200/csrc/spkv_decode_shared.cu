@@ -7,8 +7,9 @@
 //   tail    what is left of every unit, its own pages and its ring: one small block per unit (several for a long
 //           one), mma.sync tiles of the unit's G query heads as in the decode kernel; leaves (m, l, O) too;
 //   merge   joins a row's parts by their log-sum-exp weights.
-// The tail does not depend on the prefix launch.  Its blocks are small (4 warps, two page buffers), so that
-// one fits on an SM beside a prefix block, and are launched as programmatic dependents: the prefix
+// The tail does not depend on the prefix launch.  Its blocks are small (4 warps, two page buffers), so that with up to 8
+// query heads per KV head (96 registers a thread) one fits on an SM beside a prefix block; with 9 - 16 (168 registers)
+// it does not and the tail runs as the prefix blocks leave.  They are launched as programmatic dependents: the prefix
 // kernel has waited for everything earlier on the stream before it lets them start.
 // The tail launch is not complete before the prefix launch is, so that the merge, which waits for the tail,
 // may read both.
@@ -17,6 +18,10 @@
 // in registers (thread = row = TMEM lane), P in fp16 back over the scores, O += P V with the page's values
 // rescaled to fp16 by converter warps, or two bf16 terms for a unit of wide-ranging values
 // (value_scale).  No masks: common pages are full and every query sees all of them.
+// One fp16 term: a weight is rounded by at most 2^-11 of itself, so an output by at most 2^-11 sum w|v| before its own
+// rounding to bf16 (2^-8), and by far less where roundings average out.  Two bf16 terms (2^-16, what the tail's
+// mma.sync tiles take) would double P.V's MMAs and P's stores in the chain that bounds the kernel;
+// SPKV_FLAG_PREFILL_PV_BF16 asks for them.
 //   * More than 128 rows in the tile (kAlt = false): slot h holds rows [128 h, 128 h + 128), both walk
 //     every page.
 //   * At most 128 rows (kAlt): both slots hold the same rows and take alternate pages, which halves the
@@ -28,10 +33,10 @@
 // conversion.  All waits are bounded.
 //
 // What bounds it (B200; device time of a call in a graph, three caches in turn): up to 128 rows, memory while the pages
-// stream (8 sequences of 64/8 heads on 65536 common tokens, 59 MB: 19.1 us, of which 10 at 5.8 TB/s, 3 until
+// stream (8 sequences of 64/8 heads on 65536 common tokens, 59 MB: 19.6 us, of which 10 at 5.8 TB/s, 3 until
 // the first scores, 6 for the end of the tail and the merge); beyond, the chain scores -> softmax -> P -> MMA
 // (2050 cycles per page and 256 rows; the tensor pipe is busy half of that) and then the tail's mma.sync tiles, which
-// get little of the tensor pipe beside the prefix (64 sequences of 32/8 heads on 131072: 37.7 us).
+// get little of the tensor pipe beside the prefix (64 sequences of 32/8 heads on 131072: 36.9 us).
 #include <algorithm>
 #include <atomic>
 #include <math.h>
@@ -43,7 +48,8 @@ namespace spkv {
 
 namespace shp {
 // Sixteen warps, four on each of the SM's register files: at 104 registers a thread a tail block of four warps of
-// 96 finds room beside them (with 13 warps of 128 one file was full, and the tail ran after the prefix).
+// 96 finds room beside them (with 13 warps of 128 one file was full, and the tail ran after the prefix).  At 104 the two
+// prefix kernels spill 36 and 68 bytes a thread.
 // (Two converter warps instead of four, or the MMA warps on other schedulers: within 2 %.)
 constexpr int kThreads = 512, kRegs = 104;
 constexpr int kMmaWarp0 = 0, kLoaderWarp = 1, kMmaWarp1 = 2, kTmemWarp = 3;

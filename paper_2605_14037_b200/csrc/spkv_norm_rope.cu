@@ -23,8 +23,8 @@
 // in memory, no position limit.
 //
 // What bounds it: bytes; each row is read and written once.  B200, device time: 8192 tokens of 32/8 heads, bf16, 201 MB:
-// 37.6 us = 5.4 TB/s (0.83 of the measured copy rate); backward of 32768 tokens, 1.14 GB: 181 us = 6.3 TB/s
-// (0.98).  With rows held in registers on their way 50 and 271 us: too few bytes in flight.  One token: 3.1 us,
+// 37.4 us = 5.4 TB/s (0.84 of the measured copy rate); backward of 32768 tokens, 1.14 GB: 185 us = 6.2 TB/s
+// (0.96).  With rows held in registers on their way 50 and 271 us: too few bytes in flight.  One token: 2.9 us,
 // a launch and three trips to memory.
 #include <math.h>
 
@@ -173,8 +173,8 @@ __device__ inline int pair_slot(const RowArgs &a, int p) {
 template <int CE, bool kAdjacent> struct Angles { f2 c[kAdjacent ? CE : CE / 2], s[kAdjacent ? CE : CE / 2]; };
 
 // Rotates the pairs of a lane's rotated chunks in place; kBack: by the opposite angle (the transpose); kAll: every
-// dim of the head is rotated, nothing to select (8192 tokens of 32/8 heads 37.7 us on the device; half of the dims
-// rotated 42.0, the selects take 2.6 of it; with a branch in their place the same, and 1001 fp32 tokens 10.1 instead of 9.9).
+// dim of the head is rotated, nothing to select (timed in turn on the device: 8192 tokens of 32/8 heads 37.7 us, half of the
+// dims rotated 42.0, of which the selects take 2.6; with a branch in their place the same, but 1001 fp32 tokens 10.1, not 9.9).
 template <int CE, bool kAdjacent, bool kBack, bool kAll>
 __device__ inline void rotate(f2 (&f0)[CE / 2], f2 (&f1)[CE / 2], const Angles<CE, kAdjacent> &a, const LaneChunks &l) {
   if constexpr (!kAdjacent) {

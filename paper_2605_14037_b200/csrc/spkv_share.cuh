@@ -19,7 +19,7 @@ namespace spkv {
 constexpr int kSharePlanHdr = 8, kShareHdr = 4, kShareHead = 8, kShareDesc = 8;
 constexpr int kShareRows = 256;       // query rows per block: two slots of 128
 constexpr int kMinSharedPages = 1;    // fewer common pages than this are read per sequence
-constexpr int kMinSharePages = 2;     // a share is not cut shorter (2 sequences on 4096 tokens: 10.5 us a call, 10.9 with 4)
+constexpr int kMinSharePages = 2;     // a share is not cut shorter (2 sequences on 4096 tokens: 10.4 us on the device, 10.9 with 4)
 constexpr int kTailPages = 8;         // a unit's own pages are cut into pieces of about this many, more while SMs are left
 constexpr int kTailMinPages = 2;      // ... not into shorter ones than this
 constexpr int kMaxTailItems = 1024;   // ... and not into more pieces than this, all units together
