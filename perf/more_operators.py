@@ -3,6 +3,8 @@
   tree    attention of a tree of drafted tokens over the cache: every node sees what its path from the root would
           have left it -- the pairs kept before, those of the window that are still in its own window or
           pass the threshold, and its ancestors
+  logprobs  what a model's logits say of given tokens: their log probabilities, the rows' entropies and the likeliest
+          alternatives
   accept  the path of a tree that the target's tokens confirm, and the token behind it
   step    a step as it is used: the drafts of the last tree that were accepted join the cache in every layer,
           then the new tree attends, layer by layer
@@ -20,6 +22,8 @@ own = False
 DEV = "cuda:0"
 D, TAU = 128, 0.5
 VOCAB = 32000
+DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+BYTES = {"bf16": 2, "f16": 2, "f32": 4}
 
 
 # ---- cases -------------------------------------------------------------------------------------
@@ -32,6 +36,12 @@ def _tree(name, b, ctx, nodes, hq, hkv, mean, shape="tree", ragged=False, window
 
 def _accept(name, b, nodes, shape="tree", ragged=False):
     return {"name": name, "op": "accept", "b": b, "nodes": nodes, "shape": shape, "ragged": ragged}
+
+
+def _logprobs(name, rows, vocab, top, given=1, dtype="bf16", pad=0, scale=1.0):
+    """rows of `vocab` logits (pad: behind each row, as a padded projection leaves them), `given` tokens of each looked up."""
+    return {"name": name, "op": "logprobs", "rows": rows, "vocab": vocab, "top": top, "given": given, "dtype": dtype, "pad": pad,
+            "scale": scale}
 
 
 def listed():
@@ -48,6 +58,9 @@ def listed():
         _tree("tree 13 x ragged 20000, 27 nodes", 13, 20000, 27, 20, 4, 0.25, ragged=True),
         # a wide model with the largest trees: many query rows a key
         _tree("tree 8 x 65536, 64 nodes", 8, 65536, 64, 64, 8, 0.15),
+        # the rows of one small tree at an odd vocabulary, with alternatives; those of a large batch of trees
+        _logprobs("logprobs 5 x 50257 f32, top 5", 5, 50257, 5, given=3, dtype="f32", scale=1.25),
+        _logprobs("logprobs 768 x 128256, top 1", 768, 128256, 1),
         # one tree, and a large batch of the largest
         _accept("accept 1 x 8", 1, 8),
         _accept("accept 500 x 64, ragged", 500, 64, ragged=True),
@@ -67,16 +80,21 @@ def _cost(c):
 
 
 def draw(rng):
-    op = rng.choice(["tree", "tree", "tree", "accept", "step", "step"])
+    op = rng.choice(["tree", "tree", "tree", "logprobs", "logprobs", "accept", "step", "step"])
     shape, ragged = rng.choice(["tree", "tree", "chain"]), rng.random() < 0.4
     if op == "accept":
         c = _accept("", _log(rng, 1, 500), _log(rng, 2, 64), shape, ragged)
+    elif op == "logprobs":
+        c = _logprobs("", _log(rng, 1, 1000), _log(rng, 500, 200000), rng.choice([0, 1, 1, 5, 20]), rng.choice([1, 1, 4, 33]),
+                      rng.choice(["bf16", "bf16", "f16", "f32"]), rng.choice([0, 0, 7, 64]), rng.choice([1.0, 0.7]))
+        while c["rows"] * c["vocab"] * BYTES[c["dtype"]] > 768 * 128256 * 2:
+            c["rows"] = c["rows"] * 2 // 3
     else:
         hkv = rng.choice([1, 2, 4, 8])
         c = _tree("", _log(rng, 1, 64), _log(rng, 20, 131072), _log(rng, 1, 64), hkv * rng.choice([1, 3, 4, 5, 8, 16]), hkv,
                   round(rng.uniform(0.05, 0.4), 3), shape, ragged, rng.choice([32, 128, 128, 200]), op,
                   1 if op == "tree" else rng.choice([1, 2, 4]))
-        top = [_cost(x) for x in listed() if x["op"] != "accept"]
+        top = [_cost(x) for x in listed() if x["op"] in ("tree", "step")]
         while any(v > max(t[i] for t in top) for i, v in enumerate(_cost(c))):   # no dearer than the largest listed
             c["ctx"] = c["ctx"] * 2 // 3
     del c["name"]
@@ -133,6 +151,17 @@ def _draft(c, seed):
     return {k: v.to(DEV) for k, v in s.items()}
 
 
+def _scores(c, seed):
+    """Logits as a model gives them: a few tokens far above the rest; one in sixteen of the vocabulary ruled out."""
+    g = _gen(seed)
+    n, v = c["rows"], c["vocab"]
+    x = 2.5 * torch.randn((n, v + c["pad"]), generator=g, device=DEV)
+    x[:, :v // 50] += 4.0
+    x = torch.where(torch.rand((1, v + c["pad"]), generator=g, device=DEV) < 1 / 16, -math.inf, x).to(DTYPES[c["dtype"]])
+    given = torch.randint(0, v, (n, c["given"]), generator=g, device=DEV, dtype=torch.int32)
+    return {"c": c, "x": x[:, :v], "given": given}
+
+
 def _raw(c, seed):
     """Raw tokens of the contexts (per layer, per sequence [t, hkv, 128]) and the drafts' rows.  A logit >= 0 means
     utility >= 0.5, the threshold."""
@@ -168,8 +197,8 @@ def _raw(c, seed):
 
 # ---- state -------------------------------------------------------------------------------------
 def prepare(case, seed):
-    if case["op"] == "accept":
-        s = {"c": case, "new": _draft(case, seed)}
+    if case["op"] in ("accept", "logprobs"):
+        s = {"c": case, "new": _draft(case, seed)} if case["op"] == "accept" else _scores(case, seed)
         if own:
             from paper_2605_14037_b200 import spkv
             s["spkv"] = spkv
@@ -235,9 +264,11 @@ def run(s):
 
 
 def _run_own(s):
-    c, new, old = s["c"], s["new"], s.get("old")
+    c, new, old = s["c"], s.get("new"), s.get("old")
     if c["op"] == "accept":
         return s["spkv"].spkv_tree_accept(new["tokens"], new["target"], new["parent"], new["n"])
+    if c["op"] == "logprobs":
+        return s["spkv"].spkv_token_logprobs(s["x"], s["given"], top=c["top"], scale=c["scale"])
     cache, got = s["cache"], ()
     if c["op"] == "step":
         cache.spkv_cache_rollback(s["before"])           # (so that the step can be made again)
@@ -251,12 +282,36 @@ def _run_own(s):
 
 
 def _run_plain(s):
-    c, new, old = s["c"], s["new"], s.get("old")
+    c, new, old = s["c"], s.get("new"), s.get("old")
     if c["op"] == "accept":
         return _plain_accept(c, new)
+    if c["op"] == "logprobs":
+        return _plain_logprobs(c, s["x"], s["given"])
     got = _plain_accept(c, old) if c["op"] == "step" else ()
     outs = [_plain_tree(c, s["cache"][l], x, new, None if old is None else (old, l) + got) for l, x in enumerate(s["drafts"])]
     return (torch.stack([o for o, _ in outs]), torch.stack([l for _, l in outs])) + got
+
+
+def _plain_logprobs(c, x, given):
+    """(log sum of exponentials, log probabilities of the given tokens, entropy, likeliest tokens, their log probabilities)"""
+    z = x.float() * c["scale"]
+    m = z.amax(1, keepdim=True)
+    t = z - m
+    e = t.exp()
+    total = e.sum(1, dtype=torch.float64)
+    weighed = (e * t.clamp(min=-1e4)).sum(1, dtype=torch.float64)
+    lse = m[:, 0].double() + total.log()
+    logp = z.gather(1, given.long()) - lse[:, None]
+    at = torch.arange(z.shape[1], device=DEV)
+    ids, tops = [], []
+    for _ in range(c["top"]):
+        best = z.amax(1, keepdim=True)
+        i = torch.where(z == best, at, z.shape[1]).amin(1, keepdim=True)      # ties: the lowest
+        ids.append(i)
+        tops.append(best - lse[:, None])
+        z = z.scatter(1, i, -math.inf)
+    return (lse.float(), logp.float(), (total.log() - weighed / total).float(),
+            torch.cat(ids, 1).int() if ids else None, torch.cat(tops, 1).float() if ids else None)
 
 
 def _plain_accept(c, d):
@@ -330,6 +385,9 @@ def _plain_tree(c, z, x, new, commit):
 def work(c):
     if c["op"] == "accept":
         return {"bytes": c["b"] * (4 * 4 * c["nodes"] + 12), "flops": 2 * c["b"] * c["nodes"]}
+    if c["op"] == "logprobs":
+        n = c["rows"] * c["vocab"]
+        return {"bytes": n * BYTES[c["dtype"]] + c["rows"] * (8 + 8 * c["given"] + 8 * c["top"]), "flops": 6 * n}
     w, rates, g = c["window"], _rates(c), c["hq"] // c["hkv"]
     size = flops = 0.0
     for t, n in zip(_lengths(c), _nodes(c)):
@@ -345,6 +403,12 @@ def work(c):
 def exact(case, seed):
     if case["op"] == "accept":
         return None
+    if case["op"] == "logprobs":
+        s = _scores(case, seed)
+        z = s["x"].double() * case["scale"]
+        logp = torch.log_softmax(z, 1)
+        top = logp.topk(case["top"], 1).values if case["top"] else None
+        return (torch.logsumexp(z, 1), logp.gather(1, s["given"].long()), -torch.special.xlogy(logp.exp(), logp.exp()).sum(1), None, top)
     c, s = case, _raw(case, seed)
     w, g, n = c["window"], c["hq"] // c["hkv"], c["nodes"]
     out = torch.zeros((c["layers"], c["b"], n, c["hq"], D), dtype=torch.float64, device=DEV)
