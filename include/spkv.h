@@ -458,6 +458,81 @@ int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, const int32
                                  const void *d_q, void *d_out, float *d_lse_opt, float sm_scale, const void *d_plan,
                                  size_t plan_bytes, void *d_workspace, size_t workspace_bytes, spkv_stream_t stream);
 
+/* ---- drafted tokens (speculative decoding) ----------------------------------------------------- */
+
+/* (No counterpart in the paper.)  A drafted tree: up to SPKV_MAX_DRAFT tokens per sequence that may follow what it has
+ * received.  Sequence b has n[b] nodes, 0 <= n[b] <= T <= SPKV_MAX_DRAFT; node i hangs on node parent[b][i] < i, or
+ * directly on the context (-1).  Its depth d is the number of its ancestors, its position t + d, where t is the number
+ * of pairs the sequence has received.  Per-token arrays are laid out [B][T]; d_parent NULL stands for chains
+ * (parent i - 1), d_n_nodes NULL for T nodes each.  A count outside [0, T] is taken for the nearest in it and a parent
+ * outside [-1, i) for -1; the calls that take a cache record SPKV_E_BOUNDS in its status for either. */
+#define SPKV_MAX_DRAFT 64
+
+/* Attention of the drafted nodes over the cache and their ancestors, for the verification of drafts: out[b, i, j] is
+ * what spkv_decode_attention would return for query j of node i, had the pairs of the node's path (its ancestors and
+ * itself) been appended one by one with spkv_append_evict before (and every page been there that this takes).  So
+ * node i at position p sees the compact cache; of the window and of its path the pairs at positions > p - w; and of
+ * those further back the ones whose logit passes the threshold in force, sink positions always, none with a head
+ * declared local-only.  Pairs that a node does not see do not touch its result, infinities and NaN included; an infinite or
+ * NaN value that it sees goes into it with its weight.  Scores are float32, weights two bf16 terms (2^-16).
+ * The cache is only read.
+ *   q: token (b, i) = b T + i, n_q_heads heads; k, v: the nodes' own pairs, n_kv_heads heads; bf16 rows as in
+ *   spkv_norm_rope (16-byte aligned, strides multiples of 8 elements), so heads of a fused projection are read in place.
+ *   d_logits [B][T][n_kv_heads] float32: utility logits of the nodes; may be NULL when T <= window (no node then
+ *   leaves the window of another).
+ *   -> d_out [B][T][n_q_heads][128] bf16; d_lse_opt [B][T][n_q_heads] float32 as in spkv_decode_attention, or NULL.  Rows of
+ *   nodes from n[b] on, and all rows of a sequence id outside the cache (SPKV_E_BOUNDS), are left as they are.
+ *   d_workspace: >= spkv_decode_tree_workspace_bytes(cfg, B, T) bytes, 256-byte aligned, whatever it holds; calls that
+ *   share it must not overlap on the GPU.  A sequence may appear several times in the list here (several trees on one
+ *   context).  sm_scale positive and finite, B <= max_seqs, B * n_kv_heads <= 1024.  Always ordered after everything earlier on `stream`,
+ *   also under SPKV_FLAG_OVERLAP. */
+size_t spkv_decode_tree_workspace_bytes(const spkv_config_t *cfg, int32_t B, int32_t T);
+int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B, int32_t T,
+                               const int32_t *d_n_nodes, const int32_t *d_parent, const spkv_rows_t *q,
+                               const spkv_rows_t *k, const spkv_rows_t *v, const float *d_logits, void *d_out,
+                               float *d_lse_opt, float sm_scale, void *d_workspace, size_t workspace_bytes,
+                               spkv_stream_t stream);
+
+/* Appends the pairs of some of the nodes, in every layer of [layer0, layer0 + n_layers) at once: for each listed sequence and
+ * KV head what n_path[b] calls of spkv_append_evict with nodes path[b][0], path[b][1], ... would do, up to the order in
+ * which pages come off the free stack.  d_path [B][T] NULL: nodes 0, 1, 2, ...; d_n_path [B] NULL: T each; 0 leaves a
+ * sequence as it is.  (So it is also an append of several tokens, as many as each sequence has.)  The path ends at the first
+ * entry outside [0, T) (SPKV_E_BOUNDS); a node may appear twice and is then appended twice.
+ *   k, v: rows of layer0's nodes, token b T + i (n_kv_heads heads, as in spkv_decode_attention_tree), those of the next
+ *   layer k_layer_stride / v_layer_stride elements on (a multiple of 8); d_logits [n_layers][B][T][n_kv_heads] float32.
+ * A pair that finds no free page or no room in its page table is not stored, as with spkv_append_evict (SPKV_E_POOL_EXHAUSTED,
+ * SPKV_E_CONTEXT_OVERFLOW).  Always ordered after everything earlier on `stream`. */
+int spkv_append_path(spkv_cache_t *cache, int32_t layer0, int32_t n_layers, const int32_t *d_seq_ids, int32_t B, int32_t T,
+                     const int32_t *d_path, const int32_t *d_n_path, const spkv_rows_t *k, int64_t k_layer_stride,
+                     const spkv_rows_t *v, int64_t v_layer_stride, const float *d_logits, spkv_stream_t stream);
+
+/* The part of each tree that the target model confirms.  Node 0 is the sequence's newest token, accepted by
+ * definition; from an accepted node i the walk goes on to its first child c (lowest index) whose token is the one the target
+ * puts behind i, d_tokens[b][c] == d_target[b][i] -- its likeliest token, or one drawn from its distribution: either
+ * way the sequence continues as if the target alone had written it.
+ *   d_tokens, d_target [B][T] int32 -> d_path [B][T] int32: the accepted nodes in order, -1 behind them; d_n_path [B] their
+ *   number (0 for a sequence without nodes); d_next [B] the target's token behind the last of them (-1 without nodes).  Takes no cache;
+ *   counts and parents out of range are taken as above, without a status. */
+int spkv_tree_accept(int32_t B, int32_t T, const int32_t *d_n_nodes, const int32_t *d_parent, const int32_t *d_tokens,
+                     const int32_t *d_target, int32_t *d_path, int32_t *d_n_path, int32_t *d_next, spkv_stream_t stream);
+
+/* What rows of logits say.  With x = scale * logits[row] (scale: 1 / temperature, positive and finite) and lse = log sum exp(x):
+ *   d_lse [n_rows], d_entropy [n_rows] = lse - sum softmax(x) x,
+ *   d_logp [n_rows][n_given] = x[d_given[row][j]] - lse (NaN for a token outside [0, vocab), so -1 pads),
+ *   d_top_ids / d_top_logp [n_rows][n_top]: the n_top largest logits in descending order, of equal ones the lower index
+ *   first, NaN before everything else (beyond the vocabulary: -1 and NaN); n_top <= SPKV_MAX_TOP.
+ * float32 (int32) each; NULL = not wanted, and n_given or n_top = 0 ask for nothing.  A token of logit -infinity
+ * has probability zero and adds nothing.  A row with a NaN or +infinity has NaN where the formulas have it.
+ *   d_logits: rows of `vocab` contiguous elements of type `dtype` (SPKV_BF16 ...), `row_stride` elements apart, aligned to their
+ *   type only.  n_rows * n_given and n_rows * n_top below 2^31.
+ *   d_workspace: >= spkv_logprobs_workspace_bytes(n_rows, vocab, n_top) bytes, 16-byte aligned, whatever it holds; calls that share
+ *   it must not overlap on the GPU.  The sums have a fixed order: the same inputs on the same GPU give the same bits. */
+#define SPKV_MAX_TOP 32
+size_t spkv_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top);
+int spkv_token_logprobs(int32_t dtype, int32_t n_rows, int32_t vocab, const void *d_logits, int64_t row_stride, float scale,
+                        const int32_t *d_given, int32_t n_given, int32_t n_top, float *d_lse, float *d_entropy, float *d_logp,
+                        int32_t *d_top_ids, float *d_top_logp, void *d_workspace, size_t workspace_bytes, spkv_stream_t stream);
+
 /* Workspace bytes spkv_prefill needs for a chunk of C pairs. */
 size_t spkv_prefill_workspace_bytes(const spkv_config_t *cfg, int32_t C);
 

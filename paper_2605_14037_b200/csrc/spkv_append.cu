@@ -10,28 +10,6 @@
 
 namespace spkv {
 
-// Pops a free page (lane 0) and clears its value block, so that rows past a page's
-// valid count always hold zeros (the attention kernels multiply them by weight 0).
-// Returns the global page index, -1 when the pool is empty, -2 when the index popped from the stack
-// failed the debug bounds check (status set already).
-__device__ inline int alloc_page(const CacheView &c, int lane) {
-  int page = -1;
-  if (lane == 0) {
-    int top = atomicSub(&c.status[1], 1);
-    if (top <= 0) {
-      atomicAdd(&c.status[1], 1);
-    } else {
-      page = checked_page(c, __ldcg(&c.free_stack[top - 1]), -2);
-    }
-  }
-  page = __shfl_sync(0xffffffffu, page, 0);
-  if (page >= 0) {
-    uint4 *vb = reinterpret_cast<uint4 *>(c.pages + (int64_t)page * kPageElems + kBlockElems);
-    for (int i = lane; i < kBlockElems * 2 / 16; i += 32) vb[i] = make_uint4(0, 0, 0, 0);
-  }
-  return page;
-}
-
 // One warp: the append + evict of one unit.
 __device__ inline void append_unit(const CacheView &c, int layer, int item, const int32_t *__restrict__ seq_ids, int B,
                                    const uint4 *__restrict__ k_new, const uint4 *__restrict__ v_new,

@@ -63,6 +63,7 @@ BF16, F16, F32 = 0, 1, 2          # SPKV_BF16 / SPKV_F16 / SPKV_F32
 _DTYPE = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 NORM_Q, NORM_K = 1, 2             # SPKV_NORM_Q / SPKV_NORM_K
 MAX_ROW_DIM, MAX_AXES = 256, 4    # SPKV_MAX_ROW_DIM / SPKV_MAX_AXES
+MAX_DRAFT, MAX_TOP = 64, 32       # SPKV_MAX_DRAFT / SPKV_MAX_TOP
 
 
 class Rows(C.Structure):
@@ -129,6 +130,12 @@ def lib():
         "spkv_share_plan": (C.c_int, [vp, vp, i32, vp, sz, vp]),
         "spkv_decode_shared_workspace_bytes": (sz, [cfgp, i32]),
         "spkv_decode_attention_shared": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, f32, vp, sz, vp, sz, vp]),
+        "spkv_decode_tree_workspace_bytes": (sz, [cfgp, i32, i32]),
+        "spkv_decode_attention_tree": (C.c_int, [vp, i32, vp, i32, i32] + [vp] * 8 + [f32, vp, sz, vp]),
+        "spkv_append_path": (C.c_int, [vp, i32, i32, vp, i32, i32, vp, vp, vp, C.c_int64, vp, C.c_int64, vp, vp]),
+        "spkv_tree_accept": (C.c_int, [i32, i32] + [vp] * 8),
+        "spkv_logprobs_workspace_bytes": (sz, [i32, i32, i32]),
+        "spkv_token_logprobs": (C.c_int, [i32, i32, i32, vp, C.c_int64, f32, vp, i32, i32] + [vp] * 6 + [sz, vp]),
         "spkv_prefill_workspace_bytes": (sz, [cfgp, i32]),
         "spkv_prefill": (C.c_int, [vp, i32, i32, i32, vp, vp, vp, vp, vp, f32, vp, sz, vp]),
         "spkv_rope_init": (C.c_int, [vp, i32, i32, i32, f32, vp, vp]),
@@ -276,7 +283,7 @@ class Cache:
             _check(lib().spkv_cache_create(C.byref(self.cfg), _ptr(self.arena), self.arena_bytes,
                                            _stream(), C.byref(h)), "spkv_cache_create")
         self._h = h
-        self._ws, self._shared_ws, self._shared_bytes = {}, {}, {}
+        self._ws, self._shared_ws, self._shared_bytes, self._tree_ws, self._tree_bytes = {}, {}, {}, {}, {}
         self.G = n_q_heads // n_kv_heads
         self.default_scale = 1.0 / math.sqrt(head_dim)
 
@@ -303,7 +310,7 @@ class Cache:
         with torch.cuda.device(self.device):
             _check(lib().spkv_cache_attach(C.byref(self.cfg), _ptr(arena), arena.numel(), _stream(), C.byref(h)),
                    "spkv_cache_attach")
-        self._h, self._ws, self._shared_ws, self._shared_bytes = h, {}, {}, {}
+        self._h, self._ws, self._shared_ws, self._shared_bytes, self._tree_ws, self._tree_bytes = h, {}, {}, {}, {}, {}
         self.G = self.cfg.n_q_heads // self.cfg.n_kv_heads
         self.default_scale = 1.0 / math.sqrt(self.cfg.head_dim)
         return self
@@ -478,6 +485,74 @@ class Cache:
         if rc:
             raise SpkvError(rc, "spkv_decode_attention_shared")
         return (out, lse) if want_lse else out
+
+    def spkv_decode_attention_tree(self, layer, seq_ids, q, k, v, parent=None, n_nodes=None, logits=None, out=None, lse=None,
+                                   sm_scale=None, want_lse=False, stream=None):
+        """Attention of drafted nodes over the cache and their ancestors.  q [B, T, n_q_heads, 128], k, v
+        [B, T, n_kv_heads, 128] (views of one fused projection too), parent [B, T] int32 (None: chains), n_nodes
+        [B] int32 (None: T each), logits [B, T, n_kv_heads] (may be None while T <= window).  Returns out
+        [B, T, n_q_heads, 128], or (out, lse) with want_lse."""
+        dev = q.get_device()
+        if stream is not None:
+            return _under(stream, dev, self.spkv_decode_attention_tree, layer, seq_ids, q, k, v, parent, n_nodes, logits, out,
+                          lse, sm_scale, want_lse)
+        cfg = self.cfg
+        B, T = q.shape[0], q.shape[1]
+        hq, hkv = cfg.n_q_heads, cfg.n_kv_heads
+        if dev < 0 or dev != self.arena.get_device():
+            raise ValueError("all tensors of a call live on the cache's device")
+        rows = (Rows * 3)()
+        _THREE_ROWS.pack_into(rows, 0, *_draft_rows(q, B, T, hq, dev, "q"), *_draft_rows(k, B, T, hkv, dev, "k"),
+                              *_draft_rows(v, B, T, hkv, dev, "v"))
+        at = C.addressof(rows)
+        if out is None:
+            out = q.new_empty(B, T, hq, 128)
+        if lse is None and want_lse:
+            lse = q.new_empty(B, T, hq, dtype=torch.float32)
+        ptrs = (_dense(seq_ids, torch.int32, (B,), dev), _dense(n_nodes, torch.int32, (B,), dev),
+                _dense(parent, torch.int32, (B, T), dev), _dense(logits, torch.float32, (B, T, hkv), dev),
+                _dense(out, torch.bfloat16, (B, T, hq, 128), dev), _dense(lse, torch.float32, (B, T, hq), dev))
+        nbytes = self._tree_bytes.get((B, T))
+        if nbytes is None:
+            nbytes = self._tree_bytes[B, T] = max(256, lib().spkv_decode_tree_workspace_bytes(C.byref(cfg), B, T))
+        ws = _scratch(self._tree_ws, nbytes, dev)
+        rc = _on_device(dev, lib().spkv_decode_attention_tree, self._h, layer, ptrs[0], B, T, ptrs[1], ptrs[2], at, at + _ROW,
+                        at + 2 * _ROW, ptrs[3], ptrs[4], ptrs[5], self.default_scale if sm_scale is None else sm_scale,
+                        ws.data_ptr(), ws.numel())
+        if rc:
+            raise SpkvError(rc, "spkv_decode_attention_tree")
+        return (out, lse) if want_lse else out
+
+    def spkv_append_path(self, layer0, seq_ids, k, v, logits, path=None, n_path=None, stream=None):
+        """Appends n_path[b] nodes path[b] (None: 0, 1, 2, ...) of every sequence: k, v [B, T, n_kv_heads, 128] and logits
+        [B, T, n_kv_heads] of layer0, or [n, B, T, ...] of n layers from layer0 on."""
+        dev = k.get_device()
+        if stream is not None:
+            return _under(stream, dev, self.spkv_append_path, layer0, seq_ids, k, v, logits, path, n_path)
+        if dev < 0 or dev != self.arena.get_device():
+            raise ValueError("all tensors of a call live on the cache's device")
+        hkv = self.cfg.n_kv_heads
+        n = 1
+        strides = (0, 0)
+        if k.dim() == 5:
+            n = k.shape[0]
+            if v.dim() != 5 or v.shape[0] != n or logits.dim() != 4 or logits.shape[0] != n:
+                raise ValueError("k, v and logits of several layers: [n, B, T, ...] each")
+            if n > 1:
+                strides = (k.stride(0), v.stride(0))
+            if n == 0:
+                return
+            k, v = k[0], v[0]
+        elif logits.dim() != 3:
+            raise ValueError("k, v and logits of one layer: [B, T, ...] each")
+        B, T = k.shape[0], k.shape[1]
+        rows = (Rows * 2)()
+        _TWO_ROWS.pack_into(rows, 0, *_draft_rows(k, B, T, hkv, dev, "k"), *_draft_rows(v, B, T, hkv, dev, "v"))
+        at = C.addressof(rows)
+        lg = _dense(logits, torch.float32, (n, B, T, hkv) if logits.dim() == 4 else (B, T, hkv), dev)
+        _check(_on_device(dev, lib().spkv_append_path, self._h, layer0, n, _dense(seq_ids, torch.int32, (B,), dev), B, T,
+                          _dense(path, torch.int32, (B, T), dev), _dense(n_path, torch.int32, (B,), dev), at, strides[0],
+                          at + _ROW, strides[1], lg), "spkv_append_path")
 
     @_on_its_stream
     def spkv_prefill(self, layer, seq, k, v, logits, q=None, out=None, sm_scale=None, stream=None):
@@ -694,7 +769,7 @@ def make_norm_rope(n_q_heads, n_kv_heads, head_dim=128, dtype=torch.bfloat16, wq
 
 # The row calls are made once per layer and token batch, often for a handful of rows: what the binding does
 # around the launch is kept to a few microseconds (one check per tensor, all views packed at once).
-_SIX_ROWS, _EIGHT_ROWS = struct.Struct("Qqq" * 6), struct.Struct("Qqq" * 8)
+_TWO_ROWS, _THREE_ROWS, _SIX_ROWS, _EIGHT_ROWS = (struct.Struct("Qqq" * n) for n in (2, 3, 6, 8))
 _ROW = C.sizeof(Rows)
 
 
@@ -718,6 +793,29 @@ def _row_out(nr, like, t, heads, n, dev, what):
     D = nr.head_dim
     t = like.new_empty(n, heads, D)   # (separate sizes: 0.4 us less than a tuple)
     return t, (t.data_ptr(), heads * D, D)
+
+
+def _draft_rows(t, B, T, heads, dev, what):
+    """(pointer, token stride, head stride) of a bf16 [B, T, heads, 128] tensor whose tokens b T + i are evenly spaced"""
+    if t.dtype is not torch.bfloat16 or t.shape != (B, T, heads, 128):
+        raise ValueError(f"{what}: expected bfloat16 [{B}, {T}, {heads}, 128], got {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != dev:
+        raise ValueError("all tensors of a call live on one device")
+    st = t.stride()
+    tok = st[1] if T > 1 else st[0] if B > 1 else 0
+    if st[3] != 1 or (B > 1 and T > 1 and st[0] != T * tok):
+        raise ValueError(f"{what}: rows are contiguous and tokens evenly spaced")
+    return t.data_ptr(), tok, st[2] if heads > 1 else 0
+
+
+def _dense(t, dtype, shape, dev):
+    """Pointer of a contiguous tensor of this type, shape and device (None: null)"""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {dtype} tensor {tuple(shape)} on device {dev}, got {t.dtype} {tuple(t.shape)} "
+                         f"on {t.device}")
+    return t.data_ptr()
 
 
 def _positions(nr, pos, dev):
@@ -797,6 +895,62 @@ def spkv_norm_rope_backward(nr, positions, q, k, q_grad, k_grad, v_grad=None, dq
     if rc:
         raise SpkvError(rc, "spkv_norm_rope_backward")
     return dq, dk, dv, dwq, dwk
+
+
+def spkv_tree_accept(tokens, target, parent=None, n_nodes=None, path=None, n_path=None, next=None, stream=None):
+    """The nodes of each tree that the target confirms: tokens, target [B, T] int32 (target: what the target model puts
+    behind each node), parent [B, T] int32 (None: chains), n_nodes [B] int32 (None: T).  Returns (path [B, T], n_path [B],
+    next [B]), int32."""
+    dev = tokens.get_device()
+    if stream is not None:
+        return _under(stream, dev, spkv_tree_accept, tokens, target, parent, n_nodes, path, n_path, next)
+    if dev < 0 or tokens.dim() != 2:
+        raise ValueError("tokens: a device tensor [B, T]")
+    B, T = shape = tokens.shape
+    i32 = torch.int32
+    path = tokens.new_empty(B, T, dtype=i32) if path is None else path
+    n_path = tokens.new_empty(B, dtype=i32) if n_path is None else n_path
+    next = tokens.new_empty(B, dtype=i32) if next is None else next
+    _check(_on_device(dev, lib().spkv_tree_accept, B, T, _dense(n_nodes, i32, (B,), dev), _dense(parent, i32, shape, dev),
+                      _dense(tokens, i32, shape, dev), _dense(target, i32, shape, dev), _dense(path, i32, shape, dev),
+                      _dense(n_path, i32, (B,), dev), _dense(next, i32, (B,), dev)), "spkv_tree_accept")
+    return path, n_path, next
+
+
+_logprob_ws = {}
+
+
+def spkv_token_logprobs(logits, given=None, top=0, scale=1.0, lse=None, logp=None, entropy=None, top_ids=None, top_logp=None,
+                        want_entropy=True, stream=None):
+    """Of rows of logits [n, vocab] (bf16, fp16 or fp32; rows contiguous, any row stride): log sum of exponentials, log probabilities
+    of the tokens given [n, m] int32 (outside the vocabulary: NaN), entropy, and the `top` largest with their log
+    probabilities, all of scale * logits.  Returns (lse [n], logp [n, m], entropy [n], top_ids [n, top], top_logp
+    [n, top]); None for what is not asked for."""
+    dev = logits.get_device()
+    if stream is not None:
+        return _under(stream, dev, spkv_token_logprobs, logits, given, top, scale, lse, logp, entropy, top_ids, top_logp, want_entropy)
+    if dev < 0 or logits.dim() != 2 or logits.dtype not in _DTYPE or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits: bf16, fp16 or fp32 rows [n, vocab] on the device, each contiguous")
+    n, vocab = logits.shape
+    f32, i32 = torch.float32, torch.int32
+    m = 0 if given is None else given.shape[-1]
+    lse = logits.new_empty(n, dtype=f32) if lse is None else lse
+    if given is not None and logp is None:
+        logp = logits.new_empty(n, m, dtype=f32)
+    if want_entropy and entropy is None:
+        entropy = logits.new_empty(n, dtype=f32)
+    if top > 0:
+        top_ids = logits.new_empty(n, top, dtype=i32) if top_ids is None else top_ids
+        top_logp = logits.new_empty(n, top, dtype=f32) if top_logp is None else top_logp
+    ws_bytes = max(16, lib().spkv_logprobs_workspace_bytes(n, vocab, top))
+    ws = _scratch(_logprob_ws, ws_bytes, dev)
+    rc = _on_device(dev, lib().spkv_token_logprobs, _DTYPE[logits.dtype], n, vocab, logits.data_ptr(),
+                    logits.stride(0) if n > 1 else 0, scale, _dense(given, i32, (n, m), dev), m, top, _dense(lse, f32, (n,), dev),
+                    _dense(entropy, f32, (n,), dev), _dense(logp, f32, (n, m), dev), _dense(top_ids, i32, (n, top), dev),
+                    _dense(top_logp, f32, (n, top), dev), ws.data_ptr(), ws.numel())
+    if rc:
+        raise SpkvError(rc, "spkv_token_logprobs")
+    return lse, logp, entropy, top_ids, top_logp
 
 
 _softgate_ws = {}

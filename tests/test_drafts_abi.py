@@ -1,0 +1,53 @@
+"""Argument checks of the calls for drafted tokens that take no cache: no GPU is touched."""
+import pytest
+
+from paper_2605_14037_b200 import build as spkv_build
+
+FAKE = 1 << 20      # a 16-byte aligned address that is never read
+
+
+@pytest.fixture(scope="module")
+def lib():
+    spkv_build.build()
+    from paper_2605_14037_b200 import spkv as mod
+    return mod.lib()
+
+
+def accept(lib, B=2, T=8, tokens=FAKE, target=FAKE, path=FAKE, n_path=FAKE, nxt=FAKE):
+    return lib.spkv_tree_accept(B, T, None, None, tokens, target, path, n_path, nxt, None)
+
+
+@pytest.mark.parametrize("kw", [dict(B=-1), dict(T=-1), dict(T=65), dict(tokens=None), dict(target=None), dict(path=None), dict(n_path=None), dict(nxt=None)])
+def test_accept_refusals(lib, kw):
+    assert accept(lib, **kw) == -1
+
+
+def test_accept_of_no_sequences(lib):
+    assert accept(lib, B=0, tokens=None, n_path=None) == 0
+
+
+def logprobs(lib, dtype=0, n=4, v=100, x=FAKE, stride=100, scale=1.0, given=FAKE, n_given=1, n_top=1, lse=FAKE, ent=FAKE, logp=FAKE, ids=FAKE, tlp=FAKE,
+             ws=FAKE, ws_bytes=1 << 30):
+    return lib.spkv_token_logprobs(dtype, n, v, x, stride, scale, given, n_given, n_top, lse, ent, logp, ids, tlp, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=3), -1), (dict(dtype=-1), -1), (dict(n=-1), -1), (dict(v=0), -1), (dict(x=None), -1), (dict(x=FAKE + 1), -1), (dict(dtype=2, x=FAKE + 2), -1),
+    (dict(scale=0.0), -1), (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(given=None), -1),
+    (dict(n_given=-1), -1), (dict(n_top=-1), -1), (dict(n_top=33), -3), (dict(n=1 << 20, n_given=1 << 12), -3), (dict(v=2 ** 31 - 1), -3),
+    (dict(ws=None), -7), (dict(ws=FAKE + 8), -7), (dict(ws_bytes=10), -7),
+])
+def test_logprobs_refusals(lib, kw, code):
+    assert logprobs(lib, **kw) == code
+
+
+def test_logprobs_of_no_rows_and_workspace_sizes(lib):
+    assert logprobs(lib, n=0, x=None, ws=None) == 0
+    size = lib.spkv_logprobs_workspace_bytes
+    assert size(0, 100, 0) >= 16 and size(10, 100000, 0) < size(10, 100000, 1) == size(10, 100000, 32) < size(20, 100000, 1)
+    assert size(-1, 100, 0) == size(1, 0, 0) == size(1, 100, 33) == size(1, 100, -1) == 0
+
+
+def test_calls_with_a_cache_refuse_a_missing_one(lib):
+    assert lib.spkv_decode_attention_tree(None, 0, FAKE, 1, 1, None, None, FAKE, FAKE, FAKE, None, FAKE, None, 0.1, FAKE, 1 << 30, None) == -1
+    assert lib.spkv_append_path(None, 0, 1, FAKE, 1, 1, None, None, FAKE, 0, FAKE, 0, FAKE, None) == -1
