@@ -1,6 +1,8 @@
 // Declarations shared by the decode-attention kernels (one launch per layer; the whole stack in one
 // launch): arguments, workspace layout, block scan, range cuts, the merges of partial results.
 #pragma once
+#include <atomic>
+
 #include "spkv_internal.cuh"
 #include "spkv_mma.cuh"
 
@@ -469,6 +471,20 @@ inline DecodeWs decode_ws_layout(int n_items, int G) {
   w.off_acc = w.off_ml + (slots * G * 2 * 4 + 255) / 256 * 256;
   w.total = w.off_acc + slots * G * kD * 4;
   return w;
+}
+
+// The kernel may use `smem` bytes and gets the whole of an SM's shared memory to share out: with the default
+// split, which fits one prefix block, a tail block finds none left beside it.
+inline int whole_shared_memory(const void *kernel, int smem, std::atomic<unsigned long long> *ready) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return SPKV_E_CUDA;
+  const unsigned long long bit = dev < 64 ? 1ULL << dev : 0;
+  if (bit & ready->load(std::memory_order_acquire)) return SPKV_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
+    return SPKV_E_CUDA;
+  ready->fetch_or(bit, std::memory_order_release);
+  return SPKV_OK;
 }
 
 }  // namespace spkv

@@ -816,19 +816,6 @@ namespace {
 // Attributes of the two kernels, set once per device (a bit each).
 std::atomic<unsigned long long> g_ready[2][2];
 
-// The kernel may use `smem` bytes and gets the whole of an SM's shared memory to share out: with the default
-// split, which fits one prefix block, a tail block finds none left beside it.
-int whole_shared_memory(const void *kernel, int smem, std::atomic<unsigned long long> *ready) {
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return SPKV_E_CUDA;
-  const unsigned long long bit = dev < 64 ? 1ULL << dev : 0;
-  if (bit & ready->load(std::memory_order_acquire)) return SPKV_OK;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-      cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
-    return SPKV_E_CUDA;
-  ready->fetch_or(bit, std::memory_order_release);
-  return SPKV_OK;
-}
 }  // namespace
 
 extern "C" size_t spkv_decode_shared_workspace_bytes(const spkv_config_t *cfg, int32_t B) {

@@ -1,78 +1,719 @@
 // Attention of a tree of drafted tokens over the cache (spkv_decode_attention_tree).
+//
+// A unit's (sequence, KV head) queries are the rows (node, head of the group) -> node * G + g, cut into tiles of 128 that
+// are the M side of tcgen05 MMAs.  Its keys are pages of 64: those of the compact cache, those of the ring, and one
+// page of the drafts themselves.  The pages of all units of the launch stand in one line that is cut into equal ranges, one per
+// block and row tile (two blocks an SM; the tiles of a range are neighbours, so that the second finds its pages in
+// L2).  Where a unit lies inside a range its rows are written at once; otherwise the pieces leave (m, l, O) per row and
+// tree_merge_kernel joins them by their log-sum-exp weights.
+//
+// Per page: S = Q K^T (8 MMAs M128 N64 K16 into tensor memory), softmax in registers (thread = row = lane of
+// tensor memory), P as two bf16 terms back over the scores, O += P V.  Two score buffers: the scores of the next page are
+// made while this one's softmax runs.
+//   * Two bf16 terms (2^-16 of a weight) take the values as they lie in the cache: one fp16 term would halve P V's MMAs but
+//     wants the values converted to fp16 under a scale that fits all of them.
+//   * Masks: every query sees a compact page's pairs.  Of a ring page a row sees the slots in its node's window and those
+//     whose pair is kept (a bit each, by ballot over the stored logits), of the drafts' page its path.  64 bits a row
+//     and page, applied to the scores.
+//   * A pair that is masked has P = 0, which an infinite or NaN value would turn into NaN (and a weight's second
+//     term is often 0 too): one warp looks through every page's values before P V may read them, replaces what is not finite by
+//     0 and marks the segment; its epilogue then adds those elements to the rows that see them.  (Clean pages cost nothing: the
+//     warp runs ahead of P V.)
+//
+// Warps: 0 MMA issue and tensor memory, 1 page loader, 2 query rows, drafts and paths, 3 look through the values, 4-7
+// softmax.  Shared memory (113 KB, two blocks an SM): Q 32 KB, ring of five 16 KB key or value blocks in the order in which the
+// MMAs want them.  Tensor memory (256 columns): score buffers at [0, 64) and [64, 128), O at [128, 256).  All waits are bounded.
 #include <math.h>
 
+#include <algorithm>
+#include <atomic>
+
+#include "spkv_tc5.cuh"
 #include "spkv_tree.cuh"
 
 namespace spkv {
 
-// One warp per query row (node, query head): lane l owns dims 4l .. 4l + 3, keys one after the other.
-__global__ void __launch_bounds__(128) tree_rows_kernel(TreeArgs a) {
+namespace tree {
+constexpr int kThreads = 256, kBlocksPerSm = 2;
+constexpr int kMmaWarp = 0, kLoaderWarp = 1, kRowWarp = 2, kScanWarp = 3;
+constexpr int kTmemCols = 256;
+constexpr int kBlockBytes = kPageBytes / 2, kSlots = 5;
+enum { B_FULL = 0, B_EMPTY = 5, B_V_READY = 10 /* [page & 3] */, B_S_FULL = 14 /* [page & 1] */, B_P_FULL = 16, B_O_DONE = 18,
+       B_Q_FULL = 20, B_Q_EMPTY, B_TREE_FULL, B_TREE_EMPTY, B_COUNT };
+constexpr int kUnitsHere = 12;      // units of a block that shared memory holds; the others stand in the workspace
+constexpr int off_ring = 32768, off_bar = off_ring + kSlots * kBlockBytes, off_info = off_bar + B_COUNT * 8,
+              off_odd = off_info + 16, off_path = off_odd + 32, off_depth = off_path + 64 * 8, off_units = off_depth + 64,
+              kSmemBytes = off_units + kUnitsHere * 16;
+static_assert(kSmemBytes <= off_bar + 1024 && off_units % 16 == 0 && off_path % 8 == 0, "two blocks an SM");
+// while the ranges are cut, the ring holds the units' lengths and page counts
+constexpr int kMaxItems = 1024;
+constexpr int off_np = off_ring, off_pre = off_np + kMaxItems * 4, off_tmp = off_pre + (kMaxItems + 4) * 4,
+              off_meta = off_tmp + 64 * 4;
+
+// Where page i of a segment of n stands in the order in which a segment's blocks are loaded and used:
+// K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1)
+__device__ inline int key_at(int i) { return i == 0 ? 0 : 2 * i - 1; }
+__device__ inline int value_at(int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
+}  // namespace tree
+
+// A unit as the plan sees it: {its first page in the line, sequence | nodes << 25, pairs received, kept pairs}
+struct TreeUnit {
+  int pre, seq, n, t, len, nk, nr, np;   // nk, nr: compact and ring pages; np: all of them, 0 if the tile has no rows
+  __device__ inline TreeUnit(const TreeArgs &a, int4 m, int tile) {
+    pre = m.x; seq = m.y & 0x1ffffff; n = (unsigned)m.y >> 25; t = m.z; len = m.w;
+    nk = (len + kP - 1) / kP;
+    nr = (min(t, a.c.w) + kP - 1) / kP;
+    np = n * a.c.G > tile * kTreeRows ? nk + nr + 1 : 0;
+  }
+};
+
+__global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_attention_kernel(const __grid_constant__ TreeArgs a) {
+  using namespace tc5;
+  using namespace tree;
+  extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
-  const int lane = threadIdx.x & 31, r = blockIdx.x * 4 + (threadIdx.x >> 5), b = blockIdx.y;
-  const int i = r / c.Hq, j = r - i * c.Hq, kvh = j / c.G;
-  bool bad = false;
-  const int n = tree_nodes(a, b, &bad);
-  const int seq = a.seq_ids[b];
-  if (seq < 0 || seq >= c.S) bad = true;
-  if (bad && r == 0 && lane == 0) set_status(c, SPKV_E_BOUNDS);
-  if (i >= n || seq < 0 || seq >= c.S) return;
-  const int u = unit_index(c, a.layer, seq, kvh), t = __ldcg(&c.t[u]), len = __ldcg(&c.len[u]), trow = unit_table_row(c, u);
-  const float thr = head_threshold(c, a.layer, kvh, a.tau_logit);
-  uint64_t path = 0;
-  for (int x = i; x >= 0;) {
-    path |= 1ull << x;
-    int p = a.parent ? a.parent[(size_t)b * a.T + x] : x - 1;
-    if (p < -1 || p >= x) {
-      if (lane == 0) set_status(c, SPKV_E_BOUNDS);
-      p = -1;
+  uint64_t *bar = reinterpret_cast<uint64_t *>(smem + off_bar);
+  volatile int *s_info = reinterpret_cast<volatile int *>(smem + off_info);     // tensor memory, first and last unit, drafts' blocks let in
+  volatile int *s_odd = reinterpret_cast<volatile int *>(smem + off_odd);       // [segment & 7] values that are not finite
+  volatile uint64_t *s_path = reinterpret_cast<volatile uint64_t *>(smem + off_path);   // [node] nodes it sees
+  volatile uint8_t *s_depth = smem + off_depth;
+  int4 *s_units = reinterpret_cast<int4 *>(smem + off_units);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int range = blockIdx.x / a.n_tiles, tile = blockIdx.x - range * a.n_tiles;
+  if (tid == 0) {
+    for (int i = 0; i < B_COUNT; ++i) mbar_init(&bar[i], i == B_P_FULL || i == B_P_FULL + 1 ? 128 : i == B_TREE_EMPTY ? 4 : 1);
+    mbar_fence_init();
+  }
+  pdl_wait();
+  pdl_trigger();   // (only now: what follows may then rely on everything before this launch)
+  // ---- the line of pages, its cut, and this block's units
+  int r0, r1;
+  {
+    int *s_np = reinterpret_cast<int *>(smem + off_np), *s_pre = reinterpret_cast<int *>(smem + off_pre),
+        *s_tmp = reinterpret_cast<int *>(smem + off_tmp);
+    int4 *s_meta = reinterpret_cast<int4 *>(smem + off_meta);
+    for (int i = tid; i < a.n_items; i += kThreads) {
+      const int b = i / c.Hkv, kvh = i - b * c.Hkv;
+      int seq = a.seq_ids[b];
+      bool bad = false;
+      int n = tree_nodes(a, b, &bad);
+      if (seq < 0 || seq >= c.S) { bad = true; seq = 0; n = 0; }
+      if (bad && blockIdx.x == 0) set_status(c, SPKV_E_BOUNDS);
+      const int u = unit_index(c, a.layer, seq, kvh);
+      const int t = ldcg_keep(&c.t[u]), len = ldcg_keep(&c.len[u]);
+      s_meta[i] = make_int4(0, seq | n << 25, t, len);
+      s_np[i] = TreeUnit(a, s_meta[i], tile).np;
+      if (range == 0 && s_np[i] == 0) a.ends[(size_t)tile * a.n_items + i] = make_int2(-1, -1);   // nothing to join
     }
-    x = p;
+    __syncthreads();
+    block_exclusive_scan(s_np, s_pre, a.n_items, s_tmp);
+    const int total = s_pre[a.n_items];
+    const int nb = min(a.n_ranges, (total + a.min_pages - 1) / a.min_pages);
+    if (range >= nb) return;
+    const int snap = total / nb / 16;
+    r0 = range_cut(range, nb, total, snap, s_pre, a.n_items);
+    r1 = range_cut(range + 1, nb, total, snap, s_pre, a.n_items);
+    if (r0 >= r1) return;
+    if (tid < 2) {   // units of the first and the last page
+      const int p = tid ? r1 - 1 : r0;
+      int lo = 0, hi = a.n_items;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_pre[mid] <= p) lo = mid; else hi = mid;
+      }
+      s_info[1 + tid] = lo;
+    }
+    __syncthreads();
+    const int u0 = s_info[1], n_units = s_info[2] - u0 + 1;
+    for (int i = tid; i < n_units; i += kThreads) {
+      int4 m = s_meta[u0 + i];
+      m.x = s_pre[u0 + i];
+      if (i < kUnitsHere) s_units[i] = m;
+      else a.units[(size_t)blockIdx.x * a.n_items + i] = m;
+    }
+    if (tid < 8) s_odd[tid] = 0;
+    if (tid == 8) s_info[3] = 0;
   }
-  const int d = __popcll(path) - 1;
-  const __nv_bfloat16 *qr = a.q + ((int64_t)b * a.T + i) * a.q_tok + (int64_t)j * a.q_head + lane * 4;
-  float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  for (int x = 0; x < 4; ++x) q[x] = __bfloat162float(qr[x]);
-  auto take = [&](const __nv_bfloat16 *kr, const __nv_bfloat16 *vr) {   // this lane's four elements of a row
-    float s = 0.f;
-    for (int x = 0; x < 4; ++x) s = fmaf(q[x], __bfloat162float(kr[x]), s);
-    s = warp_sum(s) * a.scale_log2;
-    const float mn = s > m ? s : m, f = m == -INFINITY ? 0.f : fast_exp2(m - mn), p = fast_exp2(s - (mn == -INFINITY ? 0.f : mn));
-    l = l * f + p;
-    for (int x = 0; x < 4; ++x) o[x] = o[x] * f + p * __bfloat162float(vr[x]);
-    m = mn;
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem + off_info)),
+                 "n"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_async_smem();   // the ring's bytes go from the plan to the copies
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tbase = (uint32_t)s_info[0];
+  const int u0 = s_info[1], n_units = s_info[2] - u0 + 1;
+  bool failed = false;
+  // f(segment, unit's place among all, unit, first page in the unit, pages) for every segment of this block; f returns false to stop
+  auto segments = [&](auto f) {
+    int seg = 0;
+    for (int i = 0; i < n_units; ++i) {
+      const TreeUnit x(a, i < kUnitsHere ? s_units[i] : a.units[(size_t)blockIdx.x * a.n_items + i], tile);
+      const int s = max(x.pre, r0), e = min(x.pre + x.np, r1);
+      if (e <= s) continue;
+      if (!f(seg, u0 + i, x, s - x.pre, e - s)) return;
+      ++seg;
+    }
   };
-  auto take_row = [&](int64_t page, int row) {
-    const __nv_bfloat16 *kr = c.pages + page * kPageElems + swz_off(row, lane >> 1) + (lane & 1) * 4;
-    take(kr, kr + kBlockElems);
+  auto page_table = [&](const TreeUnit &x, int kvh) -> const int32_t * {   // null for a head that keeps nothing
+    if (kvh < 64 && ((a.local_mask >> kvh) & 1)) return nullptr;
+    const int below = kvh < 64 ? __popcll(a.local_mask & ((1ULL << kvh) - 1ULL)) : 0;
+    return unit_table(c, a.row_base + x.seq * a.row_heads + kvh - below);
   };
-  for (int x = 0; x < len; ++x)
-    take_row(checked_page(c, unit_table(c, trow)[x / kP], (int)ring_page(c, u, 0)), x % kP);
-  const int n_ring = min(t, c.w);
-  for (int x = 0; x < n_ring; ++x) {
-    const bool out = (ring_out_of_window(t, d, c.w, x / kP) >> (x % kP)) & 1;
-    if (out && !(trow >= 0 && (__ldcg(&c.ring_logit[(size_t)u * c.w + x]) >= thr || ring_position(t, c.w, x) < c.n_sink))) continue;
-    take_row(ring_page(c, u, x / kP), x % kP);
+  auto wait_slot = [&](int at) {   // the at-th block may be written to its slot
+    return at < kSlots || mbar_wait_bounded(&bar[B_EMPTY + at % kSlots], ((at / kSlots) - 1) & 1);
+  };
+
+  if (warp == kLoaderWarp) {
+    // ---------------------------------------------------------------- page loader
+    asm volatile("fence.proxy.async;" ::: "memory");   // (pages were written through generic stores)
+    const uint64_t pol = l2_evict_first_policy();
+    int base = 0, go = 0;     // blocks of the segments before; drafts' blocks let in
+    segments([&](int, int item, const TreeUnit &x, int p0, int n) {
+      const int kvh = item % c.Hkv, u = unit_index(c, a.layer, x.seq, kvh);
+      const int32_t *table = page_table(x, kvh);
+      auto entry_of = [&](int i) {   // global page index of page i of the segment, -1: the drafts' page or none
+        const int p = p0 + i;
+        if (i >= n || p >= x.nk + x.nr) return -1;
+        return p < x.nk ? checked_page(c, ldcg_keep(&table[p]), (int)ring_page(c, u, 0)) : (int)ring_page(c, u, p - x.nk);
+      };
+      int entry = entry_of(lane), older = entry;   // of this lane in the current and the previous 32 pages
+      auto load = [&](int at, int gp, int half) {  // lane 0
+        if (!wait_slot(at)) { failed = true; return; }
+        if (gp < 0) {   // the drafts' page is the row warp's (which cannot wait for the slot: it would have to follow every use)
+          __threadfence_block();
+          s_info[3] = ++go;
+          return;
+        }
+        uint64_t *full = &bar[B_FULL + at % kSlots];
+        unsigned char *dst = smem + off_ring + at % kSlots * kBlockBytes;
+        const __nv_bfloat16 *src = c.pages + (int64_t)gp * kPageElems + half * kBlockElems;
+        mbar_arrive_expect_tx(full, kBlockBytes);
+        // a page that several row tiles read stays in L2 for the others
+        if (a.n_tiles == 1) bulk_load_hint(dst, src, kBlockBytes, full, pol);
+        else bulk_load(dst, src, kBlockBytes, full);
+      };
+      int i = 0;
+      for (; i <= n && !failed; ++i) {   // keys of page i, values of page i - 1
+        if (i && (i & 31) == 0) {
+          older = entry;
+          entry = entry_of(i + lane);
+        }
+        const int gk = __shfl_sync(0xffffffffu, entry, i & 31);
+        const int gv = __shfl_sync(0xffffffffu, (i & 31) == 0 ? older : entry, (i - 1) & 31);
+        if (lane == 0) {
+          if (i < n) load(base + key_at(i), gk, 0);
+          if (i > 0 && !failed) load(base + value_at(i - 1, n), gv, 1);
+        }
+        failed = __shfl_sync(0xffffffffu, (int)failed, 0) != 0;
+      }
+      base += 2 * n;
+      if (failed && lane == 0)   // do not leave while copies may still be landing
+        for (int at = max(0, base - 2 * n + 2 * i - 2 - kSlots); at < base - 2 * n + 2 * i; ++at)
+          mbar_wait_bounded(&bar[B_FULL + at % kSlots], (at / kSlots) & 1);
+      return !failed;
+    });
+  } else if (warp == kMmaWarp) {
+    // ---------------------------------------------------------------- MMA issue (whole warp, one elected lane issues)
+    constexpr uint32_t idesc_qk = instr_desc(128, 64, false), idesc_pv = instr_desc(128, 128, true);
+    constexpr uint32_t kUnits = kBlockBytes >> 4;   // a block in descriptor address units
+    const uint64_t dQ = smem_desc(smem_u32(smem), 16, 1024);
+    const uint64_t dK = smem_desc(smem_u32(smem + off_ring), 16, 1024), dV = smem_desc(smem_u32(smem + off_ring), 8192, 1024);
+    int base = 0, j0 = 0;   // blocks and pages of the segments before
+    segments([&](int seg, int, const TreeUnit &, int, int n) {
+      auto issue_qk = [&](int i) {   // S = Q . K^T of page i into its score buffer
+        const int at = base + key_at(i), s = at % kSlots, b = (j0 + i) & 1;
+        if (!mbar_wait_bounded(&bar[B_FULL + s], (at / kSlots) & 1)) { failed = true; return; }
+        fence_after();
+        umma_qk_page<16384 / 16, 8192 / 16>(tbase + b * 64, dQ, dK + (uint64_t)s * kUnits, idesc_qk);
+        umma_commit(&bar[B_S_FULL + b]);
+        umma_commit(&bar[B_EMPTY + s]);
+        if (i == n - 1) umma_commit(&bar[B_Q_EMPTY]);
+      };
+      if (!mbar_wait_bounded(&bar[B_Q_FULL], seg & 1)) failed = true;
+      for (int i = 0; i < min(2, n) && !failed; ++i) issue_qk(i);
+      for (int i = 0; i < n && !failed; ++i) {
+        const int j = j0 + i, at = base + value_at(i, n), s = at % kSlots, b = j & 1;
+        if (!mbar_wait_bounded(&bar[B_V_READY + (j & 3)], (j >> 2) & 1) || !mbar_wait_bounded(&bar[B_P_FULL + b], (j >> 1) & 1)) {
+          failed = true;
+          break;
+        }
+        fence_after();
+        umma_pv_page(tbase + 128, tbase + b * 64, dV + (uint64_t)s * kUnits, idesc_pv, i > 0 ? 1u : 0u);
+        umma_commit(&bar[B_EMPTY + s]);
+        if (i + 2 < n) issue_qk(i + 2);   // (behind P V: the pipe runs a thread's instructions in order)
+        else umma_commit(&bar[B_O_DONE + b]);
+      }
+      base += 2 * n;
+      j0 += n;
+      return !failed;
+    });
+  } else if (warp == kRowWarp) {
+    // ---------------------------------------------------------------- query rows, drafts and paths
+    int base = 0, go = 0;
+    segments([&](int seg, int item, const TreeUnit &x, int p0, int n) {
+      const int b = item / c.Hkv, kvh = item - b * c.Hkv, n_rows = min(kTreeRows, x.n * c.G - tile * kTreeRows);
+      auto copy = [&](uint32_t dst, const __nv_bfloat16 *src, bool live) {   // (not live: zeros)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+      };
+      auto landed = [&]() {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_async_smem();
+        __syncwarp();
+      };
+      if (seg > 0 && !mbar_wait_bounded(&bar[B_Q_EMPTY], (seg - 1) & 1)) failed = true;
+      if (failed) return false;
+      // Q -> two slabs of 128 rows x 128 B, 128-byte swizzle; rows behind the last are zero
+      const int64_t tok0 = (int64_t)b * a.T;
+      const int ch = lane & 15;
+      const uint32_t sQ = smem_u32(smem) + (ch >> 3) * 16384;
+      for (int r = lane >> 4; r < kTreeRows; r += 2) {
+        const int R = tile * kTreeRows + min(r, n_rows - 1), i = (int)(((unsigned long long)R * a.g_inv) >> 32), g = R - i * c.G;
+        copy(sQ + r * 128 + (((ch & 7) ^ (r & 7)) << 4), a.q + (tok0 + i) * a.q_tok + (int64_t)(kvh * c.G + g) * a.q_head + ch * 8, r < n_rows);
+      }
+      // paths: lane holds nodes lane and lane + 32; a round doubles the stretch of ancestors known
+      int up[2];
+      uint64_t anc[2];
+      bool bad = false;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int i = lane + 32 * h;
+        up[h] = i < x.n ? (a.parent ? __ldg(&a.parent[tok0 + i]) : i - 1) : -1;
+        if (up[h] < -1 || up[h] >= i) { bad = bad || i < x.n; up[h] = -1; }
+        anc[h] = 1ull << i;
+      }
+      if (bad) set_status(c, SPKV_E_BOUNDS);
+      while (__any_sync(0xffffffffu, up[0] >= 0 || up[1] >= 0)) {
+        uint64_t more[2];
+        int far[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int from = max(up[h], 0);
+          const uint64_t m0 = __shfl_sync(0xffffffffu, anc[0], from & 31), m1 = __shfl_sync(0xffffffffu, anc[1], from & 31);
+          const int f0 = __shfl_sync(0xffffffffu, up[0], from & 31), f1 = __shfl_sync(0xffffffffu, up[1], from & 31);
+          more[h] = up[h] < 0 ? 0 : from < 32 ? m0 : m1;
+          far[h] = up[h] < 0 ? -1 : from < 32 ? f0 : f1;
+        }
+        anc[0] |= more[0]; anc[1] |= more[1];
+        up[0] = far[0]; up[1] = far[1];
+      }
+      const int depth[2] = {__popcll(anc[0]) - 1, __popcll(anc[1]) - 1};
+      // ancestors that have left a node's window, but for those that are kept
+      if (__any_sync(0xffffffffu, max(depth[0], depth[1]) >= c.w)) {
+        const bool keeps = page_table(x, kvh) != nullptr;
+        const float thr = head_threshold(c, a.layer, kvh, a.tau_logit);
+        unsigned kept[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int i = lane + 32 * h;
+          kept[h] = __ballot_sync(0xffffffffu, keeps && i < x.n && (__ldg(&a.logits[(tok0 + i) * c.Hkv + kvh]) >= thr ||
+                                                                    x.t + depth[h] < c.n_sink));
+        }
+        const uint64_t keep = (uint64_t)kept[1] << 32 | kept[0];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint64_t rest = anc[h];
+          for (int left = depth[h] + 1 - c.w; left > 0; --left) {   // (an ancestor's index is lower: the lowest are the oldest)
+            const uint64_t oldest = rest & (0 - rest);
+            rest ^= oldest;
+            if (!(keep & oldest)) anc[h] ^= oldest;
+          }
+        }
+      }
+      if (seg > 0 && !mbar_wait_bounded(&bar[B_TREE_EMPTY], (seg - 1) & 1)) failed = true;
+      if (failed) return false;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s_path[lane + 32 * h] = anc[h];
+        s_depth[lane + 32 * h] = (uint8_t)depth[h];
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar[B_TREE_FULL]);
+      landed();
+      if (lane == 0) mbar_arrive(&bar[B_Q_FULL]);
+      // the drafts' page, if it is in the segment: its last
+      if (p0 + n == x.np) {
+        for (int half = 0; half < 2; ++half) {
+          const int at = base + (half ? value_at(n - 1, n) : key_at(n - 1));
+          ++go;
+          for (const long long since = clock64(); s_info[3] < go && !failed;) failed = clock64() - since > kWaitClocks;
+          if (__any_sync(0xffffffffu, failed)) { failed = true; return false; }
+          __threadfence_block();
+          const uint32_t dst = smem_u32(smem + off_ring + at % kSlots * kBlockBytes);
+          const __nv_bfloat16 *src = (half ? a.v + (int64_t)kvh * a.v_head : a.k + (int64_t)kvh * a.k_head) + ch * 8;
+          const int64_t tok = half ? a.v_tok : a.k_tok;
+          for (int r = lane >> 4; r < kP; r += 2) copy(dst + blk_off(r, ch), src + (tok0 + min(r, x.n - 1)) * tok, r < x.n);
+          landed();
+          if (lane == 0) mbar_arrive(&bar[B_FULL + at % kSlots]);
+        }
+      }
+      base += 2 * n;
+      return true;
+    });
+  } else if (warp == kScanWarp) {
+    // ---------------------------------------------------------------- values that are not finite
+    int base = 0, j0 = 0;
+    segments([&](int seg, int, const TreeUnit &, int, int n) {
+      if (lane == 0) s_odd[(seg + 2) & 7] = 0;   // (last looked at by the epilogue of segment seg - 6)
+      for (int i = 0; i < n; ++i) {
+        const int at = base + value_at(i, n), s = at % kSlots, j = j0 + i;
+        if (!mbar_wait_bounded(&bar[B_FULL + s], (at / kSlots) & 1)) { failed = true; break; }
+        uint4 *v = reinterpret_cast<uint4 *>(smem + off_ring + s * kBlockBytes) + lane;
+        __nv_bfloat162 top = __floats2bfloat162_rn(0.f, 0.f);
+#pragma unroll 8
+        for (int y = 0; y < kBlockBytes / 16 / 32; ++y) {
+          const uint4 r = v[y * 32];
+          const __nv_bfloat162 *e = reinterpret_cast<const __nv_bfloat162 *>(&r);
+#pragma unroll
+          for (int z = 0; z < 4; ++z) top = __hmax2_nan(top, __habs2(e[z]));
+        }
+        const uint32_t bits = *reinterpret_cast<const uint32_t *>(&top);
+        if (__any_sync(0xffffffffu, (bits & 0x7f80u) == 0x7f80u || (bits & 0x7f800000u) == 0x7f800000u)) {
+          for (int y = 0; y < kBlockBytes / 16 / 32; ++y) {
+            uint4 r = v[y * 32];
+            uint32_t *e = reinterpret_cast<uint32_t *>(&r);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+              if ((e[z] & 0x7f80u) == 0x7f80u) e[z] &= 0xffff0000u;
+              if ((e[z] & 0x7f800000u) == 0x7f800000u) e[z] &= 0xffffu;
+            }
+            v[y * 32] = r;
+          }
+          if (lane == 0) s_odd[seg & 7] = 1;
+          fence_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar[B_V_READY + (j & 3)]);
+      }
+      base += 2 * n;
+      j0 += n;
+      return !failed;
+    });
+  } else {
+    // ---------------------------------------------------------------- softmax
+    const int row = tid & 127;
+    const uint32_t t_lane = tbase + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_lane + 128;
+    int j0 = 0, od[2] = {0, 0};   // pages of the segments before; commits so far of the two O_DONE barriers
+    segments([&](int seg, int item, const TreeUnit &x, int p0, int n) {
+      const int b = item / c.Hkv, kvh = item - b * c.Hkv, u = unit_index(c, a.layer, x.seq, kvh);
+      const int R = tile * kTreeRows + row, n_rows = x.n * c.G, node = (int)(((unsigned long long)R * a.g_inv) >> 32);
+      const bool live = tile * kTreeRows + (row & ~31) < n_rows;   // a warp without a live row only keeps the barriers going
+      const bool keeps = page_table(x, kvh) != nullptr;
+      const int n_ring = min(x.t, c.w);
+      const float thr = head_threshold(c, a.layer, kvh, a.tau_logit);
+      float lg0 = 0.f, lg1 = 0.f;   // stored logits of this lane's two slots of the next ring page
+      auto fetch_logits = [&](int p) {
+        const int at = (p - x.nk) * kP + lane;
+        if (p < x.nk || p >= x.nk + x.nr) return;
+        const float *z = c.ring_logit + (size_t)u * c.w;
+        if (at < n_ring) lg0 = __ldcg(&z[at]);
+        if (at + 32 < n_ring) lg1 = __ldcg(&z[at + 32]);
+      };
+      fetch_logits(p0);
+      if (!mbar_wait_bounded(&bar[B_TREE_FULL], seg & 1)) { failed = true; return false; }
+      const uint64_t path = s_path[min(node, kMaxDraft - 1)];
+      const int d = s_depth[min(node, kMaxDraft - 1)];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar[B_TREE_EMPTY]);
+      // bits of page p that this row sees (p's logits fetched; whole warps)
+      auto sees = [&](int p) -> uint64_t {
+        if (p < x.nk) return bits_below(x.len - p * kP);
+        if (p >= x.nk + x.nr) return path;
+        const int rp = p - x.nk, at = rp * kP + lane;
+        const unsigned k0 = __ballot_sync(0xffffffffu, keeps && (lg0 >= thr || ring_position(x.t, c.w, at) < c.n_sink)),
+                       k1 = __ballot_sync(0xffffffffu, keeps && (lg1 >= thr || ring_position(x.t, c.w, at + 32) < c.n_sink));
+        return bits_below(n_ring - rp * kP) & (~ring_out_of_window(x.t, d, c.w, rp) | (uint64_t)k1 << 32 | k0);
+      };
+      float m_ref = -INFINITY, l = 0.f;
+      for (int i = 0; i < n; ++i) {
+        const int j = j0 + i, bf = j & 1, p = p0 + i;
+        if (!mbar_wait_bounded(&bar[B_S_FULL + bf], (j >> 1) & 1)) { failed = true; break; }
+        fence_after();
+        if (!live) { fence_before(); mbar_arrive(&bar[B_P_FULL + bf]); continue; }
+        const uint32_t t_s = t_lane + bf * 64;
+        float v[64];
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          float t16[16];
+          tmem_ld16(t_s + q4 * 16, t16);
+#pragma unroll
+          for (int y = 0; y < 16; ++y) v[q4 * 16 + y] = t16[y];
+        }
+        tmem_ld_wait();
+        if (p >= x.nk - 1 && (p >= x.nk || (x.len & (kP - 1)))) {   // (a full compact page is seen whole)
+          const uint64_t mask = sees(p);
+          const uint32_t lo = (uint32_t)mask, hi = (uint32_t)(mask >> 32);
+#pragma unroll
+          for (int y = 0; y < 32; ++y) {
+            v[y] = (lo >> y) & 1 ? v[y] : -INFINITY;
+            v[32 + y] = (hi >> y) & 1 ? v[32 + y] : -INFINITY;
+          }
+        }
+        fetch_logits(p + 1);
+        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < 64; y += 8) {
+          mx0 = max3(mx0, v[y], v[y + 1]);
+          mx1 = max3(mx1, v[y + 2], v[y + 3]);
+          mx2 = max3(mx2, v[y + 4], v[y + 5]);
+          mx3 = max3(mx3, v[y + 6], v[y + 7]);
+        }
+        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * a.scale_log2;
+        // the reference maximum moves only when the row maximum outgrows it by 2^8
+        const bool grow = mx > m_ref + 8.f;
+        const float m_new = grow ? mx : m_ref;
+        if (i > 0 && __any_sync(0xffffffffu, grow)) {
+          // O is stable between the completion of P V of the page before and the hand-over of P.  The scores of the next
+          // page were issued behind that P V; before the last page it has a barrier of its own.
+          if (!(i + 1 < n ? mbar_wait_bounded(&bar[B_S_FULL + (bf ^ 1)], ((j + 1) >> 1) & 1)
+                          : mbar_wait_bounded(&bar[B_O_DONE + (bf ^ 1)], od[bf ^ 1] & 1))) {
+            failed = true;
+            break;
+          }
+          fence_after();
+          const float f = grow ? fast_exp2(m_ref - m_new) : 1.f;   // m_ref = -inf -> 0
+#pragma unroll
+          for (int q8 = 0; q8 < 8; ++q8) {
+            float t16[16];
+            tmem_ld16(t_o + q8 * 16, t16);
+            tmem_ld_wait();
+#pragma unroll
+            for (int y = 0; y < 16; ++y) t16[y] *= f;
+            tmem_st16(t_o + q8 * 16, t16);
+          }
+          l *= f;
+        }
+        m_ref = m_new;
+        const float ms = m_ref == -INFINITY ? 0.f : m_ref;
+        const uint64_t sc2 = pack2(a.scale_log2, a.scale_log2), nms2 = pack2(-ms, -ms);
+        uint64_t l2a = pack2(0.f, 0.f), l2b = l2a;
+        // two terms: the first in the first 32 columns of the score buffer, the second in the other 32
+#pragma unroll
+        for (int q2 = 0; q2 < 2; ++q2) {
+          uint32_t hi[16], lo[16];
+#pragma unroll
+          for (int y = 0; y < 16; ++y) {
+            float e0, e1, f0, f1;
+            unpack2(fma2(pack2(v[q2 * 32 + 2 * y], v[q2 * 32 + 2 * y + 1]), sc2, nms2), e0, e1);
+            const float w0 = fast_exp2(e0), w1 = fast_exp2(e1);
+            const uint64_t w2 = pack2(w0, w1);
+            if (y & 1) l2b = add2(l2b, w2); else l2a = add2(l2a, w2);
+            hi[y] = pack_bf16(w0, w1);
+            unpack2(sub2(w2, pack2(__uint_as_float(hi[y] << 16), __uint_as_float(hi[y] & 0xffff0000u))), f0, f1);
+            lo[y] = pack_bf16(f0, f1);
+          }
+          tmem_st16u(t_s + q2 * 16, hi);
+          tmem_st16u(t_s + 32 + q2 * 16, lo);
+        }
+        float la, lb;
+        unpack2(add2(l2a, l2b), la, lb);
+        l += la + lb;
+        tmem_st_wait();
+        fence_before();
+        mbar_arrive(&bar[B_P_FULL + bf]);
+      }
+      if (failed) return false;
+      // ---- the rows' results, or their parts
+      const int last = (j0 + n - 1) & 1;
+      if (!mbar_wait_bounded(&bar[B_O_DONE + last], od[last] & 1)) { failed = true; return false; }
+      fence_after();
+      ++od[last];
+      if (n > 1) ++od[last ^ 1];
+      j0 += n;
+      const bool whole = n == x.np, starts = p0 == 0, ends = p0 + n == x.np;
+      if (row == 0 && (starts || ends)) {
+        int *e = reinterpret_cast<int *>(&a.ends[(size_t)tile * a.n_items + item]);
+        if (starts) e[0] = range;
+        if (ends) e[1] = range;
+      }
+      if (!live) return true;
+      if (s_odd[seg & 7]) {
+        // ---- infinite and NaN values of the segment, to the rows that see them
+        for (int i = 0; i < n; ++i) {
+          const int p = p0 + i;
+          fetch_logits(p);
+          const uint64_t mask = sees(p);
+          const bool draft = p >= x.nk + x.nr;
+          const __nv_bfloat16 *vb = nullptr;
+          if (!draft)
+            vb = c.pages + (int64_t)(p < x.nk ? checked_page(c, ldcg_keep(&page_table(x, kvh)[p]), (int)ring_page(c, u, 0))
+                                              : (int)ring_page(c, u, p - x.nk)) * kPageElems + kBlockElems;
+          for (int r = 0; r < kP; r += 2) {   // lane: chunk lane & 15 of row r + (lane >> 4)
+            const int y = r + (lane >> 4);
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (!draft) q = __ldcg(reinterpret_cast<const uint4 *>(vb + swz_off(y, lane & 15)));
+            else if (y < x.n) q = *reinterpret_cast<const uint4 *>(a.v + ((int64_t)b * a.T + y) * a.v_tok + (int64_t)kvh * a.v_head + (lane & 15) * 8);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            bool odd = false;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) odd = odd || (w[z] & 0x7f80u) == 0x7f80u || (w[z] & 0x7f800000u) == 0x7f800000u;
+            for (unsigned at = __ballot_sync(0xffffffffu, odd); at; at &= at - 1) {
+              const int src = __ffs(at) - 1, ch = src & 15;
+              float add[8];
+#pragma unroll
+              for (int z = 0; z < 4; ++z) {
+                const uint32_t g = __shfl_sync(0xffffffffu, w[z], src);
+                add[2 * z] = (g & 0x7f80u) == 0x7f80u ? __uint_as_float(g << 16) : 0.f;
+                add[2 * z + 1] = (g & 0x7f800000u) == 0x7f800000u ? __uint_as_float(g & 0xffff0000u) : 0.f;
+              }
+              const bool mine = (mask >> (r + (src >> 4))) & 1;
+              float t16[16];
+              tmem_ld16(t_o + (ch >> 1) * 16, t16);
+              tmem_ld_wait();
+#pragma unroll
+              for (int z = 0; z < 16; ++z)
+                if (mine && (z >> 3) == (ch & 1)) t16[z] += add[z & 7];
+              tmem_st16(t_o + (ch >> 1) * 16, t16);
+              tmem_st_wait();
+            }
+          }
+        }
+      }
+      if (whole) {
+        const float inv = 1.f / l;
+        const bool mine = R < n_rows;
+        const size_t at = ((size_t)b * a.T + (mine ? node : 0)) * c.Hq + kvh * c.G + (mine ? R - node * c.G : 0);
+#pragma unroll
+        for (int q8 = 0; q8 < 8; ++q8) {
+          float t16[16];
+          tmem_ld16(t_o + q8 * 16, t16);
+          tmem_ld_wait();
+          uint32_t w[8];
+#pragma unroll
+          for (int y = 0; y < 8; ++y) w[y] = pack_bf16(t16[2 * y] * inv, t16[2 * y + 1] * inv);
+          if (mine) {
+            uint4 *o = reinterpret_cast<uint4 *>(a.out + at * kD + q8 * 16);
+            o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+          }
+        }
+        if (mine && a.lse) a.lse[at] = (m_ref + log2f(l)) * kLn2;
+      } else {
+        const size_t part = (size_t)blockIdx.x * 2 + (starts ? 1 : 0);
+        float *o = a.part_o + part * kD * a.rows_pad + row;
+#pragma unroll
+        for (int q8 = 0; q8 < 8; ++q8) {
+          float t16[16];
+          tmem_ld16(t_o + q8 * 16, t16);
+          tmem_ld_wait();
+#pragma unroll
+          for (int y = 0; y < 16; ++y) o[(q8 * 16 + y) * a.rows_pad] = t16[y];
+        }
+        float *ml = a.part_ml + part * 2 * a.rows_pad + row;
+        ml[0] = m_ref;
+        ml[a.rows_pad] = l;
+      }
+      return true;
+    });
   }
-  int dx = 0;
-  for (int x = 0; x < n; ++x) {
-    if (!((path >> x) & 1)) continue;
-    const size_t tok = (size_t)b * a.T + x;
-    if (d - dx < c.w || (trow >= 0 && (a.logits[tok * c.Hkv + kvh] >= thr || t + dx < c.n_sink)))
-      take(a.k + (int64_t)tok * a.k_tok + (int64_t)kvh * a.k_head + lane * 4, a.v + (int64_t)tok * a.v_tok + (int64_t)kvh * a.v_head + lane * 4);
-    ++dx;
-  }
-  const size_t row = ((size_t)b * a.T + i) * c.Hq + j;
-  for (int x = 0; x < 4; ++x) a.out[row * kD + lane * 4 + x] = __float2bfloat16(o[x] / l);
-  if (a.lse && lane == 0) a.lse[row] = (m + log2f(l)) * kLn2;
+  if (failed) set_status(c, SPKV_E_TIMEOUT);
+  fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "n"(tree::kTmemCols) : "memory");
 }
+
+// ---- joining parts -----------------------------------------------------------------------------------
+// A block joins 32 rows x 32 dims of a unit that several ranges hold pieces of: four warps take every fourth piece (lane =
+// row, all 32 dims asked for at once), then add up through shared memory.
+namespace trm {
+constexpr int kWarps = 4, kDims = 32;
+}
+__global__ void __launch_bounds__(32 * trm::kWarps) tree_merge_kernel(const __grid_constant__ TreeArgs a) {
+  using namespace trm;
+  __shared__ float s_o[kWarps][kDims][33], s_m[kWarps][32], s_l[kWarps][32];
+  const CacheView &c = a.c;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int item = blockIdx.x / a.n_tiles, tile = blockIdx.x - item * a.n_tiles;
+  const int row = blockIdx.y * 32 + lane, dim0 = blockIdx.z * kDims;
+  const int b = item / c.Hkv, kvh = item - b * c.Hkv;
+  bool bad = false;
+  const int n_rows = tree_nodes(a, b, &bad) * c.G - tile * kTreeRows;
+  pdl_trigger();
+  pdl_wait();
+  const int2 ends = __ldcg(&a.ends[(size_t)tile * a.n_items + item]);
+  if (ends.x == ends.y || (int)blockIdx.y * 32 >= n_rows) return;   // whole: written already
+  float M = -INFINITY, L = 0.f, O[kDims];
+#pragma unroll
+  for (int x = 0; x < kDims; ++x) O[x] = 0.f;
+  // A part's weight against the common maximum.  A part without a visible pair has l = 0; m = -inf with another l means
+  // NaN scores.  A weight too small for its type still leaves an infinity of the part infinite.
+  auto weight = [](float m, float l, float to) {
+    if (m == -INFINITY) return l == 0.f ? 0.f : NAN;
+    const float f = fast_exp2(m - to);
+    return f < 1e-37f ? 1e-37f : f;
+  };
+  for (int r = ends.x + warp; r <= ends.y; r += kWarps) {
+    const size_t part = ((size_t)r * a.n_tiles + tile) * 2 + (r == ends.x ? 1 : 0);
+    const float *ml = a.part_ml + part * 2 * a.rows_pad + row, *o = a.part_o + (part * kD + dim0) * a.rows_pad + row;
+    float v[kDims];
+    const float m = __ldcg(ml), l = __ldcg(ml + a.rows_pad);
+#pragma unroll
+    for (int x = 0; x < kDims; ++x) v[x] = __ldcg(o + (size_t)x * a.rows_pad);
+    const float to = fmaxf(M, m), old = L == 0.f && M == -INFINITY ? 0.f : weight(M, L, to), f = weight(m, l, to);
+    M = to;
+    L = L * old + l * f;
+#pragma unroll
+    for (int x = 0; x < kDims; ++x) O[x] = (old == 0.f ? 0.f : O[x] * old) + (f == 0.f ? 0.f : v[x] * f);
+  }
+#pragma unroll
+  for (int x = 0; x < kDims; ++x) s_o[warp][x][lane] = O[x];
+  s_m[warp][lane] = M;
+  s_l[warp][lane] = L;
+  __syncthreads();
+  const int r = threadIdx.x >> 2, q = threadIdx.x & 3, at_row = blockIdx.y * 32 + r;   // this thread: 8 dims of row r
+  M = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w][r]);
+  L = 0.f;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) O[x] = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const float f = weight(s_m[w][r], s_l[w][r], M);
+    if (f == 0.f) continue;
+    L += s_l[w][r] * f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) O[x] += s_o[w][q * 8 + x][r] * f;
+  }
+  if (at_row >= n_rows) return;
+  const int R = tile * kTreeRows + at_row, node = (int)(((unsigned long long)R * a.g_inv) >> 32);
+  const size_t at = ((size_t)b * a.T + node) * c.Hq + kvh * c.G + R - node * c.G;
+  const float inv = 1.f / L;
+  *reinterpret_cast<uint4 *>(a.out + at * kD + dim0 + q * 8) =
+      make_uint4(pack_bf16(O[0] * inv, O[1] * inv), pack_bf16(O[2] * inv, O[3] * inv), pack_bf16(O[4] * inv, O[5] * inv),
+                 pack_bf16(O[6] * inv, O[7] * inv));
+  if (a.lse && dim0 == 0 && q == 0) a.lse[at] = (M + log2f(L)) * kLn2;
+}
+
+struct TreeWs { size_t off_units, off_ml, off_o, total; int n_tiles, rows_pad; };
+static TreeWs tree_ws_layout(const spkv_config_t *cfg, int B, int T, int blocks) {
+  TreeWs w;
+  auto a256 = [](size_t x) { return (x + 255) / 256 * 256; };
+  const int G = cfg->n_q_heads / cfg->n_kv_heads;
+  const size_t items = (size_t)B * cfg->n_kv_heads;
+  w.n_tiles = std::max(1, (T * G + kTreeRows - 1) / kTreeRows);
+  w.rows_pad = std::min(kTreeRows, (T * G + 31) / 32 * 32);
+  w.off_units = a256(items * w.n_tiles * sizeof(int2));
+  w.off_ml = w.off_units + a256((size_t)blocks * items * sizeof(int4));
+  w.off_o = w.off_ml + a256((size_t)blocks * 4 * w.rows_pad * 4);
+  w.total = w.off_o + a256((size_t)blocks * 2 * kD * w.rows_pad * 4);
+  return w;
+}
+constexpr int kMaxTreeBlocks = tree::kBlocksPerSm * kMaxGrid;
 
 }  // namespace spkv
 
 using namespace spkv;
 
+static std::atomic<unsigned long long> g_tree_ready;   // devices on which the kernel's attributes are set, a bit each
+
 extern "C" size_t spkv_decode_tree_workspace_bytes(const spkv_config_t *cfg, int32_t B, int32_t T) {
   if (!cfg || B < 0 || T < 0 || T > kMaxDraft || cfg->n_kv_heads < 1 || cfg->n_q_heads < cfg->n_kv_heads) return 0;
-  return 256;
+  if (B == 0 || T == 0) return 0;
+  return tree_ws_layout(cfg, B, T, kMaxTreeBlocks).total;
 }
 
 extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, const int32_t *d_seq_ids, int32_t B, int32_t T,
@@ -90,6 +731,8 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   if (B * view.Hkv > 1024) return SPKV_E_UNSUPPORTED;
   if (!d_workspace || ((uintptr_t)d_workspace & 255) || workspace_bytes < spkv_decode_tree_workspace_bytes(&cache->cfg, B, T))
     return SPKV_E_WORKSPACE;
+  const TreeWs w = tree_ws_layout(&cache->cfg, B, T, kMaxTreeBlocks);
+  char *ws = static_cast<char *>(d_workspace);
   TreeArgs a = {};
   a.c = view; a.layer = layer; a.B = B; a.T = T; a.n_items = B * view.Hkv;
   a.seq_ids = d_seq_ids; a.n_nodes = d_n_nodes; a.parent = d_parent;
@@ -101,7 +744,28 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   a.lse = d_lse_opt;
   a.scale_log2 = sm_scale * kLog2e;
   a.tau_logit = cache->tau_logit;
+  a.g_inv = ((1ULL << 32) + view.G - 1) / view.G;
+  for (int l = 0; l < layer; ++l) a.row_base += (view.Hkv - __builtin_popcountll(cache->local_mask[l])) * view.S;
+  a.row_heads = view.Hkv - __builtin_popcountll(cache->local_mask[layer]);
+  a.local_mask = cache->local_mask[layer];
+  a.ends = reinterpret_cast<int2 *>(ws);
+  a.units = reinterpret_cast<int4 *>(ws + w.off_units);
+  a.part_ml = reinterpret_cast<float *>(ws + w.off_ml);
+  a.part_o = reinterpret_cast<float *>(ws + w.off_o);
+  a.rows_pad = w.rows_pad;
+  a.n_tiles = w.n_tiles;
+  const int blocks = tree::kBlocksPerSm * std::min(kMaxGrid, cache->sm_count);
+  a.n_ranges = std::max(1, blocks / a.n_tiles);
+  a.min_pages = 2;
+  if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(tree_attention_kernel), tree::kSmemBytes, &g_tree_ready)) return rc;
+  // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
+  // cover; a plain launch waits for all of them.
+  const bool plain = (cache->cfg.flags & SPKV_FLAG_OVERLAP) != 0;
   cache->last_kind = kLastOther;
-  tree_rows_kernel<<<dim3((T * view.Hq + 3) / 4, B), 128, 0, as_stream(stream)>>>(a);
-  return check_stream_error(cudaGetLastError());
+  cudaStream_t s = as_stream(stream);
+  if (launch_link(!plain, tree_attention_kernel, dim3(a.n_ranges * a.n_tiles), dim3(tree::kThreads), (size_t)tree::kSmemBytes, s, a) !=
+      cudaSuccess)
+    return SPKV_E_CUDA;
+  return check_stream_error(launch_overlapped(tree_merge_kernel, dim3(a.n_items * a.n_tiles, a.rows_pad / 32, kD / trm::kDims),
+                                              dim3(32 * trm::kWarps), 0, s, a));
 }

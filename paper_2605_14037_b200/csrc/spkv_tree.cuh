@@ -5,6 +5,7 @@
 namespace spkv {
 
 constexpr int kMaxDraft = SPKV_MAX_DRAFT;
+constexpr int kTreeRows = 128;     // query rows (node, head of the group) of a tile: the lanes of tensor memory
 static_assert(kMaxDraft == kP, "a sequence's drafts are one page, a path is one bit per row of it");
 
 struct TreeArgs {
@@ -17,6 +18,15 @@ struct TreeArgs {
   __nv_bfloat16 *out;           // [B][T][Hq][128]
   float *lse;                   // [B][T][Hq] or null
   float scale_log2, tau_logit;
+  // ---- the tensor-core form
+  int n_tiles, n_ranges, min_pages;            // row tiles of kTreeRows; ranges the pages are cut into, not shorter than min_pages
+  unsigned long long g_inv;                    // ceil(2^32 / G): row / G as a product and a shift
+  int row_base, row_heads;                     // page-table rows of the layer: row_base + seq * row_heads + rank of the KV head
+  unsigned long long local_mask;
+  int4 *units;                                 // [blocks][n_items]: a block's units behind the first few
+  int2 *ends;                                  // [n_tiles][n_items]: ranges of a unit's first and last page
+  float *part_o, *part_ml;                     // [blocks][2][128][rows_pad], [blocks][2][2][rows_pad]
+  int rows_pad;
 };
 
 // bf16 rows that are read sixteen bytes at a time
