@@ -45,10 +45,9 @@ constexpr int off_ring = 32768, off_bar = off_ring + kSlots * kBlockBytes, off_i
               off_odd = off_info + 16, off_path = off_odd + 32, off_depth = off_path + 64 * 8, off_units = off_depth + 64,
               kSmemBytes = off_units + kUnitsHere * 16;
 static_assert(kSmemBytes <= off_bar + 1024 && off_units % 16 == 0 && off_path % 8 == 0, "two blocks an SM");
-// while the ranges are cut, the ring holds the units' lengths and page counts
-constexpr int kMaxItems = 1024;
-constexpr int off_np = off_ring, off_pre = off_np + kMaxItems * 4, off_tmp = off_pre + (kMaxItems + 4) * 4,
-              off_meta = off_tmp + 64 * 4;
+constexpr int kPerThread = 1024 / kThreads;   // items a thread looks at while the line is cut
+// What a segment costs beside its pages, in pages: its queries, its first scores, its results.
+constexpr int kSegmentCost = 3;
 
 // Where page i of a segment of n stands in the order in which a segment's blocks are loaded and used:
 // K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1)
@@ -56,7 +55,8 @@ __device__ inline int key_at(int i) { return i == 0 ? 0 : 2 * i - 1; }
 __device__ inline int value_at(int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
 }  // namespace tree
 
-// A unit as the plan sees it: {its first page in the line, sequence | nodes << 25, pairs received, kept pairs}
+// A unit as the plan sees it: {its place in the line, sequence | nodes << 25, pairs received, kept pairs}.  In the line a
+// unit takes kSegmentCost places and then one per page.
 struct TreeUnit {
   int pre, seq, n, t, len, nk, nr, np;   // nk, nr: compact and ring pages; np: all of them, 0 if the tile has no rows
   __device__ inline TreeUnit(const TreeArgs &a, int4 m, int tile) {
@@ -78,6 +78,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   volatile uint64_t *s_path = reinterpret_cast<volatile uint64_t *>(smem + off_path);   // [node] nodes it sees
   volatile uint8_t *s_depth = smem + off_depth;
   int4 *s_units = reinterpret_cast<int4 *>(smem + off_units);
+  volatile int *s_plan = reinterpret_cast<volatile int *>(smem + off_path);     // (before the paths are)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int range = blockIdx.x / a.n_tiles, tile = blockIdx.x - range * a.n_tiles;
   if (tid == 0) {
@@ -86,50 +87,86 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   }
   pdl_wait();
   pdl_trigger();   // (only now: what follows may then rely on everything before this launch)
-  // ---- the line of pages, its cut, and this block's units
+  // ---- the line of pages, its cut, and this block's units.  Thread x holds items 4 x .. 4 x + 3.
   int r0, r1;
   {
-    int *s_np = reinterpret_cast<int *>(smem + off_np), *s_pre = reinterpret_cast<int *>(smem + off_pre),
-        *s_tmp = reinterpret_cast<int *>(smem + off_tmp);
-    int4 *s_meta = reinterpret_cast<int4 *>(smem + off_meta);
-    for (int i = tid; i < a.n_items; i += kThreads) {
-      const int b = i / c.Hkv, kvh = i - b * c.Hkv;
-      int seq = a.seq_ids[b];
-      bool bad = false;
-      int n = tree_nodes(a, b, &bad);
-      if (seq < 0 || seq >= c.S) { bad = true; seq = 0; n = 0; }
-      if (bad && blockIdx.x == 0) set_status(c, SPKV_E_BOUNDS);
-      const int u = unit_index(c, a.layer, seq, kvh);
-      const int t = ldcg_keep(&c.t[u]), len = ldcg_keep(&c.len[u]);
-      s_meta[i] = make_int4(0, seq | n << 25, t, len);
-      s_np[i] = TreeUnit(a, s_meta[i], tile).np;
-      if (range == 0 && s_np[i] == 0) a.ends[(size_t)tile * a.n_items + i] = make_int2(-1, -1);   // nothing to join
+    int4 meta[kPerThread];
+    int cost[kPerThread], sum = 0;
+    int seq[kPerThread], n[kPerThread];
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+      const int i = tid * kPerThread + k, b = i < a.n_items ? i / c.Hkv : 0;
+      seq[k] = i < a.n_items ? a.seq_ids[b] : -1;
+      n[k] = i < a.n_items ? tree_nodes(a, b, &bad) : 0;
     }
-    __syncthreads();
-    block_exclusive_scan(s_np, s_pre, a.n_items, s_tmp);
-    const int total = s_pre[a.n_items];
-    const int nb = min(a.n_ranges, (total + a.min_pages - 1) / a.min_pages);
-    if (range >= nb) return;
-    const int snap = total / nb / 16;
-    r0 = range_cut(range, nb, total, snap, s_pre, a.n_items);
-    r1 = range_cut(range + 1, nb, total, snap, s_pre, a.n_items);
-    if (r0 >= r1) return;
-    if (tid < 2) {   // units of the first and the last page
-      const int p = tid ? r1 - 1 : r0;
-      int lo = 0, hi = a.n_items;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s_pre[mid] <= p) lo = mid; else hi = mid;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+      const int i = tid * kPerThread + k;
+      const bool ok = seq[k] >= 0 && seq[k] < c.S;
+      meta[k] = make_int4(0, ok ? seq[k] | n[k] << 25 : 0, 0, 0);
+      if (i < a.n_items) {
+        bad = bad || !ok;
+        const int u = unit_index(c, a.layer, ok ? seq[k] : 0, i % c.Hkv);
+        meta[k].z = ldcg_keep(&c.t[u]);
+        meta[k].w = ldcg_keep(&c.len[u]);
       }
-      s_info[1 + tid] = lo;
+    }
+    if (bad && blockIdx.x == 0) set_status(c, SPKV_E_BOUNDS);
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+      const int i = tid * kPerThread + k, np = TreeUnit(a, meta[k], tile).np;
+      cost[k] = np ? np + kSegmentCost : 0;
+      meta[k].x = sum;
+      sum += cost[k];
+      if (range == 0 && i < a.n_items && np == 0) a.ends[(size_t)tile * a.n_items + i] = make_int2(-1, -1);   // nothing to join
+    }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    if (lane == 31) s_plan[warp] = incl;
+    if (tid == 0) s_info[1] = s_info[2] = 0;
+    __syncthreads();
+    int total = 0, before = incl - sum;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+      const int x = s_plan[w];
+      total += x;
+      if (w < warp) before += x;
+    }
+    const int nb = min(a.n_ranges, (total + a.min_cost - 1) / a.min_cost);
+    if (range >= nb) return;
+    // equal lengths, but for a cut that falls next to the border of two units: it moves onto it
+    const int snap = total / nb / 16;
+    auto cut = [&](int x) { return total < 1 << 22 ? (int)((unsigned)x * (unsigned)total / (unsigned)nb) : (int)((long long)x * total / nb); };
+    const int c0 = cut(range), c1 = cut(range + 1);
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+      meta[k].x += before;
+      const int from = meta[k].x, to = from + cost[k];
+      if (from <= c0 && c0 < to) {
+        s_info[1] = tid * kPerThread + k;
+        s_plan[8] = c0 - from <= snap ? from : to - c0 <= snap ? to : c0;
+      }
+      if (from < c1 && c1 <= to) {
+        s_info[2] = tid * kPerThread + k;
+        s_plan[9] = c1 - from <= snap ? from : to - c1 <= snap ? to : c1;
+      }
     }
     __syncthreads();
-    const int u0 = s_info[1], n_units = s_info[2] - u0 + 1;
-    for (int i = tid; i < n_units; i += kThreads) {
-      int4 m = s_meta[u0 + i];
-      m.x = s_pre[u0 + i];
-      if (i < kUnitsHere) s_units[i] = m;
-      else a.units[(size_t)blockIdx.x * a.n_items + i] = m;
+    r0 = s_plan[8];
+    r1 = s_plan[9];
+    if (r0 >= r1) return;
+    const int u0 = s_info[1], u1 = s_info[2];
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+      const int i = tid * kPerThread + k - u0;
+      if (i < 0 || i > u1 - u0) continue;
+      if (i < kUnitsHere) s_units[i] = meta[k];
+      else a.units[(size_t)blockIdx.x * a.n_items + i] = meta[k];
     }
     if (tid < 8) s_odd[tid] = 0;
     if (tid == 8) s_info[3] = 0;
@@ -139,7 +176,6 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
                  "n"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  fence_async_smem();   // the ring's bytes go from the plan to the copies
   fence_before();
   __syncthreads();
   fence_after();
@@ -151,9 +187,9 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     int seg = 0;
     for (int i = 0; i < n_units; ++i) {
       const TreeUnit x(a, i < kUnitsHere ? s_units[i] : a.units[(size_t)blockIdx.x * a.n_items + i], tile);
-      const int s = max(x.pre, r0), e = min(x.pre + x.np, r1);
+      const int first = x.pre + kSegmentCost, s = max(first, r0), e = min(first + x.np, r1);
       if (e <= s) continue;
-      if (!f(seg, u0 + i, x, s - x.pre, e - s)) return;
+      if (!f(seg, u0 + i, x, s - first, e - s)) return;
       ++seg;
     }
   };
@@ -252,7 +288,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     });
   } else if (warp == kRowWarp) {
     // ---------------------------------------------------------------- query rows, drafts and paths
-    int base = 0, go = 0;
+    int base = 0, go = 0, masked = 0;   // blocks of the segments so far; drafts' blocks waited for; segments with ring or drafts
     segments([&](int seg, int item, const TreeUnit &x, int p0, int n) {
       const int b = item / c.Hkv, kvh = item - b * c.Hkv, n_rows = min(kTreeRows, x.n * c.G - tile * kTreeRows);
       auto copy = [&](uint32_t dst, const __nv_bfloat16 *src, bool live) {   // (not live: zeros)
@@ -265,14 +301,29 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       };
       if (seg > 0 && !mbar_wait_bounded(&bar[B_Q_EMPTY], (seg - 1) & 1)) failed = true;
       if (failed) return false;
-      // Q -> two slabs of 128 rows x 128 B, 128-byte swizzle; rows behind the last are zero
+      // Q -> two slabs of 128 rows x 128 B, 128-byte swizzle (rows behind the last keep what they hold: a row of a tile
+      // does not touch another)
       const int64_t tok0 = (int64_t)b * a.T;
       const int ch = lane & 15;
-      const uint32_t sQ = smem_u32(smem) + (ch >> 3) * 16384;
-      for (int r = lane >> 4; r < kTreeRows; r += 2) {
-        const int R = tile * kTreeRows + min(r, n_rows - 1), i = (int)(((unsigned long long)R * a.g_inv) >> 32), g = R - i * c.G;
-        copy(sQ + r * 128 + (((ch & 7) ^ (r & 7)) << 4), a.q + (tok0 + i) * a.q_tok + (int64_t)(kvh * c.G + g) * a.q_head + ch * 8, r < n_rows);
+      {
+        int r = lane >> 4, R = tile * kTreeRows + r, i = (int)(((unsigned long long)R * a.g_inv) >> 32), g = R - i * c.G;
+        const __nv_bfloat16 *src = a.q + (tok0 + i) * a.q_tok + (int64_t)(kvh * c.G + g) * a.q_head + ch * 8;
+        const int64_t next_node = a.q_tok - (int64_t)c.G * a.q_head;
+        const uint32_t sQ = smem_u32(smem) + (ch >> 3) * 16384;
+#pragma unroll 4
+        for (; r < n_rows; r += 2) {
+          copy(sQ + r * 128 + (((ch & 7) ^ (r & 7)) << 4), src, true);
+          src += 2 * a.q_head;
+          g += 2;
+          if (g >= c.G) { g -= c.G; src += next_node; }
+          if (g >= c.G) { g -= c.G; src += next_node; }   // (groups of one)
+        }
       }
+      landed();
+      if (lane == 0) mbar_arrive(&bar[B_Q_FULL]);
+      base += 2 * n;
+      if (p0 + n <= x.nk) return true;   // compact pages only
+      ++masked;
       // paths: lane holds nodes lane and lane + 32; a round doubles the stretch of ancestors known
       int up[2];
       uint64_t anc[2];
@@ -322,7 +373,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
           }
         }
       }
-      if (seg > 0 && !mbar_wait_bounded(&bar[B_TREE_EMPTY], (seg - 1) & 1)) failed = true;
+      if (masked > 1 && !mbar_wait_bounded(&bar[B_TREE_EMPTY], masked & 1)) failed = true;
       if (failed) return false;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -331,12 +382,10 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar[B_TREE_FULL]);
-      landed();
-      if (lane == 0) mbar_arrive(&bar[B_Q_FULL]);
       // the drafts' page, if it is in the segment: its last
       if (p0 + n == x.np) {
         for (int half = 0; half < 2; ++half) {
-          const int at = base + (half ? value_at(n - 1, n) : key_at(n - 1));
+          const int at = base - 2 * n + (half ? value_at(n - 1, n) : key_at(n - 1));
           ++go;
           for (const long long since = clock64(); s_info[3] < go && !failed;) failed = clock64() - since > kWaitClocks;
           if (__any_sync(0xffffffffu, failed)) { failed = true; return false; }
@@ -349,7 +398,6 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
           if (lane == 0) mbar_arrive(&bar[B_FULL + at % kSlots]);
         }
       }
-      base += 2 * n;
       return true;
     });
   } else if (warp == kScanWarp) {
@@ -395,7 +443,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     // ---------------------------------------------------------------- softmax
     const int row = tid & 127;
     const uint32_t t_lane = tbase + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_lane + 128;
-    int j0 = 0, od[2] = {0, 0};   // pages of the segments before; commits so far of the two O_DONE barriers
+    int j0 = 0, masked = 0, od[2] = {0, 0};   // pages of the segments before; segments with ring or drafts; commits so far of O_DONE
     segments([&](int seg, int item, const TreeUnit &x, int p0, int n) {
       const int b = item / c.Hkv, kvh = item - b * c.Hkv, u = unit_index(c, a.layer, x.seq, kvh);
       const int R = tile * kTreeRows + row, n_rows = x.n * c.G, node = (int)(((unsigned long long)R * a.g_inv) >> 32);
@@ -412,11 +460,16 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         if (at + 32 < n_ring) lg1 = __ldcg(&z[at + 32]);
       };
       fetch_logits(p0);
-      if (!mbar_wait_bounded(&bar[B_TREE_FULL], seg & 1)) { failed = true; return false; }
-      const uint64_t path = s_path[min(node, kMaxDraft - 1)];
-      const int d = s_depth[min(node, kMaxDraft - 1)];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bar[B_TREE_EMPTY]);
+      uint64_t path = 0;
+      int d = 0;
+      auto fetch_path = [&]() {   // (once a segment with ring or drafts, before its first such page)
+        if (!mbar_wait_bounded(&bar[B_TREE_FULL], masked & 1)) failed = true;
+        ++masked;
+        path = s_path[min(node, kMaxDraft - 1)];
+        d = s_depth[min(node, kMaxDraft - 1)];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar[B_TREE_EMPTY]);
+      };
       // bits of page p that this row sees (p's logits fetched; whole warps)
       auto sees = [&](int p) -> uint64_t {
         if (p < x.nk) return bits_below(x.len - p * kP);
@@ -429,7 +482,8 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       float m_ref = -INFINITY, l = 0.f;
       for (int i = 0; i < n; ++i) {
         const int j = j0 + i, bf = j & 1, p = p0 + i;
-        if (!mbar_wait_bounded(&bar[B_S_FULL + bf], (j >> 1) & 1)) { failed = true; break; }
+        if (p >= x.nk && (i == 0 || p == x.nk)) fetch_path();
+        if (failed || !mbar_wait_bounded(&bar[B_S_FULL + bf], (j >> 1) & 1)) { failed = true; break; }
         fence_after();
         if (!live) { fence_before(); mbar_arrive(&bar[B_P_FULL + bf]); continue; }
         const uint32_t t_s = t_lane + bf * 64;
@@ -462,7 +516,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         }
         const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * a.scale_log2;
         // the reference maximum moves only when the row maximum outgrows it by 2^8
-        const bool grow = mx > m_ref + 8.f;
+        const bool grow = mx > m_ref + 8.f && R < n_rows;
         const float m_new = grow ? mx : m_ref;
         if (i > 0 && __any_sync(0xffffffffu, grow)) {
           // O is stable between the completion of P V of the page before and the hand-over of P.  The scores of the next
@@ -616,13 +670,10 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
 }
 
 // ---- joining parts -----------------------------------------------------------------------------------
-// A block joins 32 rows x 32 dims of a unit that several ranges hold pieces of: four warps take every fourth piece (lane =
-// row, all 32 dims asked for at once), then add up through shared memory.
-namespace trm {
-constexpr int kWarps = 4, kDims = 32;
-}
-__global__ void __launch_bounds__(32 * trm::kWarps) tree_merge_kernel(const __grid_constant__ TreeArgs a) {
-  using namespace trm;
+// A block joins 32 rows x kDims dims of a unit that several ranges hold pieces of: its warps take every kWarps-th piece
+// (lane = row, all its dims of kAhead pieces asked for at once), then add up through shared memory.
+template <int kWarps, int kDims, int kAhead>
+__global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_constant__ TreeArgs a) {
   __shared__ float s_o[kWarps][kDims][33], s_m[kWarps][32], s_l[kWarps][32];
   const CacheView &c = a.c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -645,47 +696,71 @@ __global__ void __launch_bounds__(32 * trm::kWarps) tree_merge_kernel(const __gr
     const float f = fast_exp2(m - to);
     return f < 1e-37f ? 1e-37f : f;
   };
-  for (int r = ends.x + warp; r <= ends.y; r += kWarps) {
-    const size_t part = ((size_t)r * a.n_tiles + tile) * 2 + (r == ends.x ? 1 : 0);
-    const float *ml = a.part_ml + part * 2 * a.rows_pad + row, *o = a.part_o + (part * kD + dim0) * a.rows_pad + row;
-    float v[kDims];
-    const float m = __ldcg(ml), l = __ldcg(ml + a.rows_pad);
+  for (int r0 = ends.x + warp; r0 <= ends.y; r0 += kWarps * kAhead) {
+    float v[kAhead][kDims], m[kAhead], l[kAhead], to = M;
 #pragma unroll
-    for (int x = 0; x < kDims; ++x) v[x] = __ldcg(o + (size_t)x * a.rows_pad);
-    const float to = fmaxf(M, m), old = L == 0.f && M == -INFINITY ? 0.f : weight(M, L, to), f = weight(m, l, to);
+    for (int y = 0; y < kAhead; ++y) {
+      const int r = min(r0 + y * kWarps, ends.y);
+      const size_t part = ((size_t)r * a.n_tiles + tile) * 2 + (r == ends.x ? 1 : 0);
+      const float *ml = a.part_ml + part * 2 * a.rows_pad + row, *o = a.part_o + (part * kD + dim0) * a.rows_pad + row;
+      m[y] = __ldcg(ml);
+      l[y] = __ldcg(ml + a.rows_pad);
+#pragma unroll
+      for (int x = 0; x < kDims; ++x) v[y][x] = __ldcg(o + x * a.rows_pad);
+      if (r0 + y * kWarps > ends.y) { m[y] = -INFINITY; l[y] = 0.f; }
+    }
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) to = fmaxf(to, m[y]);
+    const float old = weight(M, L, to);
     M = to;
-    L = L * old + l * f;
+    L *= old;
 #pragma unroll
-    for (int x = 0; x < kDims; ++x) O[x] = (old == 0.f ? 0.f : O[x] * old) + (f == 0.f ? 0.f : v[x] * f);
+    for (int x = 0; x < kDims; ++x) O[x] = old == 0.f ? 0.f : O[x] * old;
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) {
+      const float f = weight(m[y], l[y], M);
+      if (f == 0.f) continue;
+      L = fmaf(l[y], f, L);
+#pragma unroll
+      for (int x = 0; x < kDims; ++x) O[x] = fmaf(v[y][x], f, O[x]);
+    }
   }
 #pragma unroll
   for (int x = 0; x < kDims; ++x) s_o[warp][x][lane] = O[x];
   s_m[warp][lane] = M;
   s_l[warp][lane] = L;
   __syncthreads();
-  const int r = threadIdx.x >> 2, q = threadIdx.x & 3, at_row = blockIdx.y * 32 + r;   // this thread: 8 dims of row r
-  M = -INFINITY;
+  for (int z = threadIdx.x; z < 32 * kDims / 8; z += 32 * kWarps) {   // eight dims of a row
+    const int r = z / (kDims / 8), q = z % (kDims / 8), at_row = blockIdx.y * 32 + r;
+    if (at_row >= n_rows) return;
+    float Mr = -INFINITY, Lr = 0.f, o[8] = {};
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w][r]);
-  L = 0.f;
+    for (int w = 0; w < kWarps; ++w) Mr = fmaxf(Mr, s_m[w][r]);
 #pragma unroll
-  for (int x = 0; x < 8; ++x) O[x] = 0.f;
+    for (int w = 0; w < kWarps; ++w) {
+      const float f = weight(s_m[w][r], s_l[w][r], Mr);
+      if (f == 0.f) continue;
+      Lr = fmaf(s_l[w][r], f, Lr);
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    const float f = weight(s_m[w][r], s_l[w][r], M);
-    if (f == 0.f) continue;
-    L += s_l[w][r] * f;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) O[x] += s_o[w][q * 8 + x][r] * f;
+      for (int x = 0; x < 8; ++x) o[x] = fmaf(s_o[w][q * 8 + x][r], f, o[x]);
+    }
+    const int R = tile * kTreeRows + at_row, node = (int)(((unsigned long long)R * a.g_inv) >> 32);
+    const size_t at = ((size_t)b * a.T + node) * c.Hq + kvh * c.G + R - node * c.G;
+    const float inv = 1.f / Lr;
+    *reinterpret_cast<uint4 *>(a.out + at * kD + dim0 + q * 8) =
+        make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv), pack_bf16(o[4] * inv, o[5] * inv),
+                   pack_bf16(o[6] * inv, o[7] * inv));
+    if (a.lse && dim0 == 0 && q == 0) a.lse[at] = (Mr + log2f(Lr)) * kLn2;
   }
-  if (at_row >= n_rows) return;
-  const int R = tile * kTreeRows + at_row, node = (int)(((unsigned long long)R * a.g_inv) >> 32);
-  const size_t at = ((size_t)b * a.T + node) * c.Hq + kvh * c.G + R - node * c.G;
-  const float inv = 1.f / L;
-  *reinterpret_cast<uint4 *>(a.out + at * kD + dim0 + q * 8) =
-      make_uint4(pack_bf16(O[0] * inv, O[1] * inv), pack_bf16(O[2] * inv, O[3] * inv), pack_bf16(O[4] * inv, O[5] * inv),
-                 pack_bf16(O[6] * inv, O[7] * inv));
-  if (a.lse && dim0 == 0 && q == 0) a.lse[at] = (M + log2f(L)) * kLn2;
+}
+
+template <int kWarps, int kDims, int kAhead>
+static cudaError_t launch_tree_merge(const TreeArgs &a, cudaStream_t s) {
+  static std::atomic<unsigned long long> ready;
+  auto kernel = tree_merge_kernel<kWarps, kDims, kAhead>;
+  // (with another split of an SM's memory than the attention kernel's, the SM would have to change it between the two)
+  if (whole_shared_memory(reinterpret_cast<const void *>(kernel), 0, &ready)) return cudaErrorUnknown;
+  return launch_overlapped(kernel, dim3(a.n_items * a.n_tiles, a.rows_pad / 32, kD / kDims), dim3(32 * kWarps), 0, s, a);
 }
 
 struct TreeWs { size_t off_units, off_ml, off_o, total; int n_tiles, rows_pad; };
@@ -756,7 +831,7 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   a.n_tiles = w.n_tiles;
   const int blocks = tree::kBlocksPerSm * std::min(kMaxGrid, cache->sm_count);
   a.n_ranges = std::max(1, blocks / a.n_tiles);
-  a.min_pages = 2;
+  a.min_cost = 2 + tree::kSegmentCost;
   if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(tree_attention_kernel), tree::kSmemBytes, &g_tree_ready)) return rc;
   // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
   // cover; a plain launch waits for all of them.
@@ -766,6 +841,6 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   if (launch_link(!plain, tree_attention_kernel, dim3(a.n_ranges * a.n_tiles), dim3(tree::kThreads), (size_t)tree::kSmemBytes, s, a) !=
       cudaSuccess)
     return SPKV_E_CUDA;
-  return check_stream_error(launch_overlapped(tree_merge_kernel, dim3(a.n_items * a.n_tiles, a.rows_pad / 32, kD / trm::kDims),
-                                              dim3(32 * trm::kWarps), 0, s, a));
+  // pieces of a unit: about ranges / units + 1
+  return check_stream_error(a.n_ranges < 4 * a.n_items ? launch_tree_merge<2, 32, 1>(a, s) : launch_tree_merge<8, 16, 2>(a, s));
 }

@@ -19,7 +19,7 @@ struct TreeArgs {
   float *lse;                   // [B][T][Hq] or null
   float scale_log2, tau_logit;
   // ---- the tensor-core form
-  int n_tiles, n_ranges, min_pages;            // row tiles of kTreeRows; ranges the pages are cut into, not shorter than min_pages
+  int n_tiles, n_ranges, min_cost;             // row tiles of kTreeRows; ranges the line of pages is cut into, not shorter than min_cost
   unsigned long long g_inv;                    // ceil(2^32 / G): row / G as a product and a shift
   int row_base, row_heads;                     // page-table rows of the layer: row_base + seq * row_heads + rank of the KV head
   unsigned long long local_mask;
