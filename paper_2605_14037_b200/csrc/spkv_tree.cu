@@ -20,7 +20,7 @@
 //     0 and marks the segment; its epilogue then adds those elements to the rows that see them.  (Clean pages cost nothing: the
 //     warp runs ahead of P V.)
 //
-// Warps: 0 MMA issue and tensor memory, 1 page loader, 2 query rows, drafts and paths, 3 look through the values, 4-7
+// Warps: 0 MMA issue and tensor memory, 1 page loader, 2 query rows, drafts and paths, 3 look through the values, 4-11
 // softmax.  Shared memory (113 KB, two blocks an SM): Q 32 KB, ring of five 16 KB key or value blocks in the order in which the
 // MMAs want them.  Tensor memory (256 columns): score buffers at [0, 64) and [64, 128), O at [128, 256).  All waits are bounded.
 #include <math.h>
@@ -34,18 +34,18 @@
 namespace spkv {
 
 namespace tree {
-constexpr int kThreads = 256, kBlocksPerSm = 2;
+constexpr int kThreads = 384, kBlocksPerSm = 2;
 constexpr int kMmaWarp = 0, kLoaderWarp = 1, kRowWarp = 2, kScanWarp = 3;
 constexpr int kTmemCols = 256;
 constexpr int kBlockBytes = kPageBytes / 2, kSlots = 5;
 enum { B_FULL = 0, B_EMPTY = 5, B_V_READY = 10 /* [page & 3] */, B_S_FULL = 14 /* [page & 1] */, B_P_FULL = 16, B_O_DONE = 18,
        B_Q_FULL = 20, B_Q_EMPTY, B_TREE_FULL, B_TREE_EMPTY, B_COUNT };
-constexpr int kUnitsHere = 12;      // units of a block that shared memory holds; the others stand in the workspace
+constexpr int kUnitsHere = 6;       // units of a block that shared memory holds; the others stand in the workspace
 constexpr int off_ring = 32768, off_bar = off_ring + kSlots * kBlockBytes, off_info = off_bar + B_COUNT * 8,
-              off_odd = off_info + 16, off_path = off_odd + 32, off_depth = off_path + 64 * 8, off_units = off_depth + 64,
-              kSmemBytes = off_units + kUnitsHere * 16;
+              off_odd = off_info + 16, off_path = off_odd + 32, off_depth = off_path + 64 * 8, off_grow = off_depth + 64,
+              off_bad = off_grow + 2 * 8 * 4, off_units = off_bad + 32, kSmemBytes = off_units + kUnitsHere * 16;
 static_assert(kSmemBytes <= off_bar + 1024 && off_units % 16 == 0 && off_path % 8 == 0, "two blocks an SM");
-constexpr int kPerThread = 1024 / kThreads;   // items a thread looks at while the line is cut
+constexpr int kPerThread = (1024 + kThreads - 1) / kThreads;   // items a thread looks at while the line is cut
 // What a segment costs beside its pages, in pages: its queries, its first scores, its results.
 constexpr int kSegmentCost = 3;
 
@@ -67,6 +67,89 @@ struct TreeUnit {
   }
 };
 
+// the unit's page table, null for a head that keeps nothing
+__device__ inline const int32_t *tree_table(const TreeArgs &a, const TreeUnit &x, int item) {
+  const int kvh = item % a.c.Hkv;
+  if (kvh < 64 && ((a.local_mask >> kvh) & 1)) return nullptr;
+  const int below = kvh < 64 ? __popcll(a.local_mask & ((1ULL << kvh) - 1ULL)) : 0;
+  return unit_table(a.c, a.row_base + x.seq * a.row_heads + kvh - below);
+}
+__device__ inline int tree_node_of(const TreeArgs &a, int R) { return (int)(((unsigned long long)R * a.g_inv) >> 32); }
+// row of the results that query row R of an item belongs to
+__device__ inline size_t tree_out_row(const TreeArgs &a, int item, int R) {
+  const int b = item / a.c.Hkv, kvh = item - b * a.c.Hkv, node = tree_node_of(a, R);
+  return ((size_t)b * a.T + node) * a.c.Hq + kvh * a.c.G + R - node * a.c.G;
+}
+// Of the 32 slots of half h of ring page p: the stored logit of this lane's.  (No ring page: anything.)
+__device__ inline float tree_logit(const TreeArgs &a, const TreeUnit &x, int item, int p, int h) {
+  const int at = (p - x.nk) * kP + h * 32 + (threadIdx.x & 31);
+  if (p < x.nk || at >= min(x.t, a.c.w)) return 0.f;
+  return __ldcg(&a.c.ring_logit[(size_t)unit_index(a.c, a.layer, x.seq, item % a.c.Hkv) * a.c.w + at]);
+}
+// The keys of half h of page p that query row R sees; z = tree_logit(.., p, h).  Whole warps.
+__device__ inline uint32_t tree_sees(const TreeArgs &a, const TreeUnit &x, int item, int p, int h, float z,
+                                     const volatile uint64_t *s_path, const volatile uint8_t *s_depth, int R) {
+  const CacheView &c = a.c;
+  if (p < x.nk) return (uint32_t)(bits_below(x.len - p * kP) >> (32 * h));
+  const int node = min(tree_node_of(a, R), kMaxDraft - 1);
+  if (p >= x.nk + x.nr) return (uint32_t)(s_path[node] >> (32 * h));
+  const int kvh = item % c.Hkv, rp = p - x.nk, at = rp * kP + h * 32 + (threadIdx.x & 31);
+  const bool keeps = !(kvh < 64 && ((a.local_mask >> kvh) & 1));
+  const float thr = head_threshold(c, a.layer, kvh, a.tau_logit);
+  const unsigned kept = __ballot_sync(0xffffffffu, keeps && (z >= thr || ring_position(x.t, c.w, at) < c.n_sink));
+  return (uint32_t)(bits_below(min(x.t, c.w) - rp * kP) >> (32 * h)) &
+         (~(uint32_t)(ring_out_of_window(x.t, s_depth[node], c.w, rp) >> (32 * h)) | kept);
+}
+// Infinite and NaN values of a segment's pages (which P V took for 0), to the rows that see them: this half's 64 dims of O,
+// at t_o.  Whole warps; rare.
+__device__ __noinline__ void tree_add_odd_values(const TreeArgs &a, int seq_nodes, int t, int len, int tile, int item, int p0, int n,
+                                                 int half, uint32_t t_o, const volatile uint64_t *s_path,
+                                                 const volatile uint8_t *s_depth, int R) {
+  using namespace tc5;
+  const TreeUnit x(a, make_int4(0, seq_nodes, t, len), tile);
+  const CacheView &c = a.c;
+  const int lane = threadIdx.x & 31, b = item / c.Hkv, kvh = item - b * c.Hkv, u = unit_index(c, a.layer, x.seq, kvh);
+  for (int p = p0; p < p0 + n; ++p) {
+    const uint64_t mask = (uint64_t)tree_sees(a, x, item, p, 1, tree_logit(a, x, item, p, 1), s_path, s_depth, R) << 32 |
+                          tree_sees(a, x, item, p, 0, tree_logit(a, x, item, p, 0), s_path, s_depth, R);
+    const bool draft = p >= x.nk + x.nr;
+    const __nv_bfloat16 *vb = nullptr;
+    if (!draft)
+      vb = c.pages + (int64_t)(p < x.nk ? checked_page(c, ldcg_keep(&tree_table(a, x, item)[p]), (int)ring_page(c, u, 0))
+                                        : (int)ring_page(c, u, p - x.nk)) * kPageElems + kBlockElems;
+    for (int r = 0; r < kP; r += 4) {   // lane: chunk lane & 7 of this half of row r + (lane >> 3)
+      const int y = r + (lane >> 3), mine = half * 8 + (lane & 7);
+      uint4 q = make_uint4(0, 0, 0, 0);
+      if (!draft) q = __ldcg(reinterpret_cast<const uint4 *>(vb + swz_off(y, mine)));
+      else if (y < x.n) q = *reinterpret_cast<const uint4 *>(a.v + ((int64_t)b * a.T + y) * a.v_tok + (int64_t)kvh * a.v_head + mine * 8);
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+      bool odd = false;
+#pragma unroll
+      for (int z = 0; z < 4; ++z) odd = odd || (w[z] & 0x7f80u) == 0x7f80u || (w[z] & 0x7f800000u) == 0x7f800000u;
+      for (unsigned at = __ballot_sync(0xffffffffu, odd); at; at &= at - 1) {
+        const int src = __ffs(at) - 1, ch = src & 7;
+        float add[8];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          const uint32_t g = __shfl_sync(0xffffffffu, w[z], src);
+          add[2 * z] = (g & 0x7f80u) == 0x7f80u ? __uint_as_float(g << 16) : 0.f;
+          add[2 * z + 1] = (g & 0x7f800000u) == 0x7f800000u ? __uint_as_float(g & 0xffff0000u) : 0.f;
+        }
+        const bool seen = (mask >> (r + (src >> 3))) & 1;
+        float t16[16];
+        tmem_ld16(t_o + (ch >> 1) * 16, t16);
+        tmem_ld_wait();
+#pragma unroll
+        for (int z = 0; z < 16; ++z)
+          if (seen && (z >> 3) == (ch & 1)) t16[z] += add[z & 7];
+        tmem_st16(t_o + (ch >> 1) * 16, t16);
+        tmem_st_wait();
+      }
+    }
+  }
+  __syncwarp();
+}
+
 __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_attention_kernel(const __grid_constant__ TreeArgs a) {
   using namespace tc5;
   using namespace tree;
@@ -77,17 +160,19 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   volatile int *s_odd = reinterpret_cast<volatile int *>(smem + off_odd);       // [segment & 7] values that are not finite
   volatile uint64_t *s_path = reinterpret_cast<volatile uint64_t *>(smem + off_path);   // [node] nodes it sees
   volatile uint8_t *s_depth = smem + off_depth;
+  volatile unsigned *s_grow = reinterpret_cast<volatile unsigned *>(smem + off_grow);   // [page & 1][warp - 4] rows whose maximum moves
+  volatile uint8_t *s_bad = smem + off_bad;   // [page & 1 or 2][warp - 4] a wait ran out
   int4 *s_units = reinterpret_cast<int4 *>(smem + off_units);
   volatile int *s_plan = reinterpret_cast<volatile int *>(smem + off_path);     // (before the paths are)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int range = blockIdx.x / a.n_tiles, tile = blockIdx.x - range * a.n_tiles;
   if (tid == 0) {
-    for (int i = 0; i < B_COUNT; ++i) mbar_init(&bar[i], i == B_P_FULL || i == B_P_FULL + 1 ? 128 : i == B_TREE_EMPTY ? 4 : 1);
+    for (int i = 0; i < B_COUNT; ++i) mbar_init(&bar[i], i == B_P_FULL || i == B_P_FULL + 1 ? 256 : i == B_TREE_EMPTY ? 8 : 1);
     mbar_fence_init();
   }
   pdl_wait();
   pdl_trigger();   // (only now: what follows may then rely on everything before this launch)
-  // ---- the line of pages, its cut, and this block's units.  Thread x holds items 4 x .. 4 x + 3.
+  // ---- the line of pages, its cut, and this block's units.  Thread x holds items kPerThread x and on.
   int r0, r1;
   {
     int4 meta[kPerThread];
@@ -149,16 +234,16 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       const int from = meta[k].x, to = from + cost[k];
       if (from <= c0 && c0 < to) {
         s_info[1] = tid * kPerThread + k;
-        s_plan[8] = c0 - from <= snap ? from : to - c0 <= snap ? to : c0;
+        s_plan[14] = c0 - from <= snap ? from : to - c0 <= snap ? to : c0;
       }
       if (from < c1 && c1 <= to) {
         s_info[2] = tid * kPerThread + k;
-        s_plan[9] = c1 - from <= snap ? from : to - c1 <= snap ? to : c1;
+        s_plan[15] = c1 - from <= snap ? from : to - c1 <= snap ? to : c1;
       }
     }
     __syncthreads();
-    r0 = s_plan[8];
-    r1 = s_plan[9];
+    r0 = s_plan[14];
+    r1 = s_plan[15];
     if (r0 >= r1) return;
     const int u0 = s_info[1], u1 = s_info[2];
 #pragma unroll
@@ -193,11 +278,6 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       ++seg;
     }
   };
-  auto page_table = [&](const TreeUnit &x, int kvh) -> const int32_t * {   // null for a head that keeps nothing
-    if (kvh < 64 && ((a.local_mask >> kvh) & 1)) return nullptr;
-    const int below = kvh < 64 ? __popcll(a.local_mask & ((1ULL << kvh) - 1ULL)) : 0;
-    return unit_table(c, a.row_base + x.seq * a.row_heads + kvh - below);
-  };
   auto wait_slot = [&](int at) {   // the at-th block may be written to its slot
     return at < kSlots || mbar_wait_bounded(&bar[B_EMPTY + at % kSlots], ((at / kSlots) - 1) & 1);
   };
@@ -209,7 +289,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     int base = 0, go = 0;     // blocks of the segments before; drafts' blocks let in
     segments([&](int, int item, const TreeUnit &x, int p0, int n) {
       const int kvh = item % c.Hkv, u = unit_index(c, a.layer, x.seq, kvh);
-      const int32_t *table = page_table(x, kvh);
+      const int32_t *table = tree_table(a, x, item);
       auto entry_of = [&](int i) {   // global page index of page i of the segment, -1: the drafts' page or none
         const int p = p0 + i;
         if (i >= n || p >= x.nk + x.nr) return -1;
@@ -353,7 +433,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       const int depth[2] = {__popcll(anc[0]) - 1, __popcll(anc[1]) - 1};
       // ancestors that have left a node's window, but for those that are kept
       if (__any_sync(0xffffffffu, max(depth[0], depth[1]) >= c.w)) {
-        const bool keeps = page_table(x, kvh) != nullptr;
+        const bool keeps = tree_table(a, x, item) != nullptr;
         const float thr = head_threshold(c, a.layer, kvh, a.tau_logit);
         unsigned kept[2];
 #pragma unroll
@@ -441,116 +521,125 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     });
   } else {
     // ---------------------------------------------------------------- softmax
-    const int row = tid & 127;
-    const uint32_t t_lane = tbase + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_lane + 128;
-    int j0 = 0, masked = 0, od[2] = {0, 0};   // pages of the segments before; segments with ring or drafts; commits so far of O_DONE
+    // A row belongs to two threads, one in warps 4-7 (half 0) and one in warps 8-11: each has 32 of a page's 64 scores and 64
+    // of the row's 128 output dims.  They meet once a page, when both have their scores in registers: whether the row's
+    // reference maximum has to move, which it rarely does, and that P may be written over the scores.
+    const int half = (warp >> 2) - 1, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t t_lane = tbase + ((uint32_t)(quarter * 32) << 16), t_o = t_lane + 128 + half * 64,
+                   t_o_other = t_lane + 128 + (half ^ 1) * 64;
+    auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory"); };
+    // has a wait of either thread of the row run out?  (They leave together: `meet` has no limit.)
+    auto either_failed = [&](int slot) {
+      if (lane == 0) s_bad[slot * 8 + half * 4 + quarter] = failed;
+      meet();
+      return failed || s_bad[slot * 8 + (half ^ 1) * 4 + quarter];
+    };
+    // a number from the row's other thread, by way of tensor memory (`mine`, `its`: a free column of either)
+    auto swap = [&](uint32_t mine, uint32_t its, float x) {
+      tmem_st1(mine, x);
+      tmem_st_wait();
+      fence_before();
+      meet();
+      fence_after();
+      x = tmem_ld1(its);
+      tmem_ld_wait();
+      fence_before();
+      meet();      // (both have read before the columns are used again)
+      fence_after();
+      return x;
+    };
+    // pages of the segments before; segments with ring or drafts; parity of the commits so far of the two O_DONE barriers
+    int j0 = 0, masked = 0, od = 0;
     segments([&](int seg, int item, const TreeUnit &x, int p0, int n) {
-      const int b = item / c.Hkv, kvh = item - b * c.Hkv, u = unit_index(c, a.layer, x.seq, kvh);
-      const int R = tile * kTreeRows + row, n_rows = x.n * c.G, node = (int)(((unsigned long long)R * a.g_inv) >> 32);
-      const bool live = tile * kTreeRows + (row & ~31) < n_rows;   // a warp without a live row only keeps the barriers going
-      const bool keeps = page_table(x, kvh) != nullptr;
-      const int n_ring = min(x.t, c.w);
-      const float thr = head_threshold(c, a.layer, kvh, a.tau_logit);
-      float lg0 = 0.f, lg1 = 0.f;   // stored logits of this lane's two slots of the next ring page
-      auto fetch_logits = [&](int p) {
-        const int at = (p - x.nk) * kP + lane;
-        if (p < x.nk || p >= x.nk + x.nr) return;
-        const float *z = c.ring_logit + (size_t)u * c.w;
-        if (at < n_ring) lg0 = __ldcg(&z[at]);
-        if (at + 32 < n_ring) lg1 = __ldcg(&z[at + 32]);
-      };
-      fetch_logits(p0);
-      uint64_t path = 0;
-      int d = 0;
-      auto fetch_path = [&]() {   // (once a segment with ring or drafts, before its first such page)
-        if (!mbar_wait_bounded(&bar[B_TREE_FULL], masked & 1)) failed = true;
-        ++masked;
-        path = s_path[min(node, kMaxDraft - 1)];
-        d = s_depth[min(node, kMaxDraft - 1)];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar[B_TREE_EMPTY]);
-      };
-      // bits of page p that this row sees (p's logits fetched; whole warps)
-      auto sees = [&](int p) -> uint64_t {
-        if (p < x.nk) return bits_below(x.len - p * kP);
-        if (p >= x.nk + x.nr) return path;
-        const int rp = p - x.nk, at = rp * kP + lane;
-        const unsigned k0 = __ballot_sync(0xffffffffu, keeps && (lg0 >= thr || ring_position(x.t, c.w, at) < c.n_sink)),
-                       k1 = __ballot_sync(0xffffffffu, keeps && (lg1 >= thr || ring_position(x.t, c.w, at + 32) < c.n_sink));
-        return bits_below(n_ring - rp * kP) & (~ring_out_of_window(x.t, d, c.w, rp) | (uint64_t)k1 << 32 | k0);
-      };
+      // (What is needed for masks only is read again where it is needed: the loop over pages has no register to spare, and a
+      // spilled one comes back from L2.)
+      const int nk = x.nk;
+      const bool row_live = tile * kTreeRows + row < x.n * c.G;
+      const bool live = tile * kTreeRows + quarter * 32 < x.n * c.G;   // warps without a live row only keep the barriers going
+      float lg = tree_logit(a, x, item, p0, half);   // stored logit of this lane's slot of the page that comes next, if of the ring
       float m_ref = -INFINITY, l = 0.f;
+      bool left_together = false;
       for (int i = 0; i < n; ++i) {
         const int j = j0 + i, bf = j & 1, p = p0 + i;
-        if (p >= x.nk && (i == 0 || p == x.nk)) fetch_path();
-        if (failed || !mbar_wait_bounded(&bar[B_S_FULL + bf], (j >> 1) & 1)) { failed = true; break; }
+        uint32_t mask = 0xffffffffu;   // the keys that this row sees
+        if (p >= nk - 1) {
+          if (p >= nk && (i == 0 || p == nk) && !mbar_wait_bounded(&bar[B_TREE_FULL], masked & 1)) failed = true;
+          mask = tree_sees(a, x, item, p, half, lg, s_path, s_depth, tile * kTreeRows + row);
+          lg = tree_logit(a, x, item, p + 1, half);
+        }
+        if (!failed && !mbar_wait_bounded(&bar[B_S_FULL + bf], (j >> 1) & 1)) failed = true;
         fence_after();
-        if (!live) { fence_before(); mbar_arrive(&bar[B_P_FULL + bf]); continue; }
+        if (!live) {
+          if (failed) break;
+          fence_before();
+          mbar_arrive(&bar[B_P_FULL + bf]);
+          continue;
+        }
         const uint32_t t_s = t_lane + bf * 64;
-        float v[64];
+        float v[32];
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
+        for (int q2 = 0; q2 < 2; ++q2) {
           float t16[16];
-          tmem_ld16(t_s + q4 * 16, t16);
+          tmem_ld16(t_s + half * 32 + q2 * 16, t16);
 #pragma unroll
-          for (int y = 0; y < 16; ++y) v[q4 * 16 + y] = t16[y];
+          for (int y = 0; y < 16; ++y) v[q2 * 16 + y] = t16[y];
         }
         tmem_ld_wait();
-        if (p >= x.nk - 1 && (p >= x.nk || (x.len & (kP - 1)))) {   // (a full compact page is seen whole)
-          const uint64_t mask = sees(p);
-          const uint32_t lo = (uint32_t)mask, hi = (uint32_t)(mask >> 32);
+        if (p >= nk - 1) {
 #pragma unroll
-          for (int y = 0; y < 32; ++y) {
-            v[y] = (lo >> y) & 1 ? v[y] : -INFINITY;
-            v[32 + y] = (hi >> y) & 1 ? v[32 + y] : -INFINITY;
-          }
+          for (int y = 0; y < 32; ++y) v[y] = (mask >> y) & 1 ? v[y] : -INFINITY;
         }
-        fetch_logits(p + 1);
-        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+        float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
-        for (int y = 0; y < 64; y += 8) {
+        for (int y = 0; y < 32; y += 4) {
           mx0 = max3(mx0, v[y], v[y + 1]);
           mx1 = max3(mx1, v[y + 2], v[y + 3]);
-          mx2 = max3(mx2, v[y + 4], v[y + 5]);
-          mx3 = max3(mx3, v[y + 6], v[y + 7]);
         }
-        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * a.scale_log2;
+        const float mx = fmaxf(mx0, mx1) * a.scale_log2;
         // the reference maximum moves only when the row maximum outgrows it by 2^8
-        const bool grow = mx > m_ref + 8.f && R < n_rows;
-        const float m_new = grow ? mx : m_ref;
-        if (i > 0 && __any_sync(0xffffffffu, grow)) {
-          // O is stable between the completion of P V of the page before and the hand-over of P.  The scores of the next
-          // page were issued behind that P V; before the last page it has a barrier of its own.
-          if (!(i + 1 < n ? mbar_wait_bounded(&bar[B_S_FULL + (bf ^ 1)], ((j + 1) >> 1) & 1)
-                          : mbar_wait_bounded(&bar[B_O_DONE + (bf ^ 1)], od[bf ^ 1] & 1))) {
-            failed = true;
-            break;
-          }
-          fence_after();
-          const float f = grow ? fast_exp2(m_ref - m_new) : 1.f;   // m_ref = -inf -> 0
+        unsigned grown = __ballot_sync(0xffffffffu, mx > m_ref + 8.f && row_live);
+        if (lane == 0) s_grow[bf * 8 + half * 4 + quarter] = grown;
+        fence_before();
+        failed = left_together = either_failed(bf);
+        if (failed) break;
+        fence_after();
+        grown |= s_grow[bf * 8 + (half ^ 1) * 4 + quarter];
+        if (grown) {
+          const float both = fmaxf(mx, swap(t_s + half * 32, t_s + (half ^ 1) * 32, mx));
+          const bool grow = both > m_ref + 8.f && row_live;
+          const float m_new = grow ? both : m_ref;
+          if (i > 0) {
+            // O is stable between the completion of P V of the page before and the hand-over of P.  The scores of the next
+            // page were issued behind that P V; before the last page it has a barrier of its own.
+            if (!(i + 1 < n ? mbar_wait_bounded(&bar[B_S_FULL + (bf ^ 1)], ((j + 1) >> 1) & 1)
+                            : mbar_wait_bounded(&bar[B_O_DONE + (bf ^ 1)], (od >> (bf ^ 1)) & 1)))
+              failed = true;   // (noticed by both at their next meeting)
+            fence_after();
+            const float f = grow ? fast_exp2(m_ref - m_new) : 1.f;   // m_ref = -inf -> 0
 #pragma unroll
-          for (int q8 = 0; q8 < 8; ++q8) {
-            float t16[16];
-            tmem_ld16(t_o + q8 * 16, t16);
-            tmem_ld_wait();
+            for (int q4 = 0; q4 < 4; ++q4) {
+              float t16[16];
+              tmem_ld16(t_o + q4 * 16, t16);
+              tmem_ld_wait();
 #pragma unroll
-            for (int y = 0; y < 16; ++y) t16[y] *= f;
-            tmem_st16(t_o + q8 * 16, t16);
+              for (int y = 0; y < 16; ++y) t16[y] *= f;
+              tmem_st16(t_o + q4 * 16, t16);
+            }
+            l *= f;
           }
-          l *= f;
+          m_ref = m_new;
         }
-        m_ref = m_new;
         const float ms = m_ref == -INFINITY ? 0.f : m_ref;
         const uint64_t sc2 = pack2(a.scale_log2, a.scale_log2), nms2 = pack2(-ms, -ms);
         uint64_t l2a = pack2(0.f, 0.f), l2b = l2a;
-        // two terms: the first in the first 32 columns of the score buffer, the second in the other 32
+        // two terms, two keys a column: the first in columns [0, 32) of the score buffer, the second in the other 32
 #pragma unroll
         for (int q2 = 0; q2 < 2; ++q2) {
-          uint32_t hi[16], lo[16];
+          uint32_t hi[8], lo[8];
 #pragma unroll
-          for (int y = 0; y < 16; ++y) {
+          for (int y = 0; y < 8; ++y) {
             float e0, e1, f0, f1;
-            unpack2(fma2(pack2(v[q2 * 32 + 2 * y], v[q2 * 32 + 2 * y + 1]), sc2, nms2), e0, e1);
+            unpack2(fma2(pack2(v[q2 * 16 + 2 * y], v[q2 * 16 + 2 * y + 1]), sc2, nms2), e0, e1);
             const float w0 = fast_exp2(e0), w1 = fast_exp2(e1);
             const uint64_t w2 = pack2(w0, w1);
             if (y & 1) l2b = add2(l2b, w2); else l2a = add2(l2a, w2);
@@ -558,8 +647,8 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
             unpack2(sub2(w2, pack2(__uint_as_float(hi[y] << 16), __uint_as_float(hi[y] & 0xffff0000u))), f0, f1);
             lo[y] = pack_bf16(f0, f1);
           }
-          tmem_st16u(t_s + q2 * 16, hi);
-          tmem_st16u(t_s + 32 + q2 * 16, lo);
+          tmem_st8u(t_s + half * 16 + q2 * 8, hi);
+          tmem_st8u(t_s + 32 + half * 16 + q2 * 8, lo);
         }
         float la, lb;
         unpack2(add2(l2a, l2b), la, lb);
@@ -568,96 +657,66 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         fence_before();
         mbar_arrive(&bar[B_P_FULL + bf]);
       }
-      if (failed) return false;
       // ---- the rows' results, or their parts
       const int last = (j0 + n - 1) & 1;
-      if (!mbar_wait_bounded(&bar[B_O_DONE + last], od[last] & 1)) { failed = true; return false; }
+      if (!failed && !mbar_wait_bounded(&bar[B_O_DONE + last], (od >> last) & 1)) failed = true;
+      if (live && !(failed && left_together)) failed = either_failed(2);
+      if (failed) return false;
       fence_after();
-      ++od[last];
-      if (n > 1) ++od[last ^ 1];
+      od ^= n > 1 ? 3 : 1 << last;
       j0 += n;
       const bool whole = n == x.np, starts = p0 == 0, ends = p0 + n == x.np;
-      if (row == 0 && (starts || ends)) {
+      if (half == 0 && row == 0 && (starts || ends)) {
         int *e = reinterpret_cast<int *>(&a.ends[(size_t)tile * a.n_items + item]);
         if (starts) e[0] = range;
         if (ends) e[1] = range;
       }
-      if (!live) return true;
-      if (s_odd[seg & 7]) {
-        // ---- infinite and NaN values of the segment, to the rows that see them
-        for (int i = 0; i < n; ++i) {
-          const int p = p0 + i;
-          fetch_logits(p);
-          const uint64_t mask = sees(p);
-          const bool draft = p >= x.nk + x.nr;
-          const __nv_bfloat16 *vb = nullptr;
-          if (!draft)
-            vb = c.pages + (int64_t)(p < x.nk ? checked_page(c, ldcg_keep(&page_table(x, kvh)[p]), (int)ring_page(c, u, 0))
-                                              : (int)ring_page(c, u, p - x.nk)) * kPageElems + kBlockElems;
-          for (int r = 0; r < kP; r += 2) {   // lane: chunk lane & 15 of row r + (lane >> 4)
-            const int y = r + (lane >> 4);
-            uint4 q = make_uint4(0, 0, 0, 0);
-            if (!draft) q = __ldcg(reinterpret_cast<const uint4 *>(vb + swz_off(y, lane & 15)));
-            else if (y < x.n) q = *reinterpret_cast<const uint4 *>(a.v + ((int64_t)b * a.T + y) * a.v_tok + (int64_t)kvh * a.v_head + (lane & 15) * 8);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-            bool odd = false;
+      if (live) {
+        if (s_odd[seg & 7]) 
+          tree_add_odd_values(a, x.seq | x.n << 25, x.t, x.len, tile, item, p0, n, half, t_o, s_path, s_depth, tile * kTreeRows + row);
+        if (whole) {
+          // (the sums are exchanged through the first column of O, once that is in registers)
+          float t16[16];
+          tmem_ld16(t_o, t16);
+          tmem_ld_wait();
+          const float sum = l + swap(t_o, t_o_other, l), inv = 1.f / sum;
+          const size_t at = tree_out_row(a, item, row_live ? tile * kTreeRows + row : 0);
 #pragma unroll
-            for (int z = 0; z < 4; ++z) odd = odd || (w[z] & 0x7f80u) == 0x7f80u || (w[z] & 0x7f800000u) == 0x7f800000u;
-            for (unsigned at = __ballot_sync(0xffffffffu, odd); at; at &= at - 1) {
-              const int src = __ffs(at) - 1, ch = src & 15;
-              float add[8];
-#pragma unroll
-              for (int z = 0; z < 4; ++z) {
-                const uint32_t g = __shfl_sync(0xffffffffu, w[z], src);
-                add[2 * z] = (g & 0x7f80u) == 0x7f80u ? __uint_as_float(g << 16) : 0.f;
-                add[2 * z + 1] = (g & 0x7f800000u) == 0x7f800000u ? __uint_as_float(g & 0xffff0000u) : 0.f;
-              }
-              const bool mine = (mask >> (r + (src >> 4))) & 1;
-              float t16[16];
-              tmem_ld16(t_o + (ch >> 1) * 16, t16);
+          for (int q4 = 0; q4 < 4; ++q4) {
+            if (q4) {
+              tmem_ld16(t_o + q4 * 16, t16);
               tmem_ld_wait();
+            }
+            uint32_t w[8];
 #pragma unroll
-              for (int z = 0; z < 16; ++z)
-                if (mine && (z >> 3) == (ch & 1)) t16[z] += add[z & 7];
-              tmem_st16(t_o + (ch >> 1) * 16, t16);
-              tmem_st_wait();
+            for (int y = 0; y < 8; ++y) w[y] = pack_bf16(t16[2 * y] * inv, t16[2 * y + 1] * inv);
+            if (row_live) {
+              uint4 *o = reinterpret_cast<uint4 *>(a.out + at * kD + half * 64 + q4 * 16);
+              o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+              o[1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
           }
+          if (row_live && half == 0 && a.lse) a.lse[at] = (m_ref + log2f(sum)) * kLn2;
+        } else {
+          const size_t part = (size_t)blockIdx.x * 2 + (starts ? 1 : 0);
+          float *o = a.part_o + (part * kD + half * 64) * a.rows_pad + row;
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            float t16[16];
+            tmem_ld16(t_o + q4 * 16, t16);
+            tmem_ld_wait();
+#pragma unroll
+            for (int y = 0; y < 16; ++y) o[(q4 * 16 + y) * a.rows_pad] = t16[y];
+          }
+          float *ml = a.part_ml + part * 3 * a.rows_pad + row;   // m, and the two halves' l
+          if (half == 0) ml[0] = m_ref;
+          ml[(1 + half) * a.rows_pad] = l;
         }
       }
-      if (whole) {
-        const float inv = 1.f / l;
-        const bool mine = R < n_rows;
-        const size_t at = ((size_t)b * a.T + (mine ? node : 0)) * c.Hq + kvh * c.G + (mine ? R - node * c.G : 0);
-#pragma unroll
-        for (int q8 = 0; q8 < 8; ++q8) {
-          float t16[16];
-          tmem_ld16(t_o + q8 * 16, t16);
-          tmem_ld_wait();
-          uint32_t w[8];
-#pragma unroll
-          for (int y = 0; y < 8; ++y) w[y] = pack_bf16(t16[2 * y] * inv, t16[2 * y + 1] * inv);
-          if (mine) {
-            uint4 *o = reinterpret_cast<uint4 *>(a.out + at * kD + q8 * 16);
-            o[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            o[1] = make_uint4(w[4], w[5], w[6], w[7]);
-          }
-        }
-        if (mine && a.lse) a.lse[at] = (m_ref + log2f(l)) * kLn2;
-      } else {
-        const size_t part = (size_t)blockIdx.x * 2 + (starts ? 1 : 0);
-        float *o = a.part_o + part * kD * a.rows_pad + row;
-#pragma unroll
-        for (int q8 = 0; q8 < 8; ++q8) {
-          float t16[16];
-          tmem_ld16(t_o + q8 * 16, t16);
-          tmem_ld_wait();
-#pragma unroll
-          for (int y = 0; y < 16; ++y) o[(q8 * 16 + y) * a.rows_pad] = t16[y];
-        }
-        float *ml = a.part_ml + part * 2 * a.rows_pad + row;
-        ml[0] = m_ref;
-        ml[a.rows_pad] = l;
+      if (p0 + n > nk) {   // the segment's paths are done with
+        ++masked;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar[B_TREE_EMPTY]);
       }
       return true;
     });
@@ -702,9 +761,9 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
     for (int y = 0; y < kAhead; ++y) {
       const int r = min(r0 + y * kWarps, ends.y);
       const size_t part = ((size_t)r * a.n_tiles + tile) * 2 + (r == ends.x ? 1 : 0);
-      const float *ml = a.part_ml + part * 2 * a.rows_pad + row, *o = a.part_o + (part * kD + dim0) * a.rows_pad + row;
+      const float *ml = a.part_ml + part * 3 * a.rows_pad + row, *o = a.part_o + (part * kD + dim0) * a.rows_pad + row;
       m[y] = __ldcg(ml);
-      l[y] = __ldcg(ml + a.rows_pad);
+      l[y] = __ldcg(ml + a.rows_pad) + __ldcg(ml + 2 * a.rows_pad);
 #pragma unroll
       for (int x = 0; x < kDims; ++x) v[y][x] = __ldcg(o + x * a.rows_pad);
       if (r0 + y * kWarps > ends.y) { m[y] = -INFINITY; l[y] = 0.f; }
@@ -773,7 +832,7 @@ static TreeWs tree_ws_layout(const spkv_config_t *cfg, int B, int T, int blocks)
   w.rows_pad = std::min(kTreeRows, (T * G + 31) / 32 * 32);
   w.off_units = a256(items * w.n_tiles * sizeof(int2));
   w.off_ml = w.off_units + a256((size_t)blocks * items * sizeof(int4));
-  w.off_o = w.off_ml + a256((size_t)blocks * 4 * w.rows_pad * 4);
+  w.off_o = w.off_ml + a256((size_t)blocks * 6 * w.rows_pad * 4);
   w.total = w.off_o + a256((size_t)blocks * 2 * kD * w.rows_pad * 4);
   return w;
 }
