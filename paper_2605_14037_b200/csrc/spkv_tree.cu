@@ -15,13 +15,13 @@
 //   * Masks: every query sees a compact page's pairs.  Of a ring page a row sees the slots in its node's window and those
 //     whose pair is kept (a bit each, by ballot over the stored logits), of the drafts' page its path.  64 bits a row
 //     and page, applied to the scores.
-//   * A pair that is masked has P = 0, which an infinite or NaN value would turn into NaN (and a weight's second
-//     term is often 0 too): one warp looks through every page's values before P V may read them, replaces what is not finite by
-//     0 and marks the segment; its epilogue then adds those elements to the rows that see them.  (Clean pages cost nothing: the
-//     warp runs ahead of P V.)
+//   * A pair that is masked has P = 0, which an infinite or NaN value would turn into NaN (as would a weight's second
+//     term, which is often 0): whatever the rest of the row holds, the result is not finite then.  So the epilogue looks at the results, and
+//     rows of a segment with such a one are computed again key by key (tree_rows_again).  Finite caches pay one maximum
+//     per result.
 //
-// Warps: 0 MMA issue and tensor memory, 1 page loader, 2 query rows, drafts and paths, 3 look through the values, 4-11
-// softmax.  Shared memory (113 KB, two blocks an SM): Q 32 KB, ring of five 16 KB key or value blocks in the order in which the
+// Warps: 0-7 softmax, 8 MMA issue and tensor memory, 9 page loader, 10 query rows, drafts and paths.
+// Shared memory (113 KB, two blocks an SM): Q 32 KB, ring of five 16 KB key or value blocks in the order in which the
 // MMAs want them.  Tensor memory (256 columns): score buffers at [0, 64) and [64, 128), O at [128, 256).  All waits are bounded.
 #include <math.h>
 
@@ -34,15 +34,15 @@
 namespace spkv {
 
 namespace tree {
-constexpr int kThreads = 384, kBlocksPerSm = 2;
-constexpr int kMmaWarp = 0, kLoaderWarp = 1, kRowWarp = 2, kScanWarp = 3;
+constexpr int kThreads = 352, kBlocksPerSm = 2;
+constexpr int kMmaWarp = 8, kLoaderWarp = 9, kRowWarp = 10;   // 0-7: softmax
 constexpr int kTmemCols = 256;
 constexpr int kBlockBytes = kPageBytes / 2, kSlots = 5;
-enum { B_FULL = 0, B_EMPTY = 5, B_V_READY = 10 /* [page & 3] */, B_S_FULL = 14 /* [page & 1] */, B_P_FULL = 16, B_O_DONE = 18,
-       B_Q_FULL = 20, B_Q_EMPTY, B_TREE_FULL, B_TREE_EMPTY, B_COUNT };
-constexpr int kUnitsHere = 6;       // units of a block that shared memory holds; the others stand in the workspace
+enum { B_FULL = 0, B_EMPTY = 5, B_S_FULL = 10 /* [page & 1] */, B_P_FULL = 12, B_O_DONE = 14, B_Q_FULL = 16, B_Q_EMPTY,
+       B_TREE_FULL, B_TREE_EMPTY, B_COUNT };
+constexpr int kUnitsHere = 8;       // units of a block that shared memory holds; the others stand in the workspace
 constexpr int off_ring = 32768, off_bar = off_ring + kSlots * kBlockBytes, off_info = off_bar + B_COUNT * 8,
-              off_odd = off_info + 16, off_path = off_odd + 32, off_depth = off_path + 64 * 8, off_grow = off_depth + 64,
+              off_path = off_info + 16, off_depth = off_path + 64 * 8, off_grow = off_depth + 64,
               off_bad = off_grow + 2 * 8 * 4, off_units = off_bad + 32, kSmemBytes = off_units + kUnitsHere * 16;
 static_assert(kSmemBytes <= off_bar + 1024 && off_units % 16 == 0 && off_path % 8 == 0, "two blocks an SM");
 constexpr int kPerThread = (1024 + kThreads - 1) / kThreads;   // items a thread looks at while the line is cut
@@ -54,6 +54,23 @@ constexpr int kSegmentCost = 3;
 __device__ inline int key_at(int i) { return i == 0 ? 0 : 2 * i - 1; }
 __device__ inline int value_at(int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
 }  // namespace tree
+
+// mbar_wait_bounded for warps that wait long and often beside others that compute: the hardware may hold a try back for
+// up to 20 us before it is made again (three waiting warps a block issue a tenth of all instructions otherwise).
+__device__ inline bool tree_wait(uint64_t *bar, uint32_t parity) {
+  auto attempt = [&]() {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(20000u) : "memory");
+    return ok != 0;
+  };
+  if (attempt()) return true;
+  const long long t0 = clock64();
+  while (!attempt())
+    if (clock64() - t0 > kWaitClocks) return false;
+  return true;
+}
 
 // A unit as the plan sees it: {its place in the line, sequence | nodes << 25, pairs received, kept pairs}.  In the line a
 // unit takes kSegmentCost places and then one per page.
@@ -100,54 +117,61 @@ __device__ inline uint32_t tree_sees(const TreeArgs &a, const TreeUnit &x, int i
   return (uint32_t)(bits_below(min(x.t, c.w) - rp * kP) >> (32 * h)) &
          (~(uint32_t)(ring_out_of_window(x.t, s_depth[node], c.w, rp) >> (32 * h)) | kept);
 }
-// Infinite and NaN values of a segment's pages (which P V took for 0), to the rows that see them: this half's 64 dims of O,
-// at t_o.  Whole warps; rare.
-__device__ __noinline__ void tree_add_odd_values(const TreeArgs &a, int seq_nodes, int t, int len, int tile, int item, int p0, int n,
-                                                 int half, uint32_t t_o, const volatile uint64_t *s_path,
-                                                 const volatile uint8_t *s_depth, int R) {
-  using namespace tc5;
+// One warp's share (every second row of a quarter of the tile) of a segment whose results are not all finite, once more, key by
+// key: a pair that a row does not see is not touched, and an infinite value that it sees counts with its weight, however
+// small.  (P V multiplies what is masked by 0, and a weight's second term is often 0 too.)  Rare.
+__device__ __noinline__ void tree_rows_again(const TreeArgs &a, int seq_nodes, int t, int len, int tile, int item, int p0, int n, int quarter,
+                                             int half, int part, const volatile uint64_t *s_path, const volatile uint8_t *s_depth) {
   const TreeUnit x(a, make_int4(0, seq_nodes, t, len), tile);
   const CacheView &c = a.c;
   const int lane = threadIdx.x & 31, b = item / c.Hkv, kvh = item - b * c.Hkv, u = unit_index(c, a.layer, x.seq, kvh);
-  for (int p = p0; p < p0 + n; ++p) {
-    const uint64_t mask = (uint64_t)tree_sees(a, x, item, p, 1, tree_logit(a, x, item, p, 1), s_path, s_depth, R) << 32 |
-                          tree_sees(a, x, item, p, 0, tree_logit(a, x, item, p, 0), s_path, s_depth, R);
-    const bool draft = p >= x.nk + x.nr;
-    const __nv_bfloat16 *vb = nullptr;
-    if (!draft)
-      vb = c.pages + (int64_t)(p < x.nk ? checked_page(c, ldcg_keep(&tree_table(a, x, item)[p]), (int)ring_page(c, u, 0))
-                                        : (int)ring_page(c, u, p - x.nk)) * kPageElems + kBlockElems;
-    for (int r = 0; r < kP; r += 4) {   // lane: chunk lane & 7 of this half of row r + (lane >> 3)
-      const int y = r + (lane >> 3), mine = half * 8 + (lane & 7);
-      uint4 q = make_uint4(0, 0, 0, 0);
-      if (!draft) q = __ldcg(reinterpret_cast<const uint4 *>(vb + swz_off(y, mine)));
-      else if (y < x.n) q = *reinterpret_cast<const uint4 *>(a.v + ((int64_t)b * a.T + y) * a.v_tok + (int64_t)kvh * a.v_head + mine * 8);
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-      bool odd = false;
-#pragma unroll
-      for (int z = 0; z < 4; ++z) odd = odd || (w[z] & 0x7f80u) == 0x7f80u || (w[z] & 0x7f800000u) == 0x7f800000u;
-      for (unsigned at = __ballot_sync(0xffffffffu, odd); at; at &= at - 1) {
-        const int src = __ffs(at) - 1, ch = src & 7;
-        float add[8];
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          const uint32_t g = __shfl_sync(0xffffffffu, w[z], src);
-          add[2 * z] = (g & 0x7f80u) == 0x7f80u ? __uint_as_float(g << 16) : 0.f;
-          add[2 * z + 1] = (g & 0x7f800000u) == 0x7f800000u ? __uint_as_float(g & 0xffff0000u) : 0.f;
+  for (int row = quarter * 32 + half; row < quarter * 32 + 32; row += 2) {   // lane: dims 4 lane .. 4 lane + 3
+    const int R = tile * kTreeRows + row;
+    if (R >= x.n * c.G) return;
+    const int node = tree_node_of(a, R);
+    const __nv_bfloat16 *qr = a.q + ((int64_t)b * a.T + node) * a.q_tok + (int64_t)(kvh * c.G + R - node * c.G) * a.q_head + lane * 4;
+    float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
+    for (int z = 0; z < 4; ++z) q[z] = __bfloat162float(qr[z]);
+    for (int p = p0; p < p0 + n; ++p) {
+      uint64_t mask = (uint64_t)tree_sees(a, x, item, p, 1, tree_logit(a, x, item, p, 1), s_path, s_depth, R) << 32 |
+                      tree_sees(a, x, item, p, 0, tree_logit(a, x, item, p, 0), s_path, s_depth, R);
+      const bool draft = p >= x.nk + x.nr;
+      const int64_t page = draft ? 0 : p < x.nk ? checked_page(c, ldcg_keep(&tree_table(a, x, item)[p]), (int)ring_page(c, u, 0))
+                                                : (int)ring_page(c, u, p - x.nk);
+      for (; mask; mask &= mask - 1) {
+        const int y = __ffsll((long long)mask) - 1;
+        const __nv_bfloat16 *kr, *vr;
+        if (draft) {
+          const int64_t tok = (int64_t)b * a.T + y;
+          kr = a.k + tok * a.k_tok + (int64_t)kvh * a.k_head + lane * 4;
+          vr = a.v + tok * a.v_tok + (int64_t)kvh * a.v_head + lane * 4;
+        } else {
+          kr = c.pages + page * kPageElems + swz_off(y, lane >> 1) + (lane & 1) * 4;
+          vr = kr + kBlockElems;
         }
-        const bool seen = (mask >> (r + (src >> 3))) & 1;
-        float t16[16];
-        tmem_ld16(t_o + (ch >> 1) * 16, t16);
-        tmem_ld_wait();
-#pragma unroll
-        for (int z = 0; z < 16; ++z)
-          if (seen && (z >> 3) == (ch & 1)) t16[z] += add[z & 7];
-        tmem_st16(t_o + (ch >> 1) * 16, t16);
-        tmem_st_wait();
+        float s = 0.f;
+        for (int z = 0; z < 4; ++z) s = fmaf(q[z], __bfloat162float(kr[z]), s);
+        s = warp_sum(s) * a.scale_log2;
+        const float top = s > m ? s : m;
+        float f = m == -INFINITY ? 0.f : fast_exp2(m - top), w = fast_exp2(s - (top == -INFINITY ? 0.f : top));
+        if (m != -INFINITY && f < 1e-37f) f = 1e-37f;
+        if (s != -INFINITY && w < 1e-37f) w = 1e-37f;
+        l = l * f + w;
+        for (int z = 0; z < 4; ++z) o[z] = (f == 0.f ? 0.f : o[z] * f) + w * __bfloat162float(vr[z]);
+        m = top;
       }
     }
+    if (part < 0) {
+      const size_t at = tree_out_row(a, item, R);
+      const float inv = 1.f / l;
+      *reinterpret_cast<uint2 *>(a.out + at * kD + lane * 4) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+      if (a.lse && lane == 0) a.lse[at] = (m + log2f(l)) * kLn2;
+    } else {
+      reinterpret_cast<float4 *>(a.part_o)[((size_t)part * (kD / 4) + lane) * a.rows_pad + row] = make_float4(o[0], o[1], o[2], o[3]);
+      float *ml = a.part_ml + (size_t)part * 3 * a.rows_pad + row;
+      if (lane == 0) { ml[0] = m; ml[a.rows_pad] = l; ml[2 * a.rows_pad] = 0.f; }
+    }
   }
-  __syncwarp();
 }
 
 __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_attention_kernel(const __grid_constant__ TreeArgs a) {
@@ -157,11 +181,10 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   const CacheView &c = a.c;
   uint64_t *bar = reinterpret_cast<uint64_t *>(smem + off_bar);
   volatile int *s_info = reinterpret_cast<volatile int *>(smem + off_info);     // tensor memory, first and last unit, drafts' blocks let in
-  volatile int *s_odd = reinterpret_cast<volatile int *>(smem + off_odd);       // [segment & 7] values that are not finite
   volatile uint64_t *s_path = reinterpret_cast<volatile uint64_t *>(smem + off_path);   // [node] nodes it sees
   volatile uint8_t *s_depth = smem + off_depth;
-  volatile unsigned *s_grow = reinterpret_cast<volatile unsigned *>(smem + off_grow);   // [page & 1][warp - 4] rows whose maximum moves
-  volatile uint8_t *s_bad = smem + off_bad;   // [page & 1 or 2][warp - 4] a wait ran out
+  volatile unsigned *s_grow = reinterpret_cast<volatile unsigned *>(smem + off_grow);   // [page & 1][warp] rows whose maximum moves
+  volatile uint8_t *s_bad = smem + off_bad;   // [page & 1, 2, 3][warp] a wait ran out; 3: a result is not finite
   int4 *s_units = reinterpret_cast<int4 *>(smem + off_units);
   volatile int *s_plan = reinterpret_cast<volatile int *>(smem + off_path);     // (before the paths are)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -245,6 +268,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     r0 = s_plan[14];
     r1 = s_plan[15];
     if (r0 >= r1) return;
+    // (a range may hold no page, only a part of what a segment costs)
     const int u0 = s_info[1], u1 = s_info[2];
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) {
@@ -253,8 +277,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       if (i < kUnitsHere) s_units[i] = meta[k];
       else a.units[(size_t)blockIdx.x * a.n_items + i] = meta[k];
     }
-    if (tid < 8) s_odd[tid] = 0;
-    if (tid == 8) s_info[3] = 0;
+    if (tid == 0) s_info[3] = 0;
   }
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem + off_info)),
@@ -267,19 +290,47 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   const uint32_t tbase = (uint32_t)s_info[0];
   const int u0 = s_info[1], n_units = s_info[2] - u0 + 1;
   bool failed = false;
+  auto unit_at = [&](int i) { return TreeUnit(a, i < kUnitsHere ? s_units[i] : a.units[(size_t)blockIdx.x * a.n_items + i], tile); };
+  auto part_of = [&](const TreeUnit &x, int &s, int &e) {   // of the unit's pages, those of this block's range: [s, e) in the line
+    s = max(x.pre + kSegmentCost, r0);
+    e = min(x.pre + kSegmentCost + x.np, r1);
+    return s < e;
+  };
+  auto first_unit = [&](int &i) {   // the unit of the block's first segment
+    int s, e;
+    for (;; ++i) {
+      const TreeUnit x = unit_at(i);
+      if (i == n_units - 1 || part_of(x, s, e)) return x;
+    }
+  };
   // f(segment, unit's place among all, unit, first page in the unit, pages) for every segment of this block; f returns false to stop
   auto segments = [&](auto f) {
     int seg = 0;
     for (int i = 0; i < n_units; ++i) {
-      const TreeUnit x(a, i < kUnitsHere ? s_units[i] : a.units[(size_t)blockIdx.x * a.n_items + i], tile);
-      const int first = x.pre + kSegmentCost, s = max(first, r0), e = min(first + x.np, r1);
-      if (e <= s) continue;
-      if (!f(seg, u0 + i, x, s - first, e - s)) return;
+      const TreeUnit x = unit_at(i);
+      int s, e;
+      if (!part_of(x, s, e)) continue;
+      if (!f(seg, u0 + i, x, s - x.pre - kSegmentCost, e - s)) return;
       ++seg;
     }
   };
+  auto copy = [&](uint32_t dst, const __nv_bfloat16 *src, bool live) {   // 16 bytes (not live: zeros)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+  };
+  // Query rows r, r + step, ... of an item with n nodes -> two slabs of 128 rows x 128 B, 128-byte swizzle; lanes 0-15 and
+  // 16-31 of a warp take a row each.  (Rows behind the last keep what they hold: a row of a tile does not touch another.)
+  auto copy_queries = [&](int item, int n, int r, int step) {
+    const int b = item / c.Hkv, kvh = item - b * c.Hkv, ch = lane & 15, n_rows = min(kTreeRows, n * c.G - tile * kTreeRows);
+    const uint32_t sQ = smem_u32(smem) + (ch >> 3) * 16384;
+    const __nv_bfloat16 *src = a.q + (int64_t)b * a.T * a.q_tok + (int64_t)kvh * c.G * a.q_head + ch * 8;
+#pragma unroll 4
+    for (; r < n_rows; r += step) {
+      const int R = tile * kTreeRows + r, i = tree_node_of(a, R);
+      copy(sQ + r * 128 + (((ch & 7) ^ (r & 7)) << 4), src + i * a.q_tok + (R - i * c.G) * a.q_head, true);
+    }
+  };
   auto wait_slot = [&](int at) {   // the at-th block may be written to its slot
-    return at < kSlots || mbar_wait_bounded(&bar[B_EMPTY + at % kSlots], ((at / kSlots) - 1) & 1);
+    return at < kSlots || tree_wait(&bar[B_EMPTY + at % kSlots], ((at / kSlots) - 1) & 1);
   };
 
   if (warp == kLoaderWarp) {
@@ -328,7 +379,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       base += 2 * n;
       if (failed && lane == 0)   // do not leave while copies may still be landing
         for (int at = max(0, base - 2 * n + 2 * i - 2 - kSlots); at < base - 2 * n + 2 * i; ++at)
-          mbar_wait_bounded(&bar[B_FULL + at % kSlots], (at / kSlots) & 1);
+          tree_wait(&bar[B_FULL + at % kSlots], (at / kSlots) & 1);
       return !failed;
     });
   } else if (warp == kMmaWarp) {
@@ -341,18 +392,19 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     segments([&](int seg, int, const TreeUnit &, int, int n) {
       auto issue_qk = [&](int i) {   // S = Q . K^T of page i into its score buffer
         const int at = base + key_at(i), s = at % kSlots, b = (j0 + i) & 1;
-        if (!mbar_wait_bounded(&bar[B_FULL + s], (at / kSlots) & 1)) { failed = true; return; }
+        if (!tree_wait(&bar[B_FULL + s], (at / kSlots) & 1)) { failed = true; return; }
         fence_after();
         umma_qk_page<16384 / 16, 8192 / 16>(tbase + b * 64, dQ, dK + (uint64_t)s * kUnits, idesc_qk);
         umma_commit(&bar[B_S_FULL + b]);
         umma_commit(&bar[B_EMPTY + s]);
         if (i == n - 1) umma_commit(&bar[B_Q_EMPTY]);
       };
-      if (!mbar_wait_bounded(&bar[B_Q_FULL], seg & 1)) failed = true;
+      if (seg == 0) asm volatile("bar.sync 9, 288;" ::: "memory");   // the softmax warps have fetched the queries
+      else if (!tree_wait(&bar[B_Q_FULL], (seg - 1) & 1)) failed = true;
       for (int i = 0; i < min(2, n) && !failed; ++i) issue_qk(i);
       for (int i = 0; i < n && !failed; ++i) {
         const int j = j0 + i, at = base + value_at(i, n), s = at % kSlots, b = j & 1;
-        if (!mbar_wait_bounded(&bar[B_V_READY + (j & 3)], (j >> 2) & 1) || !mbar_wait_bounded(&bar[B_P_FULL + b], (j >> 1) & 1)) {
+        if (!tree_wait(&bar[B_FULL + s], (at / kSlots) & 1) || !tree_wait(&bar[B_P_FULL + b], (j >> 1) & 1)) {
           failed = true;
           break;
         }
@@ -370,37 +422,20 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     // ---------------------------------------------------------------- query rows, drafts and paths
     int base = 0, go = 0, masked = 0;   // blocks of the segments so far; drafts' blocks waited for; segments with ring or drafts
     segments([&](int seg, int item, const TreeUnit &x, int p0, int n) {
-      const int b = item / c.Hkv, kvh = item - b * c.Hkv, n_rows = min(kTreeRows, x.n * c.G - tile * kTreeRows);
-      auto copy = [&](uint32_t dst, const __nv_bfloat16 *src, bool live) {   // (not live: zeros)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-      };
+      const int b = item / c.Hkv, kvh = item - b * c.Hkv, ch = lane & 15;
       auto landed = [&]() {
         asm volatile("cp.async.wait_all;" ::: "memory");
         fence_async_smem();
         __syncwarp();
       };
-      if (seg > 0 && !mbar_wait_bounded(&bar[B_Q_EMPTY], (seg - 1) & 1)) failed = true;
+      if (seg > 0 && !tree_wait(&bar[B_Q_EMPTY], (seg - 1) & 1)) failed = true;
       if (failed) return false;
-      // Q -> two slabs of 128 rows x 128 B, 128-byte swizzle (rows behind the last keep what they hold: a row of a tile
-      // does not touch another)
       const int64_t tok0 = (int64_t)b * a.T;
-      const int ch = lane & 15;
-      {
-        int r = lane >> 4, R = tile * kTreeRows + r, i = (int)(((unsigned long long)R * a.g_inv) >> 32), g = R - i * c.G;
-        const __nv_bfloat16 *src = a.q + (tok0 + i) * a.q_tok + (int64_t)(kvh * c.G + g) * a.q_head + ch * 8;
-        const int64_t next_node = a.q_tok - (int64_t)c.G * a.q_head;
-        const uint32_t sQ = smem_u32(smem) + (ch >> 3) * 16384;
-#pragma unroll 4
-        for (; r < n_rows; r += 2) {
-          copy(sQ + r * 128 + (((ch & 7) ^ (r & 7)) << 4), src, true);
-          src += 2 * a.q_head;
-          g += 2;
-          if (g >= c.G) { g -= c.G; src += next_node; }
-          if (g >= c.G) { g -= c.G; src += next_node; }   // (groups of one)
-        }
+      if (seg > 0) {   // (the softmax warps have fetched the first segment's)
+        copy_queries(item, x.n, lane >> 4, 2);
+        landed();
+        if (lane == 0) mbar_arrive(&bar[B_Q_FULL]);
       }
-      landed();
-      if (lane == 0) mbar_arrive(&bar[B_Q_FULL]);
       base += 2 * n;
       if (p0 + n <= x.nk) return true;   // compact pages only
       ++masked;
@@ -453,7 +488,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
           }
         }
       }
-      if (masked > 1 && !mbar_wait_bounded(&bar[B_TREE_EMPTY], masked & 1)) failed = true;
+      if (masked > 1 && !tree_wait(&bar[B_TREE_EMPTY], masked & 1)) failed = true;
       if (failed) return false;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -480,59 +515,27 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       }
       return true;
     });
-  } else if (warp == kScanWarp) {
-    // ---------------------------------------------------------------- values that are not finite
-    int base = 0, j0 = 0;
-    segments([&](int seg, int, const TreeUnit &, int, int n) {
-      if (lane == 0) s_odd[(seg + 2) & 7] = 0;   // (last looked at by the epilogue of segment seg - 6)
-      for (int i = 0; i < n; ++i) {
-        const int at = base + value_at(i, n), s = at % kSlots, j = j0 + i;
-        if (!mbar_wait_bounded(&bar[B_FULL + s], (at / kSlots) & 1)) { failed = true; break; }
-        uint4 *v = reinterpret_cast<uint4 *>(smem + off_ring + s * kBlockBytes) + lane;
-        __nv_bfloat162 top = __floats2bfloat162_rn(0.f, 0.f);
-#pragma unroll 8
-        for (int y = 0; y < kBlockBytes / 16 / 32; ++y) {
-          const uint4 r = v[y * 32];
-          const __nv_bfloat162 *e = reinterpret_cast<const __nv_bfloat162 *>(&r);
-#pragma unroll
-          for (int z = 0; z < 4; ++z) top = __hmax2_nan(top, __habs2(e[z]));
-        }
-        const uint32_t bits = *reinterpret_cast<const uint32_t *>(&top);
-        if (__any_sync(0xffffffffu, (bits & 0x7f80u) == 0x7f80u || (bits & 0x7f800000u) == 0x7f800000u)) {
-          for (int y = 0; y < kBlockBytes / 16 / 32; ++y) {
-            uint4 r = v[y * 32];
-            uint32_t *e = reinterpret_cast<uint32_t *>(&r);
-#pragma unroll
-            for (int z = 0; z < 4; ++z) {
-              if ((e[z] & 0x7f80u) == 0x7f80u) e[z] &= 0xffff0000u;
-              if ((e[z] & 0x7f800000u) == 0x7f800000u) e[z] &= 0xffffu;
-            }
-            v[y * 32] = r;
-          }
-          if (lane == 0) s_odd[seg & 7] = 1;
-          fence_async_smem();
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar[B_V_READY + (j & 3)]);
-      }
-      base += 2 * n;
-      j0 += n;
-      return !failed;
-    });
   } else {
     // ---------------------------------------------------------------- softmax
-    // A row belongs to two threads, one in warps 4-7 (half 0) and one in warps 8-11: each has 32 of a page's 64 scores and 64
+    // A row belongs to two threads, one in warps 0-3 (half 0) and one in warps 4-7: each has 32 of a page's 64 scores and 64
     // of the row's 128 output dims.  They meet once a page, when both have their scores in registers: whether the row's
     // reference maximum has to move, which it rarely does, and that P may be written over the scores.
-    const int half = (warp >> 2) - 1, quarter = warp & 3, row = quarter * 32 + lane;
-    const uint32_t t_lane = tbase + ((uint32_t)(quarter * 32) << 16), t_o = t_lane + 128 + half * 64,
-                   t_o_other = t_lane + 128 + (half ^ 1) * 64;
+    const int half = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t t_lane = tbase + ((uint32_t)(quarter * 32) << 16), t_o = t_lane + 128 + half * 64;
+    {   // the first segment's queries
+      int i = 0;
+      const TreeUnit x = first_unit(i);
+      copy_queries(u0 + i, x.n, warp * 2 + (lane >> 4), 16);
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_async_smem();
+      asm volatile("bar.arrive 9, 288;" ::: "memory");
+    }
     auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory"); };
     // has a wait of either thread of the row run out?  (They leave together: `meet` has no limit.)
     auto either_failed = [&](int slot) {
-      if (lane == 0) s_bad[slot * 8 + half * 4 + quarter] = failed;
+      if (lane == 0) s_bad[slot * 8 + warp] = failed;
       meet();
-      return failed || s_bad[slot * 8 + (half ^ 1) * 4 + quarter];
+      return failed || s_bad[slot * 8 + (warp ^ 4)];
     };
     // a number from the row's other thread, by way of tensor memory (`mine`, `its`: a free column of either)
     auto swap = [&](uint32_t mine, uint32_t its, float x) {
@@ -563,11 +566,11 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         const int j = j0 + i, bf = j & 1, p = p0 + i;
         uint32_t mask = 0xffffffffu;   // the keys that this row sees
         if (p >= nk - 1) {
-          if (p >= nk && (i == 0 || p == nk) && !mbar_wait_bounded(&bar[B_TREE_FULL], masked & 1)) failed = true;
+          if (p >= nk && (i == 0 || p == nk) && !tree_wait(&bar[B_TREE_FULL], masked & 1)) failed = true;
           mask = tree_sees(a, x, item, p, half, lg, s_path, s_depth, tile * kTreeRows + row);
           lg = tree_logit(a, x, item, p + 1, half);
         }
-        if (!failed && !mbar_wait_bounded(&bar[B_S_FULL + bf], (j >> 1) & 1)) failed = true;
+        if (!failed && !tree_wait(&bar[B_S_FULL + bf], (j >> 1) & 1)) failed = true;
         fence_after();
         if (!live) {
           if (failed) break;
@@ -598,12 +601,12 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         const float mx = fmaxf(mx0, mx1) * a.scale_log2;
         // the reference maximum moves only when the row maximum outgrows it by 2^8
         unsigned grown = __ballot_sync(0xffffffffu, mx > m_ref + 8.f && row_live);
-        if (lane == 0) s_grow[bf * 8 + half * 4 + quarter] = grown;
+        if (lane == 0) s_grow[bf * 8 + warp] = grown;
         fence_before();
         failed = left_together = either_failed(bf);
         if (failed) break;
         fence_after();
-        grown |= s_grow[bf * 8 + (half ^ 1) * 4 + quarter];
+        grown |= s_grow[bf * 8 + (warp ^ 4)];
         if (grown) {
           const float both = fmaxf(mx, swap(t_s + half * 32, t_s + (half ^ 1) * 32, mx));
           const bool grow = both > m_ref + 8.f && row_live;
@@ -611,8 +614,8 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
           if (i > 0) {
             // O is stable between the completion of P V of the page before and the hand-over of P.  The scores of the next
             // page were issued behind that P V; before the last page it has a barrier of its own.
-            if (!(i + 1 < n ? mbar_wait_bounded(&bar[B_S_FULL + (bf ^ 1)], ((j + 1) >> 1) & 1)
-                            : mbar_wait_bounded(&bar[B_O_DONE + (bf ^ 1)], (od >> (bf ^ 1)) & 1)))
+            if (!(i + 1 < n ? tree_wait(&bar[B_S_FULL + (bf ^ 1)], ((j + 1) >> 1) & 1)
+                            : tree_wait(&bar[B_O_DONE + (bf ^ 1)], (od >> (bf ^ 1)) & 1)))
               failed = true;   // (noticed by both at their next meeting)
             fence_after();
             const float f = grow ? fast_exp2(m_ref - m_new) : 1.f;   // m_ref = -inf -> 0
@@ -658,29 +661,29 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         mbar_arrive(&bar[B_P_FULL + bf]);
       }
       // ---- the rows' results, or their parts
+      if (failed && left_together) return false;
       const int last = (j0 + n - 1) & 1;
-      if (!failed && !mbar_wait_bounded(&bar[B_O_DONE + last], (od >> last) & 1)) failed = true;
-      if (live && !(failed && left_together)) failed = either_failed(2);
-      if (failed) return false;
+      if (!failed && !tree_wait(&bar[B_O_DONE + last], (od >> last) & 1)) failed = true;
       fence_after();
       od ^= n > 1 ? 3 : 1 << last;
       j0 += n;
       const bool whole = n == x.np, starts = p0 == 0, ends = p0 + n == x.np;
-      if (half == 0 && row == 0 && (starts || ends)) {
+      if (warp == 0 && lane == 0 && (starts || ends)) {
         int *e = reinterpret_cast<int *>(&a.ends[(size_t)tile * a.n_items + item]);
         if (starts) e[0] = range;
         if (ends) e[1] = range;
       }
       if (live) {
-        if (s_odd[seg & 7]) 
-          tree_add_odd_values(a, x.seq | x.n << 25, x.t, x.len, tile, item, p0, n, half, t_o, s_path, s_depth, tile * kTreeRows + row);
+        const int part = whole ? -1 : (int)blockIdx.x * 2 + (starts ? 1 : 0);
+        uint64_t finite = 0;   // 0 times everything: 0, or NaN
+        float t16[16];
+        tmem_ld16(t_o, t16);
+        tmem_ld_wait();
         if (whole) {
           // (the sums are exchanged through the first column of O, once that is in registers)
-          float t16[16];
-          tmem_ld16(t_o, t16);
-          tmem_ld_wait();
-          const float sum = l + swap(t_o, t_o_other, l), inv = 1.f / sum;
+          const float sum = l + swap(t_o, t_lane + 128 + (half ^ 1) * 64, l), inv = 1.f / sum;
           const size_t at = tree_out_row(a, item, row_live ? tile * kTreeRows + row : 0);
+          uint4 *o = reinterpret_cast<uint4 *>(a.out + at * kD + half * 64);
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             if (q4) {
@@ -689,30 +692,44 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
             }
             uint32_t w[8];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) w[y] = pack_bf16(t16[2 * y] * inv, t16[2 * y + 1] * inv);
+            for (int y = 0; y < 8; ++y) {
+              finite = fma2(pack2(t16[2 * y], t16[2 * y + 1]), 0, finite);
+              w[y] = pack_bf16(t16[2 * y] * inv, t16[2 * y + 1] * inv);
+            }
             if (row_live) {
-              uint4 *o = reinterpret_cast<uint4 *>(a.out + at * kD + half * 64 + q4 * 16);
-              o[0] = make_uint4(w[0], w[1], w[2], w[3]);
-              o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+              o[2 * q4] = make_uint4(w[0], w[1], w[2], w[3]);
+              o[2 * q4 + 1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
           }
           if (row_live && half == 0 && a.lse) a.lse[at] = (m_ref + log2f(sum)) * kLn2;
         } else {
-          const size_t part = (size_t)blockIdx.x * 2 + (starts ? 1 : 0);
-          float *o = a.part_o + (part * kD + half * 64) * a.rows_pad + row;
+          float4 *o = reinterpret_cast<float4 *>(a.part_o) + ((size_t)part * (kD / 4) + half * 16) * a.rows_pad + row;
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
-            float t16[16];
-            tmem_ld16(t_o + q4 * 16, t16);
-            tmem_ld_wait();
+            if (q4) {
+              tmem_ld16(t_o + q4 * 16, t16);
+              tmem_ld_wait();
+            }
 #pragma unroll
-            for (int y = 0; y < 16; ++y) o[(q4 * 16 + y) * a.rows_pad] = t16[y];
+            for (int y = 0; y < 8; ++y) finite = fma2(pack2(t16[2 * y], t16[2 * y + 1]), 0, finite);
+#pragma unroll
+            for (int y = 0; y < 4; ++y, o += a.rows_pad) *o = make_float4(t16[4 * y], t16[4 * y + 1], t16[4 * y + 2], t16[4 * y + 3]);
           }
-          float *ml = a.part_ml + part * 3 * a.rows_pad + row;   // m, and the two halves' l
+          float *ml = a.part_ml + (size_t)part * 3 * a.rows_pad + row;   // m, and the two halves' l
           if (half == 0) ml[0] = m_ref;
           ml[(1 + half) * a.rows_pad] = l;
         }
+        float f0, f1;
+        unpack2(finite, f0, f1);
+        const bool odd = __any_sync(0xffffffffu, row_live && f0 + f1 != 0.f);
+        if (lane == 0) s_bad[3 * 8 + warp] = odd | failed << 1;
+        meet();
+        const int both = odd | failed << 1 | s_bad[3 * 8 + (warp ^ 4)];
+        failed = both >> 1;
+        if (both == 1)
+          tree_rows_again(a, x.seq | x.n << 25, x.t, x.len, tile, item, p0, n, quarter, half, part, s_path, s_depth);
       }
+      if (failed) return false;
       if (p0 + n > nk) {   // the segment's paths are done with
         ++masked;
         __syncwarp();
@@ -761,11 +778,15 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
     for (int y = 0; y < kAhead; ++y) {
       const int r = min(r0 + y * kWarps, ends.y);
       const size_t part = ((size_t)r * a.n_tiles + tile) * 2 + (r == ends.x ? 1 : 0);
-      const float *ml = a.part_ml + part * 3 * a.rows_pad + row, *o = a.part_o + (part * kD + dim0) * a.rows_pad + row;
+      const float *ml = a.part_ml + part * 3 * a.rows_pad + row;
+      const float4 *o = reinterpret_cast<const float4 *>(a.part_o) + (part * (kD / 4) + dim0 / 4) * a.rows_pad + row;
       m[y] = __ldcg(ml);
       l[y] = __ldcg(ml + a.rows_pad) + __ldcg(ml + 2 * a.rows_pad);
 #pragma unroll
-      for (int x = 0; x < kDims; ++x) v[y][x] = __ldcg(o + x * a.rows_pad);
+      for (int x = 0; x < kDims; x += 4) {
+        const float4 q = __ldcg(o + x / 4 * a.rows_pad);
+        v[y][x] = q.x; v[y][x + 1] = q.y; v[y][x + 2] = q.z; v[y][x + 3] = q.w;
+      }
       if (r0 + y * kWarps > ends.y) { m[y] = -INFINITY; l[y] = 0.f; }
     }
 #pragma unroll

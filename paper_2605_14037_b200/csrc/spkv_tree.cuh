@@ -25,7 +25,7 @@ struct TreeArgs {
   unsigned long long local_mask;
   int4 *units;                                 // [blocks][n_items]: a block's units behind the first few
   int2 *ends;                                  // [n_tiles][n_items]: ranges of a unit's first and last page
-  float *part_o, *part_ml;                     // [blocks][2][128][rows_pad], [blocks][2][3][rows_pad]
+  float *part_o, *part_ml;                     // [blocks][2][32][rows_pad][4 dims], [blocks][2][3][rows_pad]: m, two shares of l
   int rows_pad;
 };
 
