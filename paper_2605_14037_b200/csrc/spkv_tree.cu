@@ -42,7 +42,7 @@ enum { B_FULL = 0, B_EMPTY = 5, B_S_FULL = 10 /* [page & 1] */, B_P_FULL = 12, B
        B_TREE_FULL, B_TREE_EMPTY, B_COUNT };
 constexpr int kUnitsHere = 8;       // units of a block that shared memory holds; the others stand in the workspace
 constexpr int off_ring = 32768, off_bar = off_ring + kSlots * kBlockBytes, off_info = off_bar + B_COUNT * 8,
-              off_path = off_info + 16, off_depth = off_path + 64 * 8, off_grow = off_depth + 64,
+              off_path = off_info + 32, off_depth = off_path + 64 * 8, off_grow = off_depth + 64,
               off_bad = off_grow + 2 * 8 * 4, off_units = off_bad + 32, kSmemBytes = off_units + kUnitsHere * 16;
 static_assert(kSmemBytes <= off_bar + 1024 && off_units % 16 == 0 && off_path % 8 == 0, "two blocks an SM");
 constexpr int kPerThread = (1024 + kThreads - 1) / kThreads;   // items a thread looks at while the line is cut
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
   uint64_t *bar = reinterpret_cast<uint64_t *>(smem + off_bar);
-  volatile int *s_info = reinterpret_cast<volatile int *>(smem + off_info);     // tensor memory, first and last unit, drafts' blocks let in
+  volatile int *s_info = reinterpret_cast<volatile int *>(smem + off_info);     // tensor memory, first and last unit, drafts' blocks let in, range
   volatile uint64_t *s_path = reinterpret_cast<volatile uint64_t *>(smem + off_path);   // [node] nodes it sees
   volatile uint8_t *s_depth = smem + off_depth;
   volatile unsigned *s_grow = reinterpret_cast<volatile unsigned *>(smem + off_grow);   // [page & 1][warp] rows whose maximum moves
@@ -196,7 +196,6 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   pdl_wait();
   pdl_trigger();   // (only now: what follows may then rely on everything before this launch)
   // ---- the line of pages, its cut, and this block's units.  Thread x holds items kPerThread x and on.
-  int r0, r1;
   {
     int4 meta[kPerThread];
     int cost[kPerThread], sum = 0;
@@ -257,17 +256,15 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       const int from = meta[k].x, to = from + cost[k];
       if (from <= c0 && c0 < to) {
         s_info[1] = tid * kPerThread + k;
-        s_plan[14] = c0 - from <= snap ? from : to - c0 <= snap ? to : c0;
+        s_info[4] = c0 - from <= snap ? from : to - c0 <= snap ? to : c0;
       }
       if (from < c1 && c1 <= to) {
         s_info[2] = tid * kPerThread + k;
-        s_plan[15] = c1 - from <= snap ? from : to - c1 <= snap ? to : c1;
+        s_info[5] = c1 - from <= snap ? from : to - c1 <= snap ? to : c1;
       }
     }
     __syncthreads();
-    r0 = s_plan[14];
-    r1 = s_plan[15];
-    if (r0 >= r1) return;
+    if (s_info[4] >= s_info[5]) return;
     // (a range may hold no page, only a part of what a segment costs)
     const int u0 = s_info[1], u1 = s_info[2];
 #pragma unroll
@@ -288,29 +285,28 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   __syncthreads();
   fence_after();
   const uint32_t tbase = (uint32_t)s_info[0];
-  const int u0 = s_info[1], n_units = s_info[2] - u0 + 1;
-  bool failed = false;
+  bool failed = false;   // (the block's units and range are read where they are needed: no register to spare)
   auto unit_at = [&](int i) { return TreeUnit(a, i < kUnitsHere ? s_units[i] : a.units[(size_t)blockIdx.x * a.n_items + i], tile); };
   auto part_of = [&](const TreeUnit &x, int &s, int &e) {   // of the unit's pages, those of this block's range: [s, e) in the line
-    s = max(x.pre + kSegmentCost, r0);
-    e = min(x.pre + kSegmentCost + x.np, r1);
+    s = max(x.pre + kSegmentCost, s_info[4]);
+    e = min(x.pre + kSegmentCost + x.np, s_info[5]);
     return s < e;
   };
   auto first_unit = [&](int &i) {   // the unit of the block's first segment
     int s, e;
     for (;; ++i) {
       const TreeUnit x = unit_at(i);
-      if (i == n_units - 1 || part_of(x, s, e)) return x;
+      if (i == s_info[2] - s_info[1] || part_of(x, s, e)) return x;
     }
   };
   // f(segment, unit's place among all, unit, first page in the unit, pages) for every segment of this block; f returns false to stop
   auto segments = [&](auto f) {
     int seg = 0;
-    for (int i = 0; i < n_units; ++i) {
+    for (int i = 0; i <= s_info[2] - s_info[1]; ++i) {
       const TreeUnit x = unit_at(i);
       int s, e;
       if (!part_of(x, s, e)) continue;
-      if (!f(seg, u0 + i, x, s - x.pre - kSegmentCost, e - s)) return;
+      if (!f(seg, s_info[1] + i, x, s - x.pre - kSegmentCost, e - s)) return;
       ++seg;
     }
   };
@@ -525,7 +521,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
     {   // the first segment's queries
       int i = 0;
       const TreeUnit x = first_unit(i);
-      copy_queries(u0 + i, x.n, warp * 2 + (lane >> 4), 16);
+      copy_queries(s_info[1] + i, x.n, warp * 2 + (lane >> 4), 16);
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_async_smem();
       asm volatile("bar.arrive 9, 288;" ::: "memory");
@@ -580,18 +576,24 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         }
         const uint32_t t_s = t_lane + bf * 64;
         float v[32];
+        auto fetch_scores = [&]() {
 #pragma unroll
-        for (int q2 = 0; q2 < 2; ++q2) {
-          float t16[16];
-          tmem_ld16(t_s + half * 32 + q2 * 16, t16);
+          for (int q2 = 0; q2 < 2; ++q2) {
+            float t16[16];
+            tmem_ld16(t_s + half * 32 + q2 * 16, t16);
 #pragma unroll
-          for (int y = 0; y < 16; ++y) v[q2 * 16 + y] = t16[y];
-        }
-        tmem_ld_wait();
-        if (p >= nk - 1) {
+            for (int y = 0; y < 16; ++y) v[q2 * 16 + y] = t16[y];
+          }
+          tmem_ld_wait();
+        };
+        auto apply_mask = [&]() {
+          if (p >= nk - 1) {
 #pragma unroll
-          for (int y = 0; y < 32; ++y) v[y] = (mask >> y) & 1 ? v[y] : -INFINITY;
-        }
+            for (int y = 0; y < 32; ++y) v[y] = (mask >> y) & 1 ? v[y] : -INFINITY;
+          }
+        };
+        fetch_scores();
+        apply_mask();
         float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
         for (int y = 0; y < 32; y += 4) {
@@ -608,6 +610,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         fence_after();
         grown |= s_grow[bf * 8 + (warp ^ 4)];
         if (grown) {
+          const float first = v[0];   // (its column is used for the exchange)
           const float both = fmaxf(mx, swap(t_s + half * 32, t_s + (half ^ 1) * 32, mx));
           const bool grow = both > m_ref + 8.f && row_live;
           const float m_new = grow ? both : m_ref;
@@ -631,6 +634,9 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
             l *= f;
           }
           m_ref = m_new;
+          fetch_scores();             // again: kept across all this they would not fit the registers
+          v[0] = first;
+          apply_mask();
         }
         const float ms = m_ref == -INFINITY ? 0.f : m_ref;
         const uint64_t sc2 = pack2(a.scale_log2, a.scale_log2), nms2 = pack2(-ms, -ms);
