@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       else a.units[(size_t)blockIdx.x * a.n_items + i] = meta[k];
     }
     if (tid == 0) s_info[3] = 0;
+    if (tid < 32) s_bad[tid] = 0;
   }
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem + off_info)),
@@ -527,12 +528,6 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       asm volatile("bar.arrive 9, 288;" ::: "memory");
     }
     auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory"); };
-    // has a wait of either thread of the row run out?  (They leave together: `meet` has no limit.)
-    auto either_failed = [&](int slot) {
-      if (lane == 0) s_bad[slot * 8 + warp] = failed;
-      meet();
-      return failed || s_bad[slot * 8 + (warp ^ 4)];
-    };
     // a number from the row's other thread, by way of tensor memory (`mine`, `its`: a free column of either)
     auto swap = [&](uint32_t mine, uint32_t its, float x) {
       tmem_st1(mine, x);
@@ -602,14 +597,17 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         }
         const float mx = fmaxf(mx0, mx1) * a.scale_log2;
         // the reference maximum moves only when the row maximum outgrows it by 2^8
-        unsigned grown = __ballot_sync(0xffffffffu, mx > m_ref + 8.f && row_live);
+        unsigned grown = __ballot_sync(0xffffffffu, failed || (mx > m_ref + 8.f && row_live));
         if (lane == 0) s_grow[bf * 8 + warp] = grown;
+        if (failed && lane == 0) s_bad[bf * 8 + warp] = 1;
         fence_before();
-        failed = left_together = either_failed(bf);
-        if (failed) break;
+        meet();
         fence_after();
         grown |= s_grow[bf * 8 + (warp ^ 4)];
         if (grown) {
+          // (a wait that ran out stays noted: the row's threads leave together, `meet` has no limit)
+          failed = left_together = failed || s_bad[bf * 8 + (warp ^ 4)];
+          if (failed) break;
           const float first = v[0];   // (its column is used for the exchange)
           const float both = fmaxf(mx, swap(t_s + half * 32, t_s + (half ^ 1) * 32, mx));
           const bool grow = both > m_ref + 8.f && row_live;
@@ -639,29 +637,26 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
           apply_mask();
         }
         const float ms = m_ref == -INFINITY ? 0.f : m_ref;
-        const uint64_t sc2 = pack2(a.scale_log2, a.scale_log2), nms2 = pack2(-ms, -ms);
-        uint64_t l2a = pack2(0.f, 0.f), l2b = l2a;
+        const float2 sc2 = make_float2(a.scale_log2, a.scale_log2), nms2 = make_float2(-ms, -ms);
+        float2 l2a = make_float2(0.f, 0.f), l2b = l2a;
         // two terms, two keys a column: the first in columns [0, 32) of the score buffer, the second in the other 32
 #pragma unroll
         for (int q2 = 0; q2 < 2; ++q2) {
           uint32_t hi[8], lo[8];
 #pragma unroll
           for (int y = 0; y < 8; ++y) {
-            float e0, e1, f0, f1;
-            unpack2(fma2(pack2(v[q2 * 16 + 2 * y], v[q2 * 16 + 2 * y + 1]), sc2, nms2), e0, e1);
-            const float w0 = fast_exp2(e0), w1 = fast_exp2(e1);
-            const uint64_t w2 = pack2(w0, w1);
-            if (y & 1) l2b = add2(l2b, w2); else l2a = add2(l2a, w2);
-            hi[y] = pack_bf16(w0, w1);
-            unpack2(sub2(w2, pack2(__uint_as_float(hi[y] << 16), __uint_as_float(hi[y] & 0xffff0000u))), f0, f1);
-            lo[y] = pack_bf16(f0, f1);
+            const float2 e = __ffma2_rn(make_float2(v[q2 * 16 + 2 * y], v[q2 * 16 + 2 * y + 1]), sc2, nms2);
+            const float2 w = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+            if (y & 1) l2b = __fadd2_rn(l2b, w); else l2a = __fadd2_rn(l2a, w);
+            hi[y] = pack_bf16(w.x, w.y);
+            const float2 r = __fadd2_rn(w, make_float2(-__uint_as_float(hi[y] << 16), -__uint_as_float(hi[y] & 0xffff0000u)));
+            lo[y] = pack_bf16(r.x, r.y);
           }
           tmem_st8u(t_s + half * 16 + q2 * 8, hi);
           tmem_st8u(t_s + 32 + half * 16 + q2 * 8, lo);
         }
-        float la, lb;
-        unpack2(add2(l2a, l2b), la, lb);
-        l += la + lb;
+        l2a = __fadd2_rn(l2a, l2b);
+        l += l2a.x + l2a.y;
         tmem_st_wait();
         fence_before();
         mbar_arrive(&bar[B_P_FULL + bf]);
