@@ -47,7 +47,7 @@ constexpr int off_ring = 32768, off_bar = off_ring + kSlots * kBlockBytes, off_i
 static_assert(kSmemBytes <= off_bar + 1024 && off_units % 16 == 0 && off_path % 8 == 0, "two blocks an SM");
 constexpr int kPerThread = (1024 + kThreads - 1) / kThreads;   // items a thread looks at while the line is cut
 // What a segment costs beside its pages, in pages: its queries, its first scores, its results.
-constexpr int kSegmentCost = 3;
+constexpr int kSegmentCost = 7;
 
 // Where page i of a segment of n stands in the order in which a segment's blocks are loaded and used:
 // K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1)
@@ -912,7 +912,7 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   a.n_tiles = w.n_tiles;
   const int blocks = tree::kBlocksPerSm * std::min(kMaxGrid, cache->sm_count);
   a.n_ranges = std::max(1, blocks / a.n_tiles);
-  a.min_cost = 2 + tree::kSegmentCost;
+  a.min_cost = 5 + tree::kSegmentCost;   // (1 x 131072 tokens, 16 nodes: 27.7 us; 30.1 with 1, 31.4 with 11)
   if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(tree_attention_kernel), tree::kSmemBytes, &g_tree_ready)) return rc;
   // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
   // cover; a plain launch waits for all of them.
