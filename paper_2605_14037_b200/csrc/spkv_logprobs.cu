@@ -1,21 +1,23 @@
 // What rows of logits say (spkv_token_logprobs): log sum of exponentials, entropy, log probabilities of given tokens, and
 // the largest logits.
 //
-// One pass over the logits.  A row is cut into chunks of 1024 elements (the first takes the elements before the first
-// 16-byte boundary as well), a warp takes a chunk at a time: its maximum m in one round over the registers that hold
-// it, then with t = (x - m) scale log2 e
-//     S = sum 2^t,   A = sum 2^t t,      lse = scale m + ln S,   entropy = ln 2 (log2 S - A / S),
-// and the chunk's maximum to memory, where a top list is wanted.  The n_top largest elements of a row lie in the n_top
+// One pass over the logits.  A row is cut into chunks of 2 KB (the first takes the elements before the first
+// 16-byte boundary as well); a warp holds a chunk in registers and asks for its next one meanwhile.  With c = scale log2 e, M
+// a reference of the lane's own near its maximum (log2 domain) and t = c x - M
+//     S = sum 2^t,   A = sum 2^t t,      lse = ln 2 (M + log2 S),   entropy = ln 2 (log2 S - A / S),
+// and the chunk's maximum goes to memory, where a top list is wanted.  The n_top largest elements of a row lie in the n_top
 // chunks with the largest maxima (of equal ones those with the lower index), so a second, small kernel -- a
 // block per row, which also joins the row's sums -- looks into those chunks only, and the first pays nothing for the list.
-// What bounds it: memory (2 or 4 bytes an element).  The first kernel's arithmetic is 5.5 instructions an element of the
-// 11 that the SMs could issue while bf16 rows arrive at the copy rate.
+//
+// Elements below kFloor count as kFloor: 0 times -infinity has no place in A.  Their weight is 0, unless the
+// whole row lies that low (masked by a low value throughout) or the scale is so small that kFloor is near: such a row, and one
+// whose scaled maximum is 2^24 or more, is summed up again, about its own maximum, by the second kernel.
+// What bounds it: memory (2 or 4 bytes an element); 4.5 instructions an element of bf16 or fp16 (maxima and
+// floor two elements an instruction in the type itself), of the 11 that the SMs could issue while rows arrive at the copy rate.
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include <algorithm>
-
-#include <cuda_fp16.h>
-
 #include <type_traits>
 
 #include "spkv_internal.cuh"
@@ -24,9 +26,10 @@
 namespace spkv {
 
 namespace lp {
-constexpr int kChunk = 1024, kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kBlocksPerSm = 6;      // 40 registers a thread; a warp has 2 KB (bf16) or 4 KB of its chunk in flight
-constexpr int kMaxRounds = 4;        // chunks a warp takes at most
+constexpr int kChunkBytes = 2048, kWarps = 8, kThreads = 32 * kWarps;
+template <class T> constexpr int kChunk = kChunkBytes / (int)sizeof(T);   // elements
+constexpr int kBlocksPerSm = 4;      // 64 registers a thread: a chunk and the next one (4 KB chunks spill: 67 against 47 us for 768 rows of 128256)
+constexpr int kMaxRounds = 16;       // chunks a warp takes at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 }  // namespace lp
 
@@ -38,7 +41,7 @@ struct LogprobArgs {
   const int32_t *given;
   float *lse, *entropy, *logp, *top_logp;
   int32_t *top_ids;
-  float4 *part;        // [n_rows][parts] {m, S, A, a NaN was among them}
+  float4 *part;        // [n_rows][parts] {M, S, A, a NaN was among them}
   uint32_t *chunk_key; // [n_rows][max_chunks], n_top > 0 only
 };
 
@@ -61,7 +64,7 @@ template <> __device__ inline float as_float(__half x) { return __half2float(x);
 template <class T> __device__ inline int row_head(const T *row, int vocab) {
   return min(vocab, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T));
 }
-__device__ inline int row_chunks(int head, int vocab) { return max(1, (vocab - head + lp::kChunk - 1) / lp::kChunk); }
+template <class T> __device__ inline int row_chunks(int head, int vocab) { return max(1, (vocab - head + lp::kChunk<T> - 1) / lp::kChunk<T>); }
 
 // 16 bytes as floats
 template <class T, int kN = 16 / sizeof(T)> __device__ inline void unpack(const uint4 &v, float (&f)[kN]) {
@@ -81,30 +84,142 @@ template <class T, int kN = 16 / sizeof(T)> __device__ inline void unpack(const 
   }
 }
 
-// Running (m, S, A) of one lane.  m grows only when a maximum outgrows it by 2^16, so that a row's chunks hardly ever
+// Pairs of a type's elements: floor and maximum (NaN if there is one) without unpacking.  The floor lies where c x is still
+// exact to a small fraction of 1 (an M far below -2^24 is not: its rounding alone would be a large exponent).
+template <class T> struct Low;
+template <> struct Low<__nv_bfloat16> {
+  static constexpr float kFloor = -0x1p+20f;                       // 0xc980
+  static __device__ inline uint32_t floor2(uint32_t x) {
+    const __nv_bfloat162 f = __halves2bfloat162(__ushort_as_bfloat16(0xc980), __ushort_as_bfloat16(0xc980));
+    const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&x), f);
+    return *reinterpret_cast<const uint32_t *>(&r);
+  }
+  static __device__ inline uint32_t max2(uint32_t x, uint32_t y) {
+    const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
+    return *reinterpret_cast<const uint32_t *>(&r);
+  }
+};
+template <> struct Low<__half> {
+  static constexpr float kFloor = -65504.f;                        // 0xfbff: only -infinity lies below
+  static __device__ inline uint32_t floor2(uint32_t x) {
+    const __half2 f = __halves2half2(__ushort_as_half(0xfbff), __ushort_as_half(0xfbff));
+    const __half2 r = __hmax2_nan(*reinterpret_cast<const __half2 *>(&x), f);
+    return *reinterpret_cast<const uint32_t *>(&r);
+  }
+  static __device__ inline uint32_t max2(uint32_t x, uint32_t y) {
+    const __half2 r = __hmax2_nan(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&y));
+    return *reinterpret_cast<const uint32_t *>(&r);
+  }
+};
+template <> struct Low<float> {
+  static constexpr float kFloor = -0x1p+20f;
+  static __device__ inline uint32_t floor2(uint32_t x) { return __float_as_uint(__uint_as_float(x) < kFloor ? kFloor : __uint_as_float(x)); }
+  static __device__ inline uint32_t max2(uint32_t x, uint32_t y) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(x)), "f"(__uint_as_float(y)));
+    return __float_as_uint(r);
+  }
+};
+
+template <class T> __device__ inline void unpack2_of(uint32_t w, float (&f)[2]) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    f[0] = __uint_as_float(w << 16);
+    f[1] = __uint_as_float(w & 0xffff0000u);
+  } else {
+    const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    f[0] = p.x;
+    f[1] = p.y;
+  }
+}
+
+// Running (M, S, A) of one lane.  M grows only when a maximum outgrows it by 2^16, so that a row's chunks hardly ever
 // rescale; the exponentials then reach 2^16, far from the type's end.
 struct Sums {
-  float m = -INFINITY, S = 0.f, A = 0.f;
-  __device__ inline void raise(float to, float c) {      // (NaN: stays)
-    if (to > m && !((to - m) * c <= 16.f)) {
+  float M = -INFINITY, S = 0.f, A = 0.f;
+  __device__ inline void raise(float to) {      // (NaN: stays)
+    if (to > M + 16.f) {
       if (S > 0.f) {
-        const float d = (m - to) * c, f = exp2f(d);
+        const float d = M - to, f = exp2f(d);
         A = f > 0.f ? f * fmaf(S, d, A) : 0.f;
         S *= f;
       }
-      m = to;
+      M = to;
     }
   }
-  __device__ inline float base() const { return m == -INFINITY ? 0.f : m; }
 };
 
-// {m, S, A, a NaN was among them} of two sets of elements together
+// one element
+template <class T> __device__ inline void one(T x, float c, Sums &s, float &top, bool &nan) {
+  const float f = as_float(x);
+  top = fmaxf(top, f);
+  nan = nan || f != f;
+  if (!(f > Low<T>::kFloor)) return;
+  s.raise(f * c);
+  const float t = fmaf(f, c, -s.M), e = fast_exp2(t);
+  s.S += e;
+  s.A = fmaf(e, t, s.A);
+}
+
+// 16-byte words of a chunk that lies inside the row: lane l holds words l, l + 32, ...
+constexpr int kWords = lp::kChunkBytes / 512;
+template <class T> __device__ inline void load_chunk(const T *p, uint4 (&v)[kWords]) {
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) v[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + (threadIdx.x & 31) + 32 * i);
+}
+// ... into a lane's sums; top: the lane's maximum, nan: is a NaN among its elements
+template <class T>
+__device__ inline void add_chunk(const uint4 (&v)[kWords], float c, Sums &s, float &top, bool &nan) {
+  using namespace tc5;
+  constexpr int kPer = 16 / sizeof(T);
+  uint32_t mx = v[0].x;
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    mx = Low<T>::max2(mx, v[i].x); mx = Low<T>::max2(mx, v[i].y); mx = Low<T>::max2(mx, v[i].z); mx = Low<T>::max2(mx, v[i].w);
+  }
+  if constexpr (sizeof(T) == 4) {
+    top = __uint_as_float(mx);
+  } else {
+    float f[2];
+    unpack2_of<T>(mx, f);
+    top = f[0] != f[0] || f[0] > f[1] ? f[0] : f[1];
+  }
+  if (top <= Low<T>::kFloor) return;   // nothing that counts
+  s.raise(top * c);
+  const float2 nM2 = make_float2(-s.M, -s.M), c2 = make_float2(c, c);
+  float2 S2 = make_float2(0.f, 0.f), A2 = S2;
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    float f[kPer];
+    unpack<T>(make_uint4(Low<T>::floor2(v[i].x), Low<T>::floor2(v[i].y), Low<T>::floor2(v[i].z), Low<T>::floor2(v[i].w)), f);
+#pragma unroll
+    for (int x = 0; x < kPer; x += 2) {
+      const float2 t = __ffma2_rn(make_float2(f[x], f[x + 1]), c2, nM2);
+      const float2 e = make_float2(fast_exp2(t.x), fast_exp2(t.y));
+      S2 = __fadd2_rn(S2, e);
+      A2 = __ffma2_rn(e, t, A2);
+    }
+  }
+  const float add = S2.x + S2.y;
+  s.S += add;
+  s.A += A2.x + A2.y;
+  if (add != add) {   // a NaN among the elements, or an infinity less itself
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      float f[kPer];
+      unpack<T>(v[i], f);
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) nan = nan || f[x] != f[x];
+    }
+  }
+}
+
+// {M, S, A, a NaN was among them} of two sets of elements together
 __device__ inline float4 no_part() { return make_float4(-INFINITY, 0.f, 0.f, 0.f); }
-__device__ inline float4 join(float4 p, float4 q, float c) {
+__device__ inline float4 join(float4 p, float4 q) {
   const float M = fmaxf(p.x, q.x);
   auto weigh = [&](float4 &s) {
     if (s.y > 0.f && s.x < M) {
-      const float d = (s.x - M) * c, f = exp2f(d);
+      const float d = s.x - M, f = exp2f(d);
       s.z = f > 0.f ? f * fmaf(s.y, d, s.z) : 0.f;
       s.y *= f;
     }
@@ -113,64 +228,12 @@ __device__ inline float4 join(float4 p, float4 q, float c) {
   weigh(q);
   return make_float4(M, p.y + q.y, p.z + q.z, fmaxf(p.w, q.w));
 }
-__device__ inline float4 join_lanes(float4 p, float c) {
+__device__ inline float4 join_lanes(float4 p) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
     p = join(p, make_float4(__shfl_xor_sync(0xffffffffu, p.x, o), __shfl_xor_sync(0xffffffffu, p.y, o),
-                            __shfl_xor_sync(0xffffffffu, p.z, o), __shfl_xor_sync(0xffffffffu, p.w, o)), c);
+                            __shfl_xor_sync(0xffffffffu, p.z, o), __shfl_xor_sync(0xffffffffu, p.w, o)));
   return p;
-}
-
-// One warp's chunk, all of it inside the row: lane l holds vectors l, l + 32, ...
-template <class T>
-__device__ inline void full_chunk(const T *p, float c, Sums &s, float &top, bool &nan) {
-  using namespace tc5;
-  constexpr int kPer = 16 / sizeof(T), kVec = lp::kChunk / 32 / kPer;
-  const int lane = threadIdx.x & 31;
-  uint4 v[kVec];
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) v[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + lane + 32 * i);
-  float mx = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) {
-    float f[kPer];
-    unpack<T>(v[i], f);
-#pragma unroll
-    for (int x = 0; x < kPer; x += 2) mx = max3(mx, f[x], f[x + 1]);
-  }
-  s.raise(mx, c);
-  const float b = s.base();
-  const uint64_t nb2 = pack2(-b, -b), c2 = pack2(c, c);
-  uint64_t S2 = pack2(0.f, 0.f), A2 = S2;
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) {
-    float f[kPer];
-    unpack<T>(v[i], f);
-#pragma unroll
-    for (int x = 0; x < kPer; x += 2) {
-      float t0, t1;
-      unpack2(mul2(add2(pack2(f[x], f[x + 1]), nb2), c2), t0, t1);
-      const uint64_t e2 = pack2(fast_exp2(t0), fast_exp2(t1));
-      S2 = add2(S2, e2);
-      A2 = fma2(e2, pack2(fmaxf(t0, -300.f), fmaxf(t1, -300.f)), A2);   // (0 times -infinity is not wanted)
-    }
-  }
-  float a0, a1;
-  unpack2(S2, a0, a1);
-  const float add = a0 + a1;
-  s.S += add;
-  unpack2(A2, a0, a1);
-  s.A += a0 + a1;
-  top = mx;
-  if (add != add) {   // a NaN among the elements, or an infinity less itself
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      float f[kPer];
-      unpack<T>(v[i], f);
-#pragma unroll
-      for (int x = 0; x < kPer; ++x) nan = nan || f[x] != f[x];
-    }
-  }
 }
 
 template <class T>
@@ -180,51 +243,49 @@ __global__ void __launch_bounds__(lp::kThreads, lp::kBlocksPerSm) logprob_sums_k
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
   const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.stride;
-  const int head = row_head(x, a.vocab), n_chunks = row_chunks(head, a.vocab);
+  const int head = row_head(x, a.vocab), n_chunks = row_chunks<T>(head, a.vocab);
   const float c = a.scale * kLog2e;
   Sums s;
   bool nan = false;
-  auto one = [&](float f) {
-    s.raise(f, c);
-    const float t = (f - s.base()) * c, e = fast_exp2(t);
-    s.S += e;
-    s.A = fmaf(e, fmaxf(t, -300.f), s.A);
-    nan = nan || f != f;
+  // this warp's chunks: first, first + kWarps, ... < end; `full` of the row's chunks have all their elements
+  const int first = part * a.rounds * kWarps + warp, end = min(n_chunks, (part + 1) * a.rounds * kWarps), full = (a.vocab - head) / kChunk<T>;
+  auto key = [&](int ch, float top, bool odd) {
+    const uint32_t k = __reduce_max_sync(0xffffffffu, odd ? 0xffffffffu : value_key(top));
+    if (lane == 0) a.chunk_key[(size_t)row * a.max_chunks + ch] = k;
   };
-  for (int r = 0; r < a.rounds; ++r) {
-    const int ch = (part * a.rounds + r) * kWarps + warp;
-    if (ch >= n_chunks) break;
-    const int i0 = head + ch * kChunk;
+  uint4 v[2][kWords];
+  int ch = first;
+  const int stop = min(end, full);
+  if (ch < stop) load_chunk(x + head + (int64_t)ch * kChunk<T>, v[0]);
+  auto round = [&](const uint4 (&now)[kWords], uint4 (&next)[kWords]) {   // ... and ask for the warp's next chunk first
+    if (ch + kWarps < stop) load_chunk(x + head + (int64_t)(ch + kWarps) * kChunk<T>, next);
+    float top;
+    bool odd = false;
+    add_chunk<T>(now, c, s, top, odd);
+    if (ch == 0 && lane < head) one<T>(x[lane], c, s, top, odd);   // the elements before the boundary belong to it
+    if (a.n_top > 0) key(ch, top, odd);
+    nan = nan || odd;
+    ch += kWarps;
+  };
+  while (ch < stop) {
+    round(v[0], v[1]);
+    if (ch < stop) round(v[1], v[0]);
+  }
+  if (ch < end) {   // the row's last chunk, in part
     float top = -INFINITY;
-    const bool before = nan;
-    nan = false;
-    if (i0 + kChunk <= a.vocab) {
-      full_chunk(x + i0, c, s, top, nan);
-    } else {
-      for (int i = i0 + lane; i < a.vocab; i += 32) {
-        const float f = as_float(x[i]);
-        one(f);
-        top = fmaxf(top, f);
-      }
-    }
-    if (ch == 0 && lane < head) {
-      const float f = as_float(x[lane]);
-      one(f);
-      top = fmaxf(top, f);
-    }
-    if (a.n_top > 0) {
-      const uint32_t key = __reduce_max_sync(0xffffffffu, nan ? 0xffffffffu : value_key(top));
-      if (lane == 0) a.chunk_key[(size_t)row * a.max_chunks + ch] = key;
-    }
-    nan = nan || before;
+    bool odd = false;
+    for (int i = head + ch * kChunk<T> + lane; i < a.vocab; i += 32) one<T>(x[i], c, s, top, odd);
+    if (ch == 0 && lane < head) one<T>(x[lane], c, s, top, odd);
+    if (a.n_top > 0) key(ch, top, odd);
+    nan = nan || odd;
   }
   // ---- the block's sums: lanes, then warps, in a fixed order
   __shared__ float4 s_part[kWarps];
-  const float4 w = join_lanes(make_float4(s.m, s.S, s.A, nan ? 1.f : 0.f), c);
+  const float4 w = join_lanes(make_float4(s.M, s.S, s.A, nan ? 1.f : 0.f));
   if (lane == 0) s_part[warp] = w;
   __syncthreads();
   if (warp == 0) {
-    const float4 all = join_lanes(lane < kWarps ? s_part[lane] : no_part(), c);
+    const float4 all = join_lanes(lane < kWarps ? s_part[lane] : no_part());
     if (lane == 0) a.part[(size_t)row * a.parts + part] = all;
   }
 }
@@ -257,24 +318,27 @@ __global__ void __launch_bounds__(lp::kThreads) logprob_rows_kernel(LogprobArgs 
   using namespace lp;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x;
   const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.stride;
-  const int head = row_head(x, a.vocab), n_chunks = row_chunks(head, a.vocab);
+  const int head = row_head(x, a.vocab), n_chunks = row_chunks<T>(head, a.vocab);
   const float c = a.scale * kLog2e;
-  __shared__ float s_m, s_ln;            // a logit's log probability is (x - s_m) scale - s_ln
+  __shared__ float s_base, s_log2;       // a logit's log probability is ln 2 ((c x - s_base) - s_log2), or, if the row was summed again,
+  __shared__ int s_again;                // scale (x - s_base) - ln 2 s_log2
   __shared__ int s_chunk[SPKV_MAX_TOP];
   __shared__ uint32_t s_bound;           // value_key that every wanted element reaches
   __shared__ uint64_t s_list[kWarps][32];
+  __shared__ float4 s_part[kWarps];
   pdl_wait();
   if (warp == 0) {
     float4 p = no_part();
-    for (int i = lane; i < a.parts; i += 32) p = join(p, a.part[(size_t)row * a.parts + i], c);
-    p = join_lanes(p, c);
+    for (int i = lane; i < a.parts; i += 32) p = join(p, a.part[(size_t)row * a.parts + i]);
+    p = join_lanes(p);
     if (lane == 0) {
-      const float M = p.x, S = p.y;
-      const bool nan = p.w != 0.f, inf = M == INFINITY;
-      s_m = nan ? NAN : inf ? 0.f : M;
-      s_ln = inf ? INFINITY : logf(S);
-      if (a.lse) a.lse[row] = nan ? NAN : inf ? INFINITY : fmaf(M, a.scale, logf(S));
-      if (a.entropy) a.entropy[row] = nan || inf ? NAN : logf(S) - kLn2 * (p.z / S);
+      const float M = p.x, l2 = log2f(p.y);
+      const bool nan = p.w != 0.f;
+      s_again = !nan && !(M > Low<T>::kFloor * c + 200.f && M < 0x1p+24f);
+      s_base = nan ? NAN : M;
+      s_log2 = l2;
+      if (a.lse) a.lse[row] = nan ? NAN : kLn2 * (M + l2);
+      if (a.entropy) a.entropy[row] = nan ? NAN : kLn2 * (l2 - p.z / p.y);
     }
   } else if (warp == 1 && a.n_top > 0) {
     TopList list;
@@ -286,19 +350,55 @@ __global__ void __launch_bounds__(lp::kThreads) logprob_rows_kernel(LogprobArgs 
     if (lane == a.n_top - 1) s_bound = (uint32_t)(list.mine >> 32);
   }
   __syncthreads();
+  if (s_again) {   // (no NaN in the row)
+    float m = -INFINITY;
+    for (int i = threadIdx.x; i < a.vocab; i += kThreads) m = fmaxf(m, as_float(x[i]));
+    const uint32_t k = __reduce_max_sync(0xffffffffu, value_key(m));
+    if (lane == 0) s_part[warp].x = key_value(k);
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s_part[w].x);
+    __syncthreads();
+    float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (m > -INFINITY && m < INFINITY)
+      for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
+        const float t = (as_float(x[i]) - m) * c, e = fast_exp2(t);
+        p.y += e;
+        p.z = fmaf(e, fmaxf(t, -300.f), p.z);
+      }
+    p = join_lanes(p);
+    if (lane == 0) s_part[warp] = p;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      p = s_part[0];
+      for (int w = 1; w < kWarps; ++w) p = join(p, s_part[w]);
+      const bool inf = m == INFINITY;
+      const float l2 = log2f(p.y);   // (a row of -infinities: m and l2 are -infinity, the results NaN but for lse)
+      s_base = inf ? 0.f : m;
+      s_log2 = inf ? INFINITY : l2;
+      if (a.lse) a.lse[row] = inf ? INFINITY : fmaf(m, a.scale, kLn2 * l2);
+      if (a.entropy) a.entropy[row] = inf ? NAN : kLn2 * (l2 - p.z / p.y);
+    }
+    __syncthreads();
+  }
+  auto log_probability = [&](float f) {
+    const float d = fmaf(f, c, -s_base);
+    if (s_again) return (f - s_base) * a.scale - kLn2 * s_log2;
+    return d == -INFINITY ? f * a.scale : kLn2 * (d - s_log2);   // (c f may leave the type where scale f does not)
+  };
   for (int j = threadIdx.x; j < a.n_given; j += kThreads) {
     const int tok = a.given[(size_t)row * a.n_given + j];
-    a.logp[(size_t)row * a.n_given + j] =
-        tok >= 0 && tok < a.vocab ? fmaf(as_float(x[tok]) - s_m, a.scale, -s_ln) : NAN;
+    a.logp[(size_t)row * a.n_given + j] = tok >= 0 && tok < a.vocab ? log_probability(as_float(x[tok])) : NAN;
   }
   if (a.n_top <= 0) return;
   TopList list;
   if (s_bound) list.over = ((uint64_t)s_bound << 32) - 1;
-  for (int j = warp; j < a.n_top; j += kWarps) {
-    const int ch = s_chunk[j];
+  // few chunks are looked through by several warps each: a warp takes every pieces-th 256 elements
+  const int pieces = a.n_top == 1 ? 8 : a.n_top == 2 ? 4 : a.n_top <= 4 ? 2 : 1;
+  for (int j = warp; j < a.n_top * pieces; j += kWarps) {
+    const int ch = s_chunk[j / pieces];
     if (ch < 0) break;
-    const int i0 = ch ? head + ch * kChunk : 0, i1 = min(a.vocab, head + (ch + 1) * kChunk);
-    for (int b = i0; b < i1; b += 8 * 32) {
+    const int i0 = ch ? head + ch * kChunk<T> : 0, i1 = min(a.vocab, head + (ch + 1) * kChunk<T>);
+    for (int b = i0 + j % pieces * 256; b < i1; b += 256 * pieces) {
       float f[8];
 #pragma unroll
       for (int y = 0; y < 8; ++y) {
@@ -320,14 +420,14 @@ __global__ void __launch_bounds__(lp::kThreads) logprob_rows_kernel(LogprobArgs 
     const size_t at = (size_t)row * a.n_top + lane;
     const bool have = list.mine != 0;
     if (a.top_ids) a.top_ids[at] = have ? (int)(0xffffffffu - (uint32_t)list.mine) : -1;
-    if (a.top_logp) a.top_logp[at] = have ? fmaf(key_value((uint32_t)(list.mine >> 32)) - s_m, a.scale, -s_ln) : NAN;
+    if (a.top_logp) a.top_logp[at] = have ? log_probability(key_value((uint32_t)(list.mine >> 32))) : NAN;
   }
 }
 
 struct LogprobWs { size_t off_key, total; int max_chunks, max_parts; };
-static LogprobWs logprob_ws(int n_rows, int vocab, int n_top) {
+static LogprobWs logprob_ws(int n_rows, int vocab, int n_top, int elem_bytes) {
   LogprobWs w;
-  w.max_chunks = std::max(1, (int)(((int64_t)vocab + lp::kChunk - 1) / lp::kChunk));
+  w.max_chunks = std::max(1, (int)(((int64_t)vocab * elem_bytes + lp::kChunkBytes - 1) / lp::kChunkBytes));
   w.max_parts = (w.max_chunks + lp::kWarps - 1) / lp::kWarps;
   w.off_key = (size_t)n_rows * w.max_parts * sizeof(float4);
   w.total = w.off_key + (n_top > 0 ? ((size_t)n_rows * w.max_chunks * 4 + 15) / 16 * 16 : 0);
@@ -346,7 +446,7 @@ using namespace spkv;
 
 extern "C" size_t spkv_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top) {
   if (n_rows < 0 || vocab < 1 || n_top < 0 || n_top > SPKV_MAX_TOP) return 0;
-  return std::max<size_t>(16, logprob_ws(n_rows, vocab, n_top).total);
+  return std::max<size_t>(16, logprob_ws(n_rows, vocab, n_top, 4).total);
 }
 
 extern "C" int spkv_token_logprobs(int32_t dtype, int32_t n_rows, int32_t vocab, const void *d_logits, int64_t row_stride,
@@ -357,15 +457,15 @@ extern "C" int spkv_token_logprobs(int32_t dtype, int32_t n_rows, int32_t vocab,
   if (n_top > SPKV_MAX_TOP) return SPKV_E_UNSUPPORTED;
   if (!(scale > 0.f) || !isfinite(scale)) return SPKV_E_INVALID;
   if ((int64_t)n_rows * n_given > INT32_MAX || (int64_t)n_rows * n_top > INT32_MAX) return SPKV_E_UNSUPPORTED;
-  if (vocab > INT32_MAX - 2 * lp::kChunk) return SPKV_E_UNSUPPORTED;
+  if (vocab > INT32_MAX - 2 * lp::kChunkBytes) return SPKV_E_UNSUPPORTED;
   if (n_rows == 0) return SPKV_OK;
   const int bytes = dtype == SPKV_F32 ? 4 : 2;
   if (!d_logits || ((uintptr_t)d_logits & (bytes - 1))) return SPKV_E_INVALID;
   if (!d_logp) n_given = 0;
   if (!d_top_ids && !d_top_logp) n_top = 0;
   if (n_given && !d_given) return SPKV_E_INVALID;
-  const LogprobWs w = logprob_ws(n_rows, vocab, n_top);
-  if (!d_workspace || ((uintptr_t)d_workspace & 15) || workspace_bytes < w.total) return SPKV_E_WORKSPACE;
+  if (!d_workspace || ((uintptr_t)d_workspace & 15) || workspace_bytes < spkv_logprobs_workspace_bytes(n_rows, vocab, n_top)) return SPKV_E_WORKSPACE;
+  const LogprobWs w = logprob_ws(n_rows, vocab, n_top, bytes);
   int dev = -1, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return SPKV_E_CUDA;
@@ -375,9 +475,9 @@ extern "C" int spkv_token_logprobs(int32_t dtype, int32_t n_rows, int32_t vocab,
   a.part = static_cast<float4 *>(d_workspace);
   a.chunk_key = reinterpret_cast<uint32_t *>(static_cast<char *>(d_workspace) + w.off_key);
   a.max_chunks = w.max_chunks;
-  // chunks a warp takes: one while there are fewer blocks than three fill the SMs, then up to kMaxRounds
+  // chunks a warp takes: one while the blocks do not fill the SMs twice, then up to kMaxRounds
   const int64_t blocks = (int64_t)n_rows * w.max_parts;
-  a.rounds = (int)std::max<int64_t>(1, std::min<int64_t>(lp::kMaxRounds, blocks / ((int64_t)sms * lp::kBlocksPerSm * 3)));
+  a.rounds = (int)std::max<int64_t>(1, std::min<int64_t>(lp::kMaxRounds, blocks / ((int64_t)sms * lp::kBlocksPerSm * 2)));
   a.parts = (w.max_parts + a.rounds - 1) / a.rounds;
   if ((int64_t)n_rows * a.parts > INT32_MAX) return SPKV_E_UNSUPPORTED;
   note_cacheless_call();

@@ -917,7 +917,7 @@ def spkv_tree_accept(tokens, target, parent=None, n_nodes=None, path=None, n_pat
     return path, n_path, next
 
 
-_logprob_ws = {}
+_logprob_ws, _logprob_bytes = {}, {}
 
 
 def spkv_token_logprobs(logits, given=None, top=0, scale=1.0, lse=None, logp=None, entropy=None, top_ids=None, top_logp=None,
@@ -942,7 +942,9 @@ def spkv_token_logprobs(logits, given=None, top=0, scale=1.0, lse=None, logp=Non
     if top > 0:
         top_ids = logits.new_empty(n, top, dtype=i32) if top_ids is None else top_ids
         top_logp = logits.new_empty(n, top, dtype=f32) if top_logp is None else top_logp
-    ws_bytes = max(16, lib().spkv_logprobs_workspace_bytes(n, vocab, top))
+    ws_bytes = _logprob_bytes.get((n, vocab, top))
+    if ws_bytes is None:
+        ws_bytes = _logprob_bytes[n, vocab, top] = max(16, lib().spkv_logprobs_workspace_bytes(n, vocab, top))
     ws = _scratch(_logprob_ws, ws_bytes, dev)
     rc = _on_device(dev, lib().spkv_token_logprobs, _DTYPE[logits.dtype], n, vocab, logits.data_ptr(),
                     logits.stride(0) if n > 1 else 0, scale, _dense(given, i32, (n, m), dev), m, top, _dense(lse, f32, (n,), dev),
