@@ -505,19 +505,18 @@ class Cache:
         _THREE_ROWS.pack_into(rows, 0, *_draft_rows(q, B, T, hq, dev, "q"), *_draft_rows(k, B, T, hkv, dev, "k"),
                               *_draft_rows(v, B, T, hkv, dev, "v"))
         at = C.addressof(rows)
-        if out is None:
-            out = q.new_empty(B, T, hq, 128)
-        if lse is None and want_lse:
-            lse = q.new_empty(B, T, hq, dtype=torch.float32)
         ptrs = (_dense(seq_ids, torch.int32, (B,), dev), _dense(n_nodes, torch.int32, (B,), dev),
-                _dense(parent, torch.int32, (B, T), dev), _dense(logits, torch.float32, (B, T, hkv), dev),
-                _dense(out, torch.bfloat16, (B, T, hq, 128), dev), _dense(lse, torch.float32, (B, T, hq), dev))
+                _dense(parent, torch.int32, (B, T), dev), _dense(logits, torch.float32, (B, T, hkv), dev))
+        out, at_out = _result(q, out, torch.bfloat16, (B, T, hq, 128), dev)
+        at_lse = None
+        if lse is not None or want_lse:
+            lse, at_lse = _result(q, lse, torch.float32, (B, T, hq), dev)
         nbytes = self._tree_bytes.get((B, T))
         if nbytes is None:
             nbytes = self._tree_bytes[B, T] = max(256, lib().spkv_decode_tree_workspace_bytes(C.byref(cfg), B, T))
         ws = _scratch(self._tree_ws, nbytes, dev)
         rc = _on_device(dev, lib().spkv_decode_attention_tree, self._h, layer, ptrs[0], B, T, ptrs[1], ptrs[2], at, at + _ROW,
-                        at + 2 * _ROW, ptrs[3], ptrs[4], ptrs[5], self.default_scale if sm_scale is None else sm_scale,
+                        at + 2 * _ROW, ptrs[3], at_out, at_lse, self.default_scale if sm_scale is None else sm_scale,
                         ws.data_ptr(), ws.numel())
         if rc:
             raise SpkvError(rc, "spkv_decode_attention_tree")
@@ -818,6 +817,14 @@ def _dense(t, dtype, shape, dev):
     return t.data_ptr()
 
 
+def _result(like, t, dtype, shape, dev):
+    """(tensor, its pointer) of a result: the caller's, or one made here"""
+    if t is None:
+        t = like.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr()
+    return t, _dense(t, dtype, shape, dev)
+
+
 def _positions(nr, pos, dev):
     """(n_tok, pointer) of an int32 [n_tok] or [n_axes, n_tok] device tensor"""
     n = pos.shape[-1]
@@ -908,12 +915,14 @@ def spkv_tree_accept(tokens, target, parent=None, n_nodes=None, path=None, n_pat
         raise ValueError("tokens: a device tensor [B, T]")
     B, T = shape = tokens.shape
     i32 = torch.int32
-    path = tokens.new_empty(B, T, dtype=i32) if path is None else path
-    n_path = tokens.new_empty(B, dtype=i32) if n_path is None else n_path
-    next = tokens.new_empty(B, dtype=i32) if next is None else next
-    _check(_on_device(dev, lib().spkv_tree_accept, B, T, _dense(n_nodes, i32, (B,), dev), _dense(parent, i32, shape, dev),
-                      _dense(tokens, i32, shape, dev), _dense(target, i32, shape, dev), _dense(path, i32, shape, dev),
-                      _dense(n_path, i32, (B,), dev), _dense(next, i32, (B,), dev)), "spkv_tree_accept")
+    ptrs = (_dense(n_nodes, i32, (B,), dev), _dense(parent, i32, shape, dev), _dense(tokens, i32, shape, dev),
+            _dense(target, i32, shape, dev))
+    path, at_path = _result(tokens, path, i32, shape, dev)
+    n_path, at_n = _result(tokens, n_path, i32, (B,), dev)
+    next, at_next = _result(tokens, next, i32, (B,), dev)
+    rc = _on_device(dev, lib().spkv_tree_accept, B, T, *ptrs, at_path, at_n, at_next)
+    if rc:
+        raise SpkvError(rc, "spkv_tree_accept")
     return path, n_path, next
 
 
@@ -934,22 +943,23 @@ def spkv_token_logprobs(logits, given=None, top=0, scale=1.0, lse=None, logp=Non
     n, vocab = logits.shape
     f32, i32 = torch.float32, torch.int32
     m = 0 if given is None else given.shape[-1]
-    lse = logits.new_empty(n, dtype=f32) if lse is None else lse
-    if given is not None and logp is None:
-        logp = logits.new_empty(n, m, dtype=f32)
-    if want_entropy and entropy is None:
-        entropy = logits.new_empty(n, dtype=f32)
+    at_given = _dense(given, i32, (n, m), dev)
+    lse, at_lse = _result(logits, lse, f32, (n,), dev)
+    at_logp = at_entropy = at_ids = at_top = None
+    if given is not None or logp is not None:
+        logp, at_logp = _result(logits, logp, f32, (n, m), dev)
+    if want_entropy or entropy is not None:
+        entropy, at_entropy = _result(logits, entropy, f32, (n,), dev)
     if top > 0:
-        top_ids = logits.new_empty(n, top, dtype=i32) if top_ids is None else top_ids
-        top_logp = logits.new_empty(n, top, dtype=f32) if top_logp is None else top_logp
+        top_ids, at_ids = _result(logits, top_ids, i32, (n, top), dev)
+        top_logp, at_top = _result(logits, top_logp, f32, (n, top), dev)
     ws_bytes = _logprob_bytes.get((n, vocab, top))
     if ws_bytes is None:
         ws_bytes = _logprob_bytes[n, vocab, top] = max(16, lib().spkv_logprobs_workspace_bytes(n, vocab, top))
     ws = _scratch(_logprob_ws, ws_bytes, dev)
     rc = _on_device(dev, lib().spkv_token_logprobs, _DTYPE[logits.dtype], n, vocab, logits.data_ptr(),
-                    logits.stride(0) if n > 1 else 0, scale, _dense(given, i32, (n, m), dev), m, top, _dense(lse, f32, (n,), dev),
-                    _dense(entropy, f32, (n,), dev), _dense(logp, f32, (n, m), dev), _dense(top_ids, i32, (n, top), dev),
-                    _dense(top_logp, f32, (n, top), dev), ws.data_ptr(), ws.numel())
+                    logits.stride(0) if n > 1 else 0, scale, at_given, m, top, at_lse, at_entropy, at_logp, at_ids, at_top,
+                    ws.data_ptr(), ws.numel())
     if rc:
         raise SpkvError(rc, "spkv_token_logprobs")
     return lse, logp, entropy, top_ids, top_logp

@@ -51,3 +51,65 @@ def test_logprobs_of_no_rows_and_workspace_sizes(lib):
 def test_calls_with_a_cache_refuse_a_missing_one(lib):
     assert lib.spkv_decode_attention_tree(None, 0, FAKE, 1, 1, None, None, FAKE, FAKE, FAKE, None, FAKE, None, 0.1, FAKE, 1 << 30, None) == -1
     assert lib.spkv_append_path(None, 0, 1, FAKE, 1, 1, None, None, FAKE, 0, FAKE, 0, FAKE, None) == -1
+
+
+# ---- devices: the library and CUDA's current device are stand-ins (test_binding_streams.py) ------------------
+from test_binding_streams import Tensor, a_cache, raw, two_devices  # noqa: E402,F401
+
+
+@pytest.fixture(scope="module")
+def spkv(lib):
+    from paper_2605_14037_b200 import spkv as mod
+    return mod
+
+
+class Rows(Tensor):
+    device = property(lambda self: f"cuda:{self.dev}")
+
+    def stride(self, i=None):
+        st, n = [], 1
+        for x in reversed(self.shape):
+            st.append(n)
+            n *= x
+        return tuple(reversed(st)) if i is None else st[::-1][i]
+
+    def dim(self):
+        return len(self.shape)
+
+
+def drafts(dev):
+    import torch
+    t = lambda shape, dtype: Rows(shape, dtype, dev, 1 << 16)
+    return dict(ids=t((2,), torch.int32), q=t((2, 3, 4, 128), torch.bfloat16), k=t((2, 3, 2, 128), torch.bfloat16), lg=t((2, 3, 2), torch.float32),
+                tok=t((2, 3), torch.int32), n=t((2,), torch.int32), x=t((2, 50), torch.float32), f=t((2,), torch.float32), out=t((2, 3, 4, 128), torch.bfloat16))
+
+
+def calls(spkv, cache, d, e=None, **kw):
+    """The four calls; e: where one of each call's tensors comes from"""
+    e = e or d
+    return [lambda: cache.spkv_decode_attention_tree(0, d["ids"], d["q"], d["k"], e["k"], logits=d["lg"], out=d["out"], **kw),
+            lambda: cache.spkv_append_path(0, d["ids"], d["k"], d["k"], e["lg"], **kw),
+            lambda: spkv.spkv_tree_accept(d["tok"], e["tok"], None, None, d["tok"], d["n"], d["n"], **kw),
+            lambda: spkv.spkv_token_logprobs(d["x"], lse=e["f"], want_entropy=False, **kw)]
+
+
+@pytest.mark.parametrize("dev", [0, 1])
+def test_calls_run_on_their_tensors_device(spkv, two_devices, monkeypatch, dev):
+    cache = a_cache(spkv, dev)
+    cache._tree_ws, cache._tree_bytes, cache.default_scale = {}, {(2, 3): 256}, 0.1
+    monkeypatch.setattr(spkv, "_scratch", lambda store, n, d: Rows((n,), None, d, 4096))
+    monkeypatch.setattr(spkv, "_logprob_bytes", {(2, 50, 0): 16})
+    for call in calls(spkv, cache, drafts(dev)):
+        call()
+    assert [c[0] for c in two_devices] == ["spkv_decode_attention_tree", "spkv_append_path", "spkv_tree_accept", "spkv_token_logprobs"]
+    for name, current, args in two_devices:
+        assert current == dev and raw(args[-1]) == 100 + dev, name
+
+
+def test_tensors_or_streams_of_another_device_are_refused(spkv, two_devices):
+    cache, other = a_cache(spkv, 1), type("S", (), dict(device_index=0, cuda_stream=7))()
+    cache._tree_ws, cache._tree_bytes, cache.default_scale = {}, {(2, 3): 256}, 0.1
+    for call in calls(spkv, cache, drafts(1), drafts(0)) + calls(spkv, cache, drafts(0))[:2] + calls(spkv, cache, drafts(1), stream=other):
+        with pytest.raises(ValueError):
+            call()
+    assert not two_devices

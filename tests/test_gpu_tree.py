@@ -746,3 +746,95 @@ def test_refusals():
     ws = torch.zeros(need + 256, dtype=torch.uint8, device=dev())
     call = lambda w, n: l.spkv_decode_attention_tree(c.cache._h, 0, c.ids.data_ptr(), 2, 6, None, None, r, r, r, None, out.data_ptr(), None, 0.1, w, n, None)
     assert call(None, need) == -7 and call(ws.data_ptr() + 16, need) == -7 and call(ws.data_ptr(), need - 1) == -7
+
+
+def pool_of(t):
+    """The stream whose memory the tensor lies in."""
+    at = t.data_ptr()
+    return next(s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"])
+
+
+def test_results_come_from_the_memory_of_the_calls_stream():
+    spkv = load()
+    c = Case(spkv, (300, 700), 8, 2, 6, (0.5, 0.2), seed=8)
+    tokens = torch.zeros((2, 6), dtype=torch.int32, device=dev())
+    x = torch.randn((4, 3000), device=dev())
+    keep = [torch.empty_like(t) for t in (c.qd, tokens, x) for _ in range(8)]     # blocks the current stream can give away
+    del keep
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    res = [*c.run(stream=s), *spkv.spkv_tree_accept(tokens, tokens, stream=s), *spkv.spkv_token_logprobs(x, tokens[:1, :4].t().contiguous(), top=2, stream=s)]
+    s.synchronize()
+    assert len(res) == 10 and all(pool_of(t) == s.cuda_stream for t in res)
+    for a, b in zip(res, [*c.run(), *spkv.spkv_tree_accept(tokens, tokens), *spkv.spkv_token_logprobs(x, tokens[:1, :4].t().contiguous(), top=2)]):
+        assert torch.equal(a, b)
+    c.cache.spkv_append_path(0, c.ids, c.kd, c.vd, c.ld, stream=s)
+    s.synchronize()
+    assert (c.cache.spkv_read_lengths(0)[1] == np.array([[306], [706]])).all()
+
+
+def test_calls_with_results_given_do_not_reach_the_allocator():
+    spkv = load()
+    c = Case(spkv, (300, 700), 8, 2, 6, (0.5, 0.2), seed=8)
+    out, lse = c.run()
+    tokens = torch.zeros((2, 6), dtype=torch.int32, device=dev())
+    path, n, nxt = spkv.spkv_tree_accept(tokens, tokens)
+    x = torch.randn((4, 3000), device=dev())
+    r = spkv.spkv_token_logprobs(x, top=2)
+    none = torch.zeros(2, dtype=torch.int32, device=dev())
+
+    def calls():
+        c.cache.spkv_decode_attention_tree(0, c.ids, c.qd, c.kd, c.vd, c.pd, c.nd, c.ld, out, lse)
+        spkv.spkv_tree_accept(tokens, tokens, None, None, path, n, nxt)
+        c.cache.spkv_append_path(0, c.ids, c.kd, c.vd, c.ld, path, none)
+        spkv.spkv_token_logprobs(x, top=2, lse=r[0], entropy=r[2], top_ids=r[3], top_logp=r[4])
+
+    calls()
+    torch.cuda.synchronize()
+    count = lambda: (torch.cuda.memory_stats()["allocation.all.allocated"], torch.cuda.mem_get_info()[0])
+    before = count()
+    for _ in range(5):
+        calls()
+    torch.cuda.synchronize()
+    assert count() == before
+    c.cache.check()
+
+
+@pytest.mark.parametrize("w,t", [(3, 0), (3, 7), (64, 200), (65, 64), (65, 131), (128, 127), (300, 299), (300, 1000), (4096, 5000)])
+def test_windows_of_any_size(w, t):
+    """rings of one to 64 pages, before and after they have gone round"""
+    c = Case(load(), (t, max(0, t - 1)), 4, 1, 7, (0.4,), w, seed=w + t, parent="forest")
+    out, lse = c.run()
+    c.cache.check()
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("gain", [12.0, 60.0])
+def test_large_scores(gain):
+    """Scores of hundreds: the weights of a row live on a few keys, its maximum moves from page to page."""
+    c = Case(load(), (3000, 500), 8, 2, 20, (0.9, 0.3), seed=4)
+    c.q = synth.to_bf16_bits(synth.bf16_bits_to_f32(c.q) * np.float32(gain))
+    c.to_device()
+    out, lse = c.run()
+    c.cache.check()
+    c.check(out, lse)
+
+
+def test_planted_page_indices_under_range_checks():
+    """SPKV_FLAG_DEBUG_BOUNDS: an index in a page table that names no pool page is reported, nothing outside the arena is read or written"""
+    spkv = load()
+    c = Case(spkv, (700,), 4, 1, 6, (1.0,), seed=3, flags=spkv.FLAG_DEBUG_BOUNDS)
+    n_ring = 2                                   # ring pages of the only unit: global pages 0 and 1; the pool's follow
+    words = c.cache.arena.view(torch.int32)
+    ln = int(c.cache.spkv_read_lengths(0)[0][0, 0])
+    used = list(range(n_ring, n_ring + (ln + 63) // 64))
+    head = words[:1 << 16].cpu().numpy()
+    at = next(i for i in range(len(head) - len(used)) if head[i:i + len(used)].tolist() == used)
+    words[at + 2] = 1                            # a ring page of the same arena: even an unchecked read would stay inside it
+    c.run()
+    assert c.cache.spkv_status() == -13
+    c.cache.spkv_clear_status()
+    words[at + len(used) - 1] = 0
+    words[at + 2] = used[2]
+    c.cache.spkv_append_path(0, c.ids, c.kd, c.vd, torch.full_like(c.ld, 9.0))
+    assert c.cache.spkv_status() == (-13 if ln % 64 else 0)
