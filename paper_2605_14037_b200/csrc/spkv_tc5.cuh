@@ -119,6 +119,25 @@ __device__ inline void umma_pv_page(uint32_t d_tmem, uint32_t a_tmem, uint64_t b
       " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [t7], b3, %3, 1;\n}\n"
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(first) : "memory");
 }
+// ... with a page's two 32-key halves apart: hi of keys 0-31 at a_tmem, lo 16 columns later, the other 32 keys 32 columns
+// later likewise (so that a half's P takes the columns of its own scores).
+__device__ inline void umma_pv_page_halves(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t first) {
+  asm volatile(
+      "{\n .reg .pred e, p;\n .reg .b64 b1, b2, b3;\n .reg .b32 t1, t2, t3, t4, t5, t6, t7;\n"
+      " elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
+      " add.u64 b1, %2, 128; add.u64 b2, %2, 256; add.u64 b3, %2, 384;\n"
+      " add.u32 t1, %1, 8; add.u32 t2, %1, 16; add.u32 t3, %1, 24; add.u32 t4, %1, 32;\n"
+      " add.u32 t5, %1, 40; add.u32 t6, %1, 48; add.u32 t7, %1, 56;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [t1], b1, %3, 1;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [t2], %2, %3, 1;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [t3], b1, %3, 1;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [t4], b2, %3, 1;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [t5], b3, %3, 1;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [t6], b2, %3, 1;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [t7], b3, %3, 1;\n}\n"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(first) : "memory");
+}
 // One page of P.V with a single fp16 P (64 keys = 32 columns at a_tmem): four K=16 steps.
 __device__ inline void umma_pv_page_f16(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
                                         uint32_t first) {

@@ -2,9 +2,9 @@
 //
 // A unit's (sequence, KV head) queries are the rows (node, head of the group) -> node * G + g, cut into tiles of 128 that
 // are the M side of tcgen05 MMAs.  Its keys are pages of 64: those of the compact cache, those of the ring, and one
-// page of the drafts themselves.  The pages of all units of the launch stand in one line that is cut into equal ranges, one per
-// block and row tile (two blocks an SM; the tiles of a range are neighbours, so that the second finds its pages in
-// L2).  Where a unit lies inside a range its rows are written at once; otherwise the pieces leave (m, l, O) per row and
+// page of the drafts themselves.  The pages of all units of the launch stand in one line per row tile that is cut into equal ranges, one per
+// block (two blocks an SM; where all tiles have the same lines, the blocks of a range are neighbours, so that the second finds its pages in
+// L2; where trees of different sizes leave a tile few rows, it gets few blocks).  Where a unit lies inside a range its rows are written at once; otherwise the pieces leave (m, l, O) per row and
 // tree_merge_kernel joins them by their log-sum-exp weights.
 //
 // Per page: S = Q K^T (8 MMAs M128 N64 K16 into tensor memory), softmax in registers (thread = row = lane of
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
   uint64_t *bar = reinterpret_cast<uint64_t *>(smem + off_bar);
-  volatile int *s_info = reinterpret_cast<volatile int *>(smem + off_info);     // tensor memory, first and last unit, drafts' blocks let in, range
+  volatile int *s_info = reinterpret_cast<volatile int *>(smem + off_info);     // tensor memory, first and last unit, drafts' blocks let in, range, tile
   volatile uint64_t *s_path = reinterpret_cast<volatile uint64_t *>(smem + off_path);   // [node] nodes it sees
   volatile uint8_t *s_depth = smem + off_depth;
   volatile unsigned *s_grow = reinterpret_cast<volatile unsigned *>(smem + off_grow);   // [page & 1][warp] rows whose maximum moves
@@ -188,7 +188,6 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   int4 *s_units = reinterpret_cast<int4 *>(smem + off_units);
   volatile int *s_plan = reinterpret_cast<volatile int *>(smem + off_path);     // (before the paths are)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int range = blockIdx.x / a.n_tiles, tile = blockIdx.x - range * a.n_tiles;
   if (tid == 0) {
     for (int i = 0; i < B_COUNT; ++i) mbar_init(&bar[i], i == B_P_FULL || i == B_P_FULL + 1 ? 256 : i == B_TREE_EMPTY ? 8 : 1);
     mbar_fence_init();
@@ -220,13 +219,58 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       }
     }
     if (bad && blockIdx.x == 0) set_status(c, SPKV_E_BOUNDS);
+    auto cost_of = [&](int k, int of_tile) {
+      const int np = TreeUnit(a, meta[k], of_tile).np;
+      return np ? np + kSegmentCost : 0;
+    };
+    // This block's tile and its place among the tile's blocks.  Tiles of (nearly) the same length take turns block by block, so
+    // that the blocks that read the same pages do so at the same time; otherwise each tile gets blocks by its length.
+    int tile = 0, range = blockIdx.x, n_blocks = gridDim.x, step = 1;
+    if (a.n_tiles > 1) {
+      for (int x = 0; x < a.n_tiles; ++x) {
+        int length = 0;
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) length += cost_of(k, x);
+        length = __reduce_add_sync(0xffffffffu, length);
+        if (lane == 0) s_plan[x * 16 + warp] = length;
+      }
+      __syncthreads();
+      long long all = 0, before = 0;
+      int longest = 0, shortest = 0x7fffffff;
+      for (int pass = 0; pass < 2; ++pass) {
+        for (int x = 0; x < a.n_tiles; ++x) {
+          int length = 0;
+          for (int w = 0; w < kThreads / 32; ++w) length += s_plan[x * 16 + w];
+          if (pass == 0) {
+            all += length;
+            longest = max(longest, length);
+            shortest = min(shortest, length);
+          } else {
+            // blocks [from, to) of those that every tile does not get anyway are this one's
+            const int spare = gridDim.x - a.n_tiles;
+            const int from = (int)(spare * before / all) + x, to = (int)(spare * (before + length) / all) + x + 1;
+            if ((int)blockIdx.x >= from && (int)blockIdx.x < to) { tile = x; range = blockIdx.x - from; n_blocks = to - from; }
+            before += length;
+          }
+        }
+        if (pass == 0 && (all == 0 || shortest >= longest - longest / 8)) {
+          step = a.n_tiles;
+          n_blocks = gridDim.x / a.n_tiles;
+          range = blockIdx.x / a.n_tiles;
+          tile = blockIdx.x - range * a.n_tiles;
+          break;
+        }
+      }
+      __syncthreads();
+    }
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) {
-      const int i = tid * kPerThread + k, np = TreeUnit(a, meta[k], tile).np;
-      cost[k] = np ? np + kSegmentCost : 0;
+      cost[k] = cost_of(k, tile);
       meta[k].x = sum;
       sum += cost[k];
-      if (range == 0 && i < a.n_items && np == 0) a.ends[(size_t)tile * a.n_items + i] = make_int2(-1, -1);   // nothing to join
+      if (blockIdx.x == 0)
+        for (int x = 0; x < a.n_tiles; ++x)   // nothing to join
+          if (tid * kPerThread + k < a.n_items && cost_of(k, x) == 0) a.ends[(size_t)x * a.n_items + tid * kPerThread + k] = make_int4(-1, -1, 1, 0);
     }
     int incl = sum;
 #pragma unroll
@@ -244,7 +288,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       total += x;
       if (w < warp) before += x;
     }
-    const int nb = min(a.n_ranges, (total + a.min_cost - 1) / a.min_cost);
+    const int nb = min(n_blocks, (total + a.min_cost - 1) / a.min_cost);
     if (range >= nb) return;
     // equal lengths, but for a cut that falls next to the border of two units: it moves onto it
     const int snap = total / nb / 16;
@@ -274,7 +318,11 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       if (i < kUnitsHere) s_units[i] = meta[k];
       else a.units[(size_t)blockIdx.x * a.n_items + i] = meta[k];
     }
-    if (tid == 0) s_info[3] = 0;
+    if (tid == 0) {
+      s_info[3] = 0;
+      s_info[6] = tile;
+      s_info[7] = step;
+    }
     if (tid < 32) s_bad[tid] = 0;
   }
   if (warp == kMmaWarp) {
@@ -287,7 +335,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   fence_after();
   const uint32_t tbase = (uint32_t)s_info[0];
   bool failed = false;   // (the block's units and range are read where they are needed: no register to spare)
-  auto unit_at = [&](int i) { return TreeUnit(a, i < kUnitsHere ? s_units[i] : a.units[(size_t)blockIdx.x * a.n_items + i], tile); };
+  auto unit_at = [&](int i) { return TreeUnit(a, i < kUnitsHere ? s_units[i] : a.units[(size_t)blockIdx.x * a.n_items + i], s_info[6]); };
   auto part_of = [&](const TreeUnit &x, int &s, int &e) {   // of the unit's pages, those of this block's range: [s, e) in the line
     s = max(x.pre + kSegmentCost, s_info[4]);
     e = min(x.pre + kSegmentCost + x.np, s_info[5]);
@@ -317,7 +365,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   // Query rows r, r + step, ... of an item with n nodes -> two slabs of 128 rows x 128 B, 128-byte swizzle; lanes 0-15 and
   // 16-31 of a warp take a row each.  (Rows behind the last keep what they hold: a row of a tile does not touch another.)
   auto copy_queries = [&](int item, int n, int r, int step) {
-    const int b = item / c.Hkv, kvh = item - b * c.Hkv, ch = lane & 15, n_rows = min(kTreeRows, n * c.G - tile * kTreeRows);
+    const int b = item / c.Hkv, kvh = item - b * c.Hkv, ch = lane & 15, tile = s_info[6], n_rows = min(kTreeRows, n * c.G - tile * kTreeRows);
     const uint32_t sQ = smem_u32(smem) + (ch >> 3) * 16384;
     const __nv_bfloat16 *src = a.q + (int64_t)b * a.T * a.q_tok + (int64_t)kvh * c.G * a.q_head + ch * 8;
 #pragma unroll 4
@@ -406,7 +454,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
           break;
         }
         fence_after();
-        umma_pv_page(tbase + 128, tbase + b * 64, dV + (uint64_t)s * kUnits, idesc_pv, i > 0 ? 1u : 0u);
+        umma_pv_page_halves(tbase + 128, tbase + b * 64, dV + (uint64_t)s * kUnits, idesc_pv, i > 0 ? 1u : 0u);
         umma_commit(&bar[B_EMPTY + s]);
         if (i + 2 < n) issue_qk(i + 2);   // (behind P V: the pipe runs a thread's instructions in order)
         else umma_commit(&bar[B_O_DONE + b]);
@@ -515,9 +563,9 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   } else {
     // ---------------------------------------------------------------- softmax
     // A row belongs to two threads, one in warps 0-3 (half 0) and one in warps 4-7: each has 32 of a page's 64 scores and 64
-    // of the row's 128 output dims.  They meet once a page, when both have their scores in registers: whether the row's
-    // reference maximum has to move, which it rarely does, and that P may be written over the scores.
-    const int half = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    // of the row's 128 output dims.  They meet once a page: whether the row's reference maximum has to move, which
+    // it rarely does.
+    const int half = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane, R = s_info[6] * kTreeRows + row;
     const uint32_t t_lane = tbase + ((uint32_t)(quarter * 32) << 16), t_o = t_lane + 128 + half * 64;
     {   // the first segment's queries
       int i = 0;
@@ -548,8 +596,8 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       // (What is needed for masks only is read again where it is needed: the loop over pages has no register to spare, and a
       // spilled one comes back from L2.)
       const int nk = x.nk;
-      const bool row_live = tile * kTreeRows + row < x.n * c.G;
-      const bool live = tile * kTreeRows + quarter * 32 < x.n * c.G;   // warps without a live row only keep the barriers going
+      const bool row_live = R < x.n * c.G;
+      const bool live = R - lane < x.n * c.G;   // warps without a live row only keep the barriers going
       float lg = tree_logit(a, x, item, p0, half);   // stored logit of this lane's slot of the page that comes next, if of the ring
       float m_ref = -INFINITY, l = 0.f;
       bool left_together = false;
@@ -558,7 +606,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         uint32_t mask = 0xffffffffu;   // the keys that this row sees
         if (p >= nk - 1) {
           if (p >= nk && (i == 0 || p == nk) && !tree_wait(&bar[B_TREE_FULL], masked & 1)) failed = true;
-          mask = tree_sees(a, x, item, p, half, lg, s_path, s_depth, tile * kTreeRows + row);
+          mask = tree_sees(a, x, item, p, half, lg, s_path, s_depth, R);
           lg = tree_logit(a, x, item, p + 1, half);
         }
         if (!failed && !tree_wait(&bar[B_S_FULL + bf], (j >> 1) & 1)) failed = true;
@@ -639,7 +687,8 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         const float ms = m_ref == -INFINITY ? 0.f : m_ref;
         const float2 sc2 = make_float2(a.scale_log2, a.scale_log2), nms2 = make_float2(-ms, -ms);
         float2 l2a = make_float2(0.f, 0.f), l2b = l2a;
-        // two terms, two keys a column: the first in columns [0, 32) of the score buffer, the second in the other 32
+        // two terms, two keys a column, over the half's own scores (the other half may still have to fetch its own, again
+        // if the reference moved): 16 columns the first, 16 the second
 #pragma unroll
         for (int q2 = 0; q2 < 2; ++q2) {
           uint32_t hi[8], lo[8];
@@ -652,8 +701,8 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
             const float2 r = __fadd2_rn(w, make_float2(-__uint_as_float(hi[y] << 16), -__uint_as_float(hi[y] & 0xffff0000u)));
             lo[y] = pack_bf16(r.x, r.y);
           }
-          tmem_st8u(t_s + half * 16 + q2 * 8, hi);
-          tmem_st8u(t_s + 32 + half * 16 + q2 * 8, lo);
+          tmem_st8u(t_s + half * 32 + q2 * 8, hi);
+          tmem_st8u(t_s + half * 32 + 16 + q2 * 8, lo);
         }
         l2a = __fadd2_rn(l2a, l2b);
         l += l2a.x + l2a.y;
@@ -670,9 +719,9 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       j0 += n;
       const bool whole = n == x.np, starts = p0 == 0, ends = p0 + n == x.np;
       if (warp == 0 && lane == 0 && (starts || ends)) {
-        int *e = reinterpret_cast<int *>(&a.ends[(size_t)tile * a.n_items + item]);
-        if (starts) e[0] = range;
-        if (ends) e[1] = range;
+        int *e = reinterpret_cast<int *>(&a.ends[(size_t)s_info[6] * a.n_items + item]);
+        if (starts) { e[0] = blockIdx.x; e[2] = s_info[7]; }
+        if (ends) e[1] = blockIdx.x;
       }
       if (live) {
         const int part = whole ? -1 : (int)blockIdx.x * 2 + (starts ? 1 : 0);
@@ -683,7 +732,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         if (whole) {
           // (the sums are exchanged through the first column of O, once that is in registers)
           const float sum = l + swap(t_o, t_lane + 128 + (half ^ 1) * 64, l), inv = 1.f / sum;
-          const size_t at = tree_out_row(a, item, row_live ? tile * kTreeRows + row : 0);
+          const size_t at = tree_out_row(a, item, row_live ? R : 0);
           uint4 *o = reinterpret_cast<uint4 *>(a.out + at * kD + half * 64);
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
@@ -728,7 +777,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         const int both = odd | failed << 1 | s_bad[3 * 8 + (warp ^ 4)];
         failed = both >> 1;
         if (both == 1)
-          tree_rows_again(a, x.seq | x.n << 25, x.t, x.len, tile, item, p0, n, quarter, half, part, s_path, s_depth);
+          tree_rows_again(a, x.seq | x.n << 25, x.t, x.len, s_info[6], item, p0, n, quarter, half, part, s_path, s_depth);
       }
       if (failed) return false;
       if (p0 + n > nk) {   // the segment's paths are done with
@@ -761,7 +810,7 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
   const int n_rows = tree_nodes(a, b, &bad) * c.G - tile * kTreeRows;
   pdl_trigger();
   pdl_wait();
-  const int2 ends = __ldcg(&a.ends[(size_t)tile * a.n_items + item]);
+  const int4 ends = __ldcg(&a.ends[(size_t)tile * a.n_items + item]);
   if (ends.x == ends.y || (int)blockIdx.y * 32 >= n_rows) return;   // whole: written already
   float M = -INFINITY, L = 0.f, O[kDims];
 #pragma unroll
@@ -773,12 +822,12 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
     const float f = fast_exp2(m - to);
     return f < 1e-37f ? 1e-37f : f;
   };
-  for (int r0 = ends.x + warp; r0 <= ends.y; r0 += kWarps * kAhead) {
+  for (int r0 = ends.x + warp * ends.z; r0 <= ends.y; r0 += kWarps * kAhead * ends.z) {
     float v[kAhead][kDims], m[kAhead], l[kAhead], to = M;
 #pragma unroll
     for (int y = 0; y < kAhead; ++y) {
-      const int r = min(r0 + y * kWarps, ends.y);
-      const size_t part = ((size_t)r * a.n_tiles + tile) * 2 + (r == ends.x ? 1 : 0);
+      const int r = min(r0 + y * kWarps * ends.z, ends.y);
+      const size_t part = (size_t)r * 2 + (r == ends.x ? 1 : 0);
       const float *ml = a.part_ml + part * 3 * a.rows_pad + row;
       const float4 *o = reinterpret_cast<const float4 *>(a.part_o) + (part * (kD / 4) + dim0 / 4) * a.rows_pad + row;
       m[y] = __ldcg(ml);
@@ -788,7 +837,7 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
         const float4 q = __ldcg(o + x / 4 * a.rows_pad);
         v[y][x] = q.x; v[y][x + 1] = q.y; v[y][x + 2] = q.z; v[y][x + 3] = q.w;
       }
-      if (r0 + y * kWarps > ends.y) { m[y] = -INFINITY; l[y] = 0.f; }
+      if (r0 + y * kWarps * ends.z > ends.y) { m[y] = -INFINITY; l[y] = 0.f; }
     }
 #pragma unroll
     for (int y = 0; y < kAhead; ++y) to = fmaxf(to, m[y]);
@@ -852,7 +901,7 @@ static TreeWs tree_ws_layout(const spkv_config_t *cfg, int B, int T, int blocks)
   const size_t items = (size_t)B * cfg->n_kv_heads;
   w.n_tiles = std::max(1, (T * G + kTreeRows - 1) / kTreeRows);
   w.rows_pad = std::min(kTreeRows, (T * G + 31) / 32 * 32);
-  w.off_units = a256(items * w.n_tiles * sizeof(int2));
+  w.off_units = a256(items * w.n_tiles * sizeof(int4));
   w.off_ml = w.off_units + a256((size_t)blocks * items * sizeof(int4));
   w.off_o = w.off_ml + a256((size_t)blocks * 6 * w.rows_pad * 4);
   w.total = w.off_o + a256((size_t)blocks * 2 * kD * w.rows_pad * 4);
@@ -904,14 +953,13 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   for (int l = 0; l < layer; ++l) a.row_base += (view.Hkv - __builtin_popcountll(cache->local_mask[l])) * view.S;
   a.row_heads = view.Hkv - __builtin_popcountll(cache->local_mask[layer]);
   a.local_mask = cache->local_mask[layer];
-  a.ends = reinterpret_cast<int2 *>(ws);
+  a.ends = reinterpret_cast<int4 *>(ws);
   a.units = reinterpret_cast<int4 *>(ws + w.off_units);
   a.part_ml = reinterpret_cast<float *>(ws + w.off_ml);
   a.part_o = reinterpret_cast<float *>(ws + w.off_o);
   a.rows_pad = w.rows_pad;
   a.n_tiles = w.n_tiles;
   const int blocks = tree::kBlocksPerSm * std::min(kMaxGrid, cache->sm_count);
-  a.n_ranges = std::max(1, blocks / a.n_tiles);
   a.min_cost = 5 + tree::kSegmentCost;   // (1 x 131072 tokens, 16 nodes: 27.7 us; 30.1 with 1, 31.4 with 11)
   if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(tree_attention_kernel), tree::kSmemBytes, &g_tree_ready)) return rc;
   // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
@@ -919,9 +967,9 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   const bool plain = (cache->cfg.flags & SPKV_FLAG_OVERLAP) != 0;
   cache->last_kind = kLastOther;
   cudaStream_t s = as_stream(stream);
-  if (launch_link(!plain, tree_attention_kernel, dim3(a.n_ranges * a.n_tiles), dim3(tree::kThreads), (size_t)tree::kSmemBytes, s, a) !=
+  if (launch_link(!plain, tree_attention_kernel, dim3(blocks), dim3(tree::kThreads), (size_t)tree::kSmemBytes, s, a) !=
       cudaSuccess)
     return SPKV_E_CUDA;
-  // pieces of a unit: about ranges / units + 1
-  return check_stream_error(a.n_ranges < 4 * a.n_items ? launch_tree_merge<2, 32, 1>(a, s) : launch_tree_merge<8, 16, 2>(a, s));
+  // pieces of a unit's tile: about blocks / tiles + 1
+  return check_stream_error(blocks < 4 * a.n_items * a.n_tiles ? launch_tree_merge<2, 32, 1>(a, s) : launch_tree_merge<8, 16, 2>(a, s));
 }

@@ -19,12 +19,12 @@ struct TreeArgs {
   float *lse;                   // [B][T][Hq] or null
   float scale_log2, tau_logit;
   // ---- the tensor-core form
-  int n_tiles, n_ranges, min_cost;             // row tiles of kTreeRows; ranges the line of pages is cut into, not shorter than min_cost
+  int n_tiles, min_cost;                       // row tiles of kTreeRows; shortest range that the line of pages is cut into
   unsigned long long g_inv;                    // ceil(2^32 / G): row / G as a product and a shift
   int row_base, row_heads;                     // page-table rows of the layer: row_base + seq * row_heads + rank of the KV head
   unsigned long long local_mask;
   int4 *units;                                 // [blocks][n_items]: a block's units behind the first few
-  int2 *ends;                                  // [n_tiles][n_items]: ranges of a unit's first and last page
+  int4 *ends;                                  // [n_tiles][n_items]: blocks of a unit's first and last page, step between its blocks
   float *part_o, *part_ml;                     // [blocks][2][32][rows_pad][4 dims], [blocks][2][3][rows_pad]: m, two shares of l
   int rows_pad;
 };
