@@ -479,6 +479,7 @@ extern "C" int spkv_token_logprobs(int32_t dtype, int32_t n_rows, int32_t vocab,
   const int64_t blocks = (int64_t)n_rows * w.max_parts;
   a.rounds = (int)std::max<int64_t>(1, std::min<int64_t>(lp::kMaxRounds, blocks / ((int64_t)sms * lp::kBlocksPerSm * 2)));
   a.parts = (w.max_parts + a.rounds - 1) / a.rounds;
+  a.rounds = (w.max_parts + a.parts - 1) / a.parts;   // (a row's blocks alike)
   if ((int64_t)n_rows * a.parts > INT32_MAX) return SPKV_E_UNSUPPORTED;
   note_cacheless_call();
   cudaStream_t s = as_stream(stream);
