@@ -12,8 +12,9 @@
 // Elements below kFloor count as kFloor: 0 times -infinity has no place in A.  Their weight is 0, unless the
 // whole row lies that low (masked by a low value throughout) or the scale is so small that kFloor is near: such a row, and one
 // whose scaled maximum is 2^24 or more, is summed up again, about its own maximum, by the second kernel.
-// What bounds it: memory (2 or 4 bytes an element); 4.5 instructions an element of bf16 or fp16 (maxima and
-// floor two elements an instruction in the type itself), of the 11 that the SMs could issue while rows arrive at the copy rate.
+// What bounds it: 768 rows of 128256 bf16 logits, top 1: 47 us on the device, 4.2 TB/s (30 us at the copy rate); 8 instructions an
+// element (maxima and floor take two elements an instruction in the type itself), 63 % of the issue slots.  5 rows of
+// 50257 fp32, top 5: 10 us, two launches with four trips to memory between them.
 #include <cuda_fp16.h>
 #include <math.h>
 

@@ -2,13 +2,14 @@
 //
 // A unit's (sequence, KV head) queries are the rows (node, head of the group) -> node * G + g, cut into tiles of 128 that
 // are the M side of tcgen05 MMAs.  Its keys are pages of 64: those of the compact cache, those of the ring, and one
-// page of the drafts themselves.  The pages of all units of the launch stand in one line per row tile that is cut into equal ranges, one per
-// block (two blocks an SM; where all tiles have the same lines, the blocks of a range are neighbours, so that the second finds its pages in
-// L2; where trees of different sizes leave a tile few rows, it gets few blocks).  Where a unit lies inside a range its rows are written at once; otherwise the pieces leave (m, l, O) per row and
-// tree_merge_kernel joins them by their log-sum-exp weights.
+// page of the drafts themselves.  The pages of all units of the launch stand in one line per row tile, cut into
+// equal ranges, one per block, two blocks an SM.  (Where all tiles have the same lines, the blocks of a range are
+// neighbours, so that the second finds its pages in L2; where trees of different sizes leave a tile few rows, it
+// gets few blocks: 13 sequences with up to 135 rows 47 -> 44.5 us.)  Where a unit lies inside a range its rows are written at
+// once; otherwise the pieces leave (m, l, O) per row and tree_merge_kernel joins them by their log-sum-exp weights.
 //
-// Per page: S = Q K^T (8 MMAs M128 N64 K16 into tensor memory), softmax in registers (thread = row = lane of
-// tensor memory), P as two bf16 terms back over the scores, O += P V.  Two score buffers: the scores of the next page are
+// Per page: S = Q K^T (8 MMAs M128 N64 K16 into tensor memory), softmax in registers (row = lane of tensor memory, two
+// threads a row), P as two bf16 terms back over the scores, O += P V.  Two score buffers: the scores of the next page are
 // made while this one's softmax runs.
 //   * Two bf16 terms (2^-16 of a weight) take the values as they lie in the cache: one fp16 term would halve P V's MMAs but
 //     wants the values converted to fp16 under a scale that fits all of them.
@@ -16,13 +17,20 @@
 //     whose pair is kept (a bit each, by ballot over the stored logits), of the drafts' page its path.  64 bits a row
 //     and page, applied to the scores.
 //   * A pair that is masked has P = 0, which an infinite or NaN value would turn into NaN (as would a weight's second
-//     term, which is often 0): whatever the rest of the row holds, the result is not finite then.  So the epilogue looks at the results, and
-//     rows of a segment with such a one are computed again key by key (tree_rows_again).  Finite caches pay one maximum
-//     per result.
+//     term, which is often 0): whatever the rest of the row holds, the result is not finite then.  So the epilogue looks at
+//     the results, and rows of a segment with such a one are computed again key by key (tree_rows_again).  Finite caches
+//     pay one multiply-add for two results.
 //
 // Warps: 0-7 softmax, 8 MMA issue and tensor memory, 9 page loader, 10 query rows, drafts and paths.
 // Shared memory (113 KB, two blocks an SM): Q 32 KB, ring of five 16 KB key or value blocks in the order in which the
-// MMAs want them.  Tensor memory (256 columns): score buffers at [0, 64) and [64, 128), O at [128, 256).  All waits are bounded.
+// MMAs want them.  Tensor memory (256 columns): score buffers at [0, 64) and [64, 128), O at [128, 256).  All waits on copies
+// and MMAs are bounded; the two threads of a row, which meet at a barrier without a limit, go through the same meetings
+// whether or not a wait has run out.
+//
+// What bounds it (B200): the first scores come after 5 - 8 us (lengths two trips to memory, page table one, page one); then
+// memory, with up to 128 rows a unit (16 sequences on 16384 and on 32768 tokens: 5.0 ns a page between the two, 6.5 TB/s; 32768: 76.7
+// us a call on the device, of which the joining kernel 6), or, with several tiles, instructions: 2650 a page and
+// tile, 45 % of the issue slots, tensor pipe 47 % (8 x 65536, 512 rows a unit, 227 us).
 #include <math.h>
 
 #include <algorithm>
@@ -47,6 +55,7 @@ constexpr int off_ring = 32768, off_bar = off_ring + kSlots * kBlockBytes, off_i
 static_assert(kSmemBytes <= off_bar + 1024 && off_units % 16 == 0 && off_path % 8 == 0, "two blocks an SM");
 constexpr int kPerThread = (1024 + kThreads - 1) / kThreads;   // items a thread looks at while the line is cut
 // What a segment costs beside its pages, in pages: its queries, its first scores, its results.
+// (13 ragged 53.6 us with 3, 51.2 with 5, 47.1 with 7, 46.6 with 10; 64 x 4096 63.0, 63.4, 62.8, 64.4.)
 constexpr int kSegmentCost = 7;
 
 // Where page i of a segment of n stands in the order in which a segment's blocks are loaded and used:
@@ -56,7 +65,7 @@ __device__ inline int value_at(int i, int n) { return i == n - 1 ? 2 * n - 1 : 2
 }  // namespace tree
 
 // mbar_wait_bounded for warps that wait long and often beside others that compute: the hardware may hold a try back for
-// up to 20 us before it is made again (three waiting warps a block issue a tenth of all instructions otherwise).
+// up to 20 us before it is made again (0 - 2 % against the default limit).
 __device__ inline bool tree_wait(uint64_t *bar, uint32_t parity) {
   auto attempt = [&]() {
     uint32_t ok;
@@ -180,7 +189,8 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
   extern __shared__ __align__(1024) unsigned char smem[];
   const CacheView &c = a.c;
   uint64_t *bar = reinterpret_cast<uint64_t *>(smem + off_bar);
-  volatile int *s_info = reinterpret_cast<volatile int *>(smem + off_info);     // tensor memory, first and last unit, drafts' blocks let in, range, tile
+  // tensor memory, first and last unit, drafts' blocks let in, range (two), tile, step between the tile's blocks
+  volatile int *s_info = reinterpret_cast<volatile int *>(smem + off_info);
   volatile uint64_t *s_path = reinterpret_cast<volatile uint64_t *>(smem + off_path);   // [node] nodes it sees
   volatile uint8_t *s_depth = smem + off_depth;
   volatile unsigned *s_grow = reinterpret_cast<volatile unsigned *>(smem + off_grow);   // [page & 1][warp] rows whose maximum moves
