@@ -314,7 +314,8 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
       }
       if (from < c1 && c1 <= to) {
         s_info[2] = tid * kPerThread + k;
-        s_info[5] = c1 - from <= snap ? from : to - c1 <= snap ? to : c1;
+        // (a cut on a border stays there: the block behind it sees it as the start of the next unit)
+        s_info[5] = c1 == to ? to : c1 - from <= snap ? from : to - c1 <= snap ? to : c1;
       }
     }
     __syncthreads();

@@ -402,6 +402,25 @@ def test_one_long_sequence_among_many_short_ones():
     c.check(out, lse, trees=[0, 1, 25, 49, 50, 51, 80, 110])
 
 
+def test_cuts_on_the_borders_of_short_units():
+    """A long and a short sequence in turn, as many pairs of them as half the blocks, so that every second cut falls on the end of
+    a short one: none is left out."""
+    c = Case(load(), (19000, 1), 2, 1, 2, (1.0,), seed=3, max_seqs=296, pool=310)
+    n = torch.cuda.get_device_properties(0).multi_processor_count
+    ids = torch.tensor([0, 1] * n, dtype=torch.int32, device=dev())
+    wide = lambda t: t.repeat(n, *[1] * (t.dim() - 1))
+    want, wl = c.run()
+    c.check(want, wl)
+    out, lse = torch.full((2 * n, 2, 2, D), 7.0, dtype=torch.bfloat16, device=dev()), torch.full((2 * n, 2, 2), 7.0, device=dev())
+    c.cache.spkv_decode_attention_tree(0, ids, wide(c.qd), wide(c.kd), wide(c.vd), wide(c.pd), wide(c.nd), wide(c.ld), out, lse)
+    c.cache.check()
+    # (the cuts differ from those of the two alone: rounding as in `bounds`)
+    for b in range(2):
+        tol, el = c.bounds(b, 0)
+        assert ((out[b::2].float() - want[b].float()).abs().cpu().double().numpy() <= 2 * tol).all()
+        assert ((lse[b::2] - wl[b]).abs().cpu().double().numpy() <= 2 * el).all()
+
+
 def test_debug_bounds_and_overlap_caches():
     spkv = load()
     for flags in (spkv.FLAG_DEBUG_BOUNDS, spkv.FLAG_OVERLAP, spkv.FLAG_FORK):
