@@ -823,6 +823,8 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
   pdl_wait();
   const int4 ends = __ldcg(&a.ends[(size_t)tile * a.n_items + item]);
   if (ends.x == ends.y || (int)blockIdx.y * 32 >= n_rows) return;   // whole: written already
+  // (after a wait that ran out the entry may be what the workspace held before)
+  if (ends.x < 0 || ends.y >= tree::kBlocksPerSm * kMaxGrid || ends.z < 1 || ends.z > a.n_tiles) return;
   float M = -INFINITY, L = 0.f, O[kDims];
 #pragma unroll
   for (int x = 0; x < kDims; ++x) O[x] = 0.f;
