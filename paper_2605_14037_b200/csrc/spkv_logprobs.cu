@@ -5,16 +5,16 @@
 // 16-byte boundary as well); a warp holds a chunk in registers and asks for its next one meanwhile.  With c = scale log2 e, M
 // a reference of the lane's own near its maximum (log2 domain) and t = c x - M
 //     S = sum 2^t,   A = sum 2^t t,      lse = ln 2 (M + log2 S),   entropy = ln 2 (log2 S - A / S),
-// and the chunk's maximum goes to memory, where a top list is wanted.  The n_top largest elements of a row lie in the n_top
+// of a warp's chunks of a row, and the chunk's maximum goes to memory, where a top list is wanted.  The n_top largest elements of a row lie in the n_top
 // chunks with the largest maxima (of equal ones those with the lower index), so a second, small kernel -- a
 // block per row, which also joins the row's sums -- looks into those chunks only, and the first pays nothing for the list.
 //
 // Elements below kFloor count as kFloor: 0 times -infinity has no place in A.  Their weight is 0, unless the
 // whole row lies that low (masked by a low value throughout) or the scale is so small that kFloor is near: such a row, and one
 // whose scaled maximum is 2^24 or more, is summed up again, about its own maximum, by the second kernel.
-// What bounds it: 768 rows of 128256 bf16 logits, top 1: 47 us on the device, 4.2 TB/s (30 us at the copy rate); 8 instructions an
-// element (maxima and floor take two elements an instruction in the type itself), 63 % of the issue slots.  5 rows of
-// 50257 fp32, top 5: 10 us, two launches with four trips to memory between them.
+// What bounds it: 768 rows of 128256 bf16 logits, top 1: 43 us on the device, 4.5 TB/s (30 us at the copy rate), 37 of them the first
+// kernel, at 8 instructions an element (maxima and floor take two elements an instruction in the type itself), 57 % of the
+// issue slots.  5 rows of 50257 fp32, top 5: 10 us, two launches with four trips to memory between them.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -29,20 +29,19 @@ namespace spkv {
 namespace lp {
 constexpr int kChunkBytes = 2048, kWarps = 8, kThreads = 32 * kWarps;
 template <class T> constexpr int kChunk = kChunkBytes / (int)sizeof(T);   // elements
-constexpr int kBlocksPerSm = 4;      // 64 registers a thread: a chunk and the next one (4 KB chunks spill: 67 against 47 us for 768 rows of 128256)
-constexpr int kMaxRounds = 16;       // chunks a warp takes at most
+constexpr int kBlocksPerSm = 4;      // 64 registers a thread: a chunk and the next one (4 KB chunks spill: 67 against 47 us at the time for 768 rows of 128256)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 }  // namespace lp
 
 struct LogprobArgs {
   const void *x;
   int64_t stride;
-  int n_rows, vocab, n_given, n_top, parts, rounds, max_chunks;
+  int n_rows, vocab, n_given, n_top, max_chunks, per, pitch;   // per: chunks a warp takes, of all rows' in one line; pitch: parts a row has at most
   float scale;
   const int32_t *given;
   float *lse, *entropy, *logp, *top_logp;
   int32_t *top_ids;
-  float4 *part;        // [n_rows][parts] {M, S, A, a NaN was among them}
+  float4 *part;        // [n_rows][pitch] {M, S, A, a NaN was among them}: what a warp holds of a row
   uint32_t *chunk_key; // [n_rows][max_chunks], n_top > 0 only
 };
 
@@ -241,53 +240,50 @@ template <class T>
 __global__ void __launch_bounds__(lp::kThreads, lp::kBlocksPerSm) logprob_sums_kernel(LogprobArgs a) {
   using namespace lp;
   pdl_trigger();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
-  const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.stride;
-  const int head = row_head(x, a.vocab), n_chunks = row_chunks<T>(head, a.vocab);
+  const int lane = threadIdx.x & 31;
+  const long long warp = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5), all = (long long)a.n_rows * a.max_chunks;
   const float c = a.scale * kLog2e;
-  Sums s;
-  bool nan = false;
-  // this warp's chunks: first, first + kWarps, ... < end; `full` of the row's chunks have all their elements
-  const int first = part * a.rounds * kWarps + warp, end = min(n_chunks, (part + 1) * a.rounds * kWarps), full = (a.vocab - head) / kChunk<T>;
-  auto key = [&](int ch, float top, bool odd) {
-    const uint32_t k = __reduce_max_sync(0xffffffffu, odd ? 0xffffffffu : value_key(top));
-    if (lane == 0) a.chunk_key[(size_t)row * a.max_chunks + ch] = k;
-  };
-  uint4 v[2][kWords];
-  int ch = first;
-  const int stop = min(end, full);
-  if (ch < stop) load_chunk(x + head + (int64_t)ch * kChunk<T>, v[0]);
-  auto round = [&](const uint4 (&now)[kWords], uint4 (&next)[kWords]) {   // ... and ask for the warp's next chunk first
-    if (ch + kWarps < stop) load_chunk(x + head + (int64_t)(ch + kWarps) * kChunk<T>, next);
-    float top;
-    bool odd = false;
-    add_chunk<T>(now, c, s, top, odd);
-    if (ch == 0 && lane < head) one<T>(x[lane], c, s, top, odd);   // the elements before the boundary belong to it
-    if (a.n_top > 0) key(ch, top, odd);
-    nan = nan || odd;
-    ch += kWarps;
-  };
-  while (ch < stop) {
-    round(v[0], v[1]);
-    if (ch < stop) round(v[1], v[0]);
-  }
-  if (ch < end) {   // the row's last chunk, in part
-    float top = -INFINITY;
-    bool odd = false;
-    for (int i = head + ch * kChunk<T> + lane; i < a.vocab; i += 32) one<T>(x[i], c, s, top, odd);
-    if (ch == 0 && lane < head) one<T>(x[lane], c, s, top, odd);
-    if (a.n_top > 0) key(ch, top, odd);
-    nan = nan || odd;
-  }
-  // ---- the block's sums: lanes, then warps, in a fixed order
-  __shared__ float4 s_part[kWarps];
-  const float4 w = join_lanes(make_float4(s.M, s.S, s.A, nan ? 1.f : 0.f));
-  if (lane == 0) s_part[warp] = w;
-  __syncthreads();
-  if (warp == 0) {
-    const float4 all = join_lanes(lane < kWarps ? s_part[lane] : no_part());
-    if (lane == 0) a.part[(size_t)row * a.parts + part] = all;
+  for (long long g = warp * a.per, to = min(g + a.per, all); g < to;) {
+    const int row = (int)(g / a.max_chunks), first = (int)(g - (long long)row * a.max_chunks);
+    const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.stride;
+    const int head = row_head(x, a.vocab);
+    // this warp's chunks of the row: first ... < end; `full` of the row's chunks have all their elements
+    const int last = (int)min((long long)a.max_chunks, first + (to - g)), end = min(last, row_chunks<T>(head, a.vocab));
+    const int stop = min(end, (a.vocab - head) / kChunk<T>);
+    g += last - first;
+    Sums s;
+    bool nan = false;
+    auto key = [&](int ch, float top, bool odd) {
+      const uint32_t k = __reduce_max_sync(0xffffffffu, odd ? 0xffffffffu : value_key(top));
+      if (lane == 0) a.chunk_key[(size_t)row * a.max_chunks + ch] = k;
+    };
+    uint4 v[2][kWords];
+    int ch = first;
+    if (ch < stop) load_chunk(x + head + (int64_t)ch * kChunk<T>, v[0]);
+    auto round = [&](const uint4 (&now)[kWords], uint4 (&next)[kWords]) {   // ... and ask for the next chunk first
+      if (ch + 1 < stop) load_chunk(x + head + (int64_t)(ch + 1) * kChunk<T>, next);
+      float top;
+      bool odd = false;
+      add_chunk<T>(now, c, s, top, odd);
+      if (ch == 0 && lane < head) one<T>(x[lane], c, s, top, odd);   // the elements before the boundary belong to it
+      if (a.n_top > 0) key(ch, top, odd);
+      nan = nan || odd;
+      ++ch;
+    };
+    while (ch < stop) {
+      round(v[0], v[1]);
+      if (ch < stop) round(v[1], v[0]);
+    }
+    if (ch < end) {   // the row's last chunk, in part
+      float top = -INFINITY;
+      bool odd = false;
+      for (int i = head + ch * kChunk<T> + lane; i < a.vocab; i += 32) one<T>(x[i], c, s, top, odd);
+      if (ch == 0 && lane < head) one<T>(x[lane], c, s, top, odd);
+      if (a.n_top > 0) key(ch, top, odd);
+      nan = nan || odd;
+    }
+    const float4 w = join_lanes(make_float4(s.M, s.S, s.A, nan ? 1.f : 0.f));
+    if (lane == 0) a.part[(size_t)row * a.pitch + (warp - (long long)row * a.max_chunks / a.per)] = w;
   }
 }
 
@@ -313,9 +309,10 @@ struct TopList {
   }
 };
 
+// (six blocks an SM, so that 768 rows run at once: 43.4 us together with the sums, 45.9 with five)
 // One block per row: its parts joined, and its largest logits out of the chunks with the largest maxima.
 template <class T>
-__global__ void __launch_bounds__(lp::kThreads) logprob_rows_kernel(LogprobArgs a) {
+__global__ void __launch_bounds__(lp::kThreads, 6) logprob_rows_kernel(LogprobArgs a) {
   using namespace lp;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x;
   const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.stride;
@@ -330,7 +327,15 @@ __global__ void __launch_bounds__(lp::kThreads) logprob_rows_kernel(LogprobArgs 
   pdl_wait();
   if (warp == 0) {
     float4 p = no_part();
-    for (int i = lane; i < a.parts; i += 32) p = join(p, a.part[(size_t)row * a.parts + i]);
+    const long long from = (long long)row * a.max_chunks;   // (the row's first and last warp: by their chunks)
+    const int parts = (int)((from + a.max_chunks - 1) / a.per - from / a.per) + 1;
+    for (int i0 = lane; i0 < parts; i0 += 128) {
+      float4 q[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) q[y] = i0 + 32 * y < parts ? __ldcg(&a.part[(size_t)row * a.pitch + i0 + 32 * y]) : no_part();
+#pragma unroll
+      for (int y = 0; y < 4; ++y) p = join(p, q[y]);
+    }
     p = join_lanes(p);
     if (lane == 0) {
       const float M = p.x, l2 = log2f(p.y);
@@ -343,9 +348,14 @@ __global__ void __launch_bounds__(lp::kThreads) logprob_rows_kernel(LogprobArgs 
     }
   } else if (warp == 1 && a.n_top > 0) {
     TopList list;
-    for (int i0 = 0; i0 < n_chunks; i0 += 32) {
-      const int i = i0 + lane;
-      list.offer(i < n_chunks ? (uint64_t)a.chunk_key[(size_t)row * a.max_chunks + i] << 32 | (0xffffffffu - (uint32_t)i) : 0, a.n_top);
+    const uint32_t *keys = a.chunk_key + (size_t)row * a.max_chunks;
+    for (int i0 = lane; i0 - lane < n_chunks; i0 += 128) {
+      uint32_t k[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) k[y] = i0 + 32 * y < n_chunks ? __ldcg(&keys[i0 + 32 * y]) : 0;
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        list.offer(i0 + 32 * y < n_chunks ? (uint64_t)k[y] << 32 | (0xffffffffu - (uint32_t)(i0 + 32 * y)) : 0, a.n_top);
     }
     if (lane < a.n_top) s_chunk[lane] = list.mine ? (int)(0xffffffffu - (uint32_t)list.mine) : -1;
     if (lane == a.n_top - 1) s_bound = (uint32_t)(list.mine >> 32);
@@ -425,18 +435,18 @@ __global__ void __launch_bounds__(lp::kThreads) logprob_rows_kernel(LogprobArgs 
   }
 }
 
-struct LogprobWs { size_t off_key, total; int max_chunks, max_parts; };
+struct LogprobWs { size_t off_key, total; int max_chunks; };
 static LogprobWs logprob_ws(int n_rows, int vocab, int n_top, int elem_bytes) {
   LogprobWs w;
   w.max_chunks = std::max(1, (int)(((int64_t)vocab * elem_bytes + lp::kChunkBytes - 1) / lp::kChunkBytes));
-  w.max_parts = (w.max_chunks + lp::kWarps - 1) / lp::kWarps;
-  w.off_key = (size_t)n_rows * w.max_parts * sizeof(float4);
+  w.off_key = (size_t)n_rows * w.max_chunks * sizeof(float4);   // (at most a part for every chunk)
   w.total = w.off_key + (n_top > 0 ? ((size_t)n_rows * w.max_chunks * 4 + 15) / 16 * 16 : 0);
   return w;
 }
 
 template <class T> static int launch_logprobs(LogprobArgs &a, cudaStream_t s) {
-  logprob_sums_kernel<T><<<(unsigned)((int64_t)a.n_rows * a.parts), lp::kThreads, 0, s>>>(a);
+  const int64_t warps = ((int64_t)a.n_rows * a.max_chunks + a.per - 1) / a.per;
+  logprob_sums_kernel<T><<<(unsigned)((warps + lp::kWarps - 1) / lp::kWarps), lp::kThreads, 0, s>>>(a);
   if (cudaGetLastError() != cudaSuccess) return SPKV_E_CUDA;
   return check_stream_error(launch_overlapped(logprob_rows_kernel<T>, dim3(a.n_rows), dim3(lp::kThreads), 0, s, a));
 }
@@ -476,12 +486,12 @@ extern "C" int spkv_token_logprobs(int32_t dtype, int32_t n_rows, int32_t vocab,
   a.part = static_cast<float4 *>(d_workspace);
   a.chunk_key = reinterpret_cast<uint32_t *>(static_cast<char *>(d_workspace) + w.off_key);
   a.max_chunks = w.max_chunks;
-  // chunks a warp takes: one while the blocks do not fill the SMs twice, then up to kMaxRounds
-  const int64_t blocks = (int64_t)n_rows * w.max_parts;
-  a.rounds = (int)std::max<int64_t>(1, std::min<int64_t>(lp::kMaxRounds, blocks / ((int64_t)sms * lp::kBlocksPerSm * 2)));
-  a.parts = (w.max_parts + a.rounds - 1) / a.rounds;
-  a.rounds = (w.max_parts + a.parts - 1) / a.parts;   // (a row's blocks alike)
-  if ((int64_t)n_rows * a.parts > INT32_MAX) return SPKV_E_UNSUPPORTED;
+  // All rows' chunks in one line, cut into as many equal pieces as the SMs hold warps (or one chunk each, if there are fewer): all
+  // blocks start and end together, also where the rows are no multiple of them.
+  const int64_t warps = (int64_t)sms * lp::kBlocksPerSm * lp::kWarps, per = ((int64_t)n_rows * w.max_chunks + warps - 1) / warps;
+  if (per > INT32_MAX) return SPKV_E_UNSUPPORTED;
+  a.per = (int)per;
+  a.pitch = std::min(w.max_chunks, (int)((w.max_chunks + per - 1) / per) + 1);
   note_cacheless_call();
   cudaStream_t s = as_stream(stream);
   return dtype == SPKV_BF16 ? launch_logprobs<__nv_bfloat16>(a, s) : dtype == SPKV_F16 ? launch_logprobs<__half>(a, s)
