@@ -131,6 +131,16 @@ def test_strides_past_32_bits_and_given_shapes():
     assert spkv.spkv_token_logprobs(one[:0], given[:0], top=2)[0].shape == (0,)
 
 
+@pytest.mark.parametrize("dtype,n,v,top,pad,off", [
+    ("f32", 20000, 1, 2, 0, 0), ("f16", 10007, 3, 4, 2, 1), ("f32", 3001, 2571, 3, 1, 1), ("bf16", 3001, 5121, 1, 0, 3), ("bf16", 6000, 1024, 0, 0, 0),
+])
+def test_pieces_that_begin_and_end_inside_rows(dtype, n, v, top, pad, off):
+    """more chunks than the GPU has warps: several rows, and parts of rows, in a warp"""
+    spkv = load()
+    x, given = rows(n, v, dtype, n + v, pad, off)
+    check(spkv, x, given, top, scale=1.3)
+
+
 def test_many_rows_and_repeats_give_the_same_bits():
     spkv = load()
     x, given = rows(3000, 6007, "bf16", 5)
