@@ -10,8 +10,10 @@
 // block per row, which also joins the row's sums -- looks into those chunks only, and the first pays nothing for the list.
 //
 // Elements below kFloor count as kFloor: 0 times -infinity has no place in A.  Their weight is 0, unless the
-// whole row lies that low (masked by a low value throughout) or the scale is so small that kFloor is near: such a row, and one
-// whose scaled maximum is 2^24 or more, is summed up again, about its own maximum, by the second kernel.
+// whole row lies that low (masked by a low value throughout) or the scale is so small that kFloor is near.  M is c x rounded, so
+// that t is off by up to 2^-24 |M|, a weight by 2 to that power: where the row's M is 2^24 or more in size it would count, from 2^31
+// on S itself leaves float32.  Such rows, and those whose sums are not finite for another reason (a product of c that has left
+// float32), are summed up again, about their own maximum, by the second kernel.
 // What bounds it: 768 rows of 128256 bf16 logits, top 1: 43 us on the device, 4.5 TB/s (30 us at the copy rate), 37 of them the first
 // kernel, at 8 instructions an element (maxima and floor take two elements an instruction in the type itself), 57 % of the
 // issue slots.  5 rows of 50257 fp32, top 5: 10 us, two launches with four trips to memory between them.
@@ -141,7 +143,7 @@ struct Sums {
       if (S > 0.f) {
         const float d = M - to, f = exp2f(d);
         A = f > 0.f ? f * fmaf(S, d, A) : 0.f;
-        S *= f;
+        S = f > 0.f ? S * f : 0.f;   // (S about a far lower M may be infinite: see the head)
       }
       M = to;
     }
@@ -221,7 +223,7 @@ __device__ inline float4 join(float4 p, float4 q) {
     if (s.y > 0.f && s.x < M) {
       const float d = s.x - M, f = exp2f(d);
       s.z = f > 0.f ? f * fmaf(s.y, d, s.z) : 0.f;
-      s.y *= f;
+      s.y = f > 0.f ? s.y * f : 0.f;
     }
   };
   weigh(p);
@@ -320,6 +322,11 @@ __global__ void __launch_bounds__(lp::kThreads, 6) logprob_rows_kernel(LogprobAr
   const float c = a.scale * kLog2e;
   __shared__ float s_base, s_log2;       // a logit's log probability is ln 2 ((c x - s_base) - s_log2), or, if the row was summed again,
   __shared__ int s_again;                // scale (x - s_base) - ln 2 s_log2
+  // scale (x - y), also where the difference alone leaves float32
+  auto scaled = [&](float x, float y) {
+    const float d = x - y;
+    return d == -INFINITY && x > -INFINITY ? (0.5f * x - 0.5f * y) * a.scale * 2.f : d * a.scale;
+  };
   __shared__ int s_chunk[SPKV_MAX_TOP];
   __shared__ uint32_t s_bound;           // value_key that every wanted element reaches
   __shared__ uint64_t s_list[kWarps][32];
@@ -340,7 +347,7 @@ __global__ void __launch_bounds__(lp::kThreads, 6) logprob_rows_kernel(LogprobAr
     if (lane == 0) {
       const float M = p.x, l2 = log2f(p.y);
       const bool nan = p.w != 0.f;
-      s_again = !nan && !(M > Low<T>::kFloor * c + 200.f && M < 0x1p+24f);
+      s_again = !nan && !(M > Low<T>::kFloor * c + 200.f && fabsf(M) < 0x1p+24f && isfinite(p.y) && isfinite(p.z));
       s_base = nan ? NAN : M;
       s_log2 = l2;
       if (a.lse) a.lse[row] = nan ? NAN : kLn2 * (M + l2);
@@ -372,7 +379,7 @@ __global__ void __launch_bounds__(lp::kThreads, 6) logprob_rows_kernel(LogprobAr
     float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
     if (m > -INFINITY && m < INFINITY)
       for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-        const float t = (as_float(x[i]) - m) * c, e = fast_exp2(t);
+        const float t = scaled(as_float(x[i]), m), e = fast_exp2(t * kLog2e);   // (c may have left float32)
         p.y += e;
         p.z = fmaf(e, fmaxf(t, -300.f), p.z);
       }
@@ -387,13 +394,13 @@ __global__ void __launch_bounds__(lp::kThreads, 6) logprob_rows_kernel(LogprobAr
       s_base = inf ? 0.f : m;
       s_log2 = inf ? INFINITY : l2;
       if (a.lse) a.lse[row] = inf ? INFINITY : fmaf(m, a.scale, kLn2 * l2);
-      if (a.entropy) a.entropy[row] = inf ? NAN : kLn2 * (l2 - p.z / p.y);
+      if (a.entropy) a.entropy[row] = inf ? NAN : kLn2 * l2 - p.z / p.y;
     }
     __syncthreads();
   }
   auto log_probability = [&](float f) {
     const float d = fmaf(f, c, -s_base);
-    if (s_again) return (f - s_base) * a.scale - kLn2 * s_log2;
+    if (s_again) return scaled(f, s_base) - kLn2 * s_log2;
     return d == -INFINITY ? f * a.scale : kLn2 * (d - s_log2);   // (c f may leave the type where scale f does not)
   };
   for (int j = threadIdx.x; j < a.n_given; j += kThreads) {

@@ -190,3 +190,43 @@ def test_acceptance_by_the_likeliest_token():
     tokens[1, 3] = 600
     path, n, nxt = spkv.spkv_tree_accept(tokens, target)
     assert n.tolist() == [6, 3] and nxt.tolist() == [int(target[0, 5]), int(target[1, 2])]
+
+
+# ---- low and high temperatures ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("scale", [1e6, 1e8, 3e8, 3e9, 1e12, 1e20, 1e32, 1e34, 2e38, 3.4e38, 1e-30, 1e-42])
+def test_rows_of_any_sign_at_any_scale(dtype, scale):
+    """Rows whose maximum is negative, zero or positive: a scale admits every positive float32 (as float32 holds it), and the products
+    of the scale and a logit may leave it."""
+    spkv = load()
+    x, given = rows(10, 5000, dtype, 11)
+    x[0] -= 30                                  # every logit negative
+    x[1] -= 30
+    x[1, ::3] = -math.inf
+    x[2] = -x[2].abs()
+    x[2, 7] = 0.0                               # a maximum of zero
+    x[3] = -x[3].abs()
+    x[3, [9, 4000]] = 0.0                       # ... twice, the lowest value beside it
+    x[3, 5:8] = torch.finfo(TYPES[dtype]).min
+    x[4] = -20.0                                # all alike
+    x[5, :3000] -= 6e4 if dtype == "f16" else 1e6   # pieces of the row far below the others
+    x[6] -= 500
+    x[7] = -torch.rand(5000, device=dev()) / 64 - 1 / 64
+    x[8, 1:] = -math.inf                        # one token left, a negative one
+    x[8, 0] = -3.0
+    for top in (0, 3):
+        check(spkv, x, given, top, scale=float(np.float32(scale)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_differences_beyond_float32(dtype):
+    """logits of +-3e38: their difference leaves float32, its product with a small scale does not"""
+    spkv = load()
+    x, given = rows(4, 3000, dtype, 12)
+    x[0] = torch.where(x[0] > 0, 3e38, -3e38)
+    x[1] = x[1].clamp(-1, 1) * 3e38
+    x[2, ::2] = -3e38
+    x[3] = -3e38
+    x[3, 100] = 1e38
+    for scale in (1e-38, 3e-39, 1e-37):
+        check(spkv, x, given, 4, scale=float(np.float32(scale)))
