@@ -230,3 +230,20 @@ def test_differences_beyond_float32(dtype):
     x[3, 100] = 1e38
     for scale in (1e-38, 3e-39, 1e-37):
         check(spkv, x, given, 4, scale=float(np.float32(scale)))
+
+
+# ---- a fixed order -----------------------------------------------------------------------------------------
+def bits(t):
+    return t.view(torch.int32) if t.dtype == torch.float32 else t
+
+
+@pytest.mark.parametrize("dtype,n,v,top", [("bf16", 3000, 6007, 3), ("f32", 700, 20011, 32), ("f16", 5, 128256, 1), ("f32", 20000, 100, 2)])
+def test_repeats_give_the_same_bits_whatever_the_workspace_holds(dtype, n, v, top):
+    spkv = load()
+    x, given = rows(n, v, dtype, 6)
+    first = spkv.spkv_token_logprobs(x, given, top=top)
+    for byte in (0, 255, 0x7f):
+        for ws in spkv._logprob_ws.values():
+            ws.fill_(byte)
+        again = spkv.spkv_token_logprobs(x, given, top=top)
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(first, again))
