@@ -126,6 +126,9 @@ __device__ inline uint32_t tree_sees(const TreeArgs &a, const TreeUnit &x, int i
   return (uint32_t)(bits_below(min(x.t, c.w) - rp * kP) >> (32 * h)) &
          (~(uint32_t)(ring_out_of_window(x.t, s_depth[node], c.w, rp) >> (32 * h)) | kept);
 }
+// The weight f > 0 of x, which may have vanished: a finite x vanishes with it, an infinite one is infinite all the same.  (A NaN
+// weight makes the row's sum, and with it the row, NaN.)
+__device__ inline float weight_for(float x, float f) { return fabsf(x) == INFINITY ? 1.f : f; }
 // One warp's share (every second row of a quarter of the tile) of a segment whose results are not all finite, once more, key by
 // key: a pair that a row does not see is not touched, and an infinite value that it sees counts with its weight, however
 // small.  (P V multiplies what is masked by 0, and a weight's second term is often 0 too.)  Rare.
@@ -162,11 +165,12 @@ __device__ __noinline__ void tree_rows_again(const TreeArgs &a, int seq_nodes, i
         for (int z = 0; z < 4; ++z) s = fmaf(q[z], __bfloat162float(kr[z]), s);
         s = warp_sum(s) * a.scale_log2;
         const float top = s > m ? s : m;
-        float f = m == -INFINITY ? 0.f : fast_exp2(m - top), w = fast_exp2(s - (top == -INFINITY ? 0.f : top));
-        if (m != -INFINITY && f < 1e-37f) f = 1e-37f;
-        if (s != -INFINITY && w < 1e-37f) w = 1e-37f;
+        const float f = m == -INFINITY ? 1.f : fast_exp2(m - top), w = fast_exp2(s - (top == -INFINITY ? 0.f : top));
         l = l * f + w;
-        for (int z = 0; z < 4; ++z) o[z] = (f == 0.f ? 0.f : o[z] * f) + w * __bfloat162float(vr[z]);
+        for (int z = 0; z < 4; ++z) {   // (a score of -infinity: a weight that is 0)
+          const float val = __bfloat162float(vr[z]);
+          o[z] = fmaf(val, s == -INFINITY ? w : weight_for(val, w), o[z] * weight_for(o[z], f));
+        }
         m = top;
       }
     }
@@ -828,13 +832,10 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
   float M = -INFINITY, L = 0.f, O[kDims];
 #pragma unroll
   for (int x = 0; x < kDims; ++x) O[x] = 0.f;
-  // A part's weight against the common maximum.  A part without a visible pair has l = 0; m = -inf with another l means
-  // NaN scores.  A weight too small for its type still leaves an infinity of the part infinite.
-  auto weight = [](float m, float l, float to) {
-    if (m == -INFINITY) return l == 0.f ? 0.f : NAN;
-    const float f = fast_exp2(m - to);
-    return f < 1e-37f ? 1e-37f : f;
-  };
+  // A part's weight against the common maximum.  A part without a visible pair (`none`) has l = 0; m = -inf with another l
+  // means NaN scores.
+  auto none = [](float m, float l) { return m == -INFINITY && l == 0.f; };
+  auto weight = [&](float m, float l, float to) { return none(m, l) ? 0.f : m == -INFINITY ? NAN : fast_exp2(m - to); };
   for (int r0 = ends.x + warp * ends.z; r0 <= ends.y; r0 += kWarps * kAhead * ends.z) {
     float v[kAhead][kDims], m[kAhead], l[kAhead], to = M;
 #pragma unroll
@@ -858,14 +859,14 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
     M = to;
     L *= old;
 #pragma unroll
-    for (int x = 0; x < kDims; ++x) O[x] = old == 0.f ? 0.f : O[x] * old;
+    for (int x = 0; x < kDims; ++x) O[x] *= weight_for(O[x], old);
 #pragma unroll
     for (int y = 0; y < kAhead; ++y) {
+      if (none(m[y], l[y])) continue;
       const float f = weight(m[y], l[y], M);
-      if (f == 0.f) continue;
       L = fmaf(l[y], f, L);
 #pragma unroll
-      for (int x = 0; x < kDims; ++x) O[x] = fmaf(v[y][x], f, O[x]);
+      for (int x = 0; x < kDims; ++x) O[x] = fmaf(v[y][x], weight_for(v[y][x], f), O[x]);
     }
   }
 #pragma unroll
@@ -881,11 +882,14 @@ __global__ void __launch_bounds__(32 * kWarps) tree_merge_kernel(const __grid_co
     for (int w = 0; w < kWarps; ++w) Mr = fmaxf(Mr, s_m[w][r]);
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
+      if (none(s_m[w][r], s_l[w][r])) continue;
       const float f = weight(s_m[w][r], s_l[w][r], Mr);
-      if (f == 0.f) continue;
       Lr = fmaf(s_l[w][r], f, Lr);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) o[x] = fmaf(s_o[w][q * 8 + x][r], f, o[x]);
+      for (int x = 0; x < 8; ++x) {
+        const float v = s_o[w][q * 8 + x][r];
+        o[x] = fmaf(v, weight_for(v, f), o[x]);
+      }
     }
     const int R = tile * kTreeRows + at_row, node = (int)(((unsigned long long)R * a.g_inv) >> 32);
     const size_t at = ((size_t)b * a.T + node) * c.Hq + kvh * c.G + R - node * c.G;

@@ -857,3 +857,75 @@ def test_planted_page_indices_under_range_checks():
     words[at + 2] = used[2]
     c.cache.spkv_append_path(0, c.ids, c.kd, c.vd, torch.full_like(c.ld, 9.0))
     assert c.cache.spkv_status() == (-13 if ln % 64 else 0)
+
+
+# ---- weights that vanish -------------------------------------------------------------------------------------
+def vanishing(spkv, T, low, plant, keys=9000, seed=1):
+    """One sequence whose first `low` pairs score hundreds below the others (weights of e^-400 and less).  plant(V of those) -> None"""
+    c = Case(spkv, (keys,), 8, 1, T, (1.0,), seed=seed, parent="chain")
+    c.cache.spkv_cache_reset_seq(0)
+    rng = np.random.default_rng(seed)
+    e = np.where(rng.random(D) < 0.5, -1.0, 1.0).astype(np.float32)
+    c.q[:] = synth.to_bf16_bits(8 * e)                                        # every query: scores 8 <e, k> / sqrt(128)
+    K, V = synth.normal_bf16(rng, (keys, 1, D)), synth.normal_bf16(rng, (keys, 1, D))
+    K[:low, 0] = synth.to_bf16_bits(-5 * e)                                   # -452
+    plant(V[:low, 0])
+    for a in range(0, keys, 3000):
+        c.cache.spkv_prefill(0, 0, to_dev_bf16(K[a:a + 3000]), to_dev_bf16(V[a:a + 3000]), torch.full((len(K[a:a + 3000]), 1), 9.0, device=dev()))
+    c.to_device()
+    return c, e
+
+
+BIG = int(synth.to_bf16_bits(np.array([3e38], np.float32))[0])
+
+
+def check_rows(c, out):
+    """infinite where the formula is; else within `bounds` (|q| |k| scale <= 8 sqrt(128) 5 sqrt(128) / sqrt(128))"""
+    with np.errstate(invalid="ignore", over="ignore"):
+        ref, wv, _, _, keys = c.reference(0, 0)
+    mine = out[0].float().cpu().double().numpy()
+    ok = np.isfinite(ref)
+    assert np.array_equal(ref[~ok], mine[~ok])
+    es = 130 * 2.0 ** -24 * 40 * math.sqrt(D)
+    tol = 2.0 ** -8 * np.abs(ref[ok]) + (2.0 ** -16 + 2.0 ** -21 + 2 * es + (keys / 8 + 64) * 2.0 ** -23) * np.where(np.isfinite(wv[ok]), wv[ok], 0) + 1e-30
+    assert (np.abs(mine[ok] - ref[ok]) <= tol).all(), (np.abs(mine[ok] - ref[ok]) - tol).max()
+    return ok
+
+
+@pytest.mark.parametrize("low", [64, 1000, 6000])
+def test_finite_values_of_vanishing_weight_add_nothing(low):
+    """... however large, in a range of their own or beside others; an infinite one comes through"""
+    spkv = load()
+
+    def large(v):
+        v[5, 9], v[low // 2, 70] = BIG, BIG
+
+    c, _ = vanishing(spkv, 4, low, large)
+    out, lse = c.run()
+    c.cache.check()
+    assert check_rows(c, out).all()
+
+    def infinite(v):
+        large(v)
+        v[7, 3], v[low - 1, 4], v[7, 90], v[8, 90] = 0x7f80, 0xff80, 0x7f80, 0x7f80
+
+    c, _ = vanishing(spkv, 4, low, infinite)
+    out, lse = c.run()
+    c.cache.check()
+    ok = check_rows(c, out)
+    assert not ok[..., [3, 4, 90]].any() and ok.sum() == ok.size - 3 * ok.shape[0] * ok.shape[1]
+
+
+@pytest.mark.parametrize("keys", [1, 100, 9000])
+def test_finite_values_of_vanishing_weight_beside_an_infinite_one(keys):
+    """the same among the drafts, whose page is then gone through key by key"""
+    spkv = load()
+    c, e = vanishing(spkv, 6, 0, lambda v: None, keys=keys)
+    c.k[0, 1, 0] = synth.to_bf16_bits(-5 * e)
+    c.v[0, 0, 0, 3], c.v[0, 1, 0, 9], c.v[0, 1, 0, 70], c.v[0, 1, 0, 4] = 0x7f80, BIG, BIG | 0x8000, 0xff80
+    c.k[0, 0, 0] = synth.to_bf16_bits(e)                                      # (90: the largest weight of all)
+    c.to_device()
+    out, lse = c.run()
+    c.cache.check()
+    ok = check_rows(c, out)
+    assert not ok[..., 3].any() and not ok[1:, :, 4].any() and ok[..., [9, 70]].all()
