@@ -20,6 +20,9 @@
 //     term, which is often 0): whatever the rest of the row holds, the result is not finite then.  So the epilogue looks at
 //     the results, and rows of a segment with such a one are computed again key by key (tree_rows_again).  Finite caches
 //     pay one multiply-add for two results.
+//   * The reference maximum is a scaled score rounded, the exponents are taken from the unrounded products: at scores of 2^31
+//     the difference alone empties a row's weights or overflows them.  Rows whose reference is 2^24 or more in size (off by 1)
+//     are computed again likewise, from scaled scores that are rounded alike.
 //
 // Warps: 0-7 softmax, 8 MMA issue and tensor memory, 9 page loader, 10 query rows, drafts and paths.
 // Shared memory (113 KB, two blocks an SM): Q 32 KB, ring of five 16 KB key or value blocks in the order in which the
@@ -129,8 +132,8 @@ __device__ inline uint32_t tree_sees(const TreeArgs &a, const TreeUnit &x, int i
 // The weight f > 0 of x, which may have vanished: a finite x vanishes with it, an infinite one is infinite all the same.  (A NaN
 // weight makes the row's sum, and with it the row, NaN.)
 __device__ inline float weight_for(float x, float f) { return fabsf(x) == INFINITY ? 1.f : f; }
-// One warp's share (every second row of a quarter of the tile) of a segment whose results are not all finite, once more, key by
-// key: a pair that a row does not see is not touched, and an infinite value that it sees counts with its weight, however
+// One warp's share (every second row of a quarter of the tile) of a segment whose results are not all finite, or whose scores
+// are too large for the tile's arithmetic, once more, key by key: a pair that a row does not see is not touched, and an infinite value that it sees counts with its weight, however
 // small.  (P V multiplies what is masked by 0, and a weight's second term is often 0 too.)  Rare.
 __device__ __noinline__ void tree_rows_again(const TreeArgs &a, int seq_nodes, int t, int len, int tile, int item, int p0, int n, int quarter,
                                              int half, int part, const volatile uint64_t *s_path, const volatile uint8_t *s_depth) {
@@ -786,7 +789,7 @@ __global__ void __launch_bounds__(tree::kThreads, tree::kBlocksPerSm) tree_atten
         }
         float f0, f1;
         unpack2(finite, f0, f1);
-        const bool odd = __any_sync(0xffffffffu, row_live && f0 + f1 != 0.f);
+        const bool odd = __any_sync(0xffffffffu, row_live && (f0 + f1 + 0.f * l != 0.f || (fabsf(m_ref) >= 0x1p24f && m_ref != -INFINITY)));
         if (lane == 0) s_bad[3 * 8 + warp] = odd | failed << 1;
         meet();
         const int both = odd | failed << 1 | s_bad[3 * 8 + (warp ^ 4)];

@@ -929,3 +929,34 @@ def test_finite_values_of_vanishing_weight_beside_an_infinite_one(keys):
     c.cache.check()
     ok = check_rows(c, out)
     assert not ok[..., 3].any() and not ok[1:, :, 4].any() and ok[..., [9, 70]].all()
+
+
+# ---- scores beyond a float32's whole numbers -------------------------------------------------------------------
+@pytest.mark.parametrize("scale", [1e5, 3e7, 1e9, 3e10, 1e20, 1e30])
+@pytest.mark.parametrize("sign", [1, -1, 0])
+def test_scores_of_any_size(scale, sign):
+    """Queries and keys of small whole numbers, whose products and sums are exact: a row's weights then are those of the pairs with its
+    largest score, and their alike ones, whatever the scale.  sign: of all scores (0: both)"""
+    spkv = load()
+    rng = np.random.default_rng(int(math.log10(scale)) + sign)
+    lens = (9000, 300, 2)
+    c = Case(spkv, lens, 8, 2, 9, (1.0, 1.0), seed=3, parent="forest")
+    whole = lambda *shape: synth.to_bf16_bits((rng.integers(-2, 3, shape) if sign == 0 else sign * rng.integers(1, 4, shape)).astype(np.float32))
+    for b, t in enumerate(lens):
+        c.cache.spkv_cache_reset_seq(b)
+        for a in range(0, t, 4000):
+            m = min(4000, t - a)
+            c.cache.spkv_prefill(0, b, to_dev_bf16(whole(m, 2, D)), to_dev_bf16(synth.normal_bf16(rng, (m, 2, D))),
+                                 torch.from_numpy(rng.normal(size=(m, 2)).astype(np.float32)).to(dev()))
+    c.k = whole(*c.k.shape)
+    c.q = synth.to_bf16_bits(rng.integers(1, 3, c.q.shape).astype(np.float32))
+    c.to_device()
+    scale = float(np.float32(scale))
+    out, lse = c.run(sm_scale=scale)
+    c.cache.check()
+    for b in range(3):
+        for h in range(2):
+            ref, wv, rl, _, keys = c.reference(b, h, scale=scale)
+            err = np.abs(out[b, :, 4 * h:4 * h + 4].float().cpu().double().numpy() - ref)
+            assert (err <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -16 + 2.0 ** -21 + (keys / 8 + 64) * 2.0 ** -23) * wv).all(), (b, h, err.max())
+            assert (np.abs(lse[b, :, 4 * h:4 * h + 4].cpu().double().numpy() - rl) <= (keys / 8 + 64) * 2.0 ** -23 + 2.0 ** -20 * (1 + np.abs(rl))).all()
