@@ -859,6 +859,103 @@ def test_planted_page_indices_under_range_checks():
     assert c.cache.spkv_status() == (-13 if ln % 64 else 0)
 
 
+# ---- trees of different sizes in several row tiles ---------------------------------------------------------
+def ragged(B, top, seed):
+    return [int(x) for x in np.random.default_rng(seed).integers(0, top, B)]
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,T,n", [
+    (ragged(13, 4000, 1), 20, 4, 27, [27, 26, 25, 1, 13, 0, 27, 3, 26, 9, 20, 27, 2]),           # a second tile of up to seven rows
+    ([3000, 200, 9000, 0, 130, 700], 16, 1, 64, [0, 1, 8, 9, 33, 64]),                            # eight tiles, each shorter than the one before
+    ([9000, 0, 65, 300, 2000], 16, 1, 64, [64, 8, 1, 7, 3]),                                      # one long tree: upper tiles of one unit
+    ([3000, 200, 64, 0], 32, 2, 64, [8, 8, 3, 1]),                                                # upper tiles without a row
+    ([20000, 20, 500], 32, 2, 64, [5, 64, 0]),                                                    # ... and those of a short sequence
+    (ragged(60, 700, 2), 24, 3, 33, [int(x) for x in np.random.default_rng(3).integers(0, 34, 60)]),
+    ([500, 30], 32, 2, 64, [0, 0]),
+])
+def test_trees_of_different_sizes_in_several_tiles(lens, Hq, Hkv, T, n):
+    """T G > 128, and the tiles' lines of pages differ: blocks go to the tiles by their length.  Rows of absent nodes stay as they are."""
+    rates = tuple(0.2 + 0.6 * (i % 2) for i in range(Hkv))
+    c = Case(load(), lens, Hq, Hkv, T, rates, seed=len(lens) + T, n=n, parent="forest")
+    out, lse = torch.full((c.B, T, Hq, D), 7.0, dtype=torch.bfloat16, device=dev()), torch.full((c.B, T, Hq), 7.0, device=dev())
+    for byte in (None, 255):
+        for ws in c.cache._tree_ws.values() if byte else ():
+            ws.fill_(byte)       # (whatever the workspace holds)
+        out.fill_(7), lse.fill_(7)
+        c.run(out=out, lse=lse)
+        c.cache.check()
+        c.check(out, lse)
+        for b in range(c.B):
+            assert (out[b, n[b]:] == 7).all() and (lse[b, n[b]:] == 7).all(), b
+
+
+# ---- infinities and NaN where the window's mask falls --------------------------------------------------------
+def check_with_nonfinite(c, out, lse):
+    """As Case.check, with `reference` infinite or NaN where a node sees such a value.  (|q| |k| scale < 30 for these normal rows.)"""
+    G = c.Hq // c.Hkv
+    got, l = out.float().cpu().double().numpy(), lse.cpu().double().numpy()
+    seen = unseen = 0
+    for b in range(c.B):
+        for h in range(c.Hkv):
+            with np.errstate(invalid="ignore"):
+                ref, wv, rl, _, keys = c.reference(b, h)
+            mine, ml = got[b, :int(c.n[b]), h * G:(h + 1) * G], l[b, :int(c.n[b]), h * G:(h + 1) * G]
+            assert np.array_equal(np.isnan(ref), np.isnan(mine)), (b, h)
+            assert np.array_equal(ref == np.inf, mine == np.inf) and np.array_equal(ref == -np.inf, mine == -np.inf), (b, h)
+            ok, lok = np.isfinite(ref), np.isfinite(rl)
+            tol = 2.0 ** -8 * np.abs(ref[ok]) + (2.0 ** -16 + 2.0 ** -21 + 2 * 2.4e-4 + (keys / 8 + 64) * 2.0 ** -23) * wv[ok] + 1e-30
+            assert (np.abs(ref[ok] - mine[ok]) <= tol).all(), (b, h, np.abs(ref[ok] - mine[ok]).max())
+            assert np.array_equal(np.isnan(rl), np.isnan(ml))
+            assert (np.abs(rl[lok] - ml[lok]) <= 2.4e-4 + (keys / 8 + 64) * 2.0 ** -23 + 2.0 ** -20 * (1 + np.abs(rl[lok]))).all(), (b, h)
+            seen, unseen = seen + (~ok).sum(), unseen + ok.sum()
+    return seen, unseen
+
+
+@pytest.mark.parametrize("what", ["v=inf", "v=nan", "k=inf", "k=nan"])
+@pytest.mark.parametrize("w,t,clean", [(8, 40, 3), (8, 41, 5), (8, 0, 3), (70, 200, 66), (70, 0, 60), (130, 64, 122), (130, 300, 126)])
+def test_pairs_that_leave_the_window_of_deep_nodes(w, t, clean, what):
+    """Two pairs with a value or key that is not finite, not to be kept, and then `clean` others in the ring, before and after it has
+    gone round: shallow nodes see them, deep ones do not."""
+    spkv = load()
+    c = Case(spkv, (t, t + 5, max(0, t - 1)), 6, 2, 12, (0.4, 0.4), w=w, parent="chain", seed=w + t + clean, draft_rate=0.3, pool=60)
+    rng = np.random.default_rng(clean)
+    bad = 0x7f80 if what.endswith("inf") else 0x7fc0
+    for x in range(2 + clean):
+        k, v = (synth.normal_bf16(rng, (3, 2, D)) for _ in "kv")
+        if x < 2:
+            (v if what[0] == "v" else k)[:, 0, 7 + x] = bad
+        lg = torch.full((3, 2), -9.0 if x < 2 else float(9 * (x % 3 - 1)), device=dev())
+        c.cache.spkv_append_evict(0, c.ids, to_dev_bf16(k), to_dev_bf16(v), lg)
+    out, lse = c.run()
+    c.cache.check()
+    seen, unseen = check_with_nonfinite(c, out, lse)
+    assert seen and unseen, "both kinds of nodes"
+    assert torch.isfinite(out[:, :, 3:].float()).all(), "the other KV head"
+
+
+@pytest.mark.parametrize("t", [0, 1, 63, 90, 127, 200, 333])
+def test_what_an_earlier_sequence_left_behind(t):
+    """NaN in ring slots that have not been written since the sequence was reset, and behind the last kept pair of a page"""
+    spkv = load()
+    c = Case(spkv, (500, 500), 6, 2, 5, (1.0, 1.0), seed=t + 1, parent="forest")
+    rng = np.random.default_rng(t)
+    nan = torch.full((500, 2, D), math.nan, dtype=torch.bfloat16, device=dev())
+    for seq in range(2):
+        c.cache.spkv_cache_reset_seq(seq)
+        c.cache.spkv_prefill(0, seq, nan, nan, torch.full((500, 2), 9.0, device=dev()))
+        c.cache.spkv_cache_reset_seq(seq)
+    for seq in range(2):
+        for a in range(0, t, 50):
+            m = min(50, t - a)
+            k, v = (to_dev_bf16(synth.normal_bf16(rng, (m, 2, D))) for _ in "kv")
+            c.cache.spkv_prefill(0, seq, k, v, torch.from_numpy(rng.normal(size=(m, 2)).astype(np.float32)).to(dev()))
+    out, lse = c.run()
+    c.cache.check()
+    seen, _ = check_with_nonfinite(c, out, lse)
+    assert seen == 0
+    c.check(out, lse)
+
+
 # ---- weights that vanish -------------------------------------------------------------------------------------
 def vanishing(spkv, T, low, plant, keys=9000, seed=1):
     """One sequence whose first `low` pairs score hundreds below the others (weights of e^-400 and less).  plant(V of those) -> None"""
