@@ -950,7 +950,7 @@ def spkv_token_logprobs(logits, given=None, top=0, scale=1.0, lse=None, logp=Non
         logp, at_logp = _result(logits, logp, f32, (n, m), dev)
     if want_entropy or entropy is not None:
         entropy, at_entropy = _result(logits, entropy, f32, (n,), dev)
-    if top > 0:
+    if top > 0 or top_ids is not None or top_logp is not None:
         top_ids, at_ids = _result(logits, top_ids, i32, (n, top), dev)
         top_logp, at_top = _result(logits, top_logp, f32, (n, top), dev)
     ws_bytes = _logprob_bytes.get((n, vocab, top))

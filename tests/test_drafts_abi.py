@@ -113,3 +113,14 @@ def test_tensors_or_streams_of_another_device_are_refused(spkv, two_devices):
         with pytest.raises(ValueError):
             call()
     assert not two_devices
+
+
+def test_top_lists_given_but_not_asked_for_are_refused(spkv, two_devices, monkeypatch):
+    """(they would come back as they were)"""
+    import torch
+    monkeypatch.setattr(spkv, "_logprob_bytes", {(2, 50, 0): 16})
+    x, f = drafts(0)["x"], drafts(0)["f"]
+    for kw in (dict(top_ids=Rows((2, 5), torch.int32, 0, 4096)), dict(top_logp=Rows((2, 5), torch.float32, 0, 4096))):
+        with pytest.raises(ValueError):
+            spkv.spkv_token_logprobs(x, lse=f, want_entropy=False, **{"top_ids": Rows((2, 0), torch.int32, 0, 4096), **kw})
+    assert not two_devices
