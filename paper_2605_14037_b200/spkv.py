@@ -955,6 +955,8 @@ def spkv_token_logprobs(logits, given=None, top=0, scale=1.0, lse=None, logp=Non
         top_logp, at_top = _result(logits, top_logp, f32, (n, top), dev)
     ws_bytes = _logprob_bytes.get((n, vocab, top))
     if ws_bytes is None:
+        if len(_logprob_bytes) >= 1024:      # (row counts vary from call to call)
+            _logprob_bytes.clear()
         ws_bytes = _logprob_bytes[n, vocab, top] = max(16, lib().spkv_logprobs_workspace_bytes(n, vocab, top))
     ws = _scratch(_logprob_ws, ws_bytes, dev)
     rc = _on_device(dev, lib().spkv_token_logprobs, _DTYPE[logits.dtype], n, vocab, logits.data_ptr(),

@@ -124,3 +124,13 @@ def test_top_lists_given_but_not_asked_for_are_refused(spkv, two_devices, monkey
         with pytest.raises(ValueError):
             spkv.spkv_token_logprobs(x, lse=f, want_entropy=False, **{"top_ids": Rows((2, 0), torch.int32, 0, 4096), **kw})
     assert not two_devices
+
+
+def test_the_workspace_sizes_remembered_are_limited(spkv, two_devices, monkeypatch):
+    import torch
+    sizes = {}
+    monkeypatch.setattr(spkv, "_logprob_bytes", sizes)
+    monkeypatch.setattr(spkv, "_scratch", lambda store, n, d: Rows((n,), None, d, 4096))
+    for n in range(1, 3000):
+        spkv.spkv_token_logprobs(Rows((n, 50), torch.float32, 0, 4096), lse=Rows((n,), torch.float32, 0, 4096), want_entropy=False)
+    assert 0 < len(sizes) <= 1024
