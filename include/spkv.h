@@ -474,7 +474,8 @@ int spkv_decode_attention_shared(spkv_cache_t *cache, int32_t layer, const int32
  * node i at position p sees the compact cache; of the window and of its path the pairs at positions > p - w; and of
  * those further back the ones whose logit passes the threshold in force, sink positions always, none with a head
  * declared local-only.  Pairs that a node does not see do not touch its result, infinities and NaN included; an infinite or
- * NaN value that it sees goes into it with its weight.  Scores are float32, weights two bf16 terms (2^-16).
+ * NaN value that it sees goes into it with its weight, an infinite one even where that has vanished.  Scores are float32, weights
+ * two bf16 terms (2^-16), added up in float32 before they are divided by their sum (values near float32's end may leave it).
  * The cache is only read.
  *   q: token (b, i) = b T + i, n_q_heads heads; k, v: the nodes' own pairs, n_kv_heads heads; bf16 rows as in
  *   spkv_norm_rope (16-byte aligned, strides multiples of 8 elements), so heads of a fused projection are read in place.
@@ -496,7 +497,8 @@ int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, const int32_t
 /* Appends the pairs of some of the nodes, in every layer of [layer0, layer0 + n_layers) at once: for each listed sequence and
  * KV head what n_path[b] calls of spkv_append_evict with nodes path[b][0], path[b][1], ... would do, up to the order in
  * which pages come off the free stack.  d_path [B][T] NULL: nodes 0, 1, 2, ...; d_n_path [B] NULL: T each; 0 leaves a
- * sequence as it is.  (So it is also an append of several tokens, as many as each sequence has.)  The path ends at the first
+ * sequence as it is.  (So it is also an append of several tokens, as many as each sequence has.)  A sequence id may appear once in
+ * the list, as everywhere but in spkv_decode_attention_tree.  The path ends at the first
  * entry outside [0, T) (SPKV_E_BOUNDS); a node may appear twice and is then appended twice.
  *   k, v: rows of layer0's nodes, token b T + i (n_kv_heads heads, as in spkv_decode_attention_tree), those of the next
  *   layer k_layer_stride / v_layer_stride elements on (a multiple of 8); d_logits [n_layers][B][T][n_kv_heads] float32.

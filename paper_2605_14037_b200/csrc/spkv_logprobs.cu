@@ -14,9 +14,10 @@
 // that t is off by up to 2^-24 |M|, a weight by 2 to that power: where the row's M is 2^24 or more in size it would count, from 2^31
 // on S itself leaves float32.  Such rows, and those whose sums are not finite for another reason (a product of c that has left
 // float32), are summed up again, about their own maximum, by the second kernel.
-// What bounds it: 768 rows of 128256 bf16 logits, top 1: 43 us on the device, 4.5 TB/s (30 us at the copy rate), 37 of them the first
-// kernel, at 8 instructions an element (maxima and floor take two elements an instruction in the type itself), 57 % of the
-// issue slots.  5 rows of 50257 fp32, top 5: 10 us, two launches with four trips to memory between them.
+// What bounds it: 768 rows of 128256 bf16 logits, top 1: 43.5 us on the device, 4.5 TB/s (30 us at the copy rate).  37 of them are the
+// first kernel, at 8 instructions an element (maxima and floor take two elements an instruction in the type itself) and 57 % of the
+// issue slots; the other 6.5 are the second, which cannot begin before all rows are summed.  5 rows of 50257 fp32, top 5: 9.6 us, two
+// launches with four trips to memory between them.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -311,7 +312,7 @@ struct TopList {
   }
 };
 
-// (six blocks an SM, so that 768 rows run at once: 43.4 us together with the sums, 45.9 with five)
+// (six blocks an SM: 888 rows run at once; 768 rows 43.5 us together with the sums, 45.9 with five)
 // One block per row: its parts joined, and its largest logits out of the chunks with the largest maxima.
 template <class T>
 __global__ void __launch_bounds__(lp::kThreads, 6) logprob_rows_kernel(LogprobArgs a) {

@@ -22,9 +22,10 @@ struct PathArgs {
 // oldest of the ring, and the first drafts themselves where n > w.  Lane x decides for leaving pairs x and x + 32; the
 // kept ones go to the compact cache in order, at most one fresh page among them (64 pairs end in at most one page that
 // was not begun).  Only then are the ring's slots written over, by the last min(n, w) drafts.
-// What bounds it: latency for short paths, memory beyond (a pair 512 B read and written, a kept one that leaves as
-// much again): 32 layers of 24 sequences and 8 KV heads, 1 / 4 / 16 pairs each, half of the leaving ones kept: 8.9 / 12.9 / 37.8 us
-// on the device, 5.3 TB/s at 16 and more than half of that at 4.
+// What bounds it: latency.  A pair is 512 B read and 512 written, a kept one that leaves as much again.  32 layers of 24 sequences
+// and 8 KV heads, keys and values apart and from memory, 1 / 4 / 16 pairs each, half of the leaving ones kept: 9.1 / 14.7 / 42 us on
+// the device; at 16 that is 152 MB, 3.6 TB/s (23 us at the copy rate; none kept 24 us, 4.2 TB/s; all kept 53 us, 3.8 TB/s), with
+// 49 % of the issue slots taken and a third of a warp's time spent on loads that are on their way.
 constexpr int kPathWarps = 4;
 constexpr int kPathAhead = 4;   // rows a lane asks for before it writes the first of them
 

@@ -31,9 +31,11 @@
 // whether or not a wait has run out.
 //
 // What bounds it (B200): the first scores come after 5 - 8 us (lengths two trips to memory, page table one, page one); then
-// memory, with up to 128 rows a unit (16 sequences on 16384 and on 32768 tokens: 5.0 ns a page between the two, 6.5 TB/s; 32768: 76.7
-// us a call on the device, of which the joining kernel 6), or, with several tiles, instructions: 2650 a page and
-// tile, 45 % of the issue slots, tensor pipe 47 % (8 x 65536, 512 rows a unit, 227 us).
+// memory, with up to 128 rows a unit (16 sequences on 16384 and on 32768 tokens: 5.0 ns a page between the two, 6.5 TB/s; 32768: 77
+// us a call on the device, of which the joining kernel 6).  Called for seconds on end this draws 990 W and the clock goes down to
+// 1.5 GHz: 91 us.  With several tiles nothing is full: 4 sequences on 32768 tokens, 512 rows a unit, issue in 50 % of the active
+// cycles, the tensor pipe is busy 42 % of the time, DRAM 15 %; what is waited for is a page's chain (scores, softmax, P V), of two
+// blocks an SM (8 x 65536, 512 rows a unit: 226 us).
 #include <math.h>
 
 #include <algorithm>
@@ -980,7 +982,10 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   a.rows_pad = w.rows_pad;
   a.n_tiles = w.n_tiles;
   const int blocks = tree::kBlocksPerSm * std::min(kMaxGrid, cache->sm_count);
-  a.min_cost = 5 + tree::kSegmentCost;   // (1 x 131072 tokens, 16 nodes: 27.7 us; 30.1 with 1, 31.4 with 11)
+  // Shortest range, in pages: shorter ones go to more blocks and leave more pieces to join.  With 1 / 5 / 8 (us): 1 x 131072 tokens,
+  // 16 nodes 29.8 / 26.0 / 27.9, 16 x 1000 with 8 nodes 25.5 / 22.2 / 24.9; but 1 x 8000 with 16 nodes 19.3 / 22.7 / 24.3, 4 x 2000
+  // 20.0 / 23.1 / 24.8, 8 x 8000 with 32 36.4 / 38.5 / 34.3; 1 x 300, and from 24 x 16384 on: alike.
+  a.min_cost = 5 + tree::kSegmentCost;
   if (const int rc = whole_shared_memory(reinterpret_cast<const void *>(tree_attention_kernel), tree::kSmemBytes, &g_tree_ready)) return rc;
   // Overlap mode: kernels before the last one may still be running, which griddepcontrol.wait does not
   // cover; a plain launch waits for all of them.
@@ -990,6 +995,8 @@ extern "C" int spkv_decode_attention_tree(spkv_cache_t *cache, int32_t layer, co
   if (launch_link(!plain, tree_attention_kernel, dim3(blocks), dim3(tree::kThreads), (size_t)tree::kSmemBytes, s, a) !=
       cudaSuccess)
     return SPKV_E_CUDA;
-  // pieces of a unit's tile: about blocks / tiles + 1
+  // Pieces of a unit's tile: about blocks / tiles + 1.  Few: two warps a block, 32 dims; many: eight warps and 16 dims, so that more of
+  // them are on their way (16 x 32768 78 / 86 us, 24 x 16384 63 / 74, 16 x 1000 22.1 / 23.0; 1 x 131072 40.4 / 26.0, 1 x 32768
+  // 25.4 / 24.1).  Between, at 4.6 blocks a tile, the first would still be the faster one (8 x 8000 33.5 / 38.5).
   return check_stream_error(blocks < 4 * a.n_items * a.n_tiles ? launch_tree_merge<2, 32, 1>(a, s) : launch_tree_merge<8, 16, 2>(a, s));
 }
